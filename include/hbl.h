@@ -40,14 +40,16 @@ typedef enum {
   HBL_ERR_NULL = 1,        /* a required pointer is NULL */
   HBL_ERR_SHAPE = 2,       /* a dimension is negative, zero where not allowed, or not a supported multiple */
   HBL_ERR_NOT_POW2 = 3,    /* use_hadamard with in_dim not a power of two (Eq. 4 needs n = 2^m) */
-  HBL_ERR_BITS = 4,        /* bits not 4 or 8 (hbl_quantize_kv: not 3, 4 or 8) */
+  HBL_ERR_BITS = 4,        /* bits not 4 or 8 (hbl_quantize_kv: not 3, 4 or 8; a paged cache: not 3, 4, 8 or 16) */
   HBL_ERR_ALIGN = 5,       /* a pointer is not aligned as required */
   HBL_ERR_WORKSPACE = 6,   /* workspace smaller than hbl_workspace_bytes() says */
   HBL_ERR_EPS = 7,         /* eps <= 0 or not finite */
   HBL_ERR_CUDA = 8,        /* a CUDA runtime / driver call failed (launch error, no device) */
   HBL_ERR_TIMEOUT = 9,     /* a bounded device-side wait expired */
   HBL_ERR_FORMAT = 10,     /* unknown dtype / path id */
-  HBL_ERR_TOO_LARGE = 11   /* size beyond a stated maximum */
+  HBL_ERR_TOO_LARGE = 11,  /* size beyond a stated maximum */
+  HBL_ERR_RANGE = 12       /* an index held in device memory (position, page, slot, length) is out of range: found by
+                              the kernel, which skips what the index would have reached; seen by hbl_check_status */
 } hbl_status_t;
 
 typedef enum { HBL_F32 = 0, HBL_BF16 = 1 } hbl_dtype_t;
@@ -344,6 +346,136 @@ int hbl_gemm_i32_static(const int8_t* codes, const int32_t* codesum, int tokens,
 size_t hbl_kv_codes_bytes(int tokens, int n_heads, int head_dim, int bits);
 int hbl_quantize_kv(const void* x, int tokens, int n_heads, int head_dim, int bits, int seq_len, float eps, void* codes,
                     float* scale, void* bos_codes, float* bos_scale, void* stream);
+
+/* ---- from q, k, v to the input of W_o: rotary positions, a paged cache of attention states, attention over it ----
+ * The paper keeps Q, K and V in few bits "after the rotary embedding" (section 3.1) and takes the rotary embedding,
+ * the cache and the attention from the LLaMA-like model it builds on (section 2) without formulas of its own. */
+
+/* Frequencies of the rotary embedding, radians per position: freq_out[i] = base^(-2i / rot_dim), i < rot_dim / 2
+ * (fp64, HOST memory), stretched for contexts longer than the trained one:
+ *   HBL_ROPE_PLAIN    as they are
+ *   HBL_ROPE_LINEAR   freq / factor
+ *   HBL_ROPE_BASE     base * factor^(rot_dim / (rot_dim - 2)) in place of base: the slowest pair is stretched by
+ *                     exactly `factor`, the fastest not at all (rot_dim >= 4)
+ *   HBL_ROPE_PARTS    by the turns a pair makes within trained_len positions, n = trained_len * freq / (2 pi):
+ *                     n >= fast: kept; n <= slow: freq / factor; between them the two are blended linearly in n
+ * factor >= 1; fast > slow > 0 (only for HBL_ROPE_PARTS, as is trained_len > 0).  rot_dim even, 2..256. */
+typedef enum { HBL_ROPE_PLAIN = 0, HBL_ROPE_LINEAR = 1, HBL_ROPE_BASE = 2, HBL_ROPE_PARTS = 3 } hbl_rope_scaling_t;
+int hbl_rope_frequencies(double base, int rot_dim, int scaling, double factor, double trained_len, double slow,
+                         double fast, double* freq_out /* host */);
+
+/* The table the calls below rotate by: table[p][i] = amplitude * (cos, sin)(angle), angle = (first_pos + p) * freq[i],
+ * fp32 [n_pos, n_freq, 2] (device, 16-byte aligned, written).  freq: fp64 [n_freq] in HOST memory, n_freq <= 128 (read
+ * before the call returns).  Angles, cosines and sines are taken in fp64 and rounded once: at position 10^6 an fp32
+ * angle would be off by up to 0.03.  first_pos >= 0.  A program makes the table once. */
+int hbl_rope_table(const double* freq /* host */, int n_freq, double amplitude, int first_pos, int n_pos, float* table,
+                   void* stream);
+
+typedef enum {
+  HBL_ROPE_HALF = 0,        /* element i of the rotated part pairs with element i + rot_dim / 2 */
+  HBL_ROPE_INTERLEAVED = 1  /* element 2i pairs with element 2i + 1 */
+} hbl_rope_layout_t;
+
+/* Rotary positions on the first rot_dim elements of every head (the rest is copied):
+ *   o1 = c x1 - s x2,  o2 = c x2 + s x1,   (c, s) = table[positions[t]][i],  (x1, x2) the i-th pair
+ * in fp32 (each product and sum rounded once, not fused), one rounding to the output type.
+ *   x, out       device, fp32 or bf16 (dtype), [tokens, n_heads, head_dim], element strides token_stride and
+ *                head_stride (multiples of 8; elements of a head are contiguous), bases 16-byte aligned; out may be x
+ *                itself with the same strides, and may not overlap x in any other way
+ *   positions    device int32 [tokens]; one outside [0, n_pos) is reported as HBL_ERR_RANGE and its token is not written
+ *   table        from hbl_rope_table, n_pos rows of rot_dim / 2 pairs
+ *   head_dim     a multiple of 8, 8..256; rot_dim a multiple of 16, 16..head_dim
+ *   backward     1: the transposed rotation, i.e. the gradient with respect to x of a gradient with respect to out
+ *                (with an amplitude of 1 also the inverse) */
+int hbl_rope(const void* x, int dtype, int tokens, int n_heads, int head_dim, long long x_token_stride,
+             long long x_head_stride, const int32_t* positions, const float* table, int n_pos, int rot_dim, int layout,
+             int backward, void* out, long long out_token_stride, long long out_head_stride, void* stream);
+
+/* A paged cache of attention states (all pointers device, the caller's).  A page holds page_size tokens of every
+ * key/value head; row (page, head, slot) has the number  (page * n_kv_heads + head) * page_size + slot.
+ *   bits 3, 4, 8   k, v: head_dim * bits / 8 bytes per row, the codes of hbl_quantize_kv (u = q + 2^(bits-1), a
+ *                  little-endian bit string); k_scale, v_scale: one fp32 per row
+ *   bits 16        k, v: head_dim bf16 values per row; the scales are NULL
+ * bos_k, bos_v (optional, with bits 3 or 4): the first token of a sequence at 8 bits, one row of head_dim codes per
+ * (slot, head), and its scales bos_k_scale, bos_v_scale [n_slots, n_kv_heads].  With them a sequence's position 0 is read
+ * from there (the low-bit row is written all the same).
+ *   page_size a power of two, 16..4096; head_dim 64, 128 or 256; k, v, bos_k, bos_v 16-byte aligned. */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  void *bos_k, *bos_v;
+  float *bos_k_scale, *bos_v_scale;
+  int n_pages, page_size, n_kv_heads, head_dim, bits, n_slots;
+} hbl_kv_cache_t;
+
+/* A batch of sequences over a cache.  Sequence b has kv_len[b] tokens, the last q_start[b+1] - q_start[b] of which are
+ * the call's: rows q_start[b] .. q_start[b+1] - 1 of its tensors.  Its tokens [i * page_size, (i + 1) * page_size) lie
+ * in page pages[b][i].
+ *   q_start   device int32 [n_seqs + 1], not decreasing, q_start[0] = 0, q_start[n_seqs] <= tokens; rows from
+ *             q_start[n_seqs] on are neither read nor written
+ *   kv_len    device int32 [n_seqs], the tokens of the call included
+ *   pages     device int32 [n_seqs, max_pages]; entries beyond a sequence's length are not looked at
+ *   bos_slot  device int32 [n_seqs]: the sequence's row of bos_k / bos_v; NULL: sequence b has row b
+ *   max_q_len, max_kv_len   upper bounds of the lengths (host values: launch shapes go by them).  Tokens of a sequence
+ *             beyond its first max_q_len are not computed by hbl_attention; a kv_len above max_kv_len costs time only.
+ * Lengths are read on the device when the kernels run, so a captured call follows them when it is replayed.
+ * A length above max_pages * page_size or 2^30 (the rest is left out), a negative one, or a page outside [0, n_pages) (its
+ * tokens are neither written nor read) is reported as HBL_ERR_RANGE.  Several sequences may share pages that no call
+ * writes; two tokens of one hbl_kv_append call may not have the same place. */
+typedef struct {
+  const int32_t *q_start, *kv_len, *pages, *bos_slot;
+  int n_seqs, tokens, max_pages, max_q_len, max_kv_len;
+} hbl_kv_batch_t;
+
+/* The tokens of a batch into the cache, in one launch: keys are rotated and, like the values, quantized as
+ * hbl_quantize_kv does (on the rotated fp32 values: they are not rounded in between) or rounded to bf16 (bits 16), and
+ * written at positions kv_len[b] - n .. kv_len[b] - 1 of their sequence; queries, where given, are rotated to q_out.
+ *   k, v      device bf16 [tokens, n_kv_heads, head_dim] with element strides as in hbl_rope
+ *   q, q_out  device bf16 [tokens, n_heads, head_dim] (q_out may be q with the same strides); NULL: none
+ *   table     from hbl_rope_table (n_pos, rot_dim, layout as in hbl_rope); NULL: nothing is rotated, q must be NULL
+ *   positions device int32 [tokens], what to rotate by; NULL: a token's place in its sequence
+ * A head with a NaN or an infinity in it gets the scale NaN (and so reads as NaN) at bits 3, 4 and 8.
+ * eps as in hbl_quantize_kv (> 0).  A token whose position, page or slot is out of range is left out as a whole. */
+typedef struct {
+  const void *k, *v, *q;
+  void* q_out;
+  long long k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+  long long q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride;
+  const float* table;
+  const int32_t* positions;
+  int n_heads, n_pos, rot_dim, layout;
+  float eps;
+} hbl_kv_append_t;
+int hbl_kv_append(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_kv_append_t* args, void* stream);
+
+/* The batch's tokens out of the cache: k_out, v_out bf16 [tokens, n_kv_heads, head_dim] (contiguous, 16-byte aligned)
+ * = scale * (u - 2^(bits-1)), one rounding (bits 16: the values as they are).  With q_start = the running sum of kv_len
+ * whole sequences come out (to move them to another cache, or to keep a shared prefix). */
+int hbl_kv_read(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, void* k_out, void* v_out, void* stream);
+
+/* Attention of the batch's tokens over the cache (which holds their keys and values already):
+ *   out[t, h] = sum_j p_j V[j, h'] / sum_j p_j,  p_j = exp(sm_scale * q[t, h] . K[j, h']),  h' = h / (n_heads / n_kv_heads)
+ * over the tokens j of t's sequence; causal = 1: those up to t itself.  A row with no j (a sequence shorter than its
+ * number of queries) gets out = 0 and lse = -infinity.
+ *   q, out    device bf16 [tokens, n_heads, head_dim], element strides as in hbl_rope
+ *   lse       NULL, or device fp32 [tokens, n_heads]: log(sum_j p_j)
+ * Products are of bf16 values: codes are exact in bf16 and their scales are applied in fp32, to the score (keys) and
+ * to p (values), which is then rounded to bf16; scores, p's sum and the result are accumulated in fp32.
+ * bits 16: a value that is NaN or infinite may reach every row of its sequence, rows it is masked for among them
+ * (0 * inf); places beyond kv_len are never used, whatever they hold.
+ * workspace: hbl_attention_workspace_bytes, 1024-byte aligned (NULL where that is 0); scratch, nothing in it is kept.
+ * n_heads a multiple of n_kv_heads. */
+typedef struct {
+  const void* q;
+  void* out;
+  float* lse;
+  long long q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+  int n_heads, causal;
+  float sm_scale;
+} hbl_attention_t;
+size_t hbl_attention_workspace_bytes(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, int n_heads);
+int hbl_attention(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_attention_t* args, void* workspace,
+                  size_t workspace_bytes, void* stream);
 
 /* Packed ternary -> int8 [N,K] row-major, values in {-1,0,1}. */
 int hbl_unpack_weights(const void* W_packed, int out_dim, int in_dim, int8_t* w_out, void* stream);

@@ -286,6 +286,7 @@ const char* hbl_status_string(int status) {
     case HBL_ERR_TIMEOUT: return "device-side wait timed out";
     case HBL_ERR_FORMAT: return "unknown dtype or path";
     case HBL_ERR_TOO_LARGE: return "size beyond the supported maximum";
+    case HBL_ERR_RANGE: return "index in device memory out of range";
     default: return "unknown status";
   }
 }

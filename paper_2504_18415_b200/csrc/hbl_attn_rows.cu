@@ -1,0 +1,498 @@
+// Attention of few query rows over the paged cache: decoding steps.
+//
+//   s_j = sm_scale * ks_j * (q . ck_j),   p_j = 2^(s_j - m),   out = sum_j p_j vs_j cv_j / sum_j p_j
+//
+// with codes ck, cv (exact in bf16) and per-row scales ks, vs applied in fp32; bits 16: ck, cv are the bf16 values and
+// the scales are 1.  p_j vs_j is rounded to bf16 (a half step of 2^-9, independent from key to key) because that is what
+// the tensor core multiplies; p's sum is taken before that rounding, in fp32.
+//
+// Bound by the cache's bytes: every code is read once per 8 (16) query rows of its key head.  A thread block takes one
+// (sequence, key head, row tile, piece of the keys), its four warps take 16 keys in turn and meet only at the end, so there
+// is no barrier in the loop.  The keys are the M side of both products (S^T = K q^T, O^T = V^T P^T): 16 keys against 8
+// rows, no half-empty tile, and a lane's operand registers are exactly the bytes that it loads from the cache
+// (hbl_attn_frag.cuh), so nothing passes through shared memory but the queries.  The running maximum is only
+// raised when a score exceeds it by more than 2^8 (p stays below 256): most steps rescale nothing and exchange nothing.
+#include "hbl_attn_frag.cuh"
+
+namespace hbl {
+namespace {
+
+using namespace frag;
+
+constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
+constexpr float kLazy = 8.f;
+
+struct RowsParams {
+  KvView c;
+  BatchView b;
+  AttnArgs a;
+  AttnPlan p;
+  float* part_o;                 // [splits][tokens * n_heads][head_dim], normalised; splits > 1 only
+  float* part_lse;               // [splits][tokens * n_heads], log2 units
+  int* status;
+};
+
+template <int BITS, int D>
+struct Geo {
+  static constexpr int KU = D / 32, VU = D / 64;               // units of a key / value row a lane holds
+  using KLane = Lane<BITS, KU, 4>;
+  using VLane = Lane<BITS, VU, 8>;
+  static constexpr int STEP_WORDS = 2 * KLane::WORDS + 4 * VLane::WORDS + 4;
+  // steps whose loads are in flight ahead of the one at work, as far as registers go
+  static constexpr int AHEAD = STEP_WORDS <= 24 ? 3 : STEP_WORDS <= 40 ? 2 : 1;
+  static constexpr int ROW_BYTES = D * BITS / 8;
+};
+template <int BITS, int D>
+struct Step {
+  typename Geo<BITS, D>::KLane k[2];
+  typename Geo<BITS, D>::VLane v[4];
+  float ks[2], vs[2];
+};
+
+template <int BITS, int D, int NT>
+__global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_constant__ RowsParams p) {
+  using G = Geo<BITS, D>;
+  constexpr int ROWS = 8 * NT;
+  constexpr int MT = D / 16;                                  // 16-element tiles of the output
+  __shared__ uint4 sq[NT][G::KU][32];
+  __shared__ float so[ROWS][D + 4];
+  __shared__ float sm[kWarps][ROWS], sl[kWarps][ROWS];
+  grid_dependency_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  int id = blockIdx.x;
+  const int split = id % p.p.splits; id /= p.p.splits;
+  const int tile = id % p.p.tiles; id /= p.p.tiles;
+  const int head = id % p.c.n_kv_heads, b = id / p.c.n_kv_heads;
+  SeqLens len;
+  if (!sequence_lengths(p.b, b, p.c.page_shift, p.status, len)) return;
+  const int group = p.a.group;
+  const int n_rows = min(len.q_len, p.b.max_q_len) * group, r0 = tile * ROWS;
+  if (r0 >= n_rows) return;
+  const int last_tok = min(r0 + ROWS - 1, n_rows - 1) / group;
+  // keys any row of the tile sees, and the piece of them that is this block's (the last piece takes what is left)
+  const int seen = p.a.causal ? max(0, min(len.held, len.kv - len.q_len + last_tok + 1)) : len.held;
+  const int key0 = split * p.p.chunk;
+  if (split > 0 && (long)split * p.p.chunk >= len.held) return;      // no such piece in this sequence: the combine step knows
+  const int key1 = split == p.p.splits - 1 ? seen : min(seen, key0 + p.p.chunk);
+
+  // ---- queries as B fragments: row n = g of tile nt, its pairs in the order the keys' units have ----
+  for (int i = threadIdx.x; i < NT * G::KU * 32; i += kThreads) {
+    const int ln = i & 31, u = (i >> 5) % G::KU, nt = (i >> 5) / G::KU;
+    const int r = r0 + nt * 8 + (ln >> 2);
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (r < n_rows) {
+      const int tok = r / group, hq = head * group + r % group;
+      w = __ldg(reinterpret_cast<const uint4*>(p.a.q + (len.q0 + tok) * p.a.q_ts + hq * p.a.q_hs + 8 * G::KLane::unit_of(u, ln & 3)));
+    }
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    uint32_t o[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int lo = pair_lo<BITS>(j), hi = pair_hi<BITS>(j);
+      o[j] = __byte_perm(x[lo / 2], x[hi / 2], (lo & 1 ? 0x32 : 0x10) | (hi & 1 ? 0x7600 : 0x5400));
+    }
+    sq[nt][u][ln] = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+  __syncthreads();
+
+  // rows of this lane's score columns: 2t and 2t + 1 of every tile; they see keys below lim
+  int lim[NT][2], low = 0x7fffffff;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = r0 + nt * 8 + 2 * t + e;
+      lim[nt][e] = r >= n_rows ? 0 : p.a.causal ? len.kv - len.q_len + r / group + 1 : seen;
+      if (r < n_rows) low = min(low, lim[nt][e]);
+    }
+  low = min(low, key1);
+  low = __reduce_min_sync(0xffffffffu, low);                  // below it no key needs a mask
+
+  float m[NT][2], l[NT][2], o[NT][MT][4];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    m[nt][0] = m[nt][1] = -INFINITY;
+    l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
+  }
+
+  const bool bos = BITS < 8 && p.c.bos_k != nullptr;
+  int bos_row = -1;
+  if (bos && key0 == 0 && key1 > 0) {
+    const int slot = p.b.bos_slot != nullptr ? __ldg(p.b.bos_slot + b) : b;
+    if (slot >= 0 && slot < p.c.n_slots) bos_row = slot;
+    else report_device_error(p.status, HBL_ERR_RANGE);        // its first token is then left out
+  }
+  const int* page_row = p.b.pages + (long)b * p.b.max_pages;
+
+  // scores (c: keys g and g + 8, columns 2t and 2t + 1) to P^T fragments, with the running maximum
+  auto softmax = [&](float (&c)[NT][4], int kb, const float (&ks)[2], const float (&vs)[2], bool masked, bool skip_first,
+                     uint32_t (&pf)[NT][2]) {
+    bool raise = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        c[nt][e] *= ks[e >> 1];
+        const int key = kb + g + (e >> 1) * 8;
+        if (masked && (key >= min(lim[nt][e & 1], key1) || (skip_first && key == 0))) c[nt][e] = -INFINITY;
+        raise |= c[nt][e] > m[nt][e & 1] + kLazy;
+      }
+    if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float f[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float x = fmaxf(c[nt][e], c[nt][e + 2]);
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+          const float top = fmaxf(m[nt][e], x);
+          f[e] = top == -INFINITY ? 1.f : exp2_approx(m[nt][e] - top);
+          m[nt][e] = top;
+          l[nt][e] *= f[e];
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          o[nt][i][0] *= f[0]; o[nt][i][1] *= f[1]; o[nt][i][2] *= f[0]; o[nt][i][3] *= f[1];
+        }
+      }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float top = m[nt][e & 1] == -INFINITY ? 0.f : m[nt][e & 1];
+        const float x = exp2_approx(c[nt][e] - top);
+        l[nt][e & 1] += x;
+        w[e] = BITS == 16 ? x : x * vs[e >> 1];
+        if (masked && c[nt][e] == -INFINITY) w[e] = 0.f;        // (a scale that is not finite stays out, too)
+      }
+      pf[nt][0] = transpose8x8(pack2(w[0], w[1]));
+      pf[nt][1] = transpose8x8(pack2(w[2], w[3]));
+    }
+  };
+
+  // ---- the first token at 8 bits: one key, by the warp whose turn key 0 is ----
+  if (bos_row >= 0 && warp == 0) {
+    const long brow = (long)bos_row * p.c.n_kv_heads + head;
+    float c[NT][4] = {};
+#pragma unroll
+    for (int i = 0; i < G::KU; ++i) {
+      uint32_t a[4] = {0, 0, 0, 0};
+      if (g == 0) {
+        const uint2 u = __ldg(reinterpret_cast<const uint2*>(p.c.bos_k + brow * D) + G::KLane::unit_of(i, t));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int lo = pair_lo<BITS>(j), hi = pair_hi<BITS>(j);
+          a[j] = pack2((float)((int)(((lo < 4 ? u.x : u.y) >> (8 * (lo & 3))) & 255u) - 128),
+                       (float)((int)(((hi < 4 ? u.x : u.y) >> (8 * (hi & 3))) & 255u) - 128));
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const uint4 q = sq[nt][i][lane];
+        mma16816(c[nt], a[0], 0, a[1], 0, q.x, q.y);
+        mma16816(c[nt], a[2], 0, a[3], 0, q.z, q.w);
+      }
+    }
+    const float ks[2] = {__ldg(p.c.bos_k_scale + brow) * p.a.scale_log2, 0.f}, vs[2] = {__ldg(p.c.bos_v_scale + brow), 0.f};
+    // keep row 0 alone
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        c[nt][e] *= ks[e >> 1];
+        if (g != 0 || e > 1) c[nt][e] = -INFINITY;
+      }
+    const float one[2] = {1.f, 1.f};
+    uint32_t pf[NT][2];
+    softmax(c, 0, one, vs, true, false, pf);
+#pragma unroll
+    for (int i = 0; i < G::VU; ++i) {
+      uint32_t a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      if (t == 0) {
+        const uint2 u = __ldg(reinterpret_cast<const uint2*>(p.c.bos_v + brow * D) + G::VLane::unit_of(i, g));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] = pack2((float)((int)(((e < 4 ? u.x : u.y) >> (8 * (e & 3))) & 255u) - 128), 0.f);
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) mma16816(o[nt][4 * i + q], a[2 * q], a[2 * q + 1], 0, 0, pf[nt][0], pf[nt][1]);
+    }
+  }
+
+  // ---- the keys, 16 at a time ----
+  Step<BITS, D> st[G::AHEAD];
+  auto page_of = [&](int kb) { return kb < key1 ? __ldg(page_row + (kb >> p.c.page_shift)) : -1; };
+  auto load = [&](Step<BITS, D>& s, int kb, int page) {
+    const bool here = kb < key1 && page >= 0 && page < p.c.n_pages;
+    const long row0 = cache_row(p.c, here ? page : 0, head, kb & ((1 << p.c.page_shift) - 1));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool live = here && kb + g + 8 * h < key1;
+      s.k[h].load(p.c.k + (row0 + g + 8 * h) * G::ROW_BYTES, t, live);
+      if (BITS < 16) {
+        s.ks[h] = live ? __ldg(p.c.k_scale + row0 + g + 8 * h) : 0.f;
+        s.vs[h] = live ? __ldg(p.c.v_scale + row0 + g + 8 * h) : 0.f;
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const int r = 2 * t + (h & 1) + 8 * (h >> 1);
+      s.v[h].load(p.c.v + (row0 + r) * G::ROW_BYTES, g, here && kb + r < key1);
+    }
+    return here;
+  };
+  constexpr int STRIDE = 16 * kWarps;
+  int kb = key0 + 16 * warp;
+  int ahead_kb = kb, ahead_page = page_of(kb);
+  bool here[G::AHEAD];
+#pragma unroll
+  for (int d = 0; d < G::AHEAD; ++d) {
+    here[d] = load(st[d], ahead_kb, ahead_page);
+    ahead_kb += STRIDE;
+    ahead_page = page_of(ahead_kb);
+  }
+  while (kb < key1) {
+#pragma unroll
+    for (int d = 0; d < G::AHEAD; ++d) {
+      if (kb < key1) {
+        const Step<BITS, D>& s = st[d];
+        if (!here[d]) {
+          report_device_error(p.status, HBL_ERR_RANGE);
+        } else {
+          float c[NT][4] = {};
+#pragma unroll
+          for (int i = 0; i < G::KU; ++i) {
+            uint32_t x[4], y[4];
+            pairs<BITS>(s.k[0], i, t, x);
+            pairs<BITS>(s.k[1], i, t, y);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              const uint4 q = sq[nt][i][lane];
+              mma16816(c[nt], x[0], y[0], x[1], y[1], q.x, q.y);
+              mma16816(c[nt], x[2], y[2], x[3], y[3], q.z, q.w);
+            }
+          }
+          const float ks[2] = {BITS == 16 ? p.a.scale_log2 : s.ks[0] * p.a.scale_log2, BITS == 16 ? p.a.scale_log2 : s.ks[1] * p.a.scale_log2};
+          uint32_t pf[NT][2];
+          softmax(c, kb, ks, s.vs, kb + 16 > low || (bos && kb == 0), bos, pf);
+#pragma unroll
+          for (int i = 0; i < G::VU; ++i) {
+            uint32_t x[8], y[8];
+            cross<BITS>(s.v[0], s.v[1], i, g, x);
+            cross<BITS>(s.v[2], s.v[3], i, g, y);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                mma16816(o[nt][4 * i + q], x[2 * q], x[2 * q + 1], y[2 * q], y[2 * q + 1], pf[nt][0], pf[nt][1]);
+          }
+        }
+      }
+      here[d] = load(st[d], ahead_kb, ahead_page);
+      ahead_kb += STRIDE;
+      ahead_page = page_of(ahead_kb);
+      kb += STRIDE;
+    }
+  }
+
+  // ---- the four warps' results together ----
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float x = l[nt][e];
+      x += __shfl_xor_sync(0xffffffffu, x, 4);
+      x += __shfl_xor_sync(0xffffffffu, x, 8);
+      x += __shfl_xor_sync(0xffffffffu, x, 16);
+      if (g == 0) {
+        sm[warp][nt * 8 + 2 * t + e] = m[nt][e];
+        sl[warp][nt * 8 + 2 * t + e] = x;
+      }
+    }
+  __syncthreads();
+  float f[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = nt * 8 + 2 * t + e;
+      float top = sm[0][r];
+#pragma unroll
+      for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sm[w][r]);
+      f[nt][e] = exp2_approx(m[nt][e] - (top == -INFINITY ? 0.f : top));     // (0 where there was no key; a NaN stays in o)
+    }
+  for (int w = 0; w < kWarps; ++w) {
+    if (warp == w) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int d = 8 * G::VLane::unit_of(i / 4, g) + 2 * (i & 3) + (e >> 1);
+            float& x = so[nt * 8 + 2 * t + (e & 1)][d];
+            const float y = o[nt][i][e] * f[nt][e & 1];
+            x = w == 0 ? y : x + y;
+          }
+    }
+    __syncthreads();
+  }
+  const long total_rows = (long)p.b.tokens * p.a.n_heads;
+  for (int i = threadIdx.x; i < ROWS * (D / 4); i += kThreads) {
+    const int rr = i / (D / 4), d = (i % (D / 4)) * 4, r = r0 + rr;
+    if (r >= n_rows) break;
+    float top = sm[0][rr], sum = 0.f;
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sm[w][rr]);
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) sum += sl[w][rr] * exp2_approx(sm[w][rr] - (top == -INFINITY ? 0.f : top));
+    const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
+    const int tok = len.q0 + r / group, hq = head * group + r % group;
+    const float4 v = *reinterpret_cast<const float4*>(&so[rr][d]);
+    const float lse2 = sum == 0.f ? -INFINITY : top + __log2f(sum);
+    if (p.p.splits > 1) {
+      const long row = split * total_rows + (long)tok * p.a.n_heads + hq;
+      *reinterpret_cast<float4*>(p.part_o + row * D + d) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+      if (d == 0) p.part_lse[row] = lse2;
+    } else {
+      *reinterpret_cast<uint2*>(p.a.out + tok * p.a.o_ts + hq * p.a.o_hs + d) =
+          make_uint2(pack2(v.x * inv, v.y * inv), pack2(v.z * inv, v.w * inv));
+      if (d == 0 && p.a.lse != nullptr) p.a.lse[(long)tok * p.a.n_heads + hq] = lse2 * 0.6931471805599453f;
+    }
+  }
+}
+
+// The pieces of a row together: out = sum_s 2^(lse_s - top) o_s / sum_s 2^(lse_s - top).  A warp takes one row.
+struct CombineParams {
+  KvView c;
+  BatchView b;
+  AttnArgs a;
+  AttnPlan p;
+  const float *part_o, *part_lse;
+  int* status;
+};
+template <int D>
+__global__ void __launch_bounds__(256) attn_combine_kernel(const __grid_constant__ CombineParams p) {
+  grid_dependency_wait();
+  const int lane = threadIdx.x & 31;
+  const long total_rows = (long)p.b.tokens * p.a.n_heads, row = (long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= total_rows) return;
+  const int tok = (int)(row / p.a.n_heads), hq = (int)(row % p.a.n_heads);
+  const int b = find_sequence(p.b.q_start, p.b.n_seqs, tok, lane);
+  if (b >= p.b.n_seqs) return;
+  SeqLens len;
+  if (!sequence_lengths(p.b, b, p.c.page_shift, p.status, len) || tok < len.q0 || tok - len.q0 >= p.b.max_q_len) return;
+  const int pieces = max(1, min(p.p.splits, (len.held + p.p.chunk - 1) / p.p.chunk));
+  float top = -INFINITY;
+  for (int s = lane; s < pieces; s += 32) top = fmaxf(top, p.part_lse[s * total_rows + row]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  constexpr int E = D / 32;
+  float acc[E] = {}, sum = 0.f;
+  for (int s = 0; s < pieces; ++s) {
+    const float x = p.part_lse[s * total_rows + row];
+    const float w = x == -INFINITY ? 0.f : exp2_approx(x - top);      // (a NaN stays one)
+    if (w == 0.f) continue;
+    sum += w;
+    const float* src = p.part_o + (s * total_rows + row) * D + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      const float2 v = *reinterpret_cast<const float2*>(src + e);
+      acc[e] += w * v.x;
+      acc[e + 1] += w * v.y;
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
+  uint32_t* dst = reinterpret_cast<uint32_t*>(p.a.out + tok * p.a.o_ts + hq * p.a.o_hs + lane * E);
+#pragma unroll
+  for (int e = 0; e < E; e += 2) dst[e / 2] = pack2(acc[e] * inv, acc[e + 1] * inv);
+  if (lane == 0 && p.a.lse != nullptr) p.a.lse[row] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
+}
+
+int rows_per_tile(const BatchView& b, int group) { return (long)b.max_q_len * group > 8 ? 16 : 8; }
+
+template <int BITS, int D>
+int launch_rows_dim(RowsParams& p, cudaStream_t s) {
+  const long blocks = (long)p.b.n_seqs * p.c.n_kv_heads * p.p.tiles * p.p.splits;
+  if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
+  if (rows_per_tile(p.b, p.a.group) == 8)
+    HBL_CUDA_OK(launch_dependent(attn_rows_kernel<BITS, D, 1>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+  else
+    HBL_CUDA_OK(launch_dependent(attn_rows_kernel<BITS, D, 2>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+  note_launch();
+  return HBL_OK;
+}
+template <int BITS>
+int launch_rows_bits(RowsParams& p, cudaStream_t s) {
+  switch (p.c.head_dim) {
+    case 64: return launch_rows_dim<BITS, 64>(p, s);
+    case 128: return launch_rows_dim<BITS, 128>(p, s);
+    case 256: return launch_rows_dim<BITS, 256>(p, s);
+    default: return HBL_ERR_SHAPE;
+  }
+}
+
+}  // namespace
+
+AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads) {
+  AttnPlan p{};
+  const int group = n_heads / c.n_kv_heads, rows = rows_per_tile(b, group);
+  p.tiles = (int)(((long)b.max_q_len * group + rows - 1) / rows);
+  const long base = (long)b.n_seqs * c.n_kv_heads * p.tiles;
+  // pieces of at least 256 keys, as many as keep four thread blocks on every SM
+  const long want = base > 0 ? ((long)sm_count() * 4 + base - 1) / base : 1;
+  const long most = ((long)b.max_kv_len + 255) / 256;
+  const long splits = want < most ? want : most;
+  const long n = splits < 1 ? 1 : splits;
+  p.chunk = (int)((((long)b.max_kv_len + n - 1) / n + 63) / 64 * 64);
+  if (p.chunk < 64) p.chunk = 64;
+  p.splits = (int)(((long)b.max_kv_len + p.chunk - 1) / p.chunk);
+  if (p.splits < 1) p.splits = 1;
+  return p;
+}
+
+int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& plan, float* part_o,
+                          float* part_lse, cudaStream_t s) {
+  RowsParams p{};
+  p.c = c; p.b = b; p.a = a; p.p = plan; p.part_o = part_o; p.part_lse = part_lse;
+  p.status = device_status_word();
+  if (p.status == nullptr) return HBL_ERR_CUDA;
+  switch (c.bits) {
+    case 3: return launch_rows_bits<3>(p, s);
+    case 4: return launch_rows_bits<4>(p, s);
+    case 8: return launch_rows_bits<8>(p, s);
+    case 16: return launch_rows_bits<16>(p, s);
+    default: return HBL_ERR_BITS;
+  }
+}
+
+int launch_attention_combine(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& plan, const float* part_o,
+                             const float* part_lse, cudaStream_t s) {
+  CombineParams p{};
+  p.c = c; p.b = b; p.a = a; p.p = plan; p.part_o = part_o; p.part_lse = part_lse;
+  p.status = device_status_word();
+  if (p.status == nullptr) return HBL_ERR_CUDA;
+  const long blocks = ((long)b.tokens * a.n_heads + 7) / 8;
+  if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
+  const dim3 grid((unsigned)blocks), block(256);
+  switch (c.head_dim) {
+    case 64: HBL_CUDA_OK(launch_dependent(attn_combine_kernel<64>, grid, block, 0, s, p)); break;
+    case 128: HBL_CUDA_OK(launch_dependent(attn_combine_kernel<128>, grid, block, 0, s, p)); break;
+    case 256: HBL_CUDA_OK(launch_dependent(attn_combine_kernel<256>, grid, block, 0, s, p)); break;
+    default: return HBL_ERR_SHAPE;
+  }
+  note_launch();
+  return HBL_OK;
+}
+
+}  // namespace hbl

@@ -19,7 +19,7 @@ PATH_AUTO, PATH_STREAM, PATH_TENSOR, PATH_TENSOR_PACKED, PATH_STREAM_OVERLAP = 0
 STATUS_NAMES = {
     0: "HBL_OK", 1: "HBL_ERR_NULL", 2: "HBL_ERR_SHAPE", 3: "HBL_ERR_NOT_POW2", 4: "HBL_ERR_BITS",
     5: "HBL_ERR_ALIGN", 6: "HBL_ERR_WORKSPACE", 7: "HBL_ERR_EPS", 8: "HBL_ERR_CUDA", 9: "HBL_ERR_TIMEOUT",
-    10: "HBL_ERR_FORMAT", 11: "HBL_ERR_TOO_LARGE",
+    10: "HBL_ERR_FORMAT", 11: "HBL_ERR_TOO_LARGE", 12: "HBL_ERR_RANGE",
 }
 
 EXPORTS = [
@@ -29,6 +29,8 @@ EXPORTS = [
     "hbl_quantize_act", "hbl_gemm_i32", "hbl_unpack_weights", "hbl_forward_host", "hbl_launch_count",
     "hbl_profile_events", "hbl_gemm_i32_static", "hbl_kv_codes_bytes", "hbl_quantize_kv",
     "hbl_selftest_wait_timeout", "hbl_quantize_act_int4_packed", "hbl_gemm_i32_int4_packed",
+    "hbl_rope_frequencies", "hbl_rope_table", "hbl_rope", "hbl_kv_append", "hbl_kv_read",
+    "hbl_attention_workspace_bytes", "hbl_attention",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -48,6 +50,29 @@ class hbl_block_t(C.Structure):
                                           "yq", "yk", "yv", "yo", "yup", "ygate", "ydown")] + \
                [("tokens", C.c_int), ("hidden", C.c_int), ("ffn", C.c_int), ("bits", C.c_int),
                 ("x_dtype", C.c_int), ("eps", C.c_float)]
+
+
+class hbl_kv_cache_t(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "bos_k", "bos_v", "bos_k_scale", "bos_v_scale")] + \
+               [(n, C.c_int) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "bits", "n_slots")]
+
+
+class hbl_kv_batch_t(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q_start", "kv_len", "pages", "bos_slot")] + \
+               [(n, C.c_int) for n in ("n_seqs", "tokens", "max_pages", "max_q_len", "max_kv_len")]
+
+
+class hbl_kv_append_t(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "q", "q_out")] + \
+               [(n + s, C.c_longlong) for n in ("k", "v", "q", "q_out") for s in ("_token_stride", "_head_stride")] + \
+               [("table", C.c_void_p), ("positions", C.c_void_p)] + \
+               [(n, C.c_int) for n in ("n_heads", "n_pos", "rot_dim", "layout")] + [("eps", C.c_float)]
+
+
+class hbl_attention_t(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "out", "lse")] + \
+               [(n + s, C.c_longlong) for n in ("q", "out") for s in ("_token_stride", "_head_stride")] + \
+               [("n_heads", C.c_int), ("causal", C.c_int), ("sm_scale", C.c_float)]
 
 
 def lib() -> C.CDLL:
@@ -92,6 +117,17 @@ def lib() -> C.CDLL:
         L.hbl_quantize_act_int4_packed.argtypes = [vp, i, i, i, i, f, vp, vp, vp]
         L.hbl_gemm_i32_int4_packed.restype = C.c_int
         L.hbl_gemm_i32_int4_packed.argtypes = [vp, i, i, vp, i, vp, vp, sz, vp]
+        d, ll, cache, batch = C.c_double, C.c_longlong, C.POINTER(hbl_kv_cache_t), C.POINTER(hbl_kv_batch_t)
+        L.hbl_rope_frequencies.argtypes = [d, i, i, d, d, d, d, C.POINTER(d)]
+        L.hbl_rope_table.argtypes = [C.POINTER(d), i, d, i, i, vp, vp]
+        L.hbl_rope.argtypes = [vp, i, i, i, i, ll, ll, vp, vp, i, i, i, i, vp, ll, ll, vp]
+        L.hbl_kv_append.argtypes = [cache, batch, C.POINTER(hbl_kv_append_t), vp]
+        L.hbl_kv_read.argtypes = [cache, batch, vp, vp, vp]
+        L.hbl_attention_workspace_bytes.argtypes = [cache, batch, i]
+        L.hbl_attention_workspace_bytes.restype = sz
+        L.hbl_attention.argtypes = [cache, batch, C.POINTER(hbl_attention_t), vp, sz, vp]
+        for n in ("hbl_rope_frequencies", "hbl_rope_table", "hbl_rope", "hbl_kv_append", "hbl_kv_read", "hbl_attention"):
+            getattr(L, n).restype = C.c_int
         L.hbl_selftest_wait_timeout.restype = C.c_int
         L.hbl_selftest_wait_timeout.argtypes = [i, vp, vp]
         L.hbl_forward_host.argtypes = [vp, i, i, i, vp, vp, i, i, i, f, vp, vp, vp, vp, sz, i, vp]
@@ -376,6 +412,210 @@ def hbl_quantize_kv(x: torch.Tensor, bits: int, seq_len: int = 0, eps: float = 1
     _check(lib().hbl_quantize_kv(_ptr(x), T, H, D, bits, seq_len, eps, _ptr(codes), _ptr(scale), _ptr(bos_codes),
                                  _ptr(bos_scale), _stream()), "hbl_quantize_kv")
     return codes, scale, bos_codes, bos_scale
+
+
+# ---- rotary positions, the paged cache of attention states, attention over it ----
+
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
+
+
+def _raw_stream(device: torch.device) -> int:
+    """The current stream's handle; the calls below are made many times per token, so it is read the short way."""
+    index = device.index
+    if index != torch._C._cuda_getDevice():
+        raise ValueError(f"the tensors are on cuda:{index}, which is not the current device")
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _flat(t: torch.Tensor | None, dtype, shape, what: str, device) -> int | None:
+    """Address of a contiguous CUDA tensor of this type and shape (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_cuda or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+    return t.data_ptr()
+
+
+def _heads(t: torch.Tensor, shape, dtype, what: str, device) -> tuple[int, int, int]:
+    """(address, token stride, head stride) of a [tokens, heads, head_dim] tensor whose heads are contiguous."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_cuda:
+        raise ValueError(f"{what}: expected a {dtype} tensor of shape {tuple(shape)} on {device}")
+    ts, hs, es = t.stride()
+    if es != 1:
+        raise ValueError(f"{what}: the elements of a head have to be contiguous")
+    return t.data_ptr(), ts, hs
+
+
+class KvCache:
+    """A paged cache of attention states (hbl_kv_cache_t) over the caller's tensors:
+
+      k, v              bits 3, 4, 8: uint8 [n_pages, n_kv_heads, page_size, head_dim * bits / 8]; 16: bf16 [..., head_dim]
+      k_scale, v_scale  fp32 [n_pages, n_kv_heads, page_size] (None at 16 bits)
+      bos_k, bos_v      optional, uint8 [n_slots, n_kv_heads, head_dim]; bos_k_scale, bos_v_scale fp32 [n_slots, n_kv_heads]
+    """
+
+    def __init__(self, k, v, k_scale=None, v_scale=None, *, bits: int, bos_k=None, bos_v=None, bos_k_scale=None, bos_v_scale=None):
+        if bits not in (3, 4, 8, 16):
+            raise HblError(4, "KvCache")
+        n_pages, heads, page, row = k.shape
+        self.n_pages, self.n_kv_heads, self.page_size, self.bits, self.device = n_pages, heads, page, bits, k.device
+        self.head_dim = row if bits == 16 else row * 8 // bits
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.bos_k, self.bos_v, self.bos_k_scale, self.bos_v_scale = bos_k, bos_v, bos_k_scale, bos_v_scale
+        dt, dev, f32 = torch.bfloat16 if bits == 16 else torch.uint8, k.device, torch.float32
+        c = self.c = hbl_kv_cache_t()
+        c.k, c.v = _flat(k, dt, k.shape, "k", dev), _flat(v, dt, k.shape, "v", dev)
+        c.k_scale, c.v_scale = _flat(k_scale, f32, k.shape[:3], "k_scale", dev), _flat(v_scale, f32, k.shape[:3], "v_scale", dev)
+        slots = 0
+        if bos_k is not None:
+            slots = bos_k.shape[0]
+        c.bos_k = _flat(bos_k, torch.uint8, (slots, heads, self.head_dim), "bos_k", dev)
+        c.bos_v = _flat(bos_v, torch.uint8, (slots, heads, self.head_dim), "bos_v", dev)
+        c.bos_k_scale = _flat(bos_k_scale, f32, (slots, heads), "bos_k_scale", dev)
+        c.bos_v_scale = _flat(bos_v_scale, f32, (slots, heads), "bos_v_scale", dev)
+        c.n_pages, c.page_size, c.n_kv_heads, c.head_dim, c.bits, c.n_slots = n_pages, page, heads, self.head_dim, bits, slots
+        self.ref = C.byref(c)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, bits: int, bos_slots: int = 0, device="cuda"):
+        """A cache in new memory.  bos_slots > 0 (bits 3 and 4): that many sequences keep their first token at 8 bits."""
+        shape = (n_pages, n_kv_heads, page_size)
+        if bits == 16:
+            return cls(*(torch.zeros(*shape, head_dim, dtype=torch.bfloat16, device=device) for _ in range(2)), bits=16)
+        kv = [torch.zeros(*shape, head_dim * bits // 8, dtype=torch.uint8, device=device) for _ in range(2)]
+        scales = [torch.zeros(shape, dtype=torch.float32, device=device) for _ in range(2)]
+        bos = {}
+        if bos_slots > 0:
+            for n in ("bos_k", "bos_v"):
+                bos[n] = torch.zeros(bos_slots, n_kv_heads, head_dim, dtype=torch.uint8, device=device)
+                bos[n + "_scale"] = torch.zeros(bos_slots, n_kv_heads, dtype=torch.float32, device=device)
+        return cls(*kv, *scales, bits=bits, **bos)
+
+
+class KvBatch:
+    """A batch of sequences over a cache (hbl_kv_batch_t).  q_start int32 [n_seqs + 1], kv_len int32 [n_seqs] (the new
+    tokens included), pages int32 [n_seqs, max_pages]: device tensors, read when the kernels run.  tokens: rows of the
+    calls' tensors; max_q_len, max_kv_len: upper bounds that launch shapes go by (a shorter bound on q leaves rows out)."""
+
+    def __init__(self, q_start, kv_len, pages, *, tokens: int, max_q_len: int, max_kv_len: int, bos_slot=None):
+        n, i32, dev = kv_len.shape[0], torch.int32, kv_len.device
+        self.q_start, self.kv_len, self.pages, self.bos_slot, self.device = q_start, kv_len, pages, bos_slot, dev
+        self.n_seqs, self.tokens = n, tokens
+        c = self.c = hbl_kv_batch_t()
+        c.q_start = _flat(q_start, i32, (n + 1,), "q_start", dev)
+        c.kv_len = _flat(kv_len, i32, (n,), "kv_len", dev)
+        c.pages = _flat(pages, i32, (n, pages.shape[1]), "pages", dev)
+        c.bos_slot = _flat(bos_slot, i32, (n,), "bos_slot", dev)
+        c.n_seqs, c.tokens, c.max_pages, c.max_q_len, c.max_kv_len = n, tokens, pages.shape[1], max_q_len, max_kv_len
+        self.ref = C.byref(c)
+
+
+def hbl_rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = ROPE_PLAIN, factor: float = 1.0,
+                         trained_len: float = 0.0, slow: float = 1.0, fast: float = 4.0) -> list[float]:
+    """Radians per position of the rot_dim / 2 pairs (fp64), stretched for long contexts as `scaling` says."""
+    out = (C.c_double * max(1, rot_dim // 2))()
+    _check(lib().hbl_rope_frequencies(base, rot_dim, scaling, factor, trained_len, slow, fast, out), "hbl_rope_frequencies")
+    return list(out)
+
+
+def hbl_rope_table(freq, n_pos: int, first_pos: int = 0, amplitude: float = 1.0, device="cuda") -> torch.Tensor:
+    """fp32 [n_pos, len(freq), 2]: amplitude * (cos, sin)((first_pos + p) * freq[i])."""
+    table = torch.empty((max(0, n_pos), len(freq), 2), dtype=torch.float32, device=device)
+    host = (C.c_double * max(1, len(freq)))(*freq)
+    _check(lib().hbl_rope_table(host, len(freq), amplitude, first_pos, n_pos, table.data_ptr(), _raw_stream(table.device)),
+           "hbl_rope_table")
+    return table
+
+
+def _rotation(table: torch.Tensor, device) -> tuple[int, int, int]:
+    if table.dim() != 3 or table.shape[2] != 2:
+        raise ValueError("table: expected the result of hbl_rope_table")
+    return _flat(table, torch.float32, table.shape, "table", device), table.shape[0], 2 * table.shape[1]
+
+
+def hbl_rope(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, interleaved: bool = False, backward: bool = False,
+             out: torch.Tensor | None = None) -> torch.Tensor:
+    """Rotary positions on x [tokens, heads, head_dim] (bf16 or fp32; out may be x).  backward: the gradient's rotation."""
+    T, H, D = x.shape
+    dev = x.device
+    if out is None:
+        out = torch.empty((T, H, D), dtype=x.dtype, device=dev)
+    p, ts, hs = _heads(x, (T, H, D), x.dtype, "x", dev)
+    po, ots, ohs = _heads(out, (T, H, D), x.dtype, "out", dev)
+    pt, n_pos, rot = _rotation(table, dev)
+    _check(lib().hbl_rope(p, _dt(x), T, H, D, ts, hs, _flat(positions, torch.int32, (T,), "positions", dev), pt, n_pos, rot,
+                          int(interleaved), int(backward), po, ots, ohs, _raw_stream(dev)), "hbl_rope")
+    return out
+
+
+def hbl_kv_append(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor | None = None,
+                  positions: torch.Tensor | None = None, interleaved: bool = False, q: torch.Tensor | None = None,
+                  q_out: torch.Tensor | None = None, eps: float = 1e-5) -> torch.Tensor | None:
+    """The batch's tokens into the cache: k rotated by `table` (None: as it is), k and v quantized.  q, where given, is
+    rotated by the same launch and returned (q_out may be q)."""
+    dev, T = cache.device, batch.tokens
+    shape = (T, cache.n_kv_heads, cache.head_dim)
+    a = hbl_kv_append_t()
+    a.k, a.k_token_stride, a.k_head_stride = _heads(k, shape, torch.bfloat16, "k", dev)
+    a.v, a.v_token_stride, a.v_head_stride = _heads(v, shape, torch.bfloat16, "v", dev)
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+        shape = (T, q.shape[1], cache.head_dim)
+        a.q, a.q_token_stride, a.q_head_stride = _heads(q, shape, torch.bfloat16, "q", dev)
+        a.q_out, a.q_out_token_stride, a.q_out_head_stride = _heads(q_out, shape, torch.bfloat16, "q_out", dev)
+        a.n_heads = q.shape[1]
+    if table is not None:
+        a.table, a.n_pos, a.rot_dim = _rotation(table, dev)
+    a.positions = _flat(positions, torch.int32, (T,), "positions", dev)
+    a.layout, a.eps = int(interleaved), eps
+    if batch.device != dev:
+        raise ValueError("cache and batch are on different devices")
+    _check(lib().hbl_kv_append(cache.ref, batch.ref, C.byref(a), _raw_stream(dev)), "hbl_kv_append")
+    return q_out
+
+
+def hbl_kv_read(cache: KvCache, batch: KvBatch) -> tuple[torch.Tensor, torch.Tensor]:
+    """The batch's tokens out of the cache: (k, v) bf16 [tokens, n_kv_heads, head_dim]."""
+    shape = (batch.tokens, cache.n_kv_heads, cache.head_dim)
+    k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+    v = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+    if batch.device != cache.device:
+        raise ValueError("cache and batch are on different devices")
+    _check(lib().hbl_kv_read(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), _raw_stream(cache.device)), "hbl_kv_read")
+    return k, v
+
+
+def hbl_attention_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int) -> int:
+    return int(lib().hbl_attention_workspace_bytes(cache.ref, batch.ref, n_heads))
+
+
+def hbl_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, sm_scale: float | None = None, causal: bool = True,
+                  out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                  workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """softmax(sm_scale q K^T) V over the cache, q bf16 [tokens, n_heads, head_dim] -> out of the same shape.  sm_scale:
+    1 / sqrt(head_dim) by default; causal: a token sees the tokens up to itself; lse: fp32 [tokens, n_heads], written."""
+    dev, D = cache.device, cache.head_dim
+    if q.dim() != 3:
+        raise ValueError("q: expected [tokens, n_heads, head_dim]")
+    H = q.shape[1]
+    shape = (batch.tokens, H, D)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    a = hbl_attention_t()
+    a.q, a.q_token_stride, a.q_head_stride = _heads(q, shape, torch.bfloat16, "q", dev)
+    a.out, a.out_token_stride, a.out_head_stride = _heads(out, shape, torch.bfloat16, "out", dev)
+    a.lse = _flat(lse, torch.float32, shape[:2], "lse", dev)
+    a.n_heads, a.causal = H, int(causal)
+    a.sm_scale = D ** -0.5 if sm_scale is None else sm_scale
+    if batch.device != dev:
+        raise ValueError("cache and batch are on different devices")
+    if workspace is None:
+        n = hbl_attention_workspace_bytes(cache, batch, H)
+        workspace = new_workspace(n, dev) if n > 0 else None
+    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    _check(lib().hbl_attention(cache.ref, batch.ref, C.byref(a), ws, size, _raw_stream(dev)), "hbl_attention")
+    return out
 
 
 def hbl_unpack_weights(W_packed: torch.Tensor, out_dim: int, in_dim: int) -> torch.Tensor:
