@@ -73,14 +73,30 @@ int check_batch(const hbl_kv_batch_t* b, BatchView* v) {
 }
 bool nothing(const BatchView& b) { return b.n_seqs == 0 || b.tokens == 0; }
 
-// Workspace of hbl_attention: partial results where the keys of a sequence are split.
-struct AttnWs { size_t part_o, part_lse, total; };
-AttnWs carve_attention(const KvView& c, const BatchView& b, int n_heads, const AttnPlan& p) {
-  AttnWs w{};
-  if (p.splits <= 1) return w;
-  const size_t rows = (size_t)p.splits * b.tokens * n_heads;
+// How a call is made: sequences of up to `few` query rows on the streaming kernel, longer ones on the tensor-core
+// tiles; a single sequence, whose length the bound says, on one of them alone.
+constexpr int kFewRows = 16;
+struct AttnCall {
+  bool use_rows, use_tiles;
+  int few_rows, few_tiles;             // the border as each kernel sees it
+  AttnPlan rows, tiles;
+  size_t part_lse, workspace;          // partial results where the keys of a sequence are split
+};
+AttnCall plan_attention(const KvView& c, const BatchView& b, int n_heads) {
+  AttnCall w{};
+  const int group = n_heads / c.n_kv_heads;
+  w.use_tiles = (long)b.max_q_len * group > kFewRows;
+  w.use_rows = !w.use_tiles || b.n_seqs > 1;
+  w.few_rows = kFewRows;
+  w.few_tiles = w.use_rows ? kFewRows : 0;
+  w.rows.splits = w.tiles.splits = 1;
+  if (w.use_rows) w.rows = plan_attention_rows(c, b, n_heads, w.few_rows);
+  if (w.use_tiles) w.tiles = plan_attention_tiles(c, b, n_heads, w.few_tiles);
+  const int splits = w.rows.splits > w.tiles.splits ? w.rows.splits : w.tiles.splits;
+  if (splits <= 1) return w;
+  const size_t rows = (size_t)splits * b.tokens * n_heads;
   w.part_lse = align_up(rows * c.head_dim * sizeof(float), 1024);
-  w.total = w.part_lse + align_up(rows * sizeof(float), 1024);
+  w.workspace = w.part_lse + align_up(rows * sizeof(float), 1024);
   return w;
 }
 
@@ -180,7 +196,7 @@ size_t hbl_attention_workspace_bytes(const hbl_kv_cache_t* cache, const hbl_kv_b
   BatchView b{};
   if (check_cache(cache, &c) != HBL_OK || check_batch(batch, &b) != HBL_OK || nothing(b)) return 0;
   if (n_heads <= 0 || n_heads % c.n_kv_heads != 0) return 0;
-  return carve_attention(c, b, n_heads, plan_attention_rows(c, b, n_heads)).total;
+  return plan_attention(c, b, n_heads).workspace;
 }
 
 int hbl_attention(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_attention_t* args, void* workspace,
@@ -198,11 +214,10 @@ int hbl_attention(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, cons
   if ((rc = check_strided(args->q, args->q_token_stride, args->q_head_stride)) != HBL_OK) return rc;
   if ((rc = check_strided(args->out, args->out_token_stride, args->out_head_stride)) != HBL_OK) return rc;
   if (!aligned(args->lse, 4)) return HBL_ERR_ALIGN;
-  const AttnPlan plan = plan_attention_rows(c, b, args->n_heads);
-  const AttnWs w = carve_attention(c, b, args->n_heads, plan);
-  if (w.total > 0 && !workspace) return HBL_ERR_NULL;
+  const AttnCall w = plan_attention(c, b, args->n_heads);
+  if (w.workspace > 0 && !workspace) return HBL_ERR_NULL;
   if (!aligned(workspace, 1024)) return HBL_ERR_ALIGN;
-  if (workspace_bytes < w.total) return HBL_ERR_WORKSPACE;
+  if (workspace_bytes < w.workspace) return HBL_ERR_WORKSPACE;
   AttnArgs a{};
   a.q = static_cast<const __nv_bfloat16*>(args->q);
   a.out = static_cast<__nv_bfloat16*>(args->out);
@@ -216,8 +231,9 @@ int hbl_attention(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, cons
   float* part_o = static_cast<float*>(workspace);
   float* part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.part_lse);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if ((rc = launch_attention_rows(c, b, a, plan, part_o, part_lse, s)) != HBL_OK) return rc;
-  if (plan.splits > 1) return launch_attention_combine(c, b, a, plan, part_o, part_lse, s);
+  if (w.use_tiles && (rc = launch_attention_tiles(c, b, a, w.tiles, w.few_tiles, part_o, part_lse, s)) != HBL_OK) return rc;
+  if (w.use_rows && (rc = launch_attention_rows(c, b, a, w.rows, w.few_rows, part_o, part_lse, s)) != HBL_OK) return rc;
+  if (w.workspace > 0) return launch_attention_combine(c, b, a, w.rows, w.tiles, w.few_tiles, part_o, part_lse, s);
   return HBL_OK;
 }
 

@@ -31,6 +31,7 @@ struct RowsParams {
   float* part_o;                 // [splits][tokens * n_heads][head_dim], normalised; splits > 1 only
   float* part_lse;               // [splits][tokens * n_heads], log2 units
   int* status;
+  int few;                       // sequences of more rows than this are another kernel's
 };
 
 template <int BITS, int D>
@@ -68,7 +69,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
   if (!sequence_lengths(p.b, b, p.c.page_shift, p.status, len)) return;
   const int group = p.a.group;
   const int n_rows = min(len.q_len, p.b.max_q_len) * group, r0 = tile * ROWS;
-  if (r0 >= n_rows) return;
+  if (r0 >= n_rows || n_rows > p.few) return;
   const int last_tok = min(r0 + ROWS - 1, n_rows - 1) / group;
   // keys any row of the tile sees, and the piece of them that is this block's (the last piece takes what is left)
   const int seen = p.a.causal ? max(0, min(len.held, len.kv - len.q_len + last_tok + 1)) : len.held;
@@ -372,12 +373,13 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
   }
 }
 
-// The pieces of a row together: out = sum_s 2^(lse_s - top) o_s / sum_s 2^(lse_s - top).  A warp takes one row.
+// The pieces of a row together (whichever kernel computed them): out = sum_s 2^(lse_s - top) o_s / sum_s 2^(lse_s - top).  A warp takes one row.
 struct CombineParams {
   KvView c;
   BatchView b;
   AttnArgs a;
-  AttnPlan p;
+  AttnPlan rows, tiles;          // of sequences of up to `few` rows, and of the others
+  int few;
   const float *part_o, *part_lse;
   int* status;
 };
@@ -392,7 +394,9 @@ __global__ void __launch_bounds__(256) attn_combine_kernel(const __grid_constant
   if (b >= p.b.n_seqs) return;
   SeqLens len;
   if (!sequence_lengths(p.b, b, p.c.page_shift, p.status, len) || tok < len.q0 || tok - len.q0 >= p.b.max_q_len) return;
-  const int pieces = max(1, min(p.p.splits, (len.held + p.p.chunk - 1) / p.p.chunk));
+  const AttnPlan& plan = (long)min(len.q_len, p.b.max_q_len) * p.a.group > p.few ? p.tiles : p.rows;
+  if (plan.splits <= 1) return;                               // written whole
+  const int pieces = max(1, min(plan.splits, (len.held + plan.chunk - 1) / plan.chunk));
   float top = -INFINITY;
   for (int s = lane; s < pieces; s += 32) top = fmaxf(top, p.part_lse[s * total_rows + row]);
 #pragma unroll
@@ -419,13 +423,17 @@ __global__ void __launch_bounds__(256) attn_combine_kernel(const __grid_constant
   if (lane == 0 && p.a.lse != nullptr) p.a.lse[row] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
 }
 
-int rows_per_tile(const BatchView& b, int group) { return (long)b.max_q_len * group > 8 ? 16 : 8; }
+long most_rows(const BatchView& b, int group, int few) {
+  const long rows = (long)b.max_q_len * group;
+  return rows < few ? rows : few;
+}
+int rows_per_tile(const BatchView& b, int group, int few) { return most_rows(b, group, few) > 8 ? 16 : 8; }
 
 template <int BITS, int D>
 int launch_rows_dim(RowsParams& p, cudaStream_t s) {
   const long blocks = (long)p.b.n_seqs * p.c.n_kv_heads * p.p.tiles * p.p.splits;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
-  if (rows_per_tile(p.b, p.a.group) == 8)
+  if (rows_per_tile(p.b, p.a.group, p.few) == 8)
     HBL_CUDA_OK(launch_dependent(attn_rows_kernel<BITS, D, 1>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
   else
     HBL_CUDA_OK(launch_dependent(attn_rows_kernel<BITS, D, 2>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
@@ -444,10 +452,10 @@ int launch_rows_bits(RowsParams& p, cudaStream_t s) {
 
 }  // namespace
 
-AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads) {
+AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads, int few) {
   AttnPlan p{};
-  const int group = n_heads / c.n_kv_heads, rows = rows_per_tile(b, group);
-  p.tiles = (int)(((long)b.max_q_len * group + rows - 1) / rows);
+  const int group = n_heads / c.n_kv_heads, rows = rows_per_tile(b, group, few);
+  p.tiles = (int)((most_rows(b, group, few) + rows - 1) / rows);
   const long base = (long)b.n_seqs * c.n_kv_heads * p.tiles;
   // pieces of at least 256 keys, as many as keep four thread blocks on every SM
   const long want = base > 0 ? ((long)sm_count() * 4 + base - 1) / base : 1;
@@ -461,9 +469,10 @@ AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads) {
   return p;
 }
 
-int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& plan, float* part_o,
+int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& plan, int few, float* part_o,
                           float* part_lse, cudaStream_t s) {
   RowsParams p{};
+  p.few = few;
   p.c = c; p.b = b; p.a = a; p.p = plan; p.part_o = part_o; p.part_lse = part_lse;
   p.status = device_status_word();
   if (p.status == nullptr) return HBL_ERR_CUDA;
@@ -476,10 +485,10 @@ int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a
   }
 }
 
-int launch_attention_combine(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& plan, const float* part_o,
-                             const float* part_lse, cudaStream_t s) {
+int launch_attention_combine(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& rows, const AttnPlan& tiles,
+                             int few, const float* part_o, const float* part_lse, cudaStream_t s) {
   CombineParams p{};
-  p.c = c; p.b = b; p.a = a; p.p = plan; p.part_o = part_o; p.part_lse = part_lse;
+  p.c = c; p.b = b; p.a = a; p.rows = rows; p.tiles = tiles; p.few = few; p.part_o = part_o; p.part_lse = part_lse;
   p.status = device_status_word();
   if (p.status == nullptr) return HBL_ERR_CUDA;
   const long blocks = ((long)b.tokens * a.n_heads + 7) / 8;

@@ -1,0 +1,696 @@
+// Attention of many query rows over the paged cache on the 5th-generation tensor cores: prompts and chunks of them.
+//
+//   S = Q ck^T (tcgen05.mma, fp32 in tensor memory);  s = sm_scale ks_j S;  p = 2^(s - m);  O += (p vs_j) cv
+//
+// A work item is 128 * NSUB query rows of one key head (row r: token r / group, head r % group, so that the heads that
+// share a key head share its tiles) against one piece of the keys.  One thread block per SM stays for all its items:
+//   warps 0-3, 4-7   softmax of sub-tile 0, 1: a thread owns a row: scores out of tensor memory, maximum, exponentials,
+//                    P back into tensor memory as bf16 in the place of the scores; at the end O out of tensor memory
+//   warps 8-11       producers: queries and the tiles of keys and values into shared memory, 128-byte swizzle.  Codes become
+//                    bf16 (exactly) on the way; values beyond the sequence become zeros, whatever the cache holds there
+//   warp 12          one lane issues the matrix instructions
+// The two sub-tiles alternate on the tensor core: while one's scores are being exponentiated the other's products run.
+// Bound by the tensor core and the exponential unit alike at head_dim 128 (256 x 128 scores: 2048 cycles each).
+//
+// The order of the elements inside each group of 8 of a head is free for Q K^T as long as Q and K agree, and for V it only
+// names the columns of O: codes are widened in the order that takes least work (hbl_attn_frag.cuh, `pairs`), the
+// queries are put into the same order when they are loaded, and O's columns are put back when they are written.
+//
+// The maximum is only raised when a score exceeds it by more than 2^8; only then is O rescaled, by the softmax
+// threads themselves (the scores' barrier says that the products before it are complete, so O is at rest).
+#include "hbl_attn_frag.cuh"
+#include "hbl_pipeline.cuh"
+
+namespace hbl {
+namespace {
+
+using namespace frag;
+using namespace pipe;
+
+constexpr int kThreads = 512;
+constexpr float kLazy = 8.f;
+constexpr uint32_t kTmemCols = 512;
+
+template <int D>
+struct TileGeo {
+  static constexpr int NSUB = D == 256 ? 1 : 2;                // sub-tiles of 128 rows
+  static constexpr int BK = D == 256 ? 64 : 128;               // keys per tile
+  static constexpr int ROWS = 128 * NSUB;
+  static constexpr int STAGES = D == 64 ? 3 : 2;
+  static constexpr int Q_BYTES = 128 * D * 2, KV_BYTES = BK * D * 2;
+  static constexpr int HALF = BK * 128;                        // 64 elements wide column of a key / value tile
+  static constexpr size_t SMEM = (size_t)NSUB * Q_BYTES + (size_t)STAGES * 2 * KV_BYTES + (size_t)STAGES * 2 * BK * 4 + 1024;
+  static constexpr uint32_t S_COL = 0, O_COL = NSUB * BK;      // tensor-memory columns
+  // Instruction descriptor of kind::f16: D fp32 (1 at [4,6)), A and B bf16 (1 at [7,10), [10,13)), B MN-major (bit 16)
+  // for the values, N >> 3 at [17,23), M >> 4 at [24,29).
+  static constexpr uint32_t IDESC_QK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BK >> 3) << 17) | (8u << 24);
+  static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);
+};
+
+// Shared-memory descriptors in the 128-byte swizzle (8 rows of 128 bytes make an atom of 1024): start >> 4 at [0,14),
+// leading offset >> 4 at [16,30), stride offset >> 4 at [32,46), version 1 at [46,48), swizzle 2 at [61,64).
+// K-major: the stride is from 8 rows to the next 8.  MN-major (values: rows are keys, 64 elements of the head
+// to a row): the leading offset goes from 64 elements to the next 64, the stride from 8 keys to the next 8.
+__device__ __forceinline__ uint64_t desc_of(uint32_t saddr, uint32_t leading) {
+  return (uint64_t)((saddr >> 4) & 0x3FFF) | ((uint64_t)(leading >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void umma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void umma_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
+        "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]),
+        "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]),
+        "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+        "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+template <int R>
+__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
+template <int R>
+__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {   // 16 bytes to shared memory, zeros if !live
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+// two fp32 operations to an instruction
+__device__ __forceinline__ void mul2(float& a, float& b, float x, float y) {
+  asm("{\n .reg .b64 u, v;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %3};\n mul.rn.f32x2 u, u, v;\n mov.b64 {%0, %1}, u;\n}"
+      : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+__device__ __forceinline__ void fma2(float& a, float& b, float x, float y) {        // a = a * x + y, b = b * x + y
+  asm("{\n .reg .b64 u, v, w;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %2};\n mov.b64 w, {%3, %3};\n fma.rn.f32x2 u, u, v, w;\n mov.b64 {%0, %1}, u;\n}"
+      : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+__device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
+  asm("{\n .reg .b64 u, v;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %3};\n add.rn.f32x2 u, u, v;\n mov.b64 {%0, %1}, u;\n}"
+      : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+
+struct TilesParams {
+  KvView c;
+  BatchView b;
+  AttnArgs a;
+  AttnPlan p;                    // tiles: an upper bound over the whole batch
+  float* part_o;
+  float* part_lse;
+  int* status;
+  int items, few;                // sequences of up to `few` rows are another kernel's (0: none)
+};
+
+// One work item, as every role sees it.
+struct Item {
+  SeqLens len;
+  int b, head, split, r0, n_rows;
+  int key0, key1;                // keys of the piece that any row sees
+  int tiles;                     // of BK keys
+};
+// The whole warp takes part.  False: nothing to do.
+template <int D>
+__device__ __forceinline__ bool decode_item(const TilesParams& p, int item, int lane, Item& o) {
+  using G = TileGeo<D>;
+  o.split = item % p.p.splits;
+  int rest = item / p.p.splits;
+  const int tl = p.p.tiles - 1 - rest % p.p.tiles;             // later rows see more keys: they go first
+  o.head = rest / p.p.tiles;
+  // which sequence the tl-th tile of the batch belongs to
+  int before = 0, b = -1, mine = 0;
+  for (int b0 = 0; b0 < p.b.n_seqs && b < 0; b0 += 32) {
+    int n = 0;
+    if (b0 + lane < p.b.n_seqs) {
+      const int q = min(__ldg(p.b.q_start + b0 + lane + 1) - __ldg(p.b.q_start + b0 + lane), p.b.max_q_len);
+      const long rows = (long)max(q, 0) * p.a.group;
+      n = rows > p.few ? (int)((rows + G::ROWS - 1) / G::ROWS) : 0;
+    }
+    int sum = n;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, sum, s);
+      if (lane >= s) sum += x;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, before + sum > tl);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      b = b0 + l;
+      mine = tl - before - (__shfl_sync(0xffffffffu, sum, l) - __shfl_sync(0xffffffffu, n, l));
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  if (b < 0) return false;
+  o.b = b;
+  if (!sequence_lengths(p.b, b, p.c.page_shift, p.status, o.len)) return false;
+  o.n_rows = min(o.len.q_len, p.b.max_q_len) * p.a.group;
+  o.r0 = mine * G::ROWS;
+  if (o.split > 0 && (long)o.split * p.p.chunk >= o.len.held) return false;
+  const int last_tok = min(o.r0 + G::ROWS - 1, o.n_rows - 1) / p.a.group;
+  const int seen = p.a.causal ? max(0, min(o.len.held, o.len.kv - o.len.q_len + last_tok + 1)) : o.len.held;
+  o.key0 = o.split * p.p.chunk;
+  o.key1 = o.split == p.p.splits - 1 ? seen : min(seen, o.key0 + p.p.chunk);
+  o.tiles = o.key1 > o.key0 ? (o.key1 - o.key0 + G::BK - 1) / G::BK : 0;
+  return true;
+}
+
+// Element e of a group of 8 lies at this place of its 16-byte chunk in shared memory.
+template <int BITS>
+__host__ __device__ constexpr int place_of(int e) {
+  for (int j = 0; j < 4; ++j) {
+    if (pair_lo<BITS>(j) == e) return 2 * j;
+    if (pair_hi<BITS>(j) == e) return 2 * j + 1;
+  }
+  return 0;
+}
+// 16-byte chunk c of row r in a tile of [columns of 64 elements][rows][128 bytes].
+__device__ __forceinline__ uint32_t chunk_at(int r, int c, int half_bytes) {
+  return (uint32_t)((c >> 3) * half_bytes + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+}
+__device__ __forceinline__ void store16(uint32_t saddr, const uint32_t (&w)[4]) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(saddr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+}
+
+template <int BITS, int D>
+__global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_constant__ TilesParams p) {
+  using G = TileGeo<D>;
+  constexpr int NSUB = G::NSUB, BK = G::BK, STAGES = G::STAGES;
+  constexpr bool CODES = BITS < 16;
+  extern __shared__ unsigned char smem_dyn[];
+  __shared__ __align__(8) uint64_t q_full, q_empty, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES], s_full[NSUB], p_full[NSUB],
+      o_full[NSUB];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag_s;
+  volatile int* abort_flag = &abort_flag_s;
+  unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
+  const uint32_t sq = smem_u32(base), sk = sq + NSUB * G::Q_BYTES, sv = sk + STAGES * G::KV_BYTES;
+  float* scales = reinterpret_cast<float*>(base + (size_t)NSUB * G::Q_BYTES + (size_t)STAGES * 2 * G::KV_BYTES);   // [stage][2][BK]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = warp >> 2;
+
+  if (threadIdx.x == 0) {
+    mbar_init(&q_full, 128);
+    mbar_init(&q_empty, 1);
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(&k_full[s], 128);
+      mbar_init(&k_empty[s], CODES ? 1 + 4 * NSUB : 1);        // the last product that reads it, and every warp that read its scales
+      mbar_init(&v_full[s], 128);
+      mbar_init(&v_empty[s], 1);
+    }
+    for (int i = 0; i < NSUB; ++i) {
+      mbar_init(&s_full[i], 1);
+      mbar_init(&p_full[i], 4);
+      mbar_init(&o_full[i], 1);
+    }
+    abort_flag_s = 0;
+    mbar_fence_init();
+  }
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  grid_dependency_wait();
+
+  if (wg < NSUB) {
+    // ------------------------------ softmax: one row to a thread ------------------------------
+    regs_up<184>();
+    const int sub = wg;
+    const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t s_addr = lane_base + G::S_COL + sub * BK, o_addr = lane_base + G::O_COL + sub * D;
+    const float scale = fmaxf(fabsf(p.a.scale_log2), 1e-30f);  // (a negative one: the queries are negated; 0 * -inf is not -inf)
+    uint32_t tile_no = 0, it = 0, done = 0;                    // tiles and items so far: barrier phases
+    bool ok = true;
+    for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+      Item w;
+      if (!decode_item<D>(p, item, lane, w)) continue;
+      const int r = w.r0 + sub * 128 + (threadIdx.x & 127);
+      const bool row_live = r < w.n_rows;
+      const int tok = row_live ? r / p.a.group : 0;
+      int lim = row_live ? (p.a.causal ? min(w.key1, w.len.kv - w.len.q_len + tok + 1) : w.key1) : 0;
+      const int low = __reduce_min_sync(0xffffffffu, row_live ? lim : 0x7fffffff);     // below it this warp masks nothing
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < w.tiles; ++j, ++it) {
+        const int k0 = w.key0 + j * BK;
+        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s_full[sub], tile_no & 1, abort_flag, p.status)))) break;
+        ++tile_no;
+        tc_fence_after();
+        float x[BK];
+#pragma unroll
+        for (int c = 0; c < BK / 32; ++c) tmem_ld32(s_addr + 32 * c, x + 32 * c);
+        const int stage = it % STAGES;
+        const float4* ks = reinterpret_cast<const float4*>(scales + stage * 2 * BK);
+        if (CODES && !(ok = __all_sync(0xffffffffu, mbar_wait(&k_full[stage], (it / STAGES) & 1, abort_flag, p.status)))) break;
+        tmem_ld_wait();
+        if (CODES) {
+#pragma unroll
+          for (int c = 0; c < BK / 4; ++c) {
+            const float4 s = ks[c];
+            mul2(x[4 * c], x[4 * c + 1], s.x, s.y);
+            mul2(x[4 * c + 2], x[4 * c + 3], s.z, s.w);
+          }
+        }
+        const bool masked = k0 + BK > low;
+        if (masked) {
+          const int n = lim - k0;
+#pragma unroll
+          for (int c = 0; c < BK; ++c)
+            if (c >= n) x[c] = -INFINITY;
+        }
+        float t0 = fmaxf(x[0], x[1]), t1 = fmaxf(x[2], x[3]);
+#pragma unroll
+        for (int c = 4; c < BK; c += 4) {
+          t0 = fmaxf(t0, fmaxf(x[c], x[c + 1]));
+          t1 = fmaxf(t1, fmaxf(x[c + 2], x[c + 3]));
+        }
+        const float top = fmaxf(t0, t1) * (CODES ? 1.f : scale);
+        const bool raise = top > m + kLazy;
+        if (__any_sync(0xffffffffu, raise)) {
+          const float m2 = raise ? top : m;
+          const float f = raise ? exp2_approx(m - m2) : 1.f;
+          m = m2;
+          l *= f;
+          if (j > 0) {
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              float o[32];
+              tmem_ld32(o_addr + 32 * c, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] *= f;
+              tmem_st32(o_addr + 32 * c, reinterpret_cast<const uint32_t*>(o));
+            }
+          }
+        }
+        const float neg = m == -INFINITY ? 0.f : -m;
+        float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+        uint32_t pk[32];
+#pragma unroll
+        for (int h = 0; h < BK / 64; ++h) {
+#pragma unroll
+          for (int c = 0; c < 64; c += 4) {
+            float* y = x + 64 * h + c;
+            if (CODES) {
+              add2(y[0], y[1], neg, neg);
+              add2(y[2], y[3], neg, neg);
+            } else {
+              fma2(y[0], y[1], scale, neg);
+              fma2(y[2], y[3], scale, neg);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = exp2_approx(y[e]);
+            add2(s0, s1, y[0], y[1]);
+            add2(s2, s3, y[2], y[3]);
+            if (CODES) {
+              const float4 v = ks[BK / 4 + 16 * h + c / 4];
+              if (masked) {                                     // (0 * a scale that is not finite)
+                const int n = lim - k0 - 64 * h - c;
+                y[0] = n > 0 ? y[0] * v.x : 0.f;
+                y[1] = n > 1 ? y[1] * v.y : 0.f;
+                y[2] = n > 2 ? y[2] * v.z : 0.f;
+                y[3] = n > 3 ? y[3] * v.w : 0.f;
+              } else {
+                mul2(y[0], y[1], v.x, v.y);
+                mul2(y[2], y[3], v.z, v.w);
+              }
+            }
+            pk[c / 2] = pack2(y[0], y[1]);
+            pk[c / 2 + 1] = pack2(y[2], y[3]);
+          }
+          tmem_st32(s_addr + 32 * h, pk);
+        }
+        l += (s0 + s1) + (s2 + s3);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&p_full[sub]);
+          if (CODES) mbar_arrive(&k_empty[stage]);
+        }
+      }
+      if (!ok) break;
+      // ---- the row's result ----
+      if (w.tiles > 0) {
+        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&o_full[sub], done & 1, abort_flag, p.status)))) break;
+        ++done;
+        tc_fence_after();
+      }
+      const float inv = l == 0.f ? 0.f : __fdividef(1.f, l);
+      const float lse2 = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) + __log2f(l);
+      const int hq = w.head * p.a.group + r % p.a.group;
+      const long row = (long)(w.len.q0 + tok) * p.a.n_heads + hq, part = (long)w.split * p.b.tokens * p.a.n_heads + row;
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        float o[32];
+        if (w.tiles > 0) {
+          tmem_ld32(o_addr + 32 * c, o);
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+        }
+        if (row_live && p.p.splits > 1) {
+          float4* dst = reinterpret_cast<float4*>(p.part_o + part * D + 32 * c);
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            dst[e / 4] = make_float4(o[(e & ~7) + place_of<BITS>(e & 7)] * inv, o[(e & ~7) + place_of<BITS>((e + 1) & 7)] * inv,
+                                     o[(e & ~7) + place_of<BITS>((e + 2) & 7)] * inv, o[(e & ~7) + place_of<BITS>((e + 3) & 7)] * inv);
+        } else if (row_live) {
+          uint4* dst = reinterpret_cast<uint4*>(p.a.out + (w.len.q0 + tok) * p.a.o_ts + hq * p.a.o_hs + 32 * c);
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            uint32_t u[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[k] = pack2(o[e + place_of<BITS>(2 * k)] * inv, o[e + place_of<BITS>(2 * k + 1)] * inv);
+            dst[e / 8] = make_uint4(u[0], u[1], u[2], u[3]);
+          }
+        }
+        __syncwarp();
+      }
+      if (row_live) {
+        if (p.p.splits > 1) p.part_lse[part] = lse2;
+        else if (p.a.lse != nullptr) p.a.lse[row] = lse2 * 0.6931471805599453f;
+      }
+      tc_fence_before();                                        // O has been read: the next item's P says so to the issuer
+    }
+  } else if (wg == 2) {
+    // ------------------------------ producers ------------------------------
+    regs_down<88>();
+    const int tid = threadIdx.x & 127;
+    const bool negate = p.a.scale_log2 < 0.f;
+    const float scale = fmaxf(fabsf(p.a.scale_log2), 1e-30f);
+    uint32_t it = 0, items = 0;
+    bool ok = true;
+    for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+      Item w;
+      if (!decode_item<D>(p, item, lane, w) || w.tiles == 0) continue;
+      // ---- queries ----
+      if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(&q_empty, (items & 1) ^ 1, abort_flag, p.status)))) break;
+      ++items;
+      constexpr int CH = D / 8;                                 // 16-byte chunks of a row
+#pragma unroll 8
+      for (int i = tid; i < NSUB * 128 * CH; i += 128) {
+        const int rr = i / CH, c = i % CH, r = w.r0 + rr;
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (r < w.n_rows) {
+          const int tok = r / p.a.group, hq = w.head * p.a.group + r % p.a.group;
+          u = __ldg(reinterpret_cast<const uint4*>(p.a.q + (w.len.q0 + tok) * p.a.q_ts + hq * p.a.q_hs + 8 * c));
+        }
+        const uint32_t y[4] = {u.x, u.y, u.z, u.w};
+        uint32_t o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int lo = pair_lo<BITS>(k), hi = pair_hi<BITS>(k);
+          o[k] = __byte_perm(y[lo / 2], y[hi / 2], (lo & 1 ? 0x32 : 0x10) | (hi & 1 ? 0x7600 : 0x5400)) ^ (negate ? 0x80008000u : 0u);
+        }
+        store16(sq + (rr >> 7) * G::Q_BYTES + chunk_at(rr & 127, c, 128 * 128), o);
+      }
+      fence_async();
+      mbar_arrive(&q_full);
+      // ---- tiles: keys, then values.  bf16 rows are copied asynchronously and announced one copy later, so that
+      // two are in flight; nothing that a wait below needs depends on the one not announced yet ----
+      uint64_t* copied = nullptr;
+      const int* page_row = p.b.pages + (long)w.b * p.b.max_pages;
+      int bos_row = -1;
+      if (CODES && BITS < 8 && p.c.bos_k != nullptr && w.key0 == 0) {
+        const int slot = p.b.bos_slot != nullptr ? __ldg(p.b.bos_slot + w.b) : w.b;
+        if (slot >= 0 && slot < p.c.n_slots) bos_row = slot;
+        else if (tid == 0) report_device_error(p.status, HBL_ERR_RANGE);
+      }
+      for (int j = 0; j < w.tiles; ++j, ++it) {
+        const int stage = it % STAGES, k0 = w.key0 + j * BK;
+        const uint32_t phase = ((it / STAGES) & 1) ^ 1;
+        // pages of the tile's 16-key groups, one to a lane (a tile starts on a multiple of 64 keys)
+        int page = -1;
+        if (lane < BK / 16 && k0 + 16 * lane < w.key1) {
+          page = __ldg(page_row + ((k0 + 16 * lane) >> p.c.page_shift));
+          if (page < 0 || page >= p.c.n_pages) {
+            report_device_error(p.status, HBL_ERR_RANGE);
+            page = -1;
+          }
+        }
+        const bool special = CODES && BITS < 8 && k0 == 0 && p.c.bos_k != nullptr;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          uint64_t* empty = kv == 0 ? &k_empty[stage] : &v_empty[stage];
+          uint64_t* full = kv == 0 ? &k_full[stage] : &v_full[stage];
+          const uint32_t dst = (kv == 0 ? sk : sv) + stage * G::KV_BYTES;
+          const unsigned char* src = kv == 0 ? p.c.k : p.c.v;
+          if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(empty, phase, abort_flag, p.status)))) break;
+          if constexpr (!CODES) {
+            constexpr int RPP = 128 / CH;                       // rows side by side
+#pragma unroll 4
+            for (int i = 0; i < BK / RPP; ++i) {
+              const int rr = i * RPP + tid / CH, c = tid % CH;
+              const int pg = __shfl_sync(0xffffffffu, page, rr >> 4);
+              const bool live = pg >= 0 && k0 + rr < w.key1;
+              const long row = cache_row(p.c, live ? pg : 0, w.head, live ? (k0 + rr) & ((1 << p.c.page_shift) - 1) : 0);
+              copy16(dst + chunk_at(rr, c, G::HALF), src + (row * D + 8 * c) * 2, live);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if (copied != nullptr) {
+              asm volatile("cp.async.wait_group 1;" ::: "memory");
+              fence_async();                                    // what the copies wrote is read next by the tensor cores
+              mbar_arrive(copied);
+            }
+            copied = full;
+          } else {
+            // scales of both with the keys: ks_j * sm_scale * log2(e), vs_j
+            if (kv == 0) {
+              for (int rr = tid; rr < BK; rr += 128) {
+                const int pg = __shfl_sync(0xffffffffu, page, rr >> 4);
+                const bool live = pg >= 0 && k0 + rr < w.key1;
+                const long row = cache_row(p.c, live ? pg : 0, w.head, live ? (k0 + rr) & ((1 << p.c.page_shift) - 1) : 0);
+                float a = live ? __ldg(p.c.k_scale + row) : 0.f, b = live ? __ldg(p.c.v_scale + row) : 0.f;
+                if (special && rr == 0) {
+                  const long brow = (long)bos_row * p.c.n_kv_heads + w.head;
+                  a = bos_row >= 0 ? __ldg(p.c.bos_k_scale + brow) : 0.f;
+                  b = bos_row >= 0 ? __ldg(p.c.bos_v_scale + brow) : 0.f;
+                }
+                scales[stage * 2 * BK + rr] = a * scale;
+                scales[stage * 2 * BK + BK + rr] = b;
+              }
+            }
+            // a lane widens UN units (UN * BITS bytes) of a row
+            constexpr int UN = BITS == 8 ? 2 : 4, LPR = D / 8 / UN, RPP = 128 / LPR;
+            using L1 = Lane<BITS, UN, LPR>;
+            static_assert(L1::UPC == UN, "one piece of the row to a lane");
+            constexpr int BATCH = BK / RPP < 4 ? BK / RPP : 4;
+#pragma unroll 1
+            for (int i0 = 0; i0 < BK / RPP; i0 += BATCH) {
+              L1 raw[BATCH];
+#pragma unroll
+              for (int i = 0; i < BATCH; ++i) {
+                const int rr = (i0 + i) * RPP + tid / LPR;
+                const int pg = __shfl_sync(0xffffffffu, page, rr >> 4);
+                const bool live = pg >= 0 && k0 + rr < w.key1;
+                const long row = cache_row(p.c, live ? pg : 0, w.head, live ? (k0 + rr) & ((1 << p.c.page_shift) - 1) : 0);
+                raw[i].load(src + row * (D * BITS / 8), tid % LPR, live);
+              }
+#pragma unroll
+              for (int i = 0; i < BATCH; ++i) {
+                const int rr = (i0 + i) * RPP + tid / LPR, l = tid % LPR;
+                if (special && rr == 0) continue;
+#pragma unroll
+                for (int u = 0; u < UN; ++u) {
+                  uint32_t o[4];
+                  pairs<BITS>(raw[i], u, l, o);
+                  store16(dst + chunk_at(rr, l * UN + u, G::HALF), o);
+                }
+              }
+            }
+            if (special && tid < CH) {                          // the first token's row from its 8-bit codes
+              uint32_t o[4] = {0, 0, 0, 0};
+              if (bos_row >= 0) {
+                const long brow = (long)bos_row * p.c.n_kv_heads + w.head;
+                const uint2 u = __ldg(reinterpret_cast<const uint2*>((kv == 0 ? p.c.bos_k : p.c.bos_v) + brow * D) + tid);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const int lo = pair_lo<BITS>(k), hi = pair_hi<BITS>(k);
+                  o[k] = pack2((float)((int)(((lo < 4 ? u.x : u.y) >> (8 * (lo & 3))) & 255u) - 128),
+                               (float)((int)(((hi < 4 ? u.x : u.y) >> (8 * (hi & 3))) & 255u) - 128));
+                }
+              }
+              store16(dst + chunk_at(0, tid, G::HALF), o);
+            }
+          }
+          if constexpr (CODES) {
+            fence_async();                                      // generic-proxy writes, read next by the tensor cores
+            mbar_arrive(full);
+          }
+        }
+        if (!ok) break;
+      }
+      if constexpr (!CODES) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        if (ok) {
+          fence_async();
+          mbar_arrive(copied);
+        }
+      }
+    }
+  } else if (wg == 3) {
+    // ------------------------------ issuer ------------------------------
+    regs_down<56>();
+    if (warp == 12) {
+      uint32_t it = 0, items = 0, pn = 0;
+      bool ok = true;
+      for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+        Item w;
+        if (!decode_item<D>(p, item, lane, w) || w.tiles == 0) continue;
+        if (lane == 0) {
+          const uint64_t qd = desc_of(sq, 16), kd = desc_of(sk, 16), vd = desc_of(sv, G::HALF);
+          auto scores = [&](int i, int stage) {
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+              umma_ss(tmem + G::S_COL + i * BK, qd + (uint64_t)((i * G::Q_BYTES + (k >> 2) * (128 * 128) + (k & 3) * 32) >> 4),
+                      kd + (uint64_t)((stage * G::KV_BYTES + (k >> 2) * G::HALF + (k & 3) * 32) >> 4), G::IDESC_QK, k != 0);
+          };
+          do {
+            if (!(ok = mbar_wait(&q_full, items & 1, abort_flag, p.status))) break;
+            if (!(ok = mbar_wait(&k_full[it % STAGES], (it / STAGES) & 1, abort_flag, p.status))) break;
+            tc_fence_after();
+            for (int i = 0; i < NSUB; ++i) {
+              scores(i, it % STAGES);
+              umma_commit(&s_full[i]);
+            }
+            umma_commit(&k_empty[it % STAGES]);
+            if (w.tiles == 1) umma_commit(&q_empty);
+            for (int j = 0; j < w.tiles && ok; ++j, ++it, ++pn) {
+              const int stage = it % STAGES, next = (it + 1) % STAGES;
+              if (!(ok = mbar_wait(&v_full[stage], (it / STAGES) & 1, abort_flag, p.status))) break;
+              for (int i = 0; i < NSUB; ++i) {
+                if (!(ok = mbar_wait(&p_full[i], pn & 1, abort_flag, p.status))) break;
+                tc_fence_after();
+#pragma unroll
+                for (int k = 0; k < BK / 16; ++k)
+                  umma_ts(tmem + G::O_COL + i * D, tmem + G::S_COL + i * BK + 8 * k,
+                          vd + (uint64_t)((stage * G::KV_BYTES + k * 2048) >> 4), G::IDESC_PV, (j | k) != 0);
+                if (j + 1 < w.tiles) {
+                  if (i == 0) {
+                    if (!(ok = mbar_wait(&k_full[next], ((it + 1) / STAGES) & 1, abort_flag, p.status))) break;
+                    tc_fence_after();
+                  }
+                  scores(i, next);
+                  umma_commit(&s_full[i]);
+                  if (i == NSUB - 1) {
+                    umma_commit(&k_empty[next]);
+                    if (j + 2 == w.tiles) umma_commit(&q_empty);   // the item's last scores: its queries may go
+                  }
+                } else {
+                  umma_commit(&o_full[i]);
+                }
+              }
+              if (ok) umma_commit(&v_empty[stage]);
+            }
+          } while (false);
+          ++items;
+        }
+        ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+      }
+    }
+  } else {
+    regs_down<56>();                                            // (head_dim 256: the second softmax group has no sub-tile)
+  }
+
+  // ------------------------------ teardown ------------------------------
+  __syncwarp();
+  if (*abort_flag) {                                            // products in flight may still read shared memory
+    const uint64_t t0 = global_ns();
+    while (global_ns() - t0 < 200000ull) __nanosleep(1000);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 12) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+template <int BITS, int D>
+int launch_tiles_dim(TilesParams& p, cudaStream_t s) {
+  auto kern = attn_tiles_kernel<BITS, D>;
+  HBL_ALLOW_DYNAMIC_SMEM(kern, TileGeo<D>::SMEM);
+  const int grid = p.items < sm_count() ? p.items : sm_count();
+  HBL_CUDA_OK(launch_dependent(kern, dim3(grid), dim3(kThreads), TileGeo<D>::SMEM, s, p));
+  note_launch();
+  return HBL_OK;
+}
+template <int BITS>
+int launch_tiles_bits(TilesParams& p, cudaStream_t s) {
+  switch (p.c.head_dim) {
+    case 64: return launch_tiles_dim<BITS, 64>(p, s);
+    case 128: return launch_tiles_dim<BITS, 128>(p, s);
+    case 256: return launch_tiles_dim<BITS, 256>(p, s);
+    default: return HBL_ERR_SHAPE;
+  }
+}
+
+}  // namespace
+
+AttnPlan plan_attention_tiles(const KvView& c, const BatchView& b, int n_heads, int few) {
+  AttnPlan p{};
+  const int group = n_heads / c.n_kv_heads, rows = c.head_dim == 256 ? 128 : 256;
+  // Whole tiles of all sequences together, and a partial one for each that has more than `few` rows.
+  const long all = (long)b.tokens * group;
+  const long partial = all / (few + 1) < b.n_seqs ? all / (few + 1) : b.n_seqs;
+  long tiles = all / rows + partial;
+  const long by_seq = (long)b.n_seqs * (((long)b.max_q_len * group + rows - 1) / rows);
+  if (by_seq < tiles) tiles = by_seq;
+  p.tiles = (int)(tiles < 0x7fffffffL ? tiles : 0x7fffffffL);
+  const long base = tiles * c.n_kv_heads;
+  // pieces of at least 1024 keys while there are fewer items than SMs
+  const long want = base > 0 && base < sm_count() ? sm_count() / base : 1;
+  const long most = ((long)b.max_kv_len + 1023) / 1024;
+  long n = want < most ? want : most;
+  if (n < 1) n = 1;
+  p.chunk = (int)((((long)b.max_kv_len + n - 1) / n + 127) / 128 * 128);
+  if (p.chunk < 128) p.chunk = 128;
+  p.splits = (int)(((long)b.max_kv_len + p.chunk - 1) / p.chunk);
+  if (p.splits < 1) p.splits = 1;
+  return p;
+}
+
+int launch_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& plan, int few, float* part_o,
+                           float* part_lse, cudaStream_t s) {
+  TilesParams p{};
+  p.c = c; p.b = b; p.a = a; p.p = plan; p.part_o = part_o; p.part_lse = part_lse; p.few = few;
+  p.status = device_status_word();
+  if (p.status == nullptr) return HBL_ERR_CUDA;
+  const long items = (long)plan.tiles * c.n_kv_heads * plan.splits;
+  if (items > 0x7fffffffL - 65536) return HBL_ERR_TOO_LARGE;
+  p.items = (int)items;
+  switch (c.bits) {
+    case 3: return launch_tiles_bits<3>(p, s);
+    case 4: return launch_tiles_bits<4>(p, s);
+    case 8: return launch_tiles_bits<8>(p, s);
+    case 16: return launch_tiles_bits<16>(p, s);
+    default: return HBL_ERR_BITS;
+  }
+}
+
+}  // namespace hbl

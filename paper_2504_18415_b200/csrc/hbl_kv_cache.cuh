@@ -82,10 +82,14 @@ struct AttnArgs {
 };
 // How a call is split: the keys of a sequence go to `splits` thread blocks in pieces of `chunk`.
 struct AttnPlan { int splits, chunk, tiles; };
-AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads);
-int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, float* part_o,
+// Sequences of up to `few` query rows (tokens times heads that share a key head) go to one kernel, the others to the other.
+AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads, int few);
+AttnPlan plan_attention_tiles(const KvView& c, const BatchView& b, int n_heads, int few);
+int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, int few, float* part_o,
                           float* part_lse, cudaStream_t s);
-int launch_attention_combine(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, const float* part_o,
-                             const float* part_lse, cudaStream_t s);
+int launch_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, int few, float* part_o,
+                           float* part_lse, cudaStream_t s);
+int launch_attention_combine(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& rows, const AttnPlan& tiles,
+                             int few, const float* part_o, const float* part_lse, cudaStream_t s);
 
 }  // namespace hbl
