@@ -54,16 +54,25 @@ struct TileGeo {
 __device__ __forceinline__ uint64_t desc_of(uint32_t saddr, uint32_t leading) {
   return (uint64_t)((saddr >> 4) & 0x3FFF) | ((uint64_t)(leading >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
-__device__ __forceinline__ void umma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+// The whole warp comes by these, converged, and `leader` (one lane) issues: the operands then stay in uniform registers,
+// which the instruction takes.  Behind a branch of one lane each would be moved there before every instruction
+// (measured: 150 cycles from one to the next instead of the 64 that the product takes).
+__device__ __forceinline__ void umma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t leader) {
+  asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(leader) : "memory");
 }
-__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t leader) {
+  asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(leader) : "memory");
 }
-__device__ __forceinline__ void umma_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+__device__ __forceinline__ void umma_commit(uint64_t* bar, uint32_t leader) {
+  asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}"
+               ::"r"(smem_u32(bar)), "r"(leader) : "memory");
+}
+__device__ __forceinline__ uint32_t elect_one() {               // one lane of a converged warp
+  uint32_t pred;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(pred));
+  return pred;
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -557,60 +566,55 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
     // ------------------------------ issuer ------------------------------
     regs_down<56>();
     if (warp == 12) {
-      uint32_t it = 0, items = 0, pn = 0;
+      const uint32_t leader = elect_one();
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      const uint64_t qd = desc_of(sq, 16), kd = desc_of(sk, 16), vd = desc_of(sv, G::HALF);
+      uint32_t it = 0, items = 0;
       bool ok = true;
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.status));
+        tc_fence_after();
+        return ok;
+      };
+      auto scores = [&](int i, uint32_t stage) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+          umma_ss(tm + G::S_COL + i * BK, qd + (uint64_t)((i * G::Q_BYTES + (k >> 2) * (128 * 128) + (k & 3) * 32) >> 4),
+                  kd + (uint64_t)((stage * G::KV_BYTES + (k >> 2) * G::HALF + (k & 3) * 32) >> 4), G::IDESC_QK, k != 0, leader);
+        umma_commit(&s_full[i], leader);
+      };
       for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
         Item w;
         if (!decode_item<D>(p, item, lane, w) || w.tiles == 0) continue;
-        if (lane == 0) {
-          const uint64_t qd = desc_of(sq, 16), kd = desc_of(sk, 16), vd = desc_of(sv, G::HALF);
-          auto scores = [&](int i, int stage) {
+        if (!wait(&q_full, items & 1) || !wait(&k_full[it % STAGES], (it / STAGES) & 1)) break;
+        ++items;
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-              umma_ss(tmem + G::S_COL + i * BK, qd + (uint64_t)((i * G::Q_BYTES + (k >> 2) * (128 * 128) + (k & 3) * 32) >> 4),
-                      kd + (uint64_t)((stage * G::KV_BYTES + (k >> 2) * G::HALF + (k & 3) * 32) >> 4), G::IDESC_QK, k != 0);
-          };
-          do {
-            if (!(ok = mbar_wait(&q_full, items & 1, abort_flag, p.status))) break;
-            if (!(ok = mbar_wait(&k_full[it % STAGES], (it / STAGES) & 1, abort_flag, p.status))) break;
-            tc_fence_after();
-            for (int i = 0; i < NSUB; ++i) {
-              scores(i, it % STAGES);
-              umma_commit(&s_full[i]);
-            }
-            umma_commit(&k_empty[it % STAGES]);
-            if (w.tiles == 1) umma_commit(&q_empty);
-            for (int j = 0; j < w.tiles && ok; ++j, ++it, ++pn) {
-              const int stage = it % STAGES, next = (it + 1) % STAGES;
-              if (!(ok = mbar_wait(&v_full[stage], (it / STAGES) & 1, abort_flag, p.status))) break;
-              for (int i = 0; i < NSUB; ++i) {
-                if (!(ok = mbar_wait(&p_full[i], pn & 1, abort_flag, p.status))) break;
-                tc_fence_after();
+        for (int i = 0; i < NSUB; ++i) scores(i, it % STAGES);
+        umma_commit(&k_empty[it % STAGES], leader);
+        if (w.tiles == 1) umma_commit(&q_empty, leader);
+        for (int j = 0; j < w.tiles; ++j, ++it) {
+          const uint32_t stage = it % STAGES, next = (it + 1) % STAGES;
+          const bool more = j + 1 < w.tiles;
+          if (!wait(&v_full[stage], (it / STAGES) & 1)) break;
 #pragma unroll
-                for (int k = 0; k < BK / 16; ++k)
-                  umma_ts(tmem + G::O_COL + i * D, tmem + G::S_COL + i * BK + 8 * k,
-                          vd + (uint64_t)((stage * G::KV_BYTES + k * 2048) >> 4), G::IDESC_PV, (j | k) != 0);
-                if (j + 1 < w.tiles) {
-                  if (i == 0) {
-                    if (!(ok = mbar_wait(&k_full[next], ((it + 1) / STAGES) & 1, abort_flag, p.status))) break;
-                    tc_fence_after();
-                  }
-                  scores(i, next);
-                  umma_commit(&s_full[i]);
-                  if (i == NSUB - 1) {
-                    umma_commit(&k_empty[next]);
-                    if (j + 2 == w.tiles) umma_commit(&q_empty);   // the item's last scores: its queries may go
-                  }
-                } else {
-                  umma_commit(&o_full[i]);
-                }
-              }
-              if (ok) umma_commit(&v_empty[stage]);
+          for (int i = 0; i < NSUB; ++i) {
+            if (!wait(&p_full[i], it & 1)) break;
+#pragma unroll
+            for (int k = 0; k < BK / 16; ++k)
+              umma_ts(tm + G::O_COL + i * D, tm + G::S_COL + i * BK + 8 * k, vd + (uint64_t)((stage * G::KV_BYTES + k * 2048) >> 4),
+                      G::IDESC_PV, (j | k) != 0, leader);
+            if (more) {
+              if (i == 0 && !wait(&k_full[next], ((it + 1) / STAGES) & 1)) break;
+              scores(i, next);
+            } else {
+              umma_commit(&o_full[i], leader);
             }
-          } while (false);
-          ++items;
+          }
+          if (!ok) break;
+          umma_commit(&v_empty[stage], leader);
+          if (more) umma_commit(&k_empty[next], leader);
+          if (j + 2 == w.tiles) umma_commit(&q_empty, leader);   // the item's last scores: its queries may go
         }
-        ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
       }
     }
   } else {
