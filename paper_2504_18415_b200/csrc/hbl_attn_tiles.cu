@@ -39,7 +39,8 @@ struct TileGeo {
   static constexpr int STAGES = D == 64 ? 3 : 2;
   static constexpr int Q_BYTES = 128 * D * 2, KV_BYTES = BK * D * 2;
   static constexpr int HALF = BK * 128;                        // 64 elements wide column of a key / value tile
-  static constexpr size_t SMEM = (size_t)NSUB * Q_BYTES + (size_t)STAGES * 2 * KV_BYTES + (size_t)STAGES * 2 * BK * 4 + 1024;
+  static constexpr int OUT_PITCH = 80, OUT_BYTES = 32 * OUT_PITCH;   // a warp's 32 rows of 64 bytes on their way out
+  static constexpr size_t SMEM = (size_t)NSUB * Q_BYTES + (size_t)STAGES * 2 * KV_BYTES + (size_t)STAGES * 2 * BK * 4 + 4 * NSUB * OUT_BYTES + 1024;
   static constexpr uint32_t S_COL = 0, O_COL = NSUB * BK;      // tensor-memory columns
   // Instruction descriptor of kind::f16: D fp32 (1 at [4,6)), A and B bf16 (1 at [7,10), [10,13)), B MN-major (bit 16)
   // for the values, N >> 3 at [17,23), M >> 4 at [24,29).
@@ -376,8 +377,33 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
       }
       const float inv = l == 0.f ? 0.f : __fdividef(1.f, l);
       const float lse2 = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) + __log2f(l);
-      const int hq = w.head * p.a.group + r % p.a.group;
+      const int hq = w.head * p.a.group + (row_live ? r % p.a.group : 0);
       const long row = (long)(w.len.q0 + tok) * p.a.n_heads + hq, part = (long)w.split * p.b.tokens * p.a.n_heads + row;
+      // 64 bytes of every row at a time go by way of shared memory, so that four lanes write a row's together
+      const bool whole = p.p.splits <= 1;
+      char* mine = whole ? reinterpret_cast<char*>(p.a.out + (w.len.q0 + tok) * p.a.o_ts + hq * p.a.o_hs) : reinterpret_cast<char*>(p.part_o + part * D);
+      if (!row_live) mine = nullptr;
+      char* dst[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        dst[i] = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), 8 * i + lane / 4));
+      const uint32_t out = smem_u32(scales + STAGES * 2 * BK) + (sub * 4 + (warp & 3)) * G::OUT_BYTES;
+      auto write = [&](const uint32_t (&u)[16], int byte) {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t y[4] = {u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]};
+          store16(out + lane * G::OUT_PITCH + 16 * i, y);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t y[4];
+          asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3])
+                       : "r"(out + (8 * i + lane / 4) * G::OUT_PITCH + (lane & 3) * 16) : "memory");
+          if (dst[i] != nullptr) *reinterpret_cast<uint4*>(dst[i] + byte + (lane & 3) * 16) = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+      };
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
         float o[32];
@@ -388,26 +414,23 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0.f;
         }
-        if (row_live && p.p.splits > 1) {
-          float4* dst = reinterpret_cast<float4*>(p.part_o + part * D + 32 * c);
+        auto value = [&](int e) { return o[(e & ~7) + place_of<BITS>(e & 7)] * inv; };
+        uint32_t u[16];
+        if (whole) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            dst[e / 4] = make_float4(o[(e & ~7) + place_of<BITS>(e & 7)] * inv, o[(e & ~7) + place_of<BITS>((e + 1) & 7)] * inv,
-                                     o[(e & ~7) + place_of<BITS>((e + 2) & 7)] * inv, o[(e & ~7) + place_of<BITS>((e + 3) & 7)] * inv);
-        } else if (row_live) {
-          uint4* dst = reinterpret_cast<uint4*>(p.a.out + (w.len.q0 + tok) * p.a.o_ts + hq * p.a.o_hs + 32 * c);
+          for (int e = 0; e < 16; ++e) u[e] = pack2(value(2 * e), value(2 * e + 1));
+          write(u, 64 * c);
+        } else {
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            uint32_t u[4];
+          for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) u[k] = pack2(o[e + place_of<BITS>(2 * k)] * inv, o[e + place_of<BITS>(2 * k + 1)] * inv);
-            dst[e / 8] = make_uint4(u[0], u[1], u[2], u[3]);
+            for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(value(16 * h + e));
+            write(u, 128 * c + 64 * h);
           }
         }
-        __syncwarp();
       }
       if (row_live) {
-        if (p.p.splits > 1) p.part_lse[part] = lse2;
+        if (!whole) p.part_lse[part] = lse2;
         else if (p.a.lse != nullptr) p.a.lse[row] = lse2 * 0.6931471805599453f;
       }
       tc_fence_before();                                        // O has been read: the next item's P says so to the issuer
@@ -423,45 +446,45 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
     for (int n = 0; n * (int)gridDim.x < p.items && ok; ++n) {
       Item w;
       if (!decode_item<D>(p, item_at(n), lane, w) || w.tiles == 0) continue;
-      // ---- tiles: keys, then values.  bf16 rows are copied asynchronously and announced one copy later, so that
-      // two are in flight; nothing that a wait below needs depends on the one not announced yet ----
-      uint64_t* copied = nullptr;
       const int* page_row = p.b.pages + (long)w.b * p.b.max_pages;
-      int bos_row = -1;
-      if (CODES && BITS < 8 && p.c.bos_k != nullptr && w.key0 == 0) {
-        const int slot = p.b.bos_slot != nullptr ? __ldg(p.b.bos_slot + w.b) : w.b;
-        if (slot >= 0 && slot < p.c.n_slots) bos_row = slot;
-        else if (tid == 0) report_device_error(p.status, HBL_ERR_RANGE);
-      }
-      for (int j = 0; j < w.tiles; ++j, ++it) {
-        const int stage = it % STAGES, k0 = w.key0 + j * BK;
-        const uint32_t phase = ((it / STAGES) & 1) ^ 1;
-        // pages of the tile's 16-key groups, one to a lane (a tile starts on a multiple of 64 keys)
-        int page = -1;
-        if (lane < BK / 16 && k0 + 16 * lane < w.key1) {
-          page = __ldg(page_row + ((k0 + 16 * lane) >> p.c.page_shift));
-          if (page < 0 || page >= p.c.n_pages) {
-            report_device_error(p.status, HBL_ERR_RANGE);
-            page = -1;
-          }
-        }
-        const bool special = CODES && BITS < 8 && k0 == 0 && p.c.bos_k != nullptr;
+      // pages of a tile's 16-key groups, one to a lane (a tile starts on a multiple of 64 keys; a group lies in one page)
+      auto page_of = [&](int j) {
+        const int key = w.key0 + j * BK + 16 * lane;
+        return lane < BK / 16 && key < w.key1 ? __ldg(page_row + (key >> p.c.page_shift)) : -1;
+      };
+      struct Tile { long group_row; unsigned good; int there; };
+      auto open = [&](int j, int page) {
+        const int k0 = w.key0 + j * BK;
+        const bool in = page >= 0 && page < p.c.n_pages;
+        if (lane < BK / 16 && k0 + 16 * lane < w.key1 && !in) report_device_error(p.status, HBL_ERR_RANGE);
+        Tile t;
+        t.group_row = cache_row(p.c, in ? page : 0, w.head, (k0 + 16 * lane) & ((1 << p.c.page_shift) - 1));
+        t.good = __ballot_sync(0xffffffffu, in);
+        t.there = w.key1 - k0;                                  // keys of the tile that exist
+        return t;
+      };
+      auto row_of = [&](const Tile& t, int rr) { return __shfl_sync(0xffffffffu, t.group_row, rr >> 4) + (rr & 15); };
+      auto live = [&](const Tile& t, int rr) { return rr < t.there && (t.good >> (rr >> 4) & 1); };
+      int next_page = page_of(0);
+      Tile tile = open(0, next_page);
+      next_page = page_of(1);
+      if constexpr (!CODES) {
+        // bf16 rows are copied asynchronously and announced one copy later, so that two are in flight; nothing that a
+        // wait below needs depends on the one not announced yet
+        uint64_t* copied = nullptr;
+        for (int j = 0; j < w.tiles; ++j, ++it) {
+          const int stage = it % STAGES;
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          uint64_t* empty = kv == 0 ? &k_empty[stage] : &v_empty[stage];
-          uint64_t* full = kv == 0 ? &k_full[stage] : &v_full[stage];
-          const uint32_t dst = (kv == 0 ? sk : sv) + stage * G::KV_BYTES;
-          const unsigned char* src = kv == 0 ? p.c.k : p.c.v;
-          if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(empty, phase, abort_flag, p.status)))) break;
-          if constexpr (!CODES) {
+          for (int kv = 0; kv < 2; ++kv) {
+            uint64_t* empty = kv == 0 ? &k_empty[stage] : &v_empty[stage];
+            if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(empty, ((it / STAGES) & 1) ^ 1, abort_flag, p.status)))) break;
+            const uint32_t dst = (kv == 0 ? sk : sv) + stage * G::KV_BYTES;
+            const unsigned char* col = (kv == 0 ? p.c.k : p.c.v) + (tid % CH) * 16;
             constexpr int RPP = 128 / CH;                       // rows side by side
-#pragma unroll 4
+#pragma unroll
             for (int i = 0; i < BK / RPP; ++i) {
-              const int rr = i * RPP + tid / CH, c = tid % CH;
-              const int pg = __shfl_sync(0xffffffffu, page, rr >> 4);
-              const bool live = pg >= 0 && k0 + rr < w.key1;
-              const long row = cache_row(p.c, live ? pg : 0, w.head, live ? (k0 + rr) & ((1 << p.c.page_shift) - 1) : 0);
-              copy16(dst + chunk_at(rr, c, G::HALF), src + (row * D + 8 * c) * 2, live);
+              const int rr = i * RPP + tid / CH;
+              copy16(dst + chunk_at(rr, tid % CH, G::HALF), col + row_of(tile, rr) * (2 * D), live(tile, rr));
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
             if (copied != nullptr) {
@@ -469,52 +492,97 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
               fence_async();                                    // what the copies wrote is read next by the tensor cores
               mbar_arrive(copied);
             }
-            copied = full;
-          } else {
-            // scales of both with the keys: ks_j * sm_scale * log2(e), vs_j
-            if (kv == 0) {
-              for (int rr = tid; rr < BK; rr += 128) {
-                const int pg = __shfl_sync(0xffffffffu, page, rr >> 4);
-                const bool live = pg >= 0 && k0 + rr < w.key1;
-                const long row = cache_row(p.c, live ? pg : 0, w.head, live ? (k0 + rr) & ((1 << p.c.page_shift) - 1) : 0);
-                float a = live ? __ldg(p.c.k_scale + row) : 0.f, b = live ? __ldg(p.c.v_scale + row) : 0.f;
-                if (special && rr == 0) {
-                  const long brow = (long)bos_row * p.c.n_kv_heads + w.head;
-                  a = bos_row >= 0 ? __ldg(p.c.bos_k_scale + brow) : 0.f;
-                  b = bos_row >= 0 ? __ldg(p.c.bos_v_scale + brow) : 0.f;
+            copied = kv == 0 ? &k_full[stage] : &v_full[stage];
+          }
+          if (!ok) break;
+          if (j + 1 < w.tiles) {
+            tile = open(j + 1, next_page);
+            next_page = page_of(j + 2);
+          }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        if (ok) {
+          fence_async();
+          mbar_arrive(copied);
+        }
+      } else {
+        int bos_row = -1;
+        if (BITS < 8 && p.c.bos_k != nullptr && w.key0 == 0) {
+          const int slot = p.b.bos_slot != nullptr ? __ldg(p.b.bos_slot + w.b) : w.b;
+          if (slot >= 0 && slot < p.c.n_slots) bos_row = slot;
+          else if (tid == 0) report_device_error(p.status, HBL_ERR_RANGE);
+        }
+        // A lane widens UN units (UN * BITS bytes) of a row; BATCH rows of it are loaded while the batch before is
+        // widened, across tiles.
+        constexpr int UN = BITS == 8 ? 2 : 4, LPR = D / 8 / UN, RPP = 128 / LPR, PASSES = BK / RPP;
+        constexpr int BATCH = PASSES < 4 ? PASSES : 4, NB = PASSES / BATCH;
+        using L1 = Lane<BITS, UN, LPR>;
+        static_assert(L1::UPC == UN && PASSES % BATCH == 0, "one piece of a row to a lane, whole batches");
+        struct Raw { L1 r[BATCH]; };
+        auto load = [&](Raw& raw, const Tile& t, int kv, int batch) {
+          const unsigned char* src = kv == 0 ? p.c.k : p.c.v;
+#pragma unroll
+          for (int i = 0; i < BATCH; ++i) {
+            const int rr = (batch * BATCH + i) * RPP + tid / LPR;
+            raw.r[i].load(src + row_of(t, rr) * (D * BITS / 8), tid % LPR, live(t, rr));
+          }
+        };
+        float ks = 0.f, vs = 0.f;                               // scales of key row tid of the tile
+        auto load_scales = [&](const Tile& t) {
+          if (tid >= BK) return;                                // (whole warps)
+          const long row = row_of(t, tid);
+          const bool l = live(t, tid);
+          ks = l ? __ldg(p.c.k_scale + row) : 0.f;
+          vs = l ? __ldg(p.c.v_scale + row) : 0.f;
+        };
+        Raw raw, ahead;
+        load(raw, tile, 0, 0);
+        load_scales(tile);
+        for (int j = 0; j < w.tiles; ++j, ++it) {
+          const int stage = it % STAGES;
+          const bool special = BITS < 8 && w.key0 + j == 0 && p.c.bos_k != nullptr, more = j + 1 < w.tiles;
+          Tile after = tile;
+          if (more) after = open(j + 1, next_page);
+          next_page = page_of(j + 2);
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            const uint32_t dst = (kv == 0 ? sk : sv) + stage * G::KV_BYTES;
+            uint64_t* empty = kv == 0 ? &k_empty[stage] : &v_empty[stage];
+#pragma unroll
+            for (int batch = 0; batch < NB; ++batch) {
+              if (batch + 1 < NB) load(ahead, tile, kv, batch + 1);
+              else if (kv == 0) load(ahead, tile, 1, 0);
+              else if (more) load(ahead, after, 0, 0);
+              if (batch == 0) {
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(empty, ((it / STAGES) & 1) ^ 1, abort_flag, p.status)))) break;
+                if (kv == 0) {
+                  // scales of both with the keys: ks_j * sm_scale * log2(e), vs_j
+                  if (special && tid == 0) {
+                    const long brow = (long)bos_row * p.c.n_kv_heads + w.head;
+                    ks = bos_row >= 0 ? __ldg(p.c.bos_k_scale + brow) : 0.f;
+                    vs = bos_row >= 0 ? __ldg(p.c.bos_v_scale + brow) : 0.f;
+                  }
+                  if (tid < BK) {
+                    scales[stage * 2 * BK + tid] = ks * scale;
+                    scales[stage * 2 * BK + BK + tid] = vs;
+                  }
+                  if (more) load_scales(after);
                 }
-                scales[stage * 2 * BK + rr] = a * scale;
-                scales[stage * 2 * BK + BK + rr] = b;
-              }
-            }
-            // a lane widens UN units (UN * BITS bytes) of a row
-            constexpr int UN = BITS == 8 ? 2 : 4, LPR = D / 8 / UN, RPP = 128 / LPR;
-            using L1 = Lane<BITS, UN, LPR>;
-            static_assert(L1::UPC == UN, "one piece of the row to a lane");
-            constexpr int BATCH = BK / RPP < 4 ? BK / RPP : 4;
-#pragma unroll 1
-            for (int i0 = 0; i0 < BK / RPP; i0 += BATCH) {
-              L1 raw[BATCH];
-#pragma unroll
-              for (int i = 0; i < BATCH; ++i) {
-                const int rr = (i0 + i) * RPP + tid / LPR;
-                const int pg = __shfl_sync(0xffffffffu, page, rr >> 4);
-                const bool live = pg >= 0 && k0 + rr < w.key1;
-                const long row = cache_row(p.c, live ? pg : 0, w.head, live ? (k0 + rr) & ((1 << p.c.page_shift) - 1) : 0);
-                raw[i].load(src + row * (D * BITS / 8), tid % LPR, live);
               }
 #pragma unroll
               for (int i = 0; i < BATCH; ++i) {
-                const int rr = (i0 + i) * RPP + tid / LPR, l = tid % LPR;
+                const int rr = (batch * BATCH + i) * RPP + tid / LPR, l = tid % LPR;
                 if (special && rr == 0) continue;
 #pragma unroll
                 for (int u = 0; u < UN; ++u) {
                   uint32_t o[4];
-                  pairs<BITS>(raw[i], u, l, o);
+                  pairs<BITS>(raw.r[i], u, l, o);
                   store16(dst + chunk_at(rr, l * UN + u, G::HALF), o);
                 }
               }
+              raw = ahead;
             }
+            if (!ok) break;
             if (special && tid < CH) {                          // the first token's row from its 8-bit codes
               uint32_t o[4] = {0, 0, 0, 0};
               if (bos_row >= 0) {
@@ -529,19 +597,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
               }
               store16(dst + chunk_at(0, tid, G::HALF), o);
             }
-          }
-          if constexpr (CODES) {
             fence_async();                                      // generic-proxy writes, read next by the tensor cores
-            mbar_arrive(full);
+            mbar_arrive(kv == 0 ? &k_full[stage] : &v_full[stage]);
           }
-        }
-        if (!ok) break;
-      }
-      if constexpr (!CODES) {
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        if (ok) {
-          fence_async();
-          mbar_arrive(copied);
+          if (!ok) break;
+          tile = after;
         }
       }
     }
