@@ -4,7 +4,7 @@
 //
 // A work item is 128 * NSUB query rows of one key head (row r: token r / group, head r % group, so that the heads that
 // share a key head share its tiles) against one piece of the keys.  One thread block per SM stays for all its items:
-//   warps 0-3, 4-7   softmax of sub-tile 0, 1: a thread owns a row: scores out of tensor memory, maximum, exponentials,
+//   warps 0-3, 4-7   softmax of sub-tile 0, 1: scores out of tensor memory, maximum, exponentials,
 //                    P back into tensor memory as bf16 in the place of the scores; at the end O out of tensor memory
 //   warps 8-11       producers: the tiles of keys and values into shared memory, 128-byte swizzle.  Codes become bf16
 //                    (exactly) on the way; values beyond the sequence become zeros, whatever the cache holds there
@@ -20,6 +20,8 @@
 // threads themselves (the scores' barrier says that the products before it are complete, so O is at rest).
 #include "hbl_attn_frag.cuh"
 #include "hbl_pipeline.cuh"
+
+#include <type_traits>
 
 namespace hbl {
 namespace {
@@ -77,27 +79,29 @@ __device__ __forceinline__ uint32_t elect_one() {               // one lane of a
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
-        "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]),
-        "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]),
-        "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
-      : "r"(taddr)
-      : "memory");
+// Tensor memory in the layout of an mma.m16n8 result: 16 lanes (rows), a thread holds of every 8 columns the columns
+// 2t, 2t + 1 of row g (registers 0, 1) and of row g + 8 (2, 3), g = lane / 4, t = lane % 4.  Against one row to a thread
+// this leaves a thread a quarter of the columns, and so of the keys' scales, for four rows.
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float* r) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+               : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
-        "r"(r[30]), "r"(r[31])
-      : "memory");
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* r) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+               : "r"(taddr) : "memory");
+}
+// ... and 4 columns of 32 bits (8 bf16 values) at a time: row g column t (register 0), row g + 8 (1).
+__device__ __forceinline__ void tmem_st_o(uint32_t taddr, const float* r) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+               ::"r"(taddr), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15])
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_p(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+               : "memory");
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -114,9 +118,9 @@ __device__ __forceinline__ void mul2(float& a, float& b, float x, float y) {
   asm("{\n .reg .b64 u, v;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %3};\n mul.rn.f32x2 u, u, v;\n mov.b64 {%0, %1}, u;\n}"
       : "+f"(a), "+f"(b) : "f"(x), "f"(y));
 }
-__device__ __forceinline__ void fma2(float& a, float& b, float x, float y) {        // a = a * x + y, b = b * x + y
-  asm("{\n .reg .b64 u, v, w;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %2};\n mov.b64 w, {%3, %3};\n fma.rn.f32x2 u, u, v, w;\n mov.b64 {%0, %1}, u;\n}"
-      : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+__device__ __forceinline__ void fma2(float& a, float& b, float x0, float x1, float y) {   // a = a * x0 + y, b = b * x1 + y
+  asm("{\n .reg .b64 u, v, w;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %3};\n mov.b64 w, {%4, %4};\n fma.rn.f32x2 u, u, v, w;\n mov.b64 {%0, %1}, u;\n}"
+      : "+f"(a), "+f"(b) : "f"(x0), "f"(x1), "f"(y));
 }
 __device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
   asm("{\n .reg .b64 u, v;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %3};\n add.rn.f32x2 u, u, v;\n mov.b64 {%0, %1}, u;\n}"
@@ -132,7 +136,12 @@ struct TilesParams {
   float* part_lse;
   int* status;
   int items, few;                // sequences of up to `few` rows are another kernel's (0: none)
+  uint32_t div_mul;              // r / group = (umulhi(r, div_mul) + r) >> div_shift for 0 <= r < 2^31
+  int div_shift;
 };
+__device__ __forceinline__ int token_of(const TilesParams& p, int r) {
+  return (int)((__umulhi((uint32_t)r, p.div_mul) + (uint32_t)r) >> p.div_shift);
+}
 
 // The n-th item of this thread block.  Items come in falling order of work (causal); every second round of the grid
 // is dealt backwards, so that nobody gets the larger one every time (measured on an 8192-token prompt, 1024 items: the
@@ -185,7 +194,7 @@ __device__ __forceinline__ bool decode_item(const TilesParams& p, int item, int 
   o.n_rows = min(o.len.q_len, p.b.max_q_len) * p.a.group;
   o.r0 = mine * G::ROWS;
   if (o.split > 0 && (long)o.split * p.p.chunk >= o.len.held) return false;
-  const int last_tok = min(o.r0 + G::ROWS - 1, o.n_rows - 1) / p.a.group;
+  const int last_tok = token_of(p, min(o.r0 + G::ROWS - 1, o.n_rows - 1));
   const int seen = p.a.causal ? max(0, min(o.len.held, o.len.kv - o.len.q_len + last_tok + 1)) : o.len.held;
   o.key0 = o.split * p.p.chunk;
   o.key1 = o.split == p.p.splits - 1 ? seen : min(seen, o.key0 + p.p.chunk);
@@ -193,15 +202,6 @@ __device__ __forceinline__ bool decode_item(const TilesParams& p, int item, int 
   return true;
 }
 
-// Element e of a group of 8 lies at this place of its 16-byte chunk in shared memory.
-template <int BITS>
-__host__ __device__ constexpr int place_of(int e) {
-  for (int j = 0; j < 4; ++j) {
-    if (pair_lo<BITS>(j) == e) return 2 * j;
-    if (pair_hi<BITS>(j) == e) return 2 * j + 1;
-  }
-  return 0;
-}
 // 16-byte chunk c of row r in a tile of [columns of 64 elements][rows][128 bytes].
 __device__ __forceinline__ uint32_t chunk_at(int r, int c, int half_bytes) {
   return (uint32_t)((c >> 3) * half_bytes + r * 128 + (((c & 7) ^ (r & 7)) << 4));
@@ -254,190 +254,262 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
   grid_dependency_wait();
 
   if (wg < NSUB) {
-    // ------------------------------ softmax: one row to a thread ------------------------------
-    regs_up<184>();
-    const int sub = wg;
-    const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    // ------------------------------ softmax: four rows to a thread, a quarter of the columns ------------------------------
+    regs_up<192>();
+    const int sub = wg, g = lane >> 2, t = lane & 3, quad = warp & 3;
+    const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
     const uint32_t s_addr = lane_base + G::S_COL + sub * BK, o_addr = lane_base + G::O_COL + sub * D;
+    constexpr uint32_t LOWER = 16u << 16;                      // rows 16 .. 31 of the warp
     const float scale = fmaxf(fabsf(p.a.scale_log2), 1e-30f);  // (a negative one: the queries are negated; 0 * -inf is not -inf)
-    uint32_t tile_no = 0, it = 0, done = 0;                    // tiles and items so far: barrier phases
+    uint32_t it = 0, done = 0;                                 // tiles and items so far: barrier phases
     bool ok = true;
     for (int n = 0; n * (int)gridDim.x < p.items && ok; ++n) {
       Item w;
       if (!decode_item<D>(p, item_at(n), lane, w)) continue;
-      const int r = w.r0 + sub * 128 + (threadIdx.x & 127);
-      const bool row_live = r < w.n_rows;
-      const int tok = row_live ? r / p.a.group : 0;
-      int lim = row_live ? (p.a.causal ? min(w.key1, w.len.kv - w.len.q_len + tok + 1) : w.key1) : 0;
-      const int low = __reduce_min_sync(0xffffffffu, row_live ? lim : 0x7fffffff);     // below it this warp masks nothing
-      float m = -INFINITY, l = 0.f;
+      // the thread's rows: first + 8 i
+      const int first = w.r0 + sub * 128 + quad * 32 + g;
+      int lim[4], low = 0x7fffffff;                            // keys below lim are seen; below low the warp masks nothing
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = first + 8 * i;
+        lim[i] = r >= w.n_rows ? 0 : p.a.causal ? min(w.key1, w.len.kv - w.len.q_len + token_of(p, r) + 1) : w.key1;
+        if (r < w.n_rows) low = min(low, lim[i]);
+      }
+      low = __reduce_min_sync(0xffffffffu, low);
+      float m[4], l[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
       for (int j = 0; j < w.tiles; ++j, ++it) {
         const int k0 = w.key0 + j * BK;
-        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s_full[sub], tile_no & 1, abort_flag, p.status)))) break;
-        ++tile_no;
-        tc_fence_after();
-        float x[BK];
-#pragma unroll
-        for (int c = 0; c < BK / 32; ++c) tmem_ld32(s_addr + 32 * c, x + 32 * c);
         const int stage = it % STAGES;
-        const float4* ks = reinterpret_cast<const float4*>(scales + stage * 2 * BK);
-        if (CODES && !(ok = __all_sync(0xffffffffu, mbar_wait(&k_full[stage], (it / STAGES) & 1, abort_flag, p.status)))) break;
+        if (CODES && !(ok = __all_sync(0xffffffffu, mbar_wait(&k_full[stage], (it / STAGES) & 1, abort_flag, p.status)))) break;   // its scales
+        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s_full[sub], it & 1, abort_flag, p.status)))) break;
+        tc_fence_after();
+        float x[2][BK / 2];                                    // [rows 0 .. 15 | 16 .. 31][column / 8][4]
+#pragma unroll
+        for (int h = 0; h < BK / 64; ++h) {
+          tmem_ld64(s_addr + 64 * h, x[0] + 32 * h);
+          tmem_ld64(s_addr + LOWER + 64 * h, x[1] + 32 * h);
+        }
+        const float2* ks = reinterpret_cast<const float2*>(scales + stage * 2 * BK) + t;
+        const float2* vs = ks + BK / 2;
         tmem_ld_wait();
+        const bool masked = k0 + BK > low;
+        float neg[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) neg[i] = m[i] == -INFINITY ? 0.f : -m[i];
+        // codes: scores relative to the maximum so far (bf16: the products alone, in units of which the mask and the
+        // maximum are the same)
         if (CODES) {
 #pragma unroll
-          for (int c = 0; c < BK / 4; ++c) {
-            const float4 s = ks[c];
-            mul2(x[4 * c], x[4 * c + 1], s.x, s.y);
-            mul2(x[4 * c + 2], x[4 * c + 3], s.z, s.w);
+          for (int c = 0; c < BK / 8; ++c) {
+            const float2 s = ks[4 * c];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float* y = &x[i >> 1][4 * c + 2 * (i & 1)];
+              fma2(y[0], y[1], s.x, s.y, neg[i]);
+            }
           }
         }
-        const bool masked = k0 + BK > low;
         if (masked) {
-          const int n = lim - k0;
 #pragma unroll
-          for (int c = 0; c < BK; ++c)
-            if (c >= n) x[c] = -INFINITY;
+          for (int i = 0; i < 4; ++i) {
+            const int seen = lim[i] - k0 - 2 * t;
+#pragma unroll
+            for (int c = 0; c < BK / 8; ++c) {
+              float* y = &x[i >> 1][4 * c + 2 * (i & 1)];
+              if (8 * c >= seen) y[0] = -INFINITY;
+              if (8 * c + 1 >= seen) y[1] = -INFINITY;
+            }
+          }
         }
-        float t[4] = {x[0], x[1], x[2], x[3]};
+        float top[4];                                           // how far the tile's largest score lies above the maximum
+        bool raise = false;
 #pragma unroll
-        for (int c = 4; c < BK - 4; c += 8)
+        for (int i = 0; i < 4; ++i) {
+          const float* y = &x[i >> 1][2 * (i & 1)];
+          float a = fmaxf(y[0], y[1]), b = fmaxf(y[4], y[5]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) t[e] = fmaxf(t[e], fmaxf(x[c + e], x[c + 4 + e]));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) t[e] = fmaxf(t[e], x[BK - 4 + e]);
-        const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * (CODES ? 1.f : scale);
-        const bool raise = top > m + kLazy;
+          for (int c = 2; c < BK / 8; c += 2) {
+            a = fmaxf(a, fmaxf(y[4 * c], y[4 * c + 1]));
+            b = fmaxf(b, fmaxf(y[4 * c + 4], y[4 * c + 5]));
+          }
+          top[i] = CODES ? fmaxf(a, b) : fmaf(fmaxf(a, b), scale, neg[i]);
+          raise |= top[i] > (m[i] == -INFINITY ? -INFINITY : kLazy);
+        }
         if (__any_sync(0xffffffffu, raise)) {
-          const float m2 = raise ? top : m;
-          const float f = raise ? exp2_approx(m - m2) : 1.f;
-          m = m2;
-          l *= f;
+          float f[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+            top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+            const bool first_key = m[i] == -INFINITY;
+            const bool up = top[i] > (first_key ? -INFINITY : kLazy);
+            const float by = up ? top[i] : 0.f;                 // how far the maximum rises (from 0 where there was none)
+            f[i] = up ? (first_key ? 0.f : exp2_approx(-by)) : 1.f;
+            if (up) m[i] = by - neg[i];
+            l[i] *= f[i];
+            if (CODES) {
+#pragma unroll
+              for (int c = 0; c < BK / 8; ++c) {
+                float* y = &x[i >> 1][4 * c + 2 * (i & 1)];
+                add2(y[0], y[1], -by, -by);
+              }
+            } else {
+              neg[i] -= by;
+            }
+          }
           if (j > 0) {
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
-              float o[32];
-              tmem_ld32(o_addr + 32 * c, o);
-              tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] *= f;
-              tmem_st32(o_addr + 32 * c, reinterpret_cast<const uint32_t*>(o));
+              for (int h = 0; h < 2; ++h) {
+                float o[16];
+                tmem_ld32(o_addr + h * LOWER + 32 * c, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] *= f[2 * h + (e >> 1 & 1)];
+                tmem_st_o(o_addr + h * LOWER + 32 * c, o);
+              }
             }
           }
         }
-        const float neg = m == -INFINITY ? 0.f : -m;
-        float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-        uint32_t pk[32];
-#pragma unroll
-        for (int h = 0; h < BK / 64; ++h) {
-#pragma unroll
-          for (int c = 0; c < 64; c += 4) {
-            float* y = x + 64 * h + c;
-            if (CODES) {
-              add2(y[0], y[1], neg, neg);
-              add2(y[2], y[3], neg, neg);
-            } else {
-              fma2(y[0], y[1], scale, neg);
-              fma2(y[2], y[3], scale, neg);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = exp2_approx(y[e]);
-            add2(s0, s1, y[0], y[1]);
-            add2(s2, s3, y[2], y[3]);
-            if (CODES) {
-              const float4 v = ks[BK / 4 + 16 * h + c / 4];
-              if (masked) {                                     // (0 * a scale that is not finite)
-                const int n = lim - k0 - 64 * h - c;
-                y[0] = n > 0 ? y[0] * v.x : 0.f;
-                y[1] = n > 1 ? y[1] * v.y : 0.f;
-                y[2] = n > 2 ? y[2] * v.z : 0.f;
-                y[3] = n > 3 ? y[3] * v.w : 0.f;
-              } else {
-                mul2(y[0], y[1], v.x, v.y);
-                mul2(y[2], y[3], v.z, v.w);
-              }
-            }
-            pk[c / 2] = pack2(y[0], y[1]);
-            pk[c / 2 + 1] = pack2(y[2], y[3]);
-          }
-          tmem_st32(s_addr + 32 * h, pk);                       // 64 keys at a time: their product starts while the rest is computed
+        float sum[4][2] = {};
+        // 64 keys are handed over at a time, so that their product starts while the rest is computed; the hand-over waits
+        // for the stores, and so comes after the next 32 keys' exponentials have been started
+        auto hand_over = [&](int h) {
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&p_full[sub][h]);
-        }
-        l += (s0 + s1) + (s2 + s3);
+        };
+        // SELECT: a masked key's value scale may be anything (0 * it is not 0)
+        auto exponentials = [&](auto select) {
+          constexpr bool SELECT = decltype(select)::value;
+#pragma unroll
+          for (int h = 0; h < BK / 64; ++h) {
+            uint32_t pk[2][16];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              const float2 v = CODES ? vs[4 * (8 * h + c)] : make_float2(1.f, 1.f);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                float* y = &x[i >> 1][32 * h + 4 * c + 2 * (i & 1)];
+                if (!CODES) fma2(y[0], y[1], scale, scale, neg[i]);
+                y[0] = exp2_approx(y[0]);
+                y[1] = exp2_approx(y[1]);
+                add2(sum[i][0], sum[i][1], y[0], y[1]);
+                if (SELECT) {
+                  const int seen = lim[i] - k0 - 2 * t - 64 * h - 8 * c;
+                  y[0] = seen > 0 ? y[0] * v.x : 0.f;
+                  y[1] = seen > 1 ? y[1] * v.y : 0.f;
+                } else if (CODES) {
+                  mul2(y[0], y[1], v.x, v.y);
+                }
+                pk[i >> 1][2 * c + (i & 1)] = pack2(y[0], y[1]);
+              }
+              if (h > 0 && c == 3) hand_over(h - 1);
+            }
+            tmem_st_p(s_addr + 32 * h, pk[0]);
+            tmem_st_p(s_addr + LOWER + 32 * h, pk[1]);
+          }
+          hand_over(BK / 64 - 1);
+        };
+        if (CODES && masked) exponentials(std::true_type{});
+        else exponentials(std::false_type{});
+#pragma unroll
+        for (int i = 0; i < 4; ++i) l[i] += sum[i][0] + sum[i][1];
         if (CODES && lane == 0) mbar_arrive(&k_empty[stage]);
       }
       if (!ok) break;
-      // ---- the row's result ----
+      // ---- the rows' results ----
       if (w.tiles > 0) {
         if (!(ok = __all_sync(0xffffffffu, mbar_wait(&o_full[sub], done & 1, abort_flag, p.status)))) break;
         ++done;
         tc_fence_after();
       }
-      const float inv = l == 0.f ? 0.f : __fdividef(1.f, l);
-      const float lse2 = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) + __log2f(l);
-      const int hq = w.head * p.a.group + (row_live ? r % p.a.group : 0);
-      const long row = (long)(w.len.q0 + tok) * p.a.n_heads + hq, part = (long)w.split * p.b.tokens * p.a.n_heads + row;
-      // 64 bytes of every row at a time go by way of shared memory, so that four lanes write a row's together
       const bool whole = p.p.splits <= 1;
-      char* mine = whole ? reinterpret_cast<char*>(p.a.out + (w.len.q0 + tok) * p.a.o_ts + hq * p.a.o_hs) : reinterpret_cast<char*>(p.part_o + part * D);
-      if (!row_live) mine = nullptr;
-      char* dst[4];
+      float inv[4];
+      char* dst[4];                                             // of the rows that this thread writes: lane / 4 + 8 i
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        dst[i] = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), 8 * i + lane / 4));
-      const uint32_t out = smem_u32(scales + STAGES * 2 * BK) + (sub * 4 + (warp & 3)) * G::OUT_BYTES;
-      auto write = [&](const uint32_t (&u)[16], int byte) {
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t y[4] = {u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]};
-          store16(out + lane * G::OUT_PITCH + 16 * i, y);
+      for (int i = 0; i < 4; ++i) {
+        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+        inv[i] = l[i] == 0.f ? 0.f : __fdividef(1.f, l[i]);
+        const int r = first + 8 * i;
+        dst[i] = nullptr;
+        if (r < w.n_rows) {
+          const int tok = token_of(p, r), hq = w.head * p.a.group + r - tok * p.a.group;
+          const long row = (long)(w.len.q0 + tok) * p.a.n_heads + hq, part = (long)w.split * p.b.tokens * p.a.n_heads + row;
+          dst[i] = whole ? reinterpret_cast<char*>(p.a.out + (w.len.q0 + tok) * p.a.o_ts + hq * p.a.o_hs) : reinterpret_cast<char*>(p.part_o + part * D);
+          const float lse2 = l[i] == 0.f ? -INFINITY : (m[i] == -INFINITY ? 0.f : m[i]) + __log2f(l[i]);
+          if (t == 0 && !whole) p.part_lse[part] = lse2;
+          if (t == 0 && whole && p.a.lse != nullptr) p.a.lse[row] = lse2 * 0.6931471805599453f;
         }
+      }
+      // 64 bytes of every row at a time go by way of shared memory, where they get back into order and from where four
+      // lanes write a row's together
+      const uint32_t out = smem_u32(scales + STAGES * 2 * BK) + (sub * 4 + quad) * G::OUT_BYTES;
+      auto flush = [&](int byte) {
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t y[4];
           asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3])
-                       : "r"(out + (8 * i + lane / 4) * G::OUT_PITCH + (lane & 3) * 16) : "memory");
-          if (dst[i] != nullptr) *reinterpret_cast<uint4*>(dst[i] + byte + (lane & 3) * 16) = make_uint4(y[0], y[1], y[2], y[3]);
+                       : "r"(out + (8 * i + g) * G::OUT_PITCH + t * 16) : "memory");
+          if (dst[i] != nullptr) *reinterpret_cast<uint4*>(dst[i] + byte + t * 16) = make_uint4(y[0], y[1], y[2], y[3]);
         }
+        __syncwarp();
       };
+      const int e0 = BITS == 16 ? 2 * t : BITS == 8 ? pair_lo<8>(t) : t, e1 = BITS == 16 ? 2 * t + 1 : BITS == 8 ? pair_hi<8>(t) : t + 4;
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
-        float o[32];
+        float o[2][16];
         if (w.tiles > 0) {
-          tmem_ld32(o_addr + 32 * c, o);
+          tmem_ld32(o_addr + 32 * c, o[0]);
+          tmem_ld32(o_addr + LOWER + 32 * c, o[1]);
           tmem_ld_wait();
         } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+          for (int e = 0; e < 16; ++e) o[0][e] = o[1][e] = 0.f;
         }
-        auto value = [&](int e) { return o[(e & ~7) + place_of<BITS>(e & 7)] * inv; };
-        uint32_t u[16];
+        // a thread's columns 2t, 2t + 1 of each group of 8 are the head's elements e0, e1 of that group
         if (whole) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) u[e] = pack2(value(2 * e), value(2 * e + 1));
-          write(u, 64 * c);
+          for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float* y = &o[i >> 1][4 * q + 2 * (i & 1)];
+              const uint32_t u = pack2(y[0] * inv[i], y[1] * inv[i]), at = out + (8 * i + g) * G::OUT_PITCH + 16 * q;
+              if constexpr (!CODES) {
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + 4 * t), "r"(u) : "memory");
+                continue;
+              }
+              asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + 2 * e0), "h"((unsigned short)u) : "memory");
+              asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + 2 * e1), "h"((unsigned short)(u >> 16)) : "memory");
+            }
+          flush(64 * c);
         } else {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(value(16 * h + e));
-            write(u, 128 * c + 64 * h);
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float* y = &o[i >> 1][4 * (2 * h + q) + 2 * (i & 1)];
+                const uint32_t at = out + (8 * i + g) * G::OUT_PITCH + 32 * q;
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 4 * e0), "f"(y[0] * inv[i]) : "memory");
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 4 * e1), "f"(y[1] * inv[i]) : "memory");
+              }
+            flush(128 * c + 64 * h);
           }
         }
-      }
-      if (row_live) {
-        if (!whole) p.part_lse[part] = lse2;
-        else if (p.a.lse != nullptr) p.a.lse[row] = lse2 * 0.6931471805599453f;
       }
       tc_fence_before();                                        // O has been read: the next item's P says so to the issuer
     }
   } else if (wg == 2) {
     // ------------------------------ producers ------------------------------
-    regs_down<88>();
+    regs_down<80>();
     const int tid = threadIdx.x & 127;
     constexpr int CH = D / 8;                                   // 16-byte chunks of a row
     const float scale = fmaxf(fabsf(p.a.scale_log2), 1e-30f);
@@ -607,7 +679,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
     }
   } else if (wg == 3) {
     // ------------------------------ issuer, and the queries ------------------------------
-    regs_down<56>();
+    regs_down<48>();
     if (warp == 12) {
       const uint32_t leader = elect_one();
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
@@ -675,8 +747,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         if (!decode_item<D>(p, item_at(n), lane, w) || w.tiles == 0) continue;
         if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(&q_empty, (items & 1) ^ 1, abort_flag, p.status)))) break;
         ++items;
-        const int c = tid % CH, first = tid / CH, step_tok = RPP / p.a.group, step_rem = RPP % p.a.group;
-        int tok = (w.r0 + first) / p.a.group, rem = (w.r0 + first) % p.a.group;
+        const int c = tid % CH, first = tid / CH, step_tok = token_of(p, RPP), step_rem = RPP - step_tok * p.a.group;
+        int tok = token_of(p, w.r0 + first), rem = w.r0 + first - tok * p.a.group;
         const __nv_bfloat16* q = p.a.q + w.len.q0 * p.a.q_ts + (long)w.head * p.a.group * p.a.q_hs + 8 * c;
         for (int rr = first; rr < N && first < RPP; rr += RPP) {
           const bool live = w.r0 + rr < w.n_rows;
@@ -706,7 +778,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
       }
     }
   } else {
-    regs_down<56>();                                            // (head_dim 256: the second softmax group has no sub-tile)
+    regs_down<48>();                                            // (head_dim 256: the second softmax group has no sub-tile)
   }
 
   // ------------------------------ teardown ------------------------------
@@ -776,6 +848,8 @@ int launch_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& 
   const long items = (long)plan.tiles * c.n_kv_heads * plan.splits;
   if (items > 0x7fffffffL - 65536) return HBL_ERR_TOO_LARGE;
   p.items = (int)items;
+  while ((1 << p.div_shift) < a.group) ++p.div_shift;
+  p.div_mul = (uint32_t)(((((uint64_t)1 << p.div_shift) - a.group) << 32) / a.group + 1);
   switch (c.bits) {
     case 3: return launch_tiles_bits<3>(p, s);
     case 4: return launch_tiles_bits<4>(p, s);
