@@ -8,7 +8,7 @@
 //                    P back into tensor memory as bf16 in the place of the scores; at the end O out of tensor memory
 //   warps 8-11       producers: the tiles of keys and values into shared memory, 128-byte swizzle.  Codes become bf16
 //                    (exactly) on the way; values beyond the sequence become zeros, whatever the cache holds there
-//   warp 12          issues the matrix instructions;  warps 13-15: the queries into shared memory
+//   warp 12          issues the matrix instructions;  warps 13, 14: the queries into shared memory;  warp 15: looks up the items
 // The two sub-tiles alternate on the tensor core: while one's scores are being exponentiated the other's products run.
 // Bound by the tensor core and the exponential unit alike at head_dim 128 (256 x 128 scores: 2048 cycles each).
 //
@@ -79,6 +79,17 @@ __device__ __forceinline__ uint32_t elect_one() {               // one lane of a
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// Tensor memory with one row to a thread: 32 columns of it.
+__device__ __forceinline__ void tmem_ld_row(uint32_t taddr, float* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+               : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_row(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+               : "memory");
+}
 // Tensor memory in the layout of an mma.m16n8 result: 16 lanes (rows), a thread holds of every 8 columns the columns
 // 2t, 2t + 1 of row g (registers 0, 1) and of row g + 8 (2, 3), g = lane / 4, t = lane % 4.  Against one row to a thread
 // this leaves a thread a quarter of the columns, and so of the keys' scales, for four rows.
@@ -151,10 +162,11 @@ __device__ __forceinline__ int item_at(int n) {
 }
 // One work item, as every role sees it.
 struct Item {
-  SeqLens len;
-  int b, head, split, r0, n_rows;
+  int b, head, split;
+  int q0, past;                  // first row of the sequence in the call's tensors; its tokens before the call's
+  int r0, n_rows;                // rows of the item, of the sequence
   int key0, key1;                // keys of the piece that any row sees
-  int tiles;                     // of BK keys
+  int tiles;                     // of BK keys; -1: no more items
 };
 // The whole warp takes part.  False: nothing to do.
 template <int D>
@@ -190,12 +202,15 @@ __device__ __forceinline__ bool decode_item(const TilesParams& p, int item, int 
   }
   if (b < 0) return false;
   o.b = b;
-  if (!sequence_lengths(p.b, b, p.c.page_shift, p.status, o.len)) return false;
-  o.n_rows = min(o.len.q_len, p.b.max_q_len) * p.a.group;
+  SeqLens len;
+  if (!sequence_lengths(p.b, b, p.c.page_shift, p.status, len)) return false;
+  o.q0 = len.q0;
+  o.past = len.kv - len.q_len;
+  o.n_rows = min(len.q_len, p.b.max_q_len) * p.a.group;
   o.r0 = mine * G::ROWS;
-  if (o.split > 0 && (long)o.split * p.p.chunk >= o.len.held) return false;
+  if (o.split > 0 && (long)o.split * p.p.chunk >= len.held) return false;
   const int last_tok = token_of(p, min(o.r0 + G::ROWS - 1, o.n_rows - 1));
-  const int seen = p.a.causal ? max(0, min(o.len.held, o.len.kv - o.len.q_len + last_tok + 1)) : o.len.held;
+  const int seen = p.a.causal ? max(0, min(len.held, o.past + last_tok + 1)) : len.held;
   o.key0 = o.split * p.p.chunk;
   o.key1 = o.split == p.p.splits - 1 ? seen : min(seen, o.key0 + p.p.chunk);
   o.tiles = o.key1 > o.key0 ? (o.key1 - o.key0 + G::BK - 1) / G::BK : 0;
@@ -217,7 +232,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
   constexpr bool CODES = BITS < 16;
   extern __shared__ unsigned char smem_dyn[];
   __shared__ __align__(8) uint64_t q_full, q_empty, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES], s_full[NSUB], p_full[NSUB][BK / 64],
-      o_full[NSUB];
+      o_full[NSUB], item_full[2], item_empty[2];
+  __shared__ Item item_slot[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag_s;
   volatile int* abort_flag = &abort_flag_s;
@@ -227,7 +243,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = warp >> 2;
 
   if (threadIdx.x == 0) {
-    mbar_init(&q_full, 96);
+    mbar_init(&q_full, 64);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&item_full[s], 1);
+      mbar_init(&item_empty[s], 4 * NSUB + 4 + 1 + 2);          // warps that work on items
+    }
     mbar_init(&q_empty, 1);
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(&k_full[s], 128);
@@ -252,97 +272,119 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   grid_dependency_wait();
+  // The n-th item of this block, from the warp that looks them up (all lanes of the calling warp; false: gave up).
+  auto next_item = [&](uint32_t n, Item& w) {
+    const bool ok = __all_sync(0xffffffffu, mbar_wait(&item_full[n & 1], (n >> 1) & 1, abort_flag, p.status));
+    if (ok) {
+      w = item_slot[n & 1];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&item_empty[n & 1]);
+    }
+    return ok;
+  };
 
   if (wg < NSUB) {
-    // ------------------------------ softmax: four rows to a thread, a quarter of the columns ------------------------------
+    // ------------------------------ softmax ------------------------------
+    // bf16: one row to a thread.  Codes: four rows to a thread and a quarter of the columns (see tmem_ld64), because
+    // every column comes with two scales from shared memory.  Measured: bf16 prompt of 8192 tokens 590 us with one
+    // row, 627 with four; 512 queries over 16384 tokens at 8 bits 292 with one, 241 with four.
     regs_up<192>();
-    const int sub = wg, g = lane >> 2, t = lane & 3, quad = warp & 3;
+    constexpr int R = CODES ? 4 : 1, NP = BK / 2 / R, NH = BK / 64, NPH = NP / NH;     // rows; pairs of columns of a row: all, of 64 keys
+    const int sub = wg, g = lane >> 2, t = R == 4 ? lane & 3 : 0, quad = warp & 3;
     const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
     const uint32_t s_addr = lane_base + G::S_COL + sub * BK, o_addr = lane_base + G::O_COL + sub * D;
     constexpr uint32_t LOWER = 16u << 16;                      // rows 16 .. 31 of the warp
+    auto at = [](int i, int q) { return R == 4 ? (i >> 1) * (BK / 2) + 4 * q + 2 * (i & 1) : 2 * q; };   // pair q of row i among the registers
+    constexpr int STEP = R == 4 ? 8 : 2;                       // its columns: STEP q + 2t, + 1
     const float scale = fmaxf(fabsf(p.a.scale_log2), 1e-30f);  // (a negative one: the queries are negated; 0 * -inf is not -inf)
     uint32_t it = 0, done = 0;                                 // tiles and items so far: barrier phases
     bool ok = true;
-    for (int n = 0; n * (int)gridDim.x < p.items && ok; ++n) {
-      Item w;
-      if (!decode_item<D>(p, item_at(n), lane, w)) continue;
+    for (uint32_t n = 0;; ++n) {
+      if (!(ok = __all_sync(0xffffffffu, mbar_wait(&item_full[n & 1], (n >> 1) & 1, abort_flag, p.status)))) break;
+      const Item& w = item_slot[n & 1];                        // kept until the end: registers are short here
+      const int tiles = w.tiles, key0 = w.key0;
+      if (tiles < 0) break;
       // the thread's rows: first + 8 i
-      const int first = w.r0 + sub * 128 + quad * 32 + g;
-      int lim[4], low = 0x7fffffff;                            // keys below lim are seen; below low the warp masks nothing
+      const int first = w.r0 + sub * 128 + quad * 32 + (R == 4 ? g : lane);
+      int lim[R], low = 0x7fffffff;                            // keys below lim are seen; below low the warp masks nothing
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < R; ++i) {
         const int r = first + 8 * i;
-        lim[i] = r >= w.n_rows ? 0 : p.a.causal ? min(w.key1, w.len.kv - w.len.q_len + token_of(p, r) + 1) : w.key1;
+        lim[i] = r >= w.n_rows ? 0 : p.a.causal ? min(w.key1, w.past + token_of(p, r) + 1) : w.key1;
         if (r < w.n_rows) low = min(low, lim[i]);
       }
       low = __reduce_min_sync(0xffffffffu, low);
-      float m[4], l[4];
+      float m[R], l[R];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
-      for (int j = 0; j < w.tiles; ++j, ++it) {
-        const int k0 = w.key0 + j * BK;
+      for (int i = 0; i < R; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
+      for (int j = 0; j < tiles; ++j, ++it) {
+        const int k0 = key0 + j * BK;
         const int stage = it % STAGES;
         if (CODES && !(ok = __all_sync(0xffffffffu, mbar_wait(&k_full[stage], (it / STAGES) & 1, abort_flag, p.status)))) break;   // its scales
         if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s_full[sub], it & 1, abort_flag, p.status)))) break;
         tc_fence_after();
-        float x[2][BK / 2];                                    // [rows 0 .. 15 | 16 .. 31][column / 8][4]
+        float x[BK];
+        if constexpr (R == 4) {
 #pragma unroll
-        for (int h = 0; h < BK / 64; ++h) {
-          tmem_ld64(s_addr + 64 * h, x[0] + 32 * h);
-          tmem_ld64(s_addr + LOWER + 64 * h, x[1] + 32 * h);
+          for (int h = 0; h < NH; ++h) {
+            tmem_ld64(s_addr + 64 * h, x + 32 * h);
+            tmem_ld64(s_addr + LOWER + 64 * h, x + BK / 2 + 32 * h);
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < BK / 32; ++c) tmem_ld_row(s_addr + 32 * c, x + 32 * c);
         }
         const float2* ks = reinterpret_cast<const float2*>(scales + stage * 2 * BK) + t;
         const float2* vs = ks + BK / 2;
         tmem_ld_wait();
         const bool masked = k0 + BK > low;
-        float neg[4];
+        float neg[R];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) neg[i] = m[i] == -INFINITY ? 0.f : -m[i];
+        for (int i = 0; i < R; ++i) neg[i] = m[i] == -INFINITY ? 0.f : -m[i];
         // codes: scores relative to the maximum so far (bf16: the products alone, in units of which the mask and the
         // maximum are the same)
         if (CODES) {
 #pragma unroll
-          for (int c = 0; c < BK / 8; ++c) {
-            const float2 s = ks[4 * c];
+          for (int q = 0; q < NP; ++q) {
+            const float2 s = ks[4 * q];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float* y = &x[i >> 1][4 * c + 2 * (i & 1)];
-              fma2(y[0], y[1], s.x, s.y, neg[i]);
-            }
+            for (int i = 0; i < R; ++i) fma2(x[at(i, q)], x[at(i, q) + 1], s.x, s.y, neg[i]);
           }
         }
         if (masked) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < R; ++i) {
             const int seen = lim[i] - k0 - 2 * t;
 #pragma unroll
-            for (int c = 0; c < BK / 8; ++c) {
-              float* y = &x[i >> 1][4 * c + 2 * (i & 1)];
-              if (8 * c >= seen) y[0] = -INFINITY;
-              if (8 * c + 1 >= seen) y[1] = -INFINITY;
+            for (int q = 0; q < NP; ++q) {
+              if (STEP * q >= seen) x[at(i, q)] = -INFINITY;
+              if (STEP * q + 1 >= seen) x[at(i, q) + 1] = -INFINITY;
             }
           }
         }
-        float top[4];                                           // how far the tile's largest score lies above the maximum
+        float top[R];                                           // how far the tile's largest score lies above the maximum
         bool raise = false;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float* y = &x[i >> 1][2 * (i & 1)];
-          float a = fmaxf(y[0], y[1]), b = fmaxf(y[4], y[5]);
+        for (int i = 0; i < R; ++i) {
+          constexpr int CHAINS = R == 4 ? 2 : 4;                // independent ones, to hide each operation's latency
+          float c[CHAINS];
 #pragma unroll
-          for (int c = 2; c < BK / 8; c += 2) {
-            a = fmaxf(a, fmaxf(y[4 * c], y[4 * c + 1]));
-            b = fmaxf(b, fmaxf(y[4 * c + 4], y[4 * c + 5]));
-          }
-          top[i] = CODES ? fmaxf(a, b) : fmaf(fmaxf(a, b), scale, neg[i]);
+          for (int e = 0; e < CHAINS; ++e) c[e] = fmaxf(x[at(i, e)], x[at(i, e) + 1]);
+#pragma unroll
+          for (int q = CHAINS; q < NP; ++q) c[q % CHAINS] = fmaxf(c[q % CHAINS], fmaxf(x[at(i, q)], x[at(i, q) + 1]));
+#pragma unroll
+          for (int e = 1; e < CHAINS; ++e) c[0] = fmaxf(c[0], c[e]);
+          top[i] = CODES ? c[0] : fmaf(c[0], scale, neg[i]);
           raise |= top[i] > (m[i] == -INFINITY ? -INFINITY : kLazy);
         }
         if (__any_sync(0xffffffffu, raise)) {
-          float f[4];
+          float f[R];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
-            top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+          for (int i = 0; i < R; ++i) {
+            if (R == 4) {
+              top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+              top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+            }
             const bool first_key = m[i] == -INFINITY;
             const bool up = top[i] > (first_key ? -INFINITY : kLazy);
             const float by = up ? top[i] : 0.f;                 // how far the maximum rises (from 0 where there was none)
@@ -351,10 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
             l[i] *= f[i];
             if (CODES) {
 #pragma unroll
-              for (int c = 0; c < BK / 8; ++c) {
-                float* y = &x[i >> 1][4 * c + 2 * (i & 1)];
-                add2(y[0], y[1], -by, -by);
-              }
+              for (int q = 0; q < NP; ++q) add2(x[at(i, q)], x[at(i, q) + 1], -by, -by);
             } else {
               neg[i] -= by;
             }
@@ -362,19 +401,27 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
           if (j > 0) {
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                float o[16];
-                tmem_ld32(o_addr + h * LOWER + 32 * c, o);
+              float o[32];
+              if constexpr (R == 4) {
+                tmem_ld32(o_addr + 32 * c, o);
+                tmem_ld32(o_addr + LOWER + 32 * c, o + 16);
                 tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] *= f[2 * h + (e >> 1 & 1)];
-                tmem_st_o(o_addr + h * LOWER + 32 * c, o);
+                for (int e = 0; e < 32; ++e) o[e] *= f[R == 4 ? 2 * (e >> 4) + (e >> 1 & 1) : 0];
+                tmem_st_o(o_addr + 32 * c, o);
+                tmem_st_o(o_addr + LOWER + 32 * c, o + 16);
+              } else {
+                tmem_ld_row(o_addr + 32 * c, o);
+                tmem_ld_wait();
+                uint32_t u[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(o[e] * f[0]);
+                tmem_st_row(o_addr + 32 * c, u);
               }
             }
           }
         }
-        float sum[4][2] = {};
+        float sum[R][4 / R > 1 ? 4 : 2] = {};
         // 64 keys are handed over at a time, so that their product starts while the rest is computed; the hand-over waits
         // for the stores, and so comes after the next 32 keys' exponentials have been started
         auto hand_over = [&](int h) {
@@ -387,68 +434,76 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         auto exponentials = [&](auto select) {
           constexpr bool SELECT = decltype(select)::value;
 #pragma unroll
-          for (int h = 0; h < BK / 64; ++h) {
-            uint32_t pk[2][16];
+          for (int h = 0; h < NH; ++h) {
+            uint32_t pk[32];
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              const float2 v = CODES ? vs[4 * (8 * h + c)] : make_float2(1.f, 1.f);
+            for (int c = 0; c < NPH; ++c) {
+              const int q = h * NPH + c;
+              const float2 v = CODES ? vs[4 * q] : make_float2(1.f, 1.f);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                float* y = &x[i >> 1][32 * h + 4 * c + 2 * (i & 1)];
-                if (!CODES) fma2(y[0], y[1], scale, scale, neg[i]);
-                y[0] = exp2_approx(y[0]);
-                y[1] = exp2_approx(y[1]);
-                add2(sum[i][0], sum[i][1], y[0], y[1]);
+              for (int i = 0; i < R; ++i) {
+                float y0 = x[at(i, q)], y1 = x[at(i, q) + 1];
+                if (!CODES) fma2(y0, y1, scale, scale, neg[i]);
+                y0 = exp2_approx(y0);
+                y1 = exp2_approx(y1);
+                const int chain = R == 4 ? 0 : 2 * (c & 1);
+                add2(sum[i][chain], sum[i][chain + 1], y0, y1);
                 if (SELECT) {
-                  const int seen = lim[i] - k0 - 2 * t - 64 * h - 8 * c;
-                  y[0] = seen > 0 ? y[0] * v.x : 0.f;
-                  y[1] = seen > 1 ? y[1] * v.y : 0.f;
+                  const int seen = lim[i] - k0 - 2 * t - STEP * q;
+                  y0 = seen > 0 ? y0 * v.x : 0.f;
+                  y1 = seen > 1 ? y1 * v.y : 0.f;
                 } else if (CODES) {
-                  mul2(y[0], y[1], v.x, v.y);
+                  mul2(y0, y1, v.x, v.y);
                 }
-                pk[i >> 1][2 * c + (i & 1)] = pack2(y[0], y[1]);
+                pk[R == 4 ? (i >> 1) * 16 + 2 * c + (i & 1) : c] = pack2(y0, y1);
               }
-              if (h > 0 && c == 3) hand_over(h - 1);
+              if (h > 0 && c == NPH / 2 - 1) hand_over(h - 1);
             }
-            tmem_st_p(s_addr + 32 * h, pk[0]);
-            tmem_st_p(s_addr + LOWER + 32 * h, pk[1]);
+            if constexpr (R == 4) {
+              tmem_st_p(s_addr + 32 * h, pk);
+              tmem_st_p(s_addr + LOWER + 32 * h, pk + 16);
+            } else {
+              tmem_st_row(s_addr + 32 * h, pk);
+            }
           }
-          hand_over(BK / 64 - 1);
+          hand_over(NH - 1);
         };
         if (CODES && masked) exponentials(std::true_type{});
         else exponentials(std::false_type{});
 #pragma unroll
-        for (int i = 0; i < 4; ++i) l[i] += sum[i][0] + sum[i][1];
+        for (int i = 0; i < R; ++i) l[i] += R == 4 ? sum[i][0] + sum[i][1] : (sum[i][0] + sum[i][1]) + (sum[i][R == 4 ? 0 : 2] + sum[i][R == 4 ? 0 : 3]);
         if (CODES && lane == 0) mbar_arrive(&k_empty[stage]);
       }
       if (!ok) break;
       // ---- the rows' results ----
-      if (w.tiles > 0) {
-        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&o_full[sub], done & 1, abort_flag, p.status)))) break;
-        ++done;
-        tc_fence_after();
-      }
       const bool whole = p.p.splits <= 1;
-      float inv[4];
-      char* dst[4];                                             // of the rows that this thread writes: lane / 4 + 8 i
+      float inv[R];
+      char* mine[R];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+      for (int i = 0; i < R; ++i) {
+        if (R == 4) {
+          l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+          l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+        }
         inv[i] = l[i] == 0.f ? 0.f : __fdividef(1.f, l[i]);
         const int r = first + 8 * i;
-        dst[i] = nullptr;
+        mine[i] = nullptr;
         if (r < w.n_rows) {
           const int tok = token_of(p, r), hq = w.head * p.a.group + r - tok * p.a.group;
-          const long row = (long)(w.len.q0 + tok) * p.a.n_heads + hq, part = (long)w.split * p.b.tokens * p.a.n_heads + row;
-          dst[i] = whole ? reinterpret_cast<char*>(p.a.out + (w.len.q0 + tok) * p.a.o_ts + hq * p.a.o_hs) : reinterpret_cast<char*>(p.part_o + part * D);
+          const long row = (long)(w.q0 + tok) * p.a.n_heads + hq, part = (long)w.split * p.b.tokens * p.a.n_heads + row;
+          mine[i] = whole ? reinterpret_cast<char*>(p.a.out + (w.q0 + tok) * p.a.o_ts + hq * p.a.o_hs) : reinterpret_cast<char*>(p.part_o + part * D);
           const float lse2 = l[i] == 0.f ? -INFINITY : (m[i] == -INFINITY ? 0.f : m[i]) + __log2f(l[i]);
           if (t == 0 && !whole) p.part_lse[part] = lse2;
           if (t == 0 && whole && p.a.lse != nullptr) p.a.lse[row] = lse2 * 0.6931471805599453f;
         }
       }
       // 64 bytes of every row at a time go by way of shared memory, where they get back into order and from where four
-      // lanes write a row's together
+      // lanes write a row's together: this thread a quarter of the rows lane / 4 + 8 i
+      char* dst[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        dst[i] = R == 4 ? mine[R == 4 ? i : 0]
+                        : reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine[0]), 8 * i + g));
       const uint32_t out = smem_u32(scales + STAGES * 2 * BK) + (sub * 4 + quad) * G::OUT_BYTES;
       auto flush = [&](int byte) {
         __syncwarp();
@@ -456,37 +511,57 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         for (int i = 0; i < 4; ++i) {
           uint32_t y[4];
           asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3])
-                       : "r"(out + (8 * i + g) * G::OUT_PITCH + t * 16) : "memory");
-          if (dst[i] != nullptr) *reinterpret_cast<uint4*>(dst[i] + byte + t * 16) = make_uint4(y[0], y[1], y[2], y[3]);
+                       : "r"(out + (8 * i + g) * G::OUT_PITCH + (lane & 3) * 16) : "memory");
+          if (dst[i] != nullptr) *reinterpret_cast<uint4*>(dst[i] + byte + (lane & 3) * 16) = make_uint4(y[0], y[1], y[2], y[3]);
         }
         __syncwarp();
       };
-      const int e0 = BITS == 16 ? 2 * t : BITS == 8 ? pair_lo<8>(t) : t, e1 = BITS == 16 ? 2 * t + 1 : BITS == 8 ? pair_hi<8>(t) : t + 4;
+      if (tiles > 0) {
+        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&o_full[sub], done & 1, abort_flag, p.status)))) break;
+        ++done;
+        tc_fence_after();
+      }
+      const int e0 = BITS == 8 ? pair_lo<8>(t) : t, e1 = BITS == 8 ? pair_hi<8>(t) : t + 4;
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
-        float o[2][16];
-        if (w.tiles > 0) {
-          tmem_ld32(o_addr + 32 * c, o[0]);
-          tmem_ld32(o_addr + LOWER + 32 * c, o[1]);
+        float o[32];
+        if (tiles == 0) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+        } else if constexpr (R == 4) {
+          tmem_ld32(o_addr + 32 * c, o);
+          tmem_ld32(o_addr + LOWER + 32 * c, o + 16);
           tmem_ld_wait();
         } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[0][e] = o[1][e] = 0.f;
+          tmem_ld_row(o_addr + 32 * c, o);
+          tmem_ld_wait();
         }
-        // a thread's columns 2t, 2t + 1 of each group of 8 are the head's elements e0, e1 of that group
-        if (whole) {
+        if constexpr (R == 1) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] *= inv[0];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (whole && h == 1) break;
+            uint32_t u[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) u[e] = whole ? pack2(o[2 * e], o[2 * e + 1]) : __float_as_uint(o[16 * h + e]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t y[4] = {u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]};
+              store16(out + lane * G::OUT_PITCH + 16 * i, y);
+            }
+            flush(whole ? 64 * c : 128 * c + 64 * h);
+          }
+        } else if (whole) {
+          // a thread's columns 2t, 2t + 1 of each group of 8 are the head's elements e0, e1 of that group
 #pragma unroll
           for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float* y = &o[i >> 1][4 * q + 2 * (i & 1)];
-              const uint32_t u = pack2(y[0] * inv[i], y[1] * inv[i]), at = out + (8 * i + g) * G::OUT_PITCH + 16 * q;
-              if constexpr (!CODES) {
-                asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + 4 * t), "r"(u) : "memory");
-                continue;
-              }
-              asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + 2 * e0), "h"((unsigned short)u) : "memory");
-              asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + 2 * e1), "h"((unsigned short)(u >> 16)) : "memory");
+            for (int i = 0; i < R; ++i) {
+              const float* y = &o[16 * (i >> 1) + 4 * q + 2 * (i & 1)];
+              const uint32_t u = pack2(y[0] * inv[i], y[1] * inv[i]), a = out + (8 * i + g) * G::OUT_PITCH + 16 * q;
+              asm volatile("st.shared.b16 [%0], %1;" ::"r"(a + 2 * e0), "h"((unsigned short)u) : "memory");
+              asm volatile("st.shared.b16 [%0], %1;" ::"r"(a + 2 * e1), "h"((unsigned short)(u >> 16)) : "memory");
             }
           flush(64 * c);
         } else {
@@ -495,29 +570,31 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
 #pragma unroll
             for (int q = 0; q < 2; ++q)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float* y = &o[i >> 1][4 * (2 * h + q) + 2 * (i & 1)];
-                const uint32_t at = out + (8 * i + g) * G::OUT_PITCH + 32 * q;
-                asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 4 * e0), "f"(y[0] * inv[i]) : "memory");
-                asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 4 * e1), "f"(y[1] * inv[i]) : "memory");
+              for (int i = 0; i < R; ++i) {
+                const float* y = &o[16 * (i >> 1) + 4 * (2 * h + q) + 2 * (i & 1)];
+                const uint32_t a = out + (8 * i + g) * G::OUT_PITCH + 32 * q;
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(a + 4 * e0), "f"(y[0] * inv[i]) : "memory");
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(a + 4 * e1), "f"(y[1] * inv[i]) : "memory");
               }
             flush(128 * c + 64 * h);
           }
         }
       }
       tc_fence_before();                                        // O has been read: the next item's P says so to the issuer
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&item_empty[n & 1]);
     }
   } else if (wg == 2) {
     // ------------------------------ producers ------------------------------
-    regs_down<80>();
+    regs_down<64>();
     const int tid = threadIdx.x & 127;
     constexpr int CH = D / 8;                                   // 16-byte chunks of a row
     const float scale = fmaxf(fabsf(p.a.scale_log2), 1e-30f);
     uint32_t it = 0;
     bool ok = true;
-    for (int n = 0; n * (int)gridDim.x < p.items && ok; ++n) {
-      Item w;
-      if (!decode_item<D>(p, item_at(n), lane, w) || w.tiles == 0) continue;
+    Item w;
+    for (uint32_t n = 0; ok && (ok = next_item(n, w)) && w.tiles >= 0; ++n) {
+      if (w.tiles == 0) continue;
       const int* page_row = p.b.pages + (long)w.b * p.b.max_pages;
       // pages of a tile's 16-key groups, one to a lane (a tile starts on a multiple of 64 keys; a group lies in one page)
       auto page_of = [&](int j) {
@@ -678,8 +755,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
       }
     }
   } else if (wg == 3) {
-    // ------------------------------ issuer, and the queries ------------------------------
-    regs_down<48>();
+    // ------------------------------ issuer, the queries, the items ------------------------------
+    regs_down<64>();
     if (warp == 12) {
       const uint32_t leader = elect_one();
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
@@ -698,9 +775,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
                   kd + (uint64_t)((stage * G::KV_BYTES + (k >> 2) * G::HALF + (k & 3) * 32) >> 4), G::IDESC_QK, k != 0, leader);
         umma_commit(&s_full[i], leader);
       };
-      for (int n = 0; n * (int)gridDim.x < p.items && ok; ++n) {
-        Item w;
-        if (!decode_item<D>(p, item_at(n), lane, w) || w.tiles == 0) continue;
+      Item w;
+      for (uint32_t n = 0; ok && (ok = next_item(n, w)) && w.tiles >= 0; ++n) {
+        if (w.tiles == 0) continue;
         if (!wait(&q_full, items & 1) || !wait(&k_full[it % STAGES], (it / STAGES) & 1)) break;
         ++items;
 #pragma unroll
@@ -734,23 +811,40 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         }
       }
     }
-    if (warp > 12) {
+    if (warp == 15) {
+      // ---- the items, looked up one ahead of those who work on them ----
+      uint32_t made = 0;
+      bool ok = true;
+      auto give = [&](const Item& w) {
+        ok = __all_sync(0xffffffffu, mbar_wait<true>(&item_empty[made & 1], ((made >> 1) & 1) ^ 1, abort_flag, p.status));
+        if (ok && lane == 0) {
+          item_slot[made & 1] = w;
+          mbar_arrive(&item_full[made & 1]);
+        }
+        ++made;
+      };
+      Item w;
+      for (int n = 0; n * (int)gridDim.x < p.items && ok; ++n)
+        if (decode_item<D>(p, item_at(n), lane, w)) give(w);
+      w.tiles = -1;
+      if (ok) give(w);
+    } else if (warp > 12) {
       // ---- queries: as soon as the last scores of the item before are done, while its last products still run ----
-      constexpr int CH = D / 8, RPP = 96 / CH, N = NSUB * 128;
+      constexpr int CH = D / 8, RPP = 64 / CH, N = NSUB * 128;
       const int tid = threadIdx.x - 13 * 32;
       const bool reorder = CODES || p.a.scale_log2 < 0.f;
       const uint32_t flip = p.a.scale_log2 < 0.f ? 0x80008000u : 0u;
       uint32_t items = 0;
       bool ok = true;
-      for (int n = 0; n * (int)gridDim.x < p.items && ok; ++n) {
-        Item w;
-        if (!decode_item<D>(p, item_at(n), lane, w) || w.tiles == 0) continue;
+      Item w;
+      for (uint32_t n = 0; ok && (ok = next_item(n, w)) && w.tiles >= 0; ++n) {
+        if (w.tiles == 0) continue;
         if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(&q_empty, (items & 1) ^ 1, abort_flag, p.status)))) break;
         ++items;
         const int c = tid % CH, first = tid / CH, step_tok = token_of(p, RPP), step_rem = RPP - step_tok * p.a.group;
         int tok = token_of(p, w.r0 + first), rem = w.r0 + first - tok * p.a.group;
-        const __nv_bfloat16* q = p.a.q + w.len.q0 * p.a.q_ts + (long)w.head * p.a.group * p.a.q_hs + 8 * c;
-        for (int rr = first; rr < N && first < RPP; rr += RPP) {
+        const __nv_bfloat16* q = p.a.q + w.q0 * p.a.q_ts + (long)w.head * p.a.group * p.a.q_hs + 8 * c;
+        for (int rr = first; rr < N; rr += RPP) {
           const bool live = w.r0 + rr < w.n_rows;
           copy16(sq + (rr >> 7) * G::Q_BYTES + chunk_at(rr & 127, c, 128 * 128), live ? q + tok * p.a.q_ts + rem * p.a.q_hs : q, live);
           tok += step_tok;
@@ -762,7 +856,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (reorder)                                            // each thread its own pieces
-          for (int rr = first; rr < N && first < RPP; rr += RPP) {
+          for (int rr = first; rr < N; rr += RPP) {
             const uint32_t at = sq + (rr >> 7) * G::Q_BYTES + chunk_at(rr & 127, c, 128 * 128);
             uint32_t y[4], o[4];
             asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(at) : "memory");
@@ -778,7 +872,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
       }
     }
   } else {
-    regs_down<48>();                                            // (head_dim 256: the second softmax group has no sub-tile)
+    regs_down<64>();                                            // (head_dim 256: the second softmax group has no sub-tile)
   }
 
   // ------------------------------ teardown ------------------------------
