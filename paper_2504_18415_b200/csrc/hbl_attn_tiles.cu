@@ -21,8 +21,6 @@
 #include "hbl_attn_frag.cuh"
 #include "hbl_pipeline.cuh"
 
-#include <type_traits>
-
 namespace hbl {
 namespace {
 
@@ -103,12 +101,17 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* r) {
                : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
                : "r"(taddr) : "memory");
 }
-// ... and 4 columns of 32 bits (8 bf16 values) at a time: row g column t (register 0), row g + 8 (1).
-__device__ __forceinline__ void tmem_st_o(uint32_t taddr, const float* r) {
-  asm volatile("tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-               ::"r"(taddr), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15])
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* r) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
+               : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* r) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               ::"r"(taddr), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7])
                : "memory");
 }
+// ... and 4 columns of 32 bits (8 bf16 values) at a time: row g column t (register 0), row g + 8 (1).
 __device__ __forceinline__ void tmem_st_p(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
                ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
@@ -124,6 +127,7 @@ __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {   // 16 bytes to shared memory, zeros if !live
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p) : "memory"); }
 // two fp32 operations to an instruction
 __device__ __forceinline__ void mul2(float& a, float& b, float x, float y) {
   asm("{\n .reg .b64 u, v;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %3};\n mul.rn.f32x2 u, u, v;\n mov.b64 {%0, %1}, u;\n}"
@@ -230,10 +234,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
   using G = TileGeo<D>;
   constexpr int NSUB = G::NSUB, BK = G::BK, STAGES = G::STAGES;
   constexpr bool CODES = BITS < 16;
+  // Registers of a thread by role: two softmax groups (one at head_dim 256), the producers, the rest; launched with 128
+  // each, and what is taken must be given (2 SOFT + PROD + REST = 512).
+  constexpr int SOFT = CODES ? 184 : 192, PROD = CODES ? 88 : 64, REST = CODES ? 56 : 64;
+  static_assert(2 * SOFT + PROD + REST <= 512, "setmaxnreg waits for registers that nobody gives back");
   extern __shared__ unsigned char smem_dyn[];
   __shared__ __align__(8) uint64_t q_full, q_empty, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES], s_full[NSUB], p_full[NSUB][BK / 64],
       o_full[NSUB], item_full[2], item_empty[2];
   __shared__ Item item_slot[2];
+  __shared__ __align__(16) uint32_t bad_scale[STAGES][4];       // keys of the tile whose value scale is not finite
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag_s;
   volatile int* abort_flag = &abort_flag_s;
@@ -288,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
     // bf16: one row to a thread.  Codes: four rows to a thread and a quarter of the columns (see tmem_ld64), because
     // every column comes with two scales from shared memory.  Measured: bf16 prompt of 8192 tokens 590 us with one
     // row, 627 with four; 512 queries over 16384 tokens at 8 bits 292 with one, 241 with four.
-    regs_up<192>();
+    regs_up<SOFT>();
     constexpr int R = CODES ? 4 : 1, NP = BK / 2 / R, NH = BK / 64, NPH = NP / NH;     // rows; pairs of columns of a row: all, of 64 keys
     const int sub = wg, g = lane >> 2, t = R == 4 ? lane & 3 : 0, quad = warp & 3;
     const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
@@ -306,17 +315,19 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
       if (tiles < 0) break;
       // the thread's rows: first + 8 i
       const int first = w.r0 + sub * 128 + quad * 32 + (R == 4 ? g : lane);
-      int lim[R], low = 0x7fffffff;                            // keys below lim are seen; below low the warp masks nothing
-#pragma unroll
-      for (int i = 0; i < R; ++i) {
+      auto limit = [&](int i) {                                // keys below it are seen by row i
         const int r = first + 8 * i;
-        lim[i] = r >= w.n_rows ? 0 : p.a.causal ? min(w.key1, w.past + token_of(p, r) + 1) : w.key1;
-        if (r < w.n_rows) low = min(low, lim[i]);
-      }
-      low = __reduce_min_sync(0xffffffffu, low);
-      float m[R], l[R];
+        return r >= w.n_rows ? 0 : p.a.causal ? min(w.key1, w.past + token_of(p, r) + 1) : w.key1;
+      };
+      int low = 0x7fffffff;                                    // below it the warp masks nothing
 #pragma unroll
-      for (int i = 0; i < R; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
+      for (int i = 0; i < R; ++i)
+        if (first + 8 * i < w.n_rows) low = min(low, limit(i));
+      low = __reduce_min_sync(0xffffffffu, low);
+      float neg[R], l[R];                                      // minus the maximum so far (0: none yet, see `some`), p's sum
+      uint32_t some = 0;                                       // rows that have seen a key
+#pragma unroll
+      for (int i = 0; i < R; ++i) { neg[i] = 0.f; l[i] = 0.f; }
       for (int j = 0; j < tiles; ++j, ++it) {
         const int k0 = key0 + j * BK;
         const int stage = it % STAGES;
@@ -338,9 +349,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         const float2* vs = ks + BK / 2;
         tmem_ld_wait();
         const bool masked = k0 + BK > low;
-        float neg[R];
-#pragma unroll
-        for (int i = 0; i < R; ++i) neg[i] = m[i] == -INFINITY ? 0.f : -m[i];
         // codes: scores relative to the maximum so far (bf16: the products alone, in units of which the mask and the
         // maximum are the same)
         if (CODES) {
@@ -354,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         if (masked) {
 #pragma unroll
           for (int i = 0; i < R; ++i) {
-            const int seen = lim[i] - k0 - 2 * t;
+            const int seen = limit(i) - k0 - 2 * t;
 #pragma unroll
             for (int q = 0; q < NP; ++q) {
               if (STEP * q >= seen) x[at(i, q)] = -INFINITY;
@@ -375,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
 #pragma unroll
           for (int e = 1; e < CHAINS; ++e) c[0] = fmaxf(c[0], c[e]);
           top[i] = CODES ? c[0] : fmaf(c[0], scale, neg[i]);
-          raise |= top[i] > (m[i] == -INFINITY ? -INFINITY : kLazy);
+          raise |= top[i] > (some >> i & 1 ? kLazy : -INFINITY);
         }
         if (__any_sync(0xffffffffu, raise)) {
           float f[R];
@@ -385,32 +393,32 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
               top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
               top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
             }
-            const bool first_key = m[i] == -INFINITY;
-            const bool up = top[i] > (first_key ? -INFINITY : kLazy);
+            const bool old = some >> i & 1, up = top[i] > (old ? kLazy : -INFINITY);
             const float by = up ? top[i] : 0.f;                 // how far the maximum rises (from 0 where there was none)
-            f[i] = up ? (first_key ? 0.f : exp2_approx(-by)) : 1.f;
-            if (up) m[i] = by - neg[i];
+            f[i] = up ? (old ? exp2_approx(-by) : 0.f) : 1.f;
+            if (up) some |= 1u << i;
+            neg[i] -= by;
             l[i] *= f[i];
             if (CODES) {
 #pragma unroll
               for (int q = 0; q < NP; ++q) add2(x[at(i, q)], x[at(i, q) + 1], -by, -by);
-            } else {
-              neg[i] -= by;
             }
           }
           if (j > 0) {
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-              float o[32];
+            for (int c = 0; c < D / (R == 4 ? 16 : 32); ++c) {      // (few registers: the scores are held meanwhile)
               if constexpr (R == 4) {
-                tmem_ld32(o_addr + 32 * c, o);
-                tmem_ld32(o_addr + LOWER + 32 * c, o + 16);
-                tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] *= f[R == 4 ? 2 * (e >> 4) + (e >> 1 & 1) : 0];
-                tmem_st_o(o_addr + 32 * c, o);
-                tmem_st_o(o_addr + LOWER + 32 * c, o + 16);
+                for (int h = 0; h < 2; ++h) {
+                  float o[8];
+                  tmem_ld16(o_addr + h * LOWER + 16 * c, o);
+                  tmem_ld_wait();
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) o[e] *= f[R == 4 ? 2 * h + (e >> 1 & 1) : 0];
+                  tmem_st16(o_addr + h * LOWER + 16 * c, o);
+                }
               } else {
+                float o[32];
                 tmem_ld_row(o_addr + 32 * c, o);
                 tmem_ld_wait();
                 uint32_t u[32];
@@ -430,49 +438,53 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
           __syncwarp();
           if (lane == 0) mbar_arrive(&p_full[sub][h]);
         };
-        // SELECT: a masked key's value scale may be anything (0 * it is not 0)
-        auto exponentials = [&](auto select) {
-          constexpr bool SELECT = decltype(select)::value;
 #pragma unroll
-          for (int h = 0; h < NH; ++h) {
-            uint32_t pk[32];
+        for (int h = 0; h < NH; ++h) {
+          uint32_t pk[32];
 #pragma unroll
-            for (int c = 0; c < NPH; ++c) {
-              const int q = h * NPH + c;
-              const float2 v = CODES ? vs[4 * q] : make_float2(1.f, 1.f);
+          for (int c = 0; c < NPH; ++c) {
+            const int q = h * NPH + c;
+            const float2 v = CODES ? vs[4 * q] : make_float2(1.f, 1.f);
 #pragma unroll
-              for (int i = 0; i < R; ++i) {
-                float y0 = x[at(i, q)], y1 = x[at(i, q) + 1];
-                if (!CODES) fma2(y0, y1, scale, scale, neg[i]);
-                y0 = exp2_approx(y0);
-                y1 = exp2_approx(y1);
-                const int chain = R == 4 ? 0 : 2 * (c & 1);
-                add2(sum[i][chain], sum[i][chain + 1], y0, y1);
-                if (SELECT) {
-                  const int seen = lim[i] - k0 - 2 * t - STEP * q;
-                  y0 = seen > 0 ? y0 * v.x : 0.f;
-                  y1 = seen > 1 ? y1 * v.y : 0.f;
-                } else if (CODES) {
-                  mul2(y0, y1, v.x, v.y);
-                }
-                pk[R == 4 ? (i >> 1) * 16 + 2 * c + (i & 1) : c] = pack2(y0, y1);
-              }
-              if (h > 0 && c == NPH / 2 - 1) hand_over(h - 1);
+            for (int i = 0; i < R; ++i) {
+              float y0 = x[at(i, q)], y1 = x[at(i, q) + 1];
+              if (!CODES) fma2(y0, y1, scale, scale, neg[i]);
+              y0 = exp2_approx(y0);
+              y1 = exp2_approx(y1);
+              const int chain = R == 4 ? 0 : 2 * (c & 1);
+              add2(sum[i][chain], sum[i][chain + 1], y0, y1);
+              if (CODES) mul2(y0, y1, v.x, v.y);
+              pk[R == 4 ? (i >> 1) * 16 + 2 * c + (i & 1) : c] = pack2(y0, y1);
             }
-            if constexpr (R == 4) {
-              tmem_st_p(s_addr + 32 * h, pk);
-              tmem_st_p(s_addr + LOWER + 32 * h, pk + 16);
-            } else {
-              tmem_st_row(s_addr + 32 * h, pk);
-            }
+            if (h > 0 && c == NPH / 2 - 1) hand_over(h - 1);
           }
-          hand_over(NH - 1);
-        };
-        if (CODES && masked) exponentials(std::true_type{});
-        else exponentials(std::false_type{});
+          if constexpr (R == 4) {
+            tmem_st_p(s_addr + 32 * h, pk);
+            tmem_st_p(s_addr + LOWER + 32 * h, pk + 16);
+          } else {
+            tmem_st_row(s_addr + 32 * h, pk);
+          }
+        }
+        hand_over(NH - 1);
 #pragma unroll
         for (int i = 0; i < R; ++i) l[i] += R == 4 ? sum[i][0] + sum[i][1] : (sum[i][0] + sum[i][1]) + (sum[i][R == 4 ? 0 : 2] + sum[i][R == 4 ? 0 : 3]);
-        if (CODES && lane == 0) mbar_arrive(&k_empty[stage]);
+        if (CODES) {
+          // a value scale that is not finite came as zero (0 * it would reach rows it is masked for): rows that see
+          // its key are marked, and their results become NaN
+          const uint4 b = *reinterpret_cast<const uint4*>(bad_scale[stage]);
+          if (b.x | b.y | b.z | b.w) {
+            const uint32_t word[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+              const int seen = limit(i) - k0;
+              for (int e = 0; e < BK / 32; ++e) {
+                const int n_seen = seen - 32 * e;
+                if (word[e] & (n_seen <= 0 ? 0u : n_seen >= 32 ? ~0u : (1u << n_seen) - 1)) some |= 16u << i;
+              }
+            }
+          }
+          if (lane == 0) mbar_arrive(&k_empty[stage]);
+        }
       }
       if (!ok) break;
       // ---- the rows' results ----
@@ -486,13 +498,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
           l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
         }
         inv[i] = l[i] == 0.f ? 0.f : __fdividef(1.f, l[i]);
+        if (some >> i & 16) inv[i] = __uint_as_float(0x7FC00000u);
         const int r = first + 8 * i;
         mine[i] = nullptr;
         if (r < w.n_rows) {
           const int tok = token_of(p, r), hq = w.head * p.a.group + r - tok * p.a.group;
           const long row = (long)(w.q0 + tok) * p.a.n_heads + hq, part = (long)w.split * p.b.tokens * p.a.n_heads + row;
           mine[i] = whole ? reinterpret_cast<char*>(p.a.out + (w.q0 + tok) * p.a.o_ts + hq * p.a.o_hs) : reinterpret_cast<char*>(p.part_o + part * D);
-          const float lse2 = l[i] == 0.f ? -INFINITY : (m[i] == -INFINITY ? 0.f : m[i]) + __log2f(l[i]);
+          const float lse2 = l[i] == 0.f ? -INFINITY : __log2f(l[i]) - neg[i];
           if (t == 0 && !whole) p.part_lse[part] = lse2;
           if (t == 0 && whole && p.a.lse != nullptr) p.a.lse[row] = lse2 * 0.6931471805599453f;
         }
@@ -586,7 +599,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
     }
   } else if (wg == 2) {
     // ------------------------------ producers ------------------------------
-    regs_down<64>();
+    regs_down<PROD>();
     const int tid = threadIdx.x & 127;
     constexpr int CH = D / 8;                                   // 16-byte chunks of a row
     const float scale = fmaxf(fabsf(p.a.scale_log2), 1e-30f);
@@ -665,6 +678,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         // widened, across tiles.
         constexpr int UN = BITS == 8 ? 2 : 4, LPR = D / 8 / UN, RPP = 128 / LPR, PASSES = BK / RPP;
         constexpr int BATCH = PASSES < 4 ? PASSES : 4, NB = PASSES / BATCH;
+        // Eight neighbouring lanes take pieces of the same 64 elements of UN rows: their 16-byte stores then fall into
+        // eight different bank groups of the swizzle.
+        constexpr int PH = 8 / UN, HALVES = D / 64;
+        const int piece = tid / 8 % HALVES * PH + tid % PH, my_row = tid / (8 * HALVES) * UN + tid / PH % UN;
         using L1 = Lane<BITS, UN, LPR>;
         static_assert(L1::UPC == UN && PASSES % BATCH == 0, "one piece of a row to a lane, whole batches");
         struct Raw { L1 r[BATCH]; };
@@ -672,8 +689,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
           const unsigned char* src = kv == 0 ? p.c.k : p.c.v;
 #pragma unroll
           for (int i = 0; i < BATCH; ++i) {
-            const int rr = (batch * BATCH + i) * RPP + tid / LPR;
-            raw.r[i].load(src + row_of(t, rr) * (D * BITS / 8), tid % LPR, live(t, rr));
+            const int rr = (batch * BATCH + i) * RPP + my_row;
+            raw.r[i].load(src + row_of(t, rr) * (D * BITS / 8), piece, live(t, rr));
           }
         };
         float ks = 0.f, vs = 0.f;                               // scales of key row tid of the tile
@@ -693,7 +710,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
           Tile after = tile;
           if (more) after = open(j + 1, next_page);
           next_page = page_of(j + 2);
+          if (more && tid < BK) {                               // the next tile's rows towards L2 (a row: 32 .. 256 bytes)
+            const long row = row_of(after, tid) * (D * BITS / 8);
+            if (live(after, tid)) {
 #pragma unroll
+              for (int b = 0; b < D * BITS / 8; b += 128) {
+                prefetch_l2(p.c.k + row + b);
+                prefetch_l2(p.c.v + row + b);
+              }
+            }
+          }
+#pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
             const uint32_t dst = (kv == 0 ? sk : sv) + stage * G::KV_BYTES;
             uint64_t* empty = kv == 0 ? &k_empty[stage] : &v_empty[stage];
@@ -711,22 +738,25 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
                     ks = bos_row >= 0 ? __ldg(p.c.bos_k_scale + brow) : 0.f;
                     vs = bos_row >= 0 ? __ldg(p.c.bos_v_scale + brow) : 0.f;
                   }
+                  const bool bad = (__float_as_uint(vs) & 0x7F800000u) == 0x7F800000u;
+                  const unsigned word = __ballot_sync(0xffffffffu, bad);
+                  if (lane == 0) bad_scale[stage][tid >> 5] = word;      // (BK 64: the upper two hold none)
                   if (tid < BK) {
                     scales[stage * 2 * BK + tid] = ks * scale;
-                    scales[stage * 2 * BK + BK + tid] = vs;
+                    scales[stage * 2 * BK + BK + tid] = bad ? 0.f : vs;
                   }
                   if (more) load_scales(after);
                 }
               }
 #pragma unroll
               for (int i = 0; i < BATCH; ++i) {
-                const int rr = (batch * BATCH + i) * RPP + tid / LPR, l = tid % LPR;
+                const int rr = (batch * BATCH + i) * RPP + my_row;
                 if (special && rr == 0) continue;
 #pragma unroll
                 for (int u = 0; u < UN; ++u) {
                   uint32_t o[4];
-                  pairs<BITS>(raw.r[i], u, l, o);
-                  store16(dst + chunk_at(rr, l * UN + u, G::HALF), o);
+                  pairs<BITS>(raw.r[i], u, piece, o);
+                  store16(dst + chunk_at(rr, piece * UN + u, G::HALF), o);
                 }
               }
               raw = ahead;
@@ -756,7 +786,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
     }
   } else if (wg == 3) {
     // ------------------------------ issuer, the queries, the items ------------------------------
-    regs_down<64>();
+    regs_down<REST>();
     if (warp == 12) {
       const uint32_t leader = elect_one();
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
@@ -872,7 +902,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
       }
     }
   } else {
-    regs_down<64>();                                            // (head_dim 256: the second softmax group has no sub-tile)
+    regs_down<REST>();                                            // (head_dim 256: the second softmax group has no sub-tile)
   }
 
   // ------------------------------ teardown ------------------------------
