@@ -399,7 +399,8 @@ int hbl_rope(const void* x, int dtype, int tokens, int n_heads, int head_dim, lo
  * bos_k, bos_v (optional, with bits 3 or 4): the first token of a sequence at 8 bits, one row of head_dim codes per
  * (slot, head), and its scales bos_k_scale, bos_v_scale [n_slots, n_kv_heads].  With them a sequence's position 0 is read
  * from there (the low-bit row is written all the same).
- *   page_size a power of two, 16..4096; head_dim 64, 128 or 256; k, v, bos_k, bos_v 16-byte aligned. */
+ *   page_size a power of two, 16..4096; head_dim 64, 128 or 256; at most 2^31 - 1 rows; k, v, bos_k, bos_v 16-byte
+ *   aligned. */
 typedef struct {
   void *k, *v;
   float *k_scale, *v_scale;

@@ -29,6 +29,7 @@ int check_cache(const hbl_kv_cache_t* c, KvView* v) {
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return HBL_ERR_SHAPE;
   if (c->n_kv_heads <= 0 || c->n_pages <= 0) return HBL_ERR_SHAPE;
   if (c->page_size < 16 || c->page_size > 4096 || !is_pow2(c->page_size)) return HBL_ERR_SHAPE;
+  if ((long long)c->n_pages * c->n_kv_heads * c->page_size > 0x7fffffffLL) return HBL_ERR_TOO_LARGE;   // row numbers: 32 bits
   if (!c->k || !c->v) return HBL_ERR_NULL;
   if (!aligned(c->k, 16) || !aligned(c->v, 16)) return HBL_ERR_ALIGN;
   if (c->bits == 16) {

@@ -31,11 +31,14 @@ struct Lane {
   // The unit of the row (0 .. head_dim / 8 - 1) that is the lane's i-th.
   static __device__ __forceinline__ int unit_of(int i, int idx) { return ((i / UPC) * L + idx) * UPC + i % UPC; }
   __device__ __forceinline__ void load(const unsigned char* __restrict__ row, int idx, bool live) {
-    if (!live) {
+    if (live) load(row, idx);
+    else clear();
+  }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-      for (int i = 0; i < WORDS; ++i) w[i] = 0;
-      return;
-    }
+    for (int i = 0; i < WORDS; ++i) w[i] = 0;
+  }
+  __device__ __forceinline__ void load(const unsigned char* __restrict__ row, int idx) {
     if constexpr (BITS == 3) {
       const uint32_t* r = reinterpret_cast<const uint32_t*>(row);
       if constexpr (BYTES == 3) {                              // one unit, anywhere in its word or across two
@@ -114,9 +117,68 @@ __device__ __forceinline__ void pairs(const Lane<BITS, N, L>& r, int i, int idx,
     for (int j = 0; j < 4; ++j) o[j] = bsub2(((x >> (3 * j)) & 0x00070007u) | 0x43004300u, kOffset<3>);
   }
 }
+// ---- the same codes as fp16 values: 10 mantissa bits take a code at several places of a word without a shift ----
+// A code at bit k of a half word, put into the mantissa of 1024.0 (0x6400), is 1024 + 2^k u; times 2^-k minus
+// (1024 / 2^k + 2^(b-1)) is u - 2^(b-1), exactly (one operation on the multiply-add pipe, which has the room; the
+// logic pipe is what a decoding step waits for).  bf16 rows stay as they are.
+__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+__device__ __forceinline__ constexpr uint32_t f16_pair(int v) {          // a small integer (not 0) as an fp16 pair
+  const uint32_t m = (uint32_t)(v < 0 ? -v : v);
+  int e = 0;
+  while ((m >> (e + 1)) != 0) ++e;
+  const uint32_t h = (v < 0 ? 0x8000u : 0u) | (uint32_t)(15 + e) << 10 | ((e > 10 ? m >> (e - 10) : m << (10 - e)) & 0x3FFu);
+  return h | h << 16;
+}
+__device__ __forceinline__ constexpr uint32_t f16_inverse(int k) { return (uint32_t)(15 - k) << 10 | (uint32_t)(15 - k) << 26; }   // 2^-k
+// Field of BITS bits at bit K of each half of x as fp16 values u - 2^(BITS-1).
+template <int BITS, int K>
+__device__ __forceinline__ uint32_t field16(uint32_t x) {
+  constexpr uint32_t mask = ((1u << BITS) - 1) << K;
+  const uint32_t v = (x & (mask | mask << 16)) | 0x64006400u;
+  return hfma2(v, f16_inverse(K), f16_pair(-(1024 >> K) - (1 << (BITS - 1))));
+}
+// The four fields of BITS bits of each half of x.
+template <int BITS>
+__device__ __forceinline__ void fields16(uint32_t x, uint32_t* o) {
+  if constexpr (BITS == 4) {
+    o[0] = field16<4, 0>(x);
+    o[1] = field16<4, 4>(x);
+    o[2] = field16<4, 0>(x >> 8);
+    o[3] = field16<4, 4>(x >> 8);
+  } else {
+    o[0] = field16<3, 0>(x);
+    o[1] = field16<3, 3>(x);
+    o[2] = field16<3, 6>(x);
+    o[3] = field16<3, 6>(x >> 3);
+  }
+}
+template <int BITS>
+__device__ __forceinline__ constexpr int pair16_lo(int j) { return BITS >= 8 ? 2 * j : j; }
+template <int BITS>
+__device__ __forceinline__ constexpr int pair16_hi(int j) { return BITS >= 8 ? 2 * j + 1 : j + 4; }
+template <int BITS, int N, int L>
+__device__ __forceinline__ void pairs16(const Lane<BITS, N, L>& r, int i, int idx, uint32_t (&o)[4]) {
+  if constexpr (BITS == 16) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = r.w[4 * i + j];
+  } else if constexpr (BITS == 8) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      o[j] = hfma2(__byte_perm(r.w[2 * i + j / 2], 0x64646464u, j & 1 ? 0x4342 : 0x4140), f16_pair(1), f16_pair(-1152));
+  } else if constexpr (BITS == 4) {
+    fields16<4>(r.w[i], o);
+  } else {
+    const uint32_t v = r.bits24(i, idx);
+    fields16<3>((v & 0xFFFu) | ((v << 4) & 0x0FFF0000u), o);
+  }
+}
 // Unit i of two rows as eight pairs across the rows: o[e] = (row a, row b) at the unit's element e.
 template <int BITS, int N, int L>
-__device__ __forceinline__ void cross(const Lane<BITS, N, L>& a, const Lane<BITS, N, L>& b, int i, int idx, uint32_t (&o)[8]) {
+__device__ __forceinline__ void cross16(const Lane<BITS, N, L>& a, const Lane<BITS, N, L>& b, int i, int idx, uint32_t (&o)[8]) {
   if constexpr (BITS == 16) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -126,24 +188,30 @@ __device__ __forceinline__ void cross(const Lane<BITS, N, L>& a, const Lane<BITS
   } else if constexpr (BITS == 8) {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      o[e] = from_bytes(__byte_perm(a.w[2 * i + e / 4], b.w[2 * i + e / 4], ((4 + (e & 3)) << 8) | (e & 3)));
+      o[e] = hfma2((__byte_perm(a.w[2 * i + e / 4], b.w[2 * i + e / 4], ((4 + (e & 3)) << 8) | (e & 3)) & 0x00FF00FFu) | 0x64006400u,
+                   f16_pair(1), f16_pair(-1152));
   } else {
     const uint32_t x = BITS == 4 ? a.w[i] : a.bits24(i, idx), y = BITS == 4 ? b.w[i] : b.bits24(i, idx);
-    const uint32_t lo = __byte_perm(x, y, 0x5410);
-    const uint32_t hi = BITS == 4 ? __byte_perm(x, y, 0x7632) : __byte_perm(x >> 12, y >> 12, 0x5410);
-    constexpr uint32_t mask = BITS == 4 ? 0x000F000Fu : 0x00070007u;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      o[e] = bsub2(((lo >> (BITS * e)) & mask) | 0x43004300u, kOffset<BITS>);
-      o[4 + e] = bsub2(((hi >> (BITS * e)) & mask) | 0x43004300u, kOffset<BITS>);
-    }
+    fields16<BITS>(__byte_perm(x, y, 0x5410), o);
+    fields16<BITS>(BITS == 4 ? __byte_perm(x, y, 0x7632) : __byte_perm(x >> 12, y >> 12, 0x5410), o + 4);
   }
 }
-
-__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+__device__ __forceinline__ uint32_t pack2_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// bf16 rows: bf16 operands; codes: fp16 operands.
+template <int BITS>
+__device__ __forceinline__ void mma_rows(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (BITS == 16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t r;

@@ -2,9 +2,9 @@
 //
 //   s_j = sm_scale * ks_j * (q . ck_j),   p_j = 2^(s_j - m),   out = sum_j p_j vs_j cv_j / sum_j p_j
 //
-// with codes ck, cv (exact in bf16) and per-row scales ks, vs applied in fp32; bits 16: ck, cv are the bf16 values and
-// the scales are 1.  p_j vs_j is rounded to bf16 (a half step of 2^-9, independent from key to key) because that is what
-// the tensor core multiplies; p's sum is taken before that rounding, in fp32.
+// bits 16: ck, cv are the bf16 values, the scales are 1 and p_j is rounded to bf16.  Codes are exact in fp16, and so are
+// the queries once a row is scaled by a power of two; p_j vs_j is rounded to fp16 against a running power of two above
+// the value scales.  These roundings are what the tensor core's operands cost; p's sum is taken before them, in fp32.
 //
 // Bound by the cache's bytes: every code is read once per 8 (16) query rows of its key head.  A thread block takes one
 // (sequence, key head, row tile, piece of the keys), its four warps take 16 keys in turn and meet only at the end, so there
@@ -41,7 +41,7 @@ struct Geo {
   using VLane = Lane<BITS, VU, 8>;
   static constexpr int STEP_WORDS = 2 * KLane::WORDS + 4 * VLane::WORDS + 4;
   // steps whose loads are in flight ahead of the one at work, as far as registers go
-  static constexpr int AHEAD = STEP_WORDS <= 24 ? 3 : STEP_WORDS <= 40 ? 2 : 1;
+  static constexpr int AHEAD = STEP_WORDS <= 40 ? 2 : 1;
   static constexpr int ROW_BYTES = D * BITS / 8;
 };
 template <int BITS, int D>
@@ -52,11 +52,13 @@ struct Step {
 };
 
 template <int BITS, int D, int NT>
-__global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_constant__ RowsParams p) {
+__global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 4 : 2) attn_rows_kernel(const __grid_constant__ RowsParams p) {
   using G = Geo<BITS, D>;
   constexpr int ROWS = 8 * NT;
   constexpr int MT = D / 16;                                  // 16-element tiles of the output
+  constexpr bool CODES = BITS < 16;
   __shared__ uint4 sq[NT][G::KU][32];
+  __shared__ float sqs[ROWS];
   __shared__ float so[ROWS][D + 4];
   __shared__ float sm[kWarps][ROWS], sl[kWarps][ROWS];
   grid_dependency_wait();
@@ -75,25 +77,53 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
   const int seen = p.a.causal ? max(0, min(len.held, len.kv - len.q_len + last_tok + 1)) : len.held;
   const int key0 = split * p.p.chunk;
   if (split > 0 && (long)split * p.p.chunk >= len.held) return;      // no such piece in this sequence: the combine step knows
-  const int key1 = split == p.p.splits - 1 ? seen : min(seen, key0 + p.p.chunk);
+  int key1 = split == p.p.splits - 1 ? seen : min(seen, key0 + p.p.chunk);
 
-  // ---- queries as B fragments: row n = g of tile nt, its pairs in the order the keys' units have ----
-  for (int i = threadIdx.x; i < NT * G::KU * 32; i += kThreads) {
-    const int ln = i & 31, u = (i >> 5) % G::KU, nt = (i >> 5) / G::KU;
-    const int r = r0 + nt * 8 + (ln >> 2);
+  // ---- queries as B fragments: row n = g of tile nt, its pairs in the order the keys' units have.  For codes they are
+  // fp16, scaled by the power of two that brings the row's largest magnitude near 2^15: a bf16 value keeps all its bits
+  // down to 2^-29 of that.  A warp takes whole rows. ----
+  for (int rr = warp; rr < ROWS; rr += kWarps) {
+    const int r = r0 + rr, nt = rr >> 3;
+    constexpr int CH = D / 8, PER = CH > 32 ? CH / 32 : 1;     // 16-byte pieces of a row: one to a lane
+    static_assert(PER == 1, "a row is at most 32 pieces");
     uint4 w = make_uint4(0, 0, 0, 0);
-    if (r < n_rows) {
+    if (r < n_rows && lane < CH) {
       const int tok = r / group, hq = head * group + r % group;
-      w = __ldg(reinterpret_cast<const uint4*>(p.a.q + (len.q0 + tok) * p.a.q_ts + hq * p.a.q_hs + 8 * G::KLane::unit_of(u, ln & 3)));
+      w = __ldg(reinterpret_cast<const uint4*>(p.a.q + (len.q0 + tok) * p.a.q_ts + hq * p.a.q_hs + 8 * lane));
     }
-    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-    uint32_t o[4];
+    uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    if (CODES) {
+      uint32_t top = 0;                                        // exponent of the largest finite magnitude
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int lo = pair_lo<BITS>(j), hi = pair_hi<BITS>(j);
-      o[j] = __byte_perm(x[lo / 2], x[hi / 2], (lo & 1 ? 0x32 : 0x10) | (hi & 1 ? 0x7600 : 0x5400));
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t lo = x[j] << 16 & 0x7F800000u, hi = x[j] & 0x7F800000u;
+        top = max(top, max(lo == 0x7F800000u ? 0u : lo, hi == 0x7F800000u ? 0u : hi));
+      }
+      top = __reduce_max_sync(0xffffffffu, top) >> 23;
+      // times 2^(14 - (top - 127)), in two steps that stay in range; back by the inverse
+      const int up = top == 0 ? 0 : 141 - (int)top;
+      const float f0 = __uint_as_float((uint32_t)(127 + up / 2) << 23), f1 = __uint_as_float((uint32_t)(127 + up - up / 2) << 23);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        x[j] = pack2_f16(__uint_as_float(x[j] << 16) * f0 * f1, __uint_as_float(x[j] & 0xFFFF0000u) * f0 * f1);
+      if (lane == 0) sqs[rr] = p.a.scale_log2 * (1.f / f0) * (1.f / f1);
+    } else if (lane == 0) {
+      sqs[rr] = p.a.scale_log2;
     }
-    sq[nt][u][ln] = make_uint4(o[0], o[1], o[2], o[3]);
+    if (lane < CH) {
+      uint32_t o[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int lo = pair16_lo<BITS>(j), hi = pair16_hi<BITS>(j);
+        o[j] = __byte_perm(x[lo / 2], x[hi / 2], (lo & 1 ? 0x32 : 0x10) | (hi & 1 ? 0x7600 : 0x5400));
+      }
+      // which lane of the row's four, and which of its units, this piece is
+#pragma unroll
+      for (int u = 0; u < G::KU; ++u)
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt)
+          if (G::KLane::unit_of(u, tt) == lane) sq[nt][u][(rr & 7) * 4 + tt] = make_uint4(o[0], o[1], o[2], o[3]);
+    }
   }
   __syncthreads();
 
@@ -110,11 +140,20 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
   low = min(low, key1);
   low = __reduce_min_sync(0xffffffffu, low);                  // below it no key needs a mask
 
-  float m[NT][2], l[NT][2], o[NT][MT][4];
+  // Per column: minus the maximum so far (0: none yet), p's sum.  `some`: every column has a maximum.
+  // vr: a power of two no smaller than any value scale so far.  The weights go to the tensor core as p vs / vr * 2^7 in
+  // fp16: at most 2^15, rounded by 2^-12 of themselves, or by 2^-32 vr where they are that small.
+  float neg[NT][2], qs[NT][2], l[NT][2], o[NT][MT][4];
+  float vr = 0x1p-100f, inv_vr = 0x1p107f;
+  uint32_t some = 0;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    m[nt][0] = m[nt][1] = -INFINITY;
-    l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      neg[nt][e] = 0.f;
+      l[nt][e] = 0.f;
+      qs[nt][e] = sqs[nt * 8 + 2 * t + e];
+    }
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -130,20 +169,41 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
   }
   const int* page_row = p.b.pages + (long)b * p.b.max_pages;
 
-  // scores (c: keys g and g + 8, columns 2t and 2t + 1) to P^T fragments, with the running maximum
+  // scores (c: keys g and g + 8, columns 2t and 2t + 1) to P^T fragments, with the running maximum.
+  // masked: keys beyond a column's limit, and key 0 where skip_first, do not count.
   auto softmax = [&](float (&c)[NT][4], int kb, const float (&ks)[2], const float (&vs)[2], bool masked, bool skip_first,
                      uint32_t (&pf)[NT][2]) {
-    bool raise = false;
+    float top = -INFINITY;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        c[nt][e] *= ks[e >> 1];
-        const int key = kb + g + (e >> 1) * 8;
-        if (masked && (key >= min(lim[nt][e & 1], key1) || (skip_first && key == 0))) c[nt][e] = -INFINITY;
-        raise |= c[nt][e] > m[nt][e & 1] + kLazy;
+        if (CODES) c[nt][e] *= qs[nt][e & 1];
+        c[nt][e] = fmaf(c[nt][e], CODES ? ks[e >> 1] : qs[nt][e & 1], neg[nt][e & 1]);
+        if (masked) {
+          const int key = kb + g + (e >> 1) * 8;
+          if (key >= min(lim[nt][e & 1], key1) || (skip_first && key == 0)) c[nt][e] = -INFINITY;
+        }
+        top = fmaxf(top, c[nt][e]);
       }
-    if (__any_sync(0xffffffffu, raise)) {
+    const bool wide = CODES && fmaxf(fabsf(vs[0]), fabsf(vs[1])) > vr;       // (a scale that is not finite shows in the result)
+    if (__any_sync(0xffffffffu, top > (some ? kLazy : -INFINITY) || wide)) {
+      float fv = 1.f;
+      if (CODES) {
+        uint32_t v = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t x = __float_as_uint(fabsf(vs[h]));
+          const int key = kb + g + 8 * h;
+          if (x < 0x7F000000u && key < key1) v = max(v, x);
+        }
+        v = (__reduce_max_sync(0xffffffffu, v) + 0x7FFFFFu) & 0x7F800000u;
+        const float to = fmaxf(vr, __uint_as_float(v));
+        fv = vr / to;                                          // a power of two (0 where it leaves the range)
+        vr = to;
+        inv_vr = 128.f / to;
+      }
+      bool all = true;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float f[2];
@@ -153,102 +213,109 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-          const float top = fmaxf(m[nt][e], x);
-          f[e] = top == -INFINITY ? 1.f : exp2_approx(m[nt][e] - top);
-          m[nt][e] = top;
+          const bool old = l[nt][e] != 0.f || neg[nt][e] != 0.f;     // (this lane's part of a sum may be 0 after a first key)
+          const bool seen = (__ballot_sync(0xffffffffu, old) & (0x11111111u << t)) != 0;
+          const float by = x > (seen ? kLazy : -INFINITY) ? x : 0.f;
+          f[e] = seen ? exp2_approx(-by) : 0.f;
+          neg[nt][e] -= by;
+          c[nt][e] -= by;
+          c[nt][e + 2] -= by;
           l[nt][e] *= f[e];
+          all = all && (seen || x > -INFINITY);
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          o[nt][i][0] *= f[0]; o[nt][i][1] *= f[1]; o[nt][i][2] *= f[0]; o[nt][i][3] *= f[1];
+          o[nt][i][0] *= f[0] * fv; o[nt][i][1] *= f[1] * fv; o[nt][i][2] *= f[0] * fv; o[nt][i][3] *= f[1] * fv;
         }
       }
+      some = __all_sync(0xffffffffu, all);
     }
+    const float vf[2] = {vs[0] * inv_vr, vs[1] * inv_vr};
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float w[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float top = m[nt][e & 1] == -INFINITY ? 0.f : m[nt][e & 1];
-        const float x = exp2_approx(c[nt][e] - top);
+        const float x = exp2_approx(c[nt][e]);
         l[nt][e & 1] += x;
-        w[e] = BITS == 16 ? x : x * vs[e >> 1];
+        w[e] = CODES ? x * vf[e >> 1] : x;
         if (masked && c[nt][e] == -INFINITY) w[e] = 0.f;        // (a scale that is not finite stays out, too)
       }
-      pf[nt][0] = transpose8x8(pack2(w[0], w[1]));
-      pf[nt][1] = transpose8x8(pack2(w[2], w[3]));
+      pf[nt][0] = transpose8x8(CODES ? pack2_f16(w[0], w[1]) : pack2(w[0], w[1]));
+      pf[nt][1] = transpose8x8(CODES ? pack2_f16(w[2], w[3]) : pack2(w[2], w[3]));
     }
   };
 
   // ---- the first token at 8 bits: one key, by the warp whose turn key 0 is ----
-  if (bos_row >= 0 && warp == 0) {
-    const long brow = (long)bos_row * p.c.n_kv_heads + head;
-    float c[NT][4] = {};
+  if constexpr (BITS < 8) {
+    if (bos_row >= 0 && warp == 0) {
+      auto value = [](const uint2& u, int e) { return (float)((int)(((e < 4 ? u.x : u.y) >> (8 * (e & 3))) & 255u) - 128); };
+      const long brow = (long)bos_row * p.c.n_kv_heads + head;
+      float c[NT][4] = {};
 #pragma unroll
-    for (int i = 0; i < G::KU; ++i) {
-      uint32_t a[4] = {0, 0, 0, 0};
-      if (g == 0) {
-        const uint2 u = __ldg(reinterpret_cast<const uint2*>(p.c.bos_k + brow * D) + G::KLane::unit_of(i, t));
+      for (int i = 0; i < G::KU; ++i) {
+        uint32_t a[4] = {0, 0, 0, 0};
+        if (g == 0) {
+          const uint2 u = __ldg(reinterpret_cast<const uint2*>(p.c.bos_k + brow * D) + G::KLane::unit_of(i, t));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int lo = pair_lo<BITS>(j), hi = pair_hi<BITS>(j);
-          a[j] = pack2((float)((int)(((lo < 4 ? u.x : u.y) >> (8 * (lo & 3))) & 255u) - 128),
-                       (float)((int)(((hi < 4 ? u.x : u.y) >> (8 * (hi & 3))) & 255u) - 128));
+          for (int j = 0; j < 4; ++j) a[j] = pack2_f16(value(u, pair16_lo<BITS>(j)), value(u, pair16_hi<BITS>(j)));
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const uint4 q = sq[nt][i][lane];
+          mma_rows<BITS>(c[nt], a[0], 0, a[1], 0, q.x, q.y);
+          mma_rows<BITS>(c[nt], a[2], 0, a[3], 0, q.z, q.w);
         }
       }
+      // key 0 alone: the other rows of the step are put out of it
+      const float ks[2] = {__ldg(p.c.bos_k_scale + brow), 0.f}, vs[2] = {g == 0 ? __ldg(p.c.bos_v_scale + brow) : 0.f, 0.f};
+      const int whole = key1;
+      key1 = 1;
+      uint32_t pf[NT][2];
+      softmax(c, 0, ks, vs, true, false, pf);
+      key1 = whole;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const uint4 q = sq[nt][i][lane];
-        mma16816(c[nt], a[0], 0, a[1], 0, q.x, q.y);
-        mma16816(c[nt], a[2], 0, a[3], 0, q.z, q.w);
+      for (int i = 0; i < G::VU; ++i) {
+        uint32_t a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (t == 0) {
+          const uint2 u = __ldg(reinterpret_cast<const uint2*>(p.c.bos_v + brow * D) + G::VLane::unit_of(i, g));
+#pragma unroll
+          for (int e = 0; e < 8; ++e) a[e] = pack2_f16(value(u, e), 0.f);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) mma_rows<BITS>(o[nt][4 * i + q], a[2 * q], a[2 * q + 1], 0, 0, pf[nt][0], pf[nt][1]);
       }
-    }
-    const float ks[2] = {__ldg(p.c.bos_k_scale + brow) * p.a.scale_log2, 0.f}, vs[2] = {__ldg(p.c.bos_v_scale + brow), 0.f};
-    // keep row 0 alone
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        c[nt][e] *= ks[e >> 1];
-        if (g != 0 || e > 1) c[nt][e] = -INFINITY;
-      }
-    const float one[2] = {1.f, 1.f};
-    uint32_t pf[NT][2];
-    softmax(c, 0, one, vs, true, false, pf);
-#pragma unroll
-    for (int i = 0; i < G::VU; ++i) {
-      uint32_t a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (t == 0) {
-        const uint2 u = __ldg(reinterpret_cast<const uint2*>(p.c.bos_v + brow * D) + G::VLane::unit_of(i, g));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) a[e] = pack2((float)((int)(((e < 4 ? u.x : u.y) >> (8 * (e & 3))) & 255u) - 128), 0.f);
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) mma16816(o[nt][4 * i + q], a[2 * q], a[2 * q + 1], 0, 0, pf[nt][0], pf[nt][1]);
     }
   }
 
-  // ---- the keys, 16 at a time ----
+  // ---- the keys, 16 at a time.  All 16 rows of a step are read, those beyond the last key too: a page is there as a
+  // whole, and what they hold is masked.  Row numbers fit 32 bits (checked on the host): one multiply-add an address. ----
   Step<BITS, D> st[G::AHEAD];
+  const unsigned char* kp = p.c.k + (g * G::ROW_BYTES);
+  const unsigned char* vp = p.c.v + (2 * t * G::ROW_BYTES);
+  const float* ksp = CODES ? p.c.k_scale + g : nullptr;
+  const float* vsp = CODES ? p.c.v_scale + g : nullptr;
+  const uint32_t page_rows = (uint32_t)p.c.n_kv_heads << p.c.page_shift, head_rows = (uint32_t)head << p.c.page_shift;
+  const int slot_mask = (1 << p.c.page_shift) - 1;
   auto page_of = [&](int kb) { return kb < key1 ? __ldg(page_row + (kb >> p.c.page_shift)) : -1; };
   auto load = [&](Step<BITS, D>& s, int kb, int page) {
-    const bool here = kb < key1 && page >= 0 && page < p.c.n_pages;
-    const long row0 = cache_row(p.c, here ? page : 0, head, kb & ((1 << p.c.page_shift) - 1));
+    const bool here = page >= 0 && page < p.c.n_pages;         // (-1 beyond the last key)
+    if (here) {
+      const uint32_t row0 = (uint32_t)page * page_rows + head_rows + (uint32_t)(kb & slot_mask);
+      const unsigned char* k = kp + (uint64_t)row0 * G::ROW_BYTES;
+      const unsigned char* v = vp + (uint64_t)row0 * G::ROW_BYTES;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const bool live = here && kb + g + 8 * h < key1;
-      s.k[h].load(p.c.k + (row0 + g + 8 * h) * G::ROW_BYTES, t, live);
-      if (BITS < 16) {
-        s.ks[h] = live ? __ldg(p.c.k_scale + row0 + g + 8 * h) : 0.f;
-        s.vs[h] = live ? __ldg(p.c.v_scale + row0 + g + 8 * h) : 0.f;
+      for (int h = 0; h < 2; ++h) {
+        s.k[h].load(k + 8 * h * G::ROW_BYTES, t);
+        if (CODES) {
+          s.ks[h] = __ldg(ksp + (uint64_t)row0 + 8 * h);
+          s.vs[h] = __ldg(vsp + (uint64_t)row0 + 8 * h);
+        }
       }
-    }
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      const int r = 2 * t + (h & 1) + 8 * (h >> 1);
-      s.v[h].load(p.c.v + (row0 + r) * G::ROW_BYTES, g, here && kb + r < key1);
+      for (int h = 0; h < 4; ++h) s.v[h].load(v + ((h & 1) + 8 * (h >> 1)) * G::ROW_BYTES, g);
     }
     return here;
   };
@@ -266,36 +333,41 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
 #pragma unroll
     for (int d = 0; d < G::AHEAD; ++d) {
       if (kb < key1) {
-        const Step<BITS, D>& s = st[d];
+        Step<BITS, D>& s = st[d];
         if (!here[d]) {
           report_device_error(p.status, HBL_ERR_RANGE);
         } else {
+          const bool masked = kb + 16 > low || (bos && kb == 0);
+          if (!CODES && kb + 16 > key1) {                      // 0 * what lies beyond the last key may not be 0
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+              if (kb + 2 * t + (h & 1) + 8 * (h >> 1) >= key1) s.v[h].clear();
+          }
           float c[NT][4] = {};
 #pragma unroll
           for (int i = 0; i < G::KU; ++i) {
             uint32_t x[4], y[4];
-            pairs<BITS>(s.k[0], i, t, x);
-            pairs<BITS>(s.k[1], i, t, y);
+            pairs16<BITS>(s.k[0], i, t, x);
+            pairs16<BITS>(s.k[1], i, t, y);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               const uint4 q = sq[nt][i][lane];
-              mma16816(c[nt], x[0], y[0], x[1], y[1], q.x, q.y);
-              mma16816(c[nt], x[2], y[2], x[3], y[3], q.z, q.w);
+              mma_rows<BITS>(c[nt], x[0], y[0], x[1], y[1], q.x, q.y);
+              mma_rows<BITS>(c[nt], x[2], y[2], x[3], y[3], q.z, q.w);
             }
           }
-          const float ks[2] = {BITS == 16 ? p.a.scale_log2 : s.ks[0] * p.a.scale_log2, BITS == 16 ? p.a.scale_log2 : s.ks[1] * p.a.scale_log2};
           uint32_t pf[NT][2];
-          softmax(c, kb, ks, s.vs, kb + 16 > low || (bos && kb == 0), bos, pf);
+          softmax(c, kb, s.ks, s.vs, masked, bos, pf);
 #pragma unroll
           for (int i = 0; i < G::VU; ++i) {
             uint32_t x[8], y[8];
-            cross<BITS>(s.v[0], s.v[1], i, g, x);
-            cross<BITS>(s.v[2], s.v[3], i, g, y);
+            cross16<BITS>(s.v[0], s.v[1], i, g, x);
+            cross16<BITS>(s.v[2], s.v[3], i, g, y);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
               for (int q = 0; q < 4; ++q)
-                mma16816(o[nt][4 * i + q], x[2 * q], x[2 * q + 1], y[2 * q], y[2 * q + 1], pf[nt][0], pf[nt][1]);
+                mma_rows<BITS>(o[nt][4 * i + q], x[2 * q], x[2 * q + 1], y[2 * q], y[2 * q + 1], pf[nt][0], pf[nt][1]);
           }
         }
       }
@@ -307,6 +379,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
   }
 
   // ---- the four warps' results together ----
+  float m[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -315,6 +388,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
       x += __shfl_xor_sync(0xffffffffu, x, 4);
       x += __shfl_xor_sync(0xffffffffu, x, 8);
       x += __shfl_xor_sync(0xffffffffu, x, 16);
+      m[nt][e] = x == 0.f ? -INFINITY : -neg[nt][e];           // (a NaN has a place in the sum, too)
       if (g == 0) {
         sm[warp][nt * 8 + 2 * t + e] = m[nt][e];
         sl[warp][nt * 8 + 2 * t + e] = x;
@@ -330,7 +404,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
       float top = sm[0][r];
 #pragma unroll
       for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sm[w][r]);
-      f[nt][e] = exp2_approx(m[nt][e] - (top == -INFINITY ? 0.f : top));     // (0 where there was no key; a NaN stays in o)
+      f[nt][e] = exp2_approx(m[nt][e] - (top == -INFINITY ? 0.f : top)) * (CODES ? vr * 0x1p-7f : 1.f);     // (0 where there was no key)
     }
   for (int w = 0; w < kWarps; ++w) {
     if (warp == w) {
@@ -373,49 +447,79 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
   }
 }
 
-// The pieces of a row together (whichever kernel computed them): out = sum_s 2^(lse_s - top) o_s / sum_s 2^(lse_s - top).  A warp takes one row.
+// The pieces of a row together (whichever kernel computed them): out = sum_s 2^(lse_s - top) o_s / sum_s 2^(lse_s - top).
+// `share` warps (1, 2, 4 or 8, by the number of pieces) take the pieces of a row in turn, four loads in flight each, and
+// add up through shared memory in a fixed order.
 struct CombineParams {
   KvView c;
   BatchView b;
   AttnArgs a;
   AttnPlan rows, tiles;          // of sequences of up to `few` rows, and of the others
-  int few;
+  int few, share;
   const float *part_o, *part_lse;
   int* status;
 };
 template <int D>
 __global__ void __launch_bounds__(256) attn_combine_kernel(const __grid_constant__ CombineParams p) {
+  constexpr int E = D / 32;
+  __shared__ float s_acc[8][D], s_sum[8];
   grid_dependency_wait();
-  const int lane = threadIdx.x & 31;
-  const long total_rows = (long)p.b.tokens * p.a.n_heads, row = (long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (row >= total_rows) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = warp % p.share;
+  const long total_rows = (long)p.b.tokens * p.a.n_heads, row = ((long)blockIdx.x * 8 + warp) / p.share;
   const int tok = (int)(row / p.a.n_heads), hq = (int)(row % p.a.n_heads);
-  const int b = find_sequence(p.b.q_start, p.b.n_seqs, tok, lane);
-  if (b >= p.b.n_seqs) return;
-  SeqLens len;
-  if (!sequence_lengths(p.b, b, p.c.page_shift, p.status, len) || tok < len.q0 || tok - len.q0 >= p.b.max_q_len) return;
-  const AttnPlan& plan = (long)min(len.q_len, p.b.max_q_len) * p.a.group > p.few ? p.tiles : p.rows;
-  if (plan.splits <= 1) return;                               // written whole
-  const int pieces = max(1, min(plan.splits, (len.held + plan.chunk - 1) / plan.chunk));
+  int pieces = 0;                                             // 0: nothing to do
+  if (row < total_rows) {
+    const int b = find_sequence(p.b.q_start, p.b.n_seqs, tok, lane);
+    SeqLens len;
+    if (b < p.b.n_seqs && sequence_lengths(p.b, b, p.c.page_shift, p.status, len) && tok >= len.q0 && tok - len.q0 < p.b.max_q_len) {
+      const AttnPlan& plan = (long)min(len.q_len, p.b.max_q_len) * p.a.group > p.few ? p.tiles : p.rows;
+      if (plan.splits > 1) pieces = max(1, min(plan.splits, (len.held + plan.chunk - 1) / plan.chunk));      // else written whole
+    }
+  }
   float top = -INFINITY;
   for (int s = lane; s < pieces; s += 32) top = fmaxf(top, p.part_lse[s * total_rows + row]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  constexpr int E = D / 32;
   float acc[E] = {}, sum = 0.f;
-  for (int s = 0; s < pieces; ++s) {
-    const float x = p.part_lse[s * total_rows + row];
-    const float w = x == -INFINITY ? 0.f : exp2_approx(x - top);      // (a NaN stays one)
-    if (w == 0.f) continue;
-    sum += w;
-    const float* src = p.part_o + (s * total_rows + row) * D + lane * E;
+  for (int s0 = mine; s0 < pieces; s0 += 4 * p.share) {
+    float w[4], v[4][E];
 #pragma unroll
-    for (int e = 0; e < E; e += 2) {
-      const float2 v = *reinterpret_cast<const float2*>(src + e);
-      acc[e] += w * v.x;
-      acc[e + 1] += w * v.y;
+    for (int k = 0; k < 4; ++k) {
+      const int s = s0 + k * p.share;
+      const float x = s < pieces ? p.part_lse[s * total_rows + row] : -INFINITY;
+      w[k] = x == -INFINITY ? 0.f : exp2_approx(x - top);     // (a NaN stays one)
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[k][e] = 0.f;
+      if (s < pieces) {
+        const float* src = p.part_o + (s * total_rows + row) * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          const float2 y = *reinterpret_cast<const float2*>(src + e);
+          v[k][e] = y.x;
+          v[k][e + 1] = y.y;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      sum += w[k];
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += w[k] * v[k][e];    // (a piece without a key holds zeros)
     }
   }
+  if (p.share > 1) {
+    if (lane == 0) s_sum[warp] = sum;
+#pragma unroll
+    for (int e = 0; e < E; ++e) s_acc[warp][lane * E + e] = acc[e];
+    __syncthreads();
+    if (mine != 0) return;
+    for (int w = 1; w < p.share; ++w) {
+      sum += s_sum[warp + w];
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += s_acc[warp + w][lane * E + e];
+    }
+  }
+  if (pieces == 0) return;
   const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
   uint32_t* dst = reinterpret_cast<uint32_t*>(p.a.out + tok * p.a.o_ts + hq * p.a.o_hs + lane * E);
 #pragma unroll
@@ -491,7 +595,9 @@ int launch_attention_combine(const KvView& c, const BatchView& b, const AttnArgs
   p.c = c; p.b = b; p.a = a; p.rows = rows; p.tiles = tiles; p.few = few; p.part_o = part_o; p.part_lse = part_lse;
   p.status = device_status_word();
   if (p.status == nullptr) return HBL_ERR_CUDA;
-  const long blocks = ((long)b.tokens * a.n_heads + 7) / 8;
+  const int most = rows.splits > tiles.splits ? rows.splits : tiles.splits;
+  p.share = most <= 4 ? 1 : most <= 8 ? 2 : most <= 16 ? 4 : 8;
+  const long blocks = ((long)b.tokens * a.n_heads * p.share + 7) / 8;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
   const dim3 grid((unsigned)blocks), block(256);
   switch (c.head_dim) {

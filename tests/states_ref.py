@@ -8,6 +8,11 @@ the attention is rounded once to bf16, and each p_j (times the value row's scale
 where e collects what fp32 adds: the scores, sums of head_dim products, are off by at most (head_dim + 4) 2^-23 times the
 sum of the products' magnitudes, which moves p by that factor and p's sum with it (twice); N additions to an
 accumulator by at most N 2^-23 of A; 2^-20 covers exp2, the scales' products and the division.
+
+Codes: where p_j vs_j goes through fp16 instead (2^-12 of the value), it is held as p_j vs_j / vr * 2^7 with vr the power
+of two above the largest value scale, vr <= 2 max vs, and below 2^-14 fp16 has a fixed step of 2^-24: a weight is then off by
+at most 2^-25 2^-7 vr <= 2^-31 max vs.  p's sum is at least 1 (the maximum is one of the scores), a code is at most
+2^(b-1) <= 4/3 of what makes max |v| out of max vs, so n keys add at most n 2^-30 max |v|.
 """
 import math
 
@@ -92,6 +97,8 @@ def attention64(cache, q, q_lens, kv_lens, tables, sm_scale, causal, slots=None)
                 steps = (nk / 16 + 64) * 2.0 ** -23
                 e = 2 * e_s + steps + 2.0 ** -20
                 tol[r, hh] = 2.0 ** -8 * out[r, hh].abs() + (2.0 ** -8 + e)[:, None] * (p @ clean.abs()) * 1.01 + 1e-30
+                if cache.bits < 16:
+                    tol[r, hh] += nk * 2.0 ** -30 * clean.abs().max()
                 tol_lse[r, hh] = e_s + steps + 2.0 ** -20 * (1 + z.abs())
         at += nq
     return out, lse, tol, tol_lse
