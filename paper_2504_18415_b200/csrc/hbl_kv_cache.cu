@@ -60,49 +60,63 @@ struct AppendParams {
   float eps;
 };
 
+// Where a token goes: the block's token t, looked up by every warp for itself.  False: nowhere (reported, or behind the
+// last sequence).
+struct Place { int b, pos, page, slot, slot8; };             // slot8: row of the 8-bit first tokens, -1: none
+template <bool BOS>
+__device__ __forceinline__ bool find_place(const KvView& c, const BatchView& s, int t, int lane, int* status, Place& o) {
+  o.b = find_sequence(s.q_start, s.n_seqs, t, lane);
+  if (o.b >= s.n_seqs) return false;                          // a row behind the last sequence
+  SeqLens len;
+  if (!sequence_lengths(s, o.b, c.page_shift, status, len)) return false;
+  const long place = (long)len.kv - len.q_len + (t - len.q0);
+  o.pos = (int)place;
+  o.slot8 = -1;
+  bool good = place >= 0 && place < len.held && t >= len.q0;
+  if (good) {
+    o.page = __ldg(s.pages + (long)o.b * s.max_pages + (place >> c.page_shift));
+    o.slot = (int)place & ((1 << c.page_shift) - 1);
+    good = o.page >= 0 && o.page < c.n_pages;
+    if (BOS && good && place == 0 && c.bos_k != nullptr) {
+      o.slot8 = s.bos_slot != nullptr ? __ldg(s.bos_slot + o.b) : o.b;
+      good = o.slot8 >= 0 && o.slot8 < c.n_slots;
+    }
+  }
+  if (!good) report_device_error(status, HBL_ERR_RANGE);
+  return good;
+}
+
 // BITS 3, 4, 8 or 16; LPH = head_dim / 8 lanes to a head; a thread takes ROWS heads (queries, then keys, then
 // values) of one token.  A thread block works on one token.
 template <int BITS, int LPH, bool INTERLEAVED, int ROWS>
 __global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int GROUPS = kThreads / LPH;                      // heads side by side in the block
+  constexpr int HPW = 32 / LPH;                               // ... and in a warp
   grid_dependency_wait();
   const int t = blockIdx.x / p.blocks_per_token, part = blockIdx.x % p.blocks_per_token;
   const int lane = threadIdx.x & 31, j = threadIdx.x % LPH, group = threadIdx.x / LPH;
-  const int kvh = p.c.n_kv_heads, rows = p.n_heads + 2 * kvh;
+  const int kvh = p.c.n_kv_heads, first_v = p.n_heads + kvh, rows = first_v + kvh;
+  const __nv_bfloat16 *q = p.q + t * p.q_ts + 8 * j, *k = p.k + t * p.k_ts + 8 * j, *v = p.v + t * p.v_ts + 8 * j;
+  const int r0 = part * (ROWS * GROUPS) + group;              // the thread's rows: r0 + i * GROUPS
   uint4 raw[ROWS];
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {
-    const int r = (part * ROWS + i) * GROUPS + group;
+    const int r = r0 + i * GROUPS;
     raw[i] = make_uint4(0, 0, 0, 0);
     if (r < rows) {
-      const __nv_bfloat16* src = r < p.n_heads         ? p.q + t * p.q_ts + r * p.q_hs
-                                 : r < p.n_heads + kvh ? p.k + t * p.k_ts + (r - p.n_heads) * p.k_hs
-                                                       : p.v + t * p.v_ts + (r - p.n_heads - kvh) * p.v_hs;
-      raw[i] = *reinterpret_cast<const uint4*>(src + 8 * j);
+      const __nv_bfloat16* src = r < p.n_heads ? q + r * p.q_hs : r < first_v ? k + (r - p.n_heads) * p.k_hs : v + (r - first_v) * p.v_hs;
+      raw[i] = *reinterpret_cast<const uint4*>(src);
     }
   }
-  // ---- where the token goes ----
-  const int b = find_sequence(p.b.q_start, p.b.n_seqs, t, lane);
-  if (b >= p.b.n_seqs) return;                                // a row behind the last sequence
-  SeqLens len;
-  if (!sequence_lengths(p.b, b, p.c.page_shift, p.status, len)) return;
-  const long place = (long)len.kv - len.q_len + (t - len.q0);
-  bool good = place >= 0 && place < len.held && t >= len.q0;
-  const int at = p.positions != nullptr ? __ldg(p.positions + t) : (int)place;
-  int page = 0, slot8 = -1;
-  if (good) {
-    page = __ldg(p.b.pages + (long)b * p.b.max_pages + (place >> p.c.page_shift));
-    good = page >= 0 && page < p.c.n_pages && (p.table == nullptr || (at >= 0 && at < p.n_pos));
-    if (good && place == 0 && p.c.bos_k != nullptr) {
-      slot8 = p.b.bos_slot != nullptr ? __ldg(p.b.bos_slot + b) : b;
-      good = slot8 >= 0 && slot8 < p.c.n_slots;
-    }
-  }
-  if (!good) {
+  Place at;
+  if (!find_place<(BITS < 8)>(p.c, p.b, t, lane, p.status, at)) return;
+  const int turn = p.positions != nullptr ? __ldg(p.positions + t) : at.pos;
+  if (p.table != nullptr && (turn < 0 || turn >= p.n_pos)) {
     report_device_error(p.status, HBL_ERR_RANGE);
     return;
   }
-  // ---- the lane's pairs: 4 of the interleaved layout, 8 of the half layout (elements 8j .. 8j + 7 and their partners) ----
+  // ---- the lane's pairs: 4 of the interleaved layout, 8 of the half layout (elements 8j .. 8j + 7 and their partners).
+  // Lower half: c x1 - s x2; upper half: c x2 + s x1: the sign goes into s, products and sum are rounded one by one. ----
   constexpr int PAIRS = INTERLEAVED ? 4 : 8;
   const int half8 = p.rot_dim / 16;                           // lanes to half of the rotated part
   const bool turned = p.table != nullptr && 8 * j < p.rot_dim;
@@ -111,91 +125,120 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_consta
   float c[PAIRS], s[PAIRS];
   if (turned) {
     const int first = INTERLEAVED ? 4 * j : 8 * (upper ? j - half8 : j);
-    const float4* row = p.table + ((long)at * (p.rot_dim / 2) + first) / 2;
+    const float4* row = p.table + ((long)turn * (p.rot_dim / 2) + first) / 2;
 #pragma unroll
     for (int i = 0; i < PAIRS / 2; ++i) {
-      const float4 v = __ldg(row + i);
-      c[2 * i] = v.x; s[2 * i] = v.y; c[2 * i + 1] = v.z; s[2 * i + 1] = v.w;
+      const float4 x = __ldg(row + i);
+      c[2 * i] = x.x; s[2 * i] = upper ? x.y : -x.y; c[2 * i + 1] = x.z; s[2 * i + 1] = upper ? x.w : -x.w;
     }
   } else {
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) { c[i] = 1.f; s[i] = 0.f; }
   }
+  const long row0 = cache_row(p.c, at.page, 0, at.slot);      // head h: row0 + (h << page_shift)
+  float f[BITS == 16 ? 1 : ROWS][8];
+  uint32_t top[ROWS];
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {
-    const int r = (part * ROWS + i) * GROUPS + group;
-    const int kind = r < p.n_heads ? 0 : r < p.n_heads + kvh ? 1 : 2;
-    float f[8];
-    widen8(raw[i], f);
-    // (every lane of the warp takes part in the shuffles, whatever its rows are)
-    if constexpr (!INTERLEAVED) {
-      uint4 other;
-      other.x = __shfl_sync(0xffffffffu, raw[i].x, partner);
-      other.y = __shfl_sync(0xffffffffu, raw[i].y, partner);
-      other.z = __shfl_sync(0xffffffffu, raw[i].z, partner);
-      other.w = __shfl_sync(0xffffffffu, raw[i].w, partner);
-      if (turned && kind != 2) {
-        float g[8];
-        widen8(other, g);
+    const int r = r0 + i * GROUPS;
+    float (&x)[8] = f[BITS == 16 ? 0 : i];
+    top[i] = 0;
+    widen8(raw[i], x);
+    const bool rotate = turned && r < first_v;
+    if (__any_sync(0xffffffffu, rotate)) {                     // (the whole warp: it shuffles)
+      if constexpr (!INTERLEAVED) {
+        uint4 other;
+        other.x = __shfl_sync(0xffffffffu, raw[i].x, partner);
+        other.y = __shfl_sync(0xffffffffu, raw[i].y, partner);
+        other.z = __shfl_sync(0xffffffffu, raw[i].z, partner);
+        other.w = __shfl_sync(0xffffffffu, raw[i].w, partner);
+        if (rotate) {
+          float g[8];
+          widen8(other, g);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)                            // lower half: c x1 - s x2; upper half: c x2 + s x1
-          f[k] = upper ? __fadd_rn(__fmul_rn(f[k], c[k]), __fmul_rn(g[k], s[k]))
-                       : __fsub_rn(__fmul_rn(f[k], c[k]), __fmul_rn(g[k], s[k]));
-      }
-    } else if (turned && kind != 2) {
+          for (int e = 0; e < 8; ++e) x[e] = __fadd_rn(__fmul_rn(x[e], c[e]), __fmul_rn(g[e], s[e]));
+        }
+      } else if (rotate) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float x1 = f[2 * k], x2 = f[2 * k + 1];
-        f[2 * k] = __fsub_rn(__fmul_rn(x1, c[k]), __fmul_rn(x2, s[k]));
-        f[2 * k + 1] = __fadd_rn(__fmul_rn(x2, c[k]), __fmul_rn(x1, s[k]));
+        for (int e = 0; e < 4; ++e) {
+          const float x1 = x[2 * e], x2 = x[2 * e + 1];
+          x[2 * e] = __fadd_rn(__fmul_rn(x1, c[e]), __fmul_rn(x2, s[e]));
+          x[2 * e + 1] = __fsub_rn(__fmul_rn(x2, c[e]), __fmul_rn(x1, s[e]));
+        }
       }
     }
-    const int head = kind == 1 ? r - p.n_heads : r - p.n_heads - kvh;
-    const bool live = r < rows;
-    if (kind == 0 && live) *reinterpret_cast<uint4*>(p.q_out + t * p.qo_ts + r * p.qo_hs + 8 * j) = narrow8(f);
-    const bool store = live && kind != 0;
-    const long row = store ? cache_row(p.c, page, head, (int)(place & ((1 << p.c.page_shift) - 1))) : 0;
-    unsigned char* base = kind == 1 ? p.c.k : p.c.v;
-    if constexpr (BITS == 16) {
-      if (store) *reinterpret_cast<uint4*>(base + (row * LPH + j) * 16) = narrow8(f);
-    } else {
+    if (r < p.n_heads) {
+      *reinterpret_cast<uint4*>(p.q_out + t * p.qo_ts + r * p.qo_hs + 8 * j) = narrow8(x);
+    } else if (BITS == 16 && r < rows) {
+      const bool key = r < first_v;
+      const long row = row0 + ((long)(r - (key ? p.n_heads : first_v)) << p.c.page_shift);
+      *reinterpret_cast<uint4*>((key ? p.c.k : p.c.v) + (row * LPH + j) * 16) = narrow8(x);
+    }
+    if (BITS < 16) {
       // the head's largest magnitude, on the bit patterns: a NaN is larger than everything and is not lost
-      uint32_t m = 0;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) m = max(m, __float_as_uint(f[k]) & 0x7FFFFFFFu);
+      for (int e = 0; e < 8; ++e) top[i] = max(top[i], __float_as_uint(x[e]) & 0x7FFFFFFFu);
+    }
+  }
+  if constexpr (BITS < 16) {
+    if (r0 + (ROWS - 1) * GROUPS - (lane / LPH) + HPW - 1 < p.n_heads) return;     // (uniform: the warp has queries only)
+    constexpr float C = (float)((1 << (BITS - 1)) - 1);
+    // Both divisions of a head cost what they cost for a whole warp, so the warp's ROWS * HPW heads are put one to a lane
+    // and divided together.
+    uint32_t mine = 0;
 #pragma unroll
-      for (int o = LPH / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-      const bool finite = m < 0x7F800000u;
-      const float gamma = __uint_as_float(m);
-      constexpr float C = (float)((1 << (BITS - 1)) - 1);
-      const float rq = finite ? __fdiv_rn(C, __fadd_rn(gamma, p.eps)) : 0.f;
-      const float scale = finite ? __fdiv_rn(gamma, C) : __uint_as_float(0x7FC00000u);
-      if (!finite) {
+    for (int i = 0; i < ROWS; ++i) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = 0.f;
+      for (int o = LPH / 2; o > 0; o >>= 1) top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
+      const uint32_t x = __shfl_sync(0xffffffffu, top[i], (lane % HPW) * LPH);
+      if (lane / HPW == i) mine = x;
+    }
+    const bool finite = mine < 0x7F800000u;
+    const float gamma = finite ? __uint_as_float(mine) : 0.f;
+    const float rq_mine = finite ? __fdiv_rn(C, __fadd_rn(gamma, p.eps)) : 0.f;
+    if (lane < ROWS * HPW) {
+      const int r = r0 - lane / LPH + lane % HPW + (lane / HPW) * GROUPS;            // this lane's head
+      if (r >= p.n_heads && r < rows) {
+        const bool key = r < first_v;
+        const long row = row0 + ((long)(r - (key ? p.n_heads : first_v)) << p.c.page_shift);
+        (key ? p.c.k_scale : p.c.v_scale)[row] = finite ? __fdiv_rn(gamma, C) : __uint_as_float(0x7FC00000u);
       }
-      const uint2 u = codes8<BITS>(f, rq);
-      unsigned char* dst = base + row * (LPH * BITS);
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const int r = r0 + i * GROUPS;
+      const float rq = __shfl_sync(0xffffffffu, rq_mine, i * HPW + lane / LPH);
+      float (&x)[8] = f[BITS == 16 ? 0 : i];
+      if (top[i] >= 0x7F800000u) {                             // the head reads as NaN: its codes are those of zero
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.f;
+      }
+      const bool store = r >= p.n_heads && r < rows;
+      const bool key = r < first_v;
+      const int head = r - (key ? p.n_heads : first_v);
+      const long row = row0 + ((long)head << p.c.page_shift);
+      const uint2 u = codes8<BITS>(x, rq);
+      unsigned char* dst = (key ? p.c.k : p.c.v) + row * (LPH * BITS);
       if constexpr (BITS == 8) {
         if (store) *reinterpret_cast<uint2*>(dst + 8 * j) = u;
       } else if constexpr (BITS == 4) {
         if (store) *reinterpret_cast<uint32_t*>(dst + 4 * j) = __byte_perm(u.x | (u.x >> 4), u.y | (u.y >> 4), 0x6420);
       } else {
-        // 24 bits a lane; four neighbouring lanes make three 32-bit words
-        uint32_t o = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) o |= (((u.x >> (8 * k)) & 7u) << (3 * k)) | (((u.y >> (8 * k)) & 7u) << (3 * k + 12));
+        // 24 bits a lane (four codes: bits 0-2, 8-10, .. moved together); four neighbouring lanes make three 32-bit words
+        auto twelve = [](uint32_t y) { y = (y & 0x00070007u) | ((y >> 5) & 0x00380038u); return (y & 0x3Fu) | ((y >> 10) & 0xFC0u); };
+        const uint32_t o = twelve(u.x) | twelve(u.y) << 12;
         const uint32_t next = __shfl_down_sync(0xffffffffu, o, 1);
-        const int q = j & 3;
-        const uint32_t word = q == 0 ? (o | (next << 24)) : q == 1 ? ((o >> 8) | (next << 16)) : ((o >> 16) | (next << 8));
-        if (store && q < 3) *reinterpret_cast<uint32_t*>(dst + 12 * (j >> 2) + 4 * q) = word;
+        const int w = j & 3;
+        const uint32_t word = w == 0 ? (o | (next << 24)) : w == 1 ? ((o >> 8) | (next << 16)) : ((o >> 16) | (next << 8));
+        if (store && w < 3) *reinterpret_cast<uint32_t*>(dst + 12 * (j >> 2) + 4 * w) = word;
       }
-      if (store && j == 0) (kind == 1 ? p.c.k_scale : p.c.v_scale)[row] = scale;
-      if (BITS < 8 && store && slot8 >= 0) {                  // the sequence's first token, at 8 bits as well
-        const long brow = (long)slot8 * kvh + head;
-        const float rq8 = finite ? __fdiv_rn(127.0f, __fadd_rn(gamma, p.eps)) : 0.f;
-        *reinterpret_cast<uint2*>((kind == 1 ? p.c.bos_k : p.c.bos_v) + (brow * LPH + j) * 8) = codes8<8>(f, rq8);
-        if (j == 0) (kind == 1 ? p.c.bos_k_scale : p.c.bos_v_scale)[brow] = finite ? __fdiv_rn(gamma, 127.0f) : scale;
+      if (BITS < 8 && store && at.slot8 >= 0) {                // the sequence's first token, at 8 bits as well
+        const bool sane = top[i] < 0x7F800000u;
+        const float g = __uint_as_float(top[i]);
+        const long brow = (long)at.slot8 * kvh + head;
+        const float rq8 = sane ? __fdiv_rn(127.0f, __fadd_rn(g, p.eps)) : 0.f;
+        *reinterpret_cast<uint2*>((key ? p.c.bos_k : p.c.bos_v) + (brow * LPH + j) * 8) = codes8<8>(x, rq8);
+        if (j == 0) (key ? p.c.bos_k_scale : p.c.bos_v_scale)[brow] = sane ? __fdiv_rn(g, 127.0f) : __uint_as_float(0x7FC00000u);
       }
     }
   }
@@ -209,65 +252,67 @@ struct ReadParams {
   int blocks_per_token;
 };
 
-template <int BITS, int LPH>
+// A thread takes ROWS heads (keys, then values) of one token; a thread block works on one token.
+template <int BITS, int LPH, int ROWS>
 __global__ void __launch_bounds__(kThreads) kv_read_kernel(const __grid_constant__ ReadParams p) {
   constexpr int GROUPS = kThreads / LPH;
   grid_dependency_wait();
   const int t = blockIdx.x / p.blocks_per_token, part = blockIdx.x % p.blocks_per_token;
-  const int lane = threadIdx.x & 31, j = threadIdx.x % LPH;
-  const int b = find_sequence(p.b.q_start, p.b.n_seqs, t, lane);
-  if (b >= p.b.n_seqs) return;
-  SeqLens len;
-  if (!sequence_lengths(p.b, b, p.c.page_shift, p.status, len)) return;
-  const int r = part * GROUPS + threadIdx.x / LPH, kvh = p.c.n_kv_heads;
-  if (r >= 2 * kvh) return;
-  const long place = (long)len.kv - len.q_len + (t - len.q0);
-  bool good = place >= 0 && place < len.held && t >= len.q0;
-  int page = 0, slot8 = -1;
-  if (good) {
-    page = __ldg(p.b.pages + (long)b * p.b.max_pages + (place >> p.c.page_shift));
-    good = page >= 0 && page < p.c.n_pages;
-    if (BITS < 8 && place == 0 && p.c.bos_k != nullptr) {
-      slot8 = p.b.bos_slot != nullptr ? __ldg(p.b.bos_slot + b) : b;
-      good = good && slot8 >= 0 && slot8 < p.c.n_slots;
-    }
-  }
-  if (!good) {
-    report_device_error(p.status, HBL_ERR_RANGE);
-    return;
-  }
-  const bool key = r < kvh;
-  const int head = key ? r : r - kvh;
-  const long row = cache_row(p.c, page, head, (int)(place & ((1 << p.c.page_shift) - 1)));
-  const unsigned char* base = key ? p.c.k : p.c.v;
-  uint4 o;
-  if constexpr (BITS == 16) {
-    o = *reinterpret_cast<const uint4*>(base + (row * LPH + j) * 16);
-  } else {
-    float f[8];
-    float scale = (key ? p.c.k_scale : p.c.v_scale)[row];
-    if (slot8 >= 0 || BITS == 8) {
-      const long brow = (long)slot8 * kvh + head;
-      const unsigned char* src = slot8 >= 0 ? (key ? p.c.bos_k : p.c.bos_v) + brow * LPH * 8 : base + row * LPH * 8;
-      if (slot8 >= 0) scale = (key ? p.c.bos_k_scale : p.c.bos_v_scale)[brow];
-      const uint2 u = *reinterpret_cast<const uint2*>(src + 8 * j);
+  const int lane = threadIdx.x & 31, j = threadIdx.x % LPH, group = threadIdx.x / LPH, kvh = p.c.n_kv_heads;
+  Place at;
+  if (!find_place<(BITS < 8)>(p.c, p.b, t, lane, p.status, at)) return;
+  const long row0 = cache_row(p.c, at.page, 0, at.slot);
+  uint2 u[ROWS];
+  uint4 whole[ROWS];
+  float scale[ROWS];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] = (float)((int)(((k < 4 ? u.x : u.y) >> (8 * (k & 3))) & 255u) - 128);
-    } else if constexpr (BITS == 4) {
-      const uint32_t u = *reinterpret_cast<const uint32_t*>(base + (row * LPH + j) * 4);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] = (float)((int)((u >> (4 * k)) & 15u) - 8);
+  for (int i = 0; i < ROWS; ++i) {
+    const int r = (part * ROWS + i) * GROUPS + group;
+    u[i] = make_uint2(0, 0);
+    whole[i] = make_uint4(0, 0, 0, 0);
+    scale[i] = 0.f;
+    if (r >= 2 * kvh) continue;
+    const bool key = r < kvh;
+    const int head = key ? r : r - kvh;
+    const long row = row0 + ((long)head << p.c.page_shift);
+    const unsigned char* base = key ? p.c.k : p.c.v;
+    if (BITS == 16) {
+      whole[i] = *reinterpret_cast<const uint4*>(base + (row * LPH + j) * 16);
+    } else if (BITS == 8 || at.slot8 >= 0) {
+      const long brow = (long)at.slot8 * kvh + head;
+      u[i] = *(reinterpret_cast<const uint2*>(BITS < 8 ? (key ? p.c.bos_k : p.c.bos_v) + brow * LPH * 8 : base + row * LPH * 8) + j);
+      scale[i] = BITS < 8 ? (key ? p.c.bos_k_scale : p.c.bos_v_scale)[brow] : (key ? p.c.k_scale : p.c.v_scale)[row];
     } else {
-      const unsigned char* src = base + (row * LPH + j) * 3;
-      const uint32_t u = src[0] | ((uint32_t)src[1] << 8) | ((uint32_t)src[2] << 16);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] = (float)((int)((u >> (3 * k)) & 7u) - 4);
+      scale[i] = (key ? p.c.k_scale : p.c.v_scale)[row];
+      if (BITS == 4) {
+        u[i].x = *reinterpret_cast<const uint32_t*>(base + (row * LPH + j) * 4);
+      } else {                                                 // 24 bits, anywhere in a word or across two of the row
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(base + row * (LPH * 3)) + (3 * j >> 2);
+        u[i] = make_uint2(w[0], w[(3 * j & 3) > 1 ? 1 : 0]);
+      }
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) f[k] *= scale;
-    o = narrow8(f);
   }
-  (key ? p.k_out : p.v_out)[((long)t * kvh + head) * LPH + j] = o;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    const int r = (part * ROWS + i) * GROUPS + group;
+    if (r >= 2 * kvh) continue;
+    uint4 o = whole[i];
+    if constexpr (BITS < 16) {
+      float x[8];
+      if (BITS == 8 || at.slot8 >= 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (float)((int)(((e < 4 ? u[i].x : u[i].y) >> (8 * (e & 3))) & 255u) - 128);
+      } else {
+        const uint32_t bits = BITS == 4 ? u[i].x : __funnelshift_r(u[i].x, u[i].y, (3 * j & 3) * 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (float)((int)((bits >> (BITS * e)) & ((1u << BITS) - 1)) - (1 << (BITS - 1)));
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= scale[i];
+      o = narrow8(x);
+    }
+    (r < kvh ? p.k_out : p.v_out)[((long)t * kvh + (r < kvh ? r : r - kvh)) * LPH + j] = o;
+  }
 }
 
 template <int BITS, int LPH, bool INTERLEAVED, int ROWS>
@@ -297,15 +342,21 @@ int launch_append_bits(AppendParams& p, bool interleaved, cudaStream_t s) {
   }
 }
 
-template <int BITS, int LPH>
-int launch_read_one(ReadParams& p, cudaStream_t s) {
-  const int per_block = kThreads / LPH;
+template <int BITS, int LPH, int ROWS>
+int launch_read_rows(ReadParams& p, cudaStream_t s) {
+  const int per_block = kThreads / LPH * ROWS;
   p.blocks_per_token = (2 * p.c.n_kv_heads + per_block - 1) / per_block;
   const long blocks = (long)p.b.tokens * p.blocks_per_token;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
-  HBL_CUDA_OK(launch_dependent(kv_read_kernel<BITS, LPH>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+  HBL_CUDA_OK(launch_dependent(kv_read_kernel<BITS, LPH, ROWS>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
   note_launch();
   return HBL_OK;
+}
+template <int BITS, int LPH>
+int launch_read_one(ReadParams& p, cudaStream_t s) {
+  const long threads = (long)p.b.tokens * 2 * p.c.n_kv_heads * LPH;
+  if (threads >= (long)sm_count() * 2048 * 4) return launch_read_rows<BITS, LPH, 4>(p, s);
+  return launch_read_rows<BITS, LPH, 1>(p, s);
 }
 template <int BITS>
 int launch_read_bits(ReadParams& p, cudaStream_t s) {
