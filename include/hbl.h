@@ -387,9 +387,15 @@ typedef enum {
  *   head_dim     a multiple of 8, 8..256; rot_dim a multiple of 16, 16..head_dim
  *   backward     1: the transposed rotation, i.e. the gradient with respect to x of a gradient with respect to out
  *                (with an amplitude of 1 also the inverse) */
-int hbl_rope(const void* x, int dtype, int tokens, int n_heads, int head_dim, long long x_token_stride,
-             long long x_head_stride, const int32_t* positions, const float* table, int n_pos, int rot_dim, int layout,
-             int backward, void* out, long long out_token_stride, long long out_head_stride, void* stream);
+typedef struct {
+  const void* x;
+  void* out;
+  const int32_t* positions;
+  const float* table;
+  long long x_token_stride, x_head_stride, out_token_stride, out_head_stride;
+  int dtype, tokens, n_heads, head_dim, n_pos, rot_dim, layout, backward;
+} hbl_rope_t;
+int hbl_rope(const hbl_rope_t* args /* host */, void* stream);
 
 /* A paged cache of attention states (all pointers device, the caller's).  A page holds page_size tokens of every
  * key/value head; row (page, head, slot) has the number  (page * n_kv_heads + head) * page_size + slot.

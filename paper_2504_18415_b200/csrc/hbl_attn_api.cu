@@ -139,21 +139,21 @@ int hbl_rope_table(const double* freq, int n_freq, double amplitude, int first_p
   return launch_rope_table(freq, n_freq, amplitude, first_pos, n_pos, table, static_cast<cudaStream_t>(stream));
 }
 
-int hbl_rope(const void* x, int dtype, int tokens, int n_heads, int head_dim, long long x_token_stride, long long x_head_stride,
-             const int32_t* positions, const float* table, int n_pos, int rot_dim, int layout, int backward, void* out,
-             long long out_token_stride, long long out_head_stride, void* stream) {
-  if (dtype != HBL_F32 && dtype != HBL_BF16) return HBL_ERR_FORMAT;
-  if (tokens < 0 || n_heads <= 0 || head_dim < 8 || head_dim > kMaxRotDim || head_dim % 8 != 0) return HBL_ERR_SHAPE;
-  int rc = check_rotation(table, n_pos, rot_dim, head_dim, layout);
+int hbl_rope(const hbl_rope_t* a, void* stream) {
+  if (!a) return HBL_ERR_NULL;
+  if (a->dtype != HBL_F32 && a->dtype != HBL_BF16) return HBL_ERR_FORMAT;
+  if (a->tokens < 0 || a->n_heads <= 0 || a->head_dim < 8 || a->head_dim > kMaxRotDim || a->head_dim % 8 != 0) return HBL_ERR_SHAPE;
+  int rc = check_rotation(a->table, a->n_pos, a->rot_dim, a->head_dim, a->layout);
   if (rc != HBL_OK) return rc;
-  if (tokens == 0) return HBL_OK;
-  if (!x || !positions || !table || !out) return HBL_ERR_NULL;
-  if ((rc = check_strided(x, x_token_stride, x_head_stride)) != HBL_OK) return rc;
-  if ((rc = check_strided(out, out_token_stride, out_head_stride)) != HBL_OK) return rc;
-  if (x == out && (x_token_stride != out_token_stride || x_head_stride != out_head_stride)) return HBL_ERR_SHAPE;
-  if (!aligned(positions, 4)) return HBL_ERR_ALIGN;
-  return launch_rope(x, dtype, tokens, n_heads, head_dim, x_token_stride, x_head_stride, positions, table, n_pos, rot_dim, layout,
-                     backward != 0, out, out_token_stride, out_head_stride, static_cast<cudaStream_t>(stream));
+  if (a->tokens == 0) return HBL_OK;
+  if (!a->x || !a->positions || !a->table || !a->out) return HBL_ERR_NULL;
+  if ((rc = check_strided(a->x, a->x_token_stride, a->x_head_stride)) != HBL_OK) return rc;
+  if ((rc = check_strided(a->out, a->out_token_stride, a->out_head_stride)) != HBL_OK) return rc;
+  if (a->x == a->out && (a->x_token_stride != a->out_token_stride || a->x_head_stride != a->out_head_stride)) return HBL_ERR_SHAPE;
+  if (!aligned(a->positions, 4)) return HBL_ERR_ALIGN;
+  return launch_rope(a->x, a->dtype, a->tokens, a->n_heads, a->head_dim, a->x_token_stride, a->x_head_stride, a->positions, a->table,
+                     a->n_pos, a->rot_dim, a->layout, a->backward != 0, a->out, a->out_token_stride, a->out_head_stride,
+                     static_cast<cudaStream_t>(stream));
 }
 
 int hbl_kv_append(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_kv_append_t* a, void* stream) {

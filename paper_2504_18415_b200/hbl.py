@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -62,17 +63,11 @@ class hbl_kv_batch_t(C.Structure):
                [(n, C.c_int) for n in ("n_seqs", "tokens", "max_pages", "max_q_len", "max_kv_len")]
 
 
-class hbl_kv_append_t(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "q", "q_out")] + \
-               [(n + s, C.c_longlong) for n in ("k", "v", "q", "q_out") for s in ("_token_stride", "_head_stride")] + \
-               [("table", C.c_void_p), ("positions", C.c_void_p)] + \
-               [(n, C.c_int) for n in ("n_heads", "n_pos", "rot_dim", "layout")] + [("eps", C.c_float)]
-
-
-class hbl_attention_t(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("q", "out", "lse")] + \
-               [(n + s, C.c_longlong) for n in ("q", "out") for s in ("_token_stride", "_head_stride")] + \
-               [("n_heads", C.c_int), ("causal", C.c_int), ("sm_scale", C.c_float)]
+# The calls of a decoding step are made for every layer and token, so their argument structures are packed in one go
+# (native alignment, field by field as in include/hbl.h) instead of being filled member by member.
+_ROPE_T = struct.Struct("4P4q8i")          # x out positions table | strides of x, out | dtype tokens n_heads head_dim n_pos rot_dim layout backward
+_APPEND_T = struct.Struct("4P8q2P4if0P")     # k v q q_out | strides of k, v, q, q_out | table positions | n_heads n_pos rot_dim layout eps
+_ATTENTION_T = struct.Struct("3P4q2if0P")    # q out lse | strides of q, out | n_heads causal sm_scale
 
 
 def lib() -> C.CDLL:
@@ -117,15 +112,15 @@ def lib() -> C.CDLL:
         L.hbl_quantize_act_int4_packed.argtypes = [vp, i, i, i, i, f, vp, vp, vp]
         L.hbl_gemm_i32_int4_packed.restype = C.c_int
         L.hbl_gemm_i32_int4_packed.argtypes = [vp, i, i, vp, i, vp, vp, sz, vp]
-        d, ll, cache, batch = C.c_double, C.c_longlong, C.POINTER(hbl_kv_cache_t), C.POINTER(hbl_kv_batch_t)
+        d, args = C.c_double, C.c_char_p                   # args: a packed structure
         L.hbl_rope_frequencies.argtypes = [d, i, i, d, d, d, d, C.POINTER(d)]
         L.hbl_rope_table.argtypes = [C.POINTER(d), i, d, i, i, vp, vp]
-        L.hbl_rope.argtypes = [vp, i, i, i, i, ll, ll, vp, vp, i, i, i, i, vp, ll, ll, vp]
-        L.hbl_kv_append.argtypes = [cache, batch, C.POINTER(hbl_kv_append_t), vp]
-        L.hbl_kv_read.argtypes = [cache, batch, vp, vp, vp]
-        L.hbl_attention_workspace_bytes.argtypes = [cache, batch, i]
+        L.hbl_rope.argtypes = [args, vp]
+        L.hbl_kv_append.argtypes = [vp, vp, args, vp]
+        L.hbl_kv_read.argtypes = [vp, vp, vp, vp, vp]
+        L.hbl_attention_workspace_bytes.argtypes = [vp, vp, i]
         L.hbl_attention_workspace_bytes.restype = sz
-        L.hbl_attention.argtypes = [cache, batch, C.POINTER(hbl_attention_t), vp, sz, vp]
+        L.hbl_attention.argtypes = [vp, vp, args, vp, sz, vp]
         for n in ("hbl_rope_frequencies", "hbl_rope_table", "hbl_rope", "hbl_kv_append", "hbl_kv_read", "hbl_attention"):
             getattr(L, n).restype = C.c_int
         L.hbl_selftest_wait_timeout.restype = C.c_int
@@ -420,30 +415,36 @@ ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
 
 
 def _raw_stream(device: torch.device) -> int:
-    """The current stream's handle; the calls below are made many times per token, so it is read the short way."""
+    """The current stream's handle, read the short way; the library launches on the current device."""
     index = device.index
     if index != torch._C._cuda_getDevice():
-        raise ValueError(f"the tensors are on cuda:{index}, which is not the current device")
+        raise ValueError(f"the tensors are on {device}, which is not the current device")
     return torch._C._cuda_getCurrentRawStream(index)
 
 
-def _flat(t: torch.Tensor | None, dtype, shape, what: str, device) -> int | None:
-    """Address of a contiguous CUDA tensor of this type and shape (None: NULL)."""
+def _flat(t: torch.Tensor | None, dtype, shape, what: str, device) -> int:
+    """Address of a contiguous tensor of this type and shape on the device (None: 0)."""
     if t is None:
-        return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_cuda or not t.is_contiguous() or t.device != device:
+        return 0
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
     return t.data_ptr()
 
 
-def _heads(t: torch.Tensor, shape, dtype, what: str, device) -> tuple[int, int, int]:
-    """(address, token stride, head stride) of a [tokens, heads, head_dim] tensor whose heads are contiguous."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_cuda:
+def _strided(t: torch.Tensor, dtype, shape, what: str, device) -> tuple[int, int]:
+    """(token stride, head stride) of a [tokens, heads, head_dim] tensor whose heads are contiguous."""
+    if t.dtype is not dtype or t.shape != shape or t.device != device:
         raise ValueError(f"{what}: expected a {dtype} tensor of shape {tuple(shape)} on {device}")
     ts, hs, es = t.stride()
     if es != 1:
         raise ValueError(f"{what}: the elements of a head have to be contiguous")
-    return t.data_ptr(), ts, hs
+    return ts, hs
+
+
+def _on_gpu(t: torch.Tensor, what: str) -> torch.device:
+    if not t.is_cuda:
+        raise ValueError(f"{what}: expected a CUDA tensor")
+    return t.device
 
 
 class KvCache:
@@ -462,7 +463,7 @@ class KvCache:
         self.head_dim = row if bits == 16 else row * 8 // bits
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.bos_k, self.bos_v, self.bos_k_scale, self.bos_v_scale = bos_k, bos_v, bos_k_scale, bos_v_scale
-        dt, dev, f32 = torch.bfloat16 if bits == 16 else torch.uint8, k.device, torch.float32
+        dt, dev, f32 = torch.bfloat16 if bits == 16 else torch.uint8, _on_gpu(k, "k"), torch.float32
         c = self.c = hbl_kv_cache_t()
         c.k, c.v = _flat(k, dt, k.shape, "k", dev), _flat(v, dt, k.shape, "v", dev)
         c.k_scale, c.v_scale = _flat(k_scale, f32, k.shape[:3], "k_scale", dev), _flat(v_scale, f32, k.shape[:3], "v_scale", dev)
@@ -474,7 +475,7 @@ class KvCache:
         c.bos_k_scale = _flat(bos_k_scale, f32, (slots, heads), "bos_k_scale", dev)
         c.bos_v_scale = _flat(bos_v_scale, f32, (slots, heads), "bos_v_scale", dev)
         c.n_pages, c.page_size, c.n_kv_heads, c.head_dim, c.bits, c.n_slots = n_pages, page, heads, self.head_dim, bits, slots
-        self.ref = C.byref(c)
+        self.ref = C.addressof(c)
 
     @classmethod
     def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, bits: int, bos_slots: int = 0, device="cuda"):
@@ -498,7 +499,7 @@ class KvBatch:
     calls' tensors; max_q_len, max_kv_len: upper bounds that launch shapes go by (a shorter bound on q leaves rows out)."""
 
     def __init__(self, q_start, kv_len, pages, *, tokens: int, max_q_len: int, max_kv_len: int, bos_slot=None):
-        n, i32, dev = kv_len.shape[0], torch.int32, kv_len.device
+        n, i32, dev = kv_len.shape[0], torch.int32, _on_gpu(kv_len, "kv_len")
         self.q_start, self.kv_len, self.pages, self.bos_slot, self.device = q_start, kv_len, pages, bos_slot, dev
         self.n_seqs, self.tokens = n, tokens
         c = self.c = hbl_kv_batch_t()
@@ -507,7 +508,7 @@ class KvBatch:
         c.pages = _flat(pages, i32, (n, pages.shape[1]), "pages", dev)
         c.bos_slot = _flat(bos_slot, i32, (n,), "bos_slot", dev)
         c.n_seqs, c.tokens, c.max_pages, c.max_q_len, c.max_kv_len = n, tokens, pages.shape[1], max_q_len, max_kv_len
-        self.ref = C.byref(c)
+        self.ref = C.addressof(c)
 
 
 def hbl_rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = ROPE_PLAIN, factor: float = 1.0,
@@ -528,23 +529,26 @@ def hbl_rope_table(freq, n_pos: int, first_pos: int = 0, amplitude: float = 1.0,
 
 
 def _rotation(table: torch.Tensor, device) -> tuple[int, int, int]:
-    if table.dim() != 3 or table.shape[2] != 2:
+    """(address, positions, rotated elements) of a table."""
+    shape = table.shape
+    if len(shape) != 3 or shape[2] != 2:
         raise ValueError("table: expected the result of hbl_rope_table")
-    return _flat(table, torch.float32, table.shape, "table", device), table.shape[0], 2 * table.shape[1]
+    return _flat(table, torch.float32, shape, "table", device), shape[0], 2 * shape[1]
 
 
 def hbl_rope(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, interleaved: bool = False, backward: bool = False,
              out: torch.Tensor | None = None) -> torch.Tensor:
     """Rotary positions on x [tokens, heads, head_dim] (bf16 or fp32; out may be x).  backward: the gradient's rotation."""
-    T, H, D = x.shape
-    dev = x.device
+    dev, shape, dtype = _on_gpu(x, "x"), x.shape, x.dtype
+    T, H, D = shape
     if out is None:
-        out = torch.empty((T, H, D), dtype=x.dtype, device=dev)
-    p, ts, hs = _heads(x, (T, H, D), x.dtype, "x", dev)
-    po, ots, ohs = _heads(out, (T, H, D), x.dtype, "out", dev)
-    pt, n_pos, rot = _rotation(table, dev)
-    _check(lib().hbl_rope(p, _dt(x), T, H, D, ts, hs, _flat(positions, torch.int32, (T,), "positions", dev), pt, n_pos, rot,
-                          int(interleaved), int(backward), po, ots, ohs, _raw_stream(dev)), "hbl_rope")
+        out = torch.empty(shape, dtype=dtype, device=dev)
+    ts, hs = _strided(x, dtype, shape, "x", dev)
+    ots, ohs = _strided(out, dtype, shape, "out", dev)
+    at, n_pos, rot = _rotation(table, dev)
+    args = _ROPE_T.pack(x.data_ptr(), out.data_ptr(), _flat(positions, torch.int32, (T,), "positions", dev), at, ts, hs, ots, ohs,
+                        _dt(x), T, H, D, n_pos, rot, interleaved, backward)
+    _check(lib().hbl_rope(args, _raw_stream(dev)), "hbl_rope")
     return out
 
 
@@ -553,36 +557,36 @@ def hbl_kv_append(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tens
                   q_out: torch.Tensor | None = None, eps: float = 1e-5) -> torch.Tensor | None:
     """The batch's tokens into the cache: k rotated by `table` (None: as it is), k and v quantized.  q, where given, is
     rotated by the same launch and returned (q_out may be q)."""
-    dev, T = cache.device, batch.tokens
-    shape = (T, cache.n_kv_heads, cache.head_dim)
-    a = hbl_kv_append_t()
-    a.k, a.k_token_stride, a.k_head_stride = _heads(k, shape, torch.bfloat16, "k", dev)
-    a.v, a.v_token_stride, a.v_head_stride = _heads(v, shape, torch.bfloat16, "v", dev)
-    if q is not None:
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
-        shape = (T, q.shape[1], cache.head_dim)
-        a.q, a.q_token_stride, a.q_head_stride = _heads(q, shape, torch.bfloat16, "q", dev)
-        a.q_out, a.q_out_token_stride, a.q_out_head_stride = _heads(q_out, shape, torch.bfloat16, "q_out", dev)
-        a.n_heads = q.shape[1]
-    if table is not None:
-        a.table, a.n_pos, a.rot_dim = _rotation(table, dev)
-    a.positions = _flat(positions, torch.int32, (T,), "positions", dev)
-    a.layout, a.eps = int(interleaved), eps
+    dev, bf16 = cache.device, torch.bfloat16
     if batch.device != dev:
         raise ValueError("cache and batch are on different devices")
-    _check(lib().hbl_kv_append(cache.ref, batch.ref, C.byref(a), _raw_stream(dev)), "hbl_kv_append")
+    shape = (batch.tokens, cache.n_kv_heads, cache.head_dim)
+    kts, khs = _strided(k, bf16, shape, "k", dev)
+    vts, vhs = _strided(v, bf16, shape, "v", dev)
+    qp = op = qts = qhs = ots = ohs = heads = at = n_pos = rot = 0
+    if q is not None:
+        heads = q.shape[1]
+        shape = (batch.tokens, heads, cache.head_dim)
+        if q_out is None:
+            q_out = torch.empty(shape, dtype=bf16, device=dev)
+        qts, qhs = _strided(q, bf16, shape, "q", dev)
+        ots, ohs = _strided(q_out, bf16, shape, "q_out", dev)
+        qp, op = q.data_ptr(), q_out.data_ptr()
+    if table is not None:
+        at, n_pos, rot = _rotation(table, dev)
+    args = _APPEND_T.pack(k.data_ptr(), v.data_ptr(), qp, op, kts, khs, vts, vhs, qts, qhs, ots, ohs, at,
+                          _flat(positions, torch.int32, (batch.tokens,), "positions", dev), heads, n_pos, rot, interleaved, eps)
+    _check(lib().hbl_kv_append(cache.ref, batch.ref, args, _raw_stream(dev)), "hbl_kv_append")
     return q_out
 
 
 def hbl_kv_read(cache: KvCache, batch: KvBatch) -> tuple[torch.Tensor, torch.Tensor]:
     """The batch's tokens out of the cache: (k, v) bf16 [tokens, n_kv_heads, head_dim]."""
-    shape = (batch.tokens, cache.n_kv_heads, cache.head_dim)
-    k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
-    v = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
-    if batch.device != cache.device:
+    dev = cache.device
+    if batch.device != dev:
         raise ValueError("cache and batch are on different devices")
-    _check(lib().hbl_kv_read(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), _raw_stream(cache.device)), "hbl_kv_read")
+    k, v = torch.empty((2, batch.tokens, cache.n_kv_heads, cache.head_dim), dtype=torch.bfloat16, device=dev).unbind(0)
+    _check(lib().hbl_kv_read(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), _raw_stream(dev)), "hbl_kv_read")
     return k, v
 
 
@@ -595,26 +599,24 @@ def hbl_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, sm_scale: flo
                   workspace: torch.Tensor | None = None) -> torch.Tensor:
     """softmax(sm_scale q K^T) V over the cache, q bf16 [tokens, n_heads, head_dim] -> out of the same shape.  sm_scale:
     1 / sqrt(head_dim) by default; causal: a token sees the tokens up to itself; lse: fp32 [tokens, n_heads], written."""
-    dev, D = cache.device, cache.head_dim
+    dev, D, bf16 = cache.device, cache.head_dim, torch.bfloat16
+    if batch.device != dev:
+        raise ValueError("cache and batch are on different devices")
     if q.dim() != 3:
         raise ValueError("q: expected [tokens, n_heads, head_dim]")
     H = q.shape[1]
     shape = (batch.tokens, H, D)
     if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
-    a = hbl_attention_t()
-    a.q, a.q_token_stride, a.q_head_stride = _heads(q, shape, torch.bfloat16, "q", dev)
-    a.out, a.out_token_stride, a.out_head_stride = _heads(out, shape, torch.bfloat16, "out", dev)
-    a.lse = _flat(lse, torch.float32, shape[:2], "lse", dev)
-    a.n_heads, a.causal = H, int(causal)
-    a.sm_scale = D ** -0.5 if sm_scale is None else sm_scale
-    if batch.device != dev:
-        raise ValueError("cache and batch are on different devices")
+        out = torch.empty(shape, dtype=bf16, device=dev)
+    qts, qhs = _strided(q, bf16, shape, "q", dev)
+    ots, ohs = _strided(out, bf16, shape, "out", dev)
+    args = _ATTENTION_T.pack(q.data_ptr(), out.data_ptr(), _flat(lse, torch.float32, (batch.tokens, H), "lse", dev), qts, qhs, ots, ohs,
+                             H, causal, D ** -0.5 if sm_scale is None else sm_scale)
     if workspace is None:
         n = hbl_attention_workspace_bytes(cache, batch, H)
         workspace = new_workspace(n, dev) if n > 0 else None
-    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
-    _check(lib().hbl_attention(cache.ref, batch.ref, C.byref(a), ws, size, _raw_stream(dev)), "hbl_attention")
+    ws, size = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    _check(lib().hbl_attention(cache.ref, batch.ref, args, ws, size, _raw_stream(dev)), "hbl_attention")
     return out
 
 

@@ -17,6 +17,28 @@ def L():
 P, N = C.c_void_p(1024), C.c_void_p(0)          # P is never dereferenced on the host: validation must stop first
 
 
+def fields(*groups):
+    return [(n, t) for t, names in groups for n in names.split()]
+
+
+def strides(names):
+    return " ".join(f"{n}_{s}_stride" for n in names.split() for s in ("token", "head"))
+
+
+class Rope(C.Structure):                        # the argument structures as include/hbl.h declares them
+    _fields_ = fields((C.c_void_p, "x out positions table"), (C.c_longlong, strides("x out")),
+                      (C.c_int, "dtype tokens n_heads head_dim n_pos rot_dim layout backward"))
+
+
+class Append(C.Structure):
+    _fields_ = fields((C.c_void_p, "k v q q_out"), (C.c_longlong, strides("k v q q_out")), (C.c_void_p, "table positions"),
+                      (C.c_int, "n_heads n_pos rot_dim layout"), (C.c_float, "eps"))
+
+
+class Attention(C.Structure):
+    _fields_ = fields((C.c_void_p, "q out lse"), (C.c_longlong, strides("q out")), (C.c_int, "n_heads causal"), (C.c_float, "sm_scale"))
+
+
 def test_frequencies_follow_their_formulas(L):
     for rot in (2, 64, 128, 256):
         f = hbl.hbl_rope_frequencies(rot, 10000.0)
@@ -56,9 +78,13 @@ def test_table_and_rope_refusals(L):
     assert t(first=0x7fffffff, pos=1) == 11
     assert t(amp=math.inf) == 2
     assert t(freq=None) == 1 and t(table=N) == 1 and t(table=C.c_void_p(1032)) == 5
-    r = lambda **k: L.hbl_rope(k.get("x", P), k.get("dt", 1), k.get("T", 4), k.get("H", 8), k.get("D", 128), k.get("ts", 1024),
-                               k.get("hs", 128), k.get("pos", P), k.get("table", P), k.get("n_pos", 16), k.get("rot", 128),
-                               k.get("layout", 0), 0, k.get("out", C.c_void_p(1 << 20)), k.get("ots", 1024), k.get("ohs", 128), N)
+    def r(**k):
+        a = Rope(1024, 1 << 20, 1024, 1024, 1024, 128, 1024, 128, 1, 4, 8, 128, 16, 128, 0, 0)
+        for n, v in k.items():
+            setattr(a, dict(dt="dtype", T="tokens", H="n_heads", D="head_dim", ts="x_token_stride", hs="x_head_stride", ots="out_token_stride",
+                            ohs="out_head_stride", pos="positions", rot="rot_dim").get(n, n), v.value or 0 if isinstance(v, C.c_void_p) else v)
+        return L.hbl_rope(bytes(a), N)
+    assert L.hbl_rope(None, N) == 1
     assert r(T=0) == 0
     assert r(dt=2) == 10 and r(layout=2) == 10
     assert r(T=-1) == 2 and r(H=0) == 2 and r(D=12) == 2 and r(D=264) == 2
@@ -87,8 +113,16 @@ def batch_t(**k):
     return b
 
 
+@pytest.mark.parametrize("kind,packed", [(Rope, hbl._ROPE_T), (Append, hbl._APPEND_T), (Attention, hbl._ATTENTION_T)])
+def test_packed_arguments_are_the_structures_of_the_header(kind, packed):
+    assert packed.size == C.sizeof(kind)
+    values = [0.5 + i if t is C.c_float else 1 + i for i, (_, t) in enumerate(kind._fields_)]
+    got = kind.from_buffer_copy(packed.pack(*values))
+    assert [getattr(got, n) for n, _ in kind._fields_] == values
+
+
 def append_t(**k):
-    a = hbl.hbl_kv_append_t()
+    a = Append()
     a.k = a.v = 1 << 20
     for n in ("k", "v", "q", "q_out"):
         setattr(a, n + "_token_stride", 512)
@@ -96,11 +130,11 @@ def append_t(**k):
     a.n_heads, a.n_pos, a.rot_dim, a.layout, a.eps = 4, 128, 128, 0, 1e-5
     for n, v in k.items():
         setattr(a, n, v)
-    return a
+    return bytes(a)
 
 
 def attention_t(**k):
-    a = hbl.hbl_attention_t()
+    a = Attention()
     a.q = a.out = 1 << 20
     for n in ("q", "out"):
         setattr(a, n + "_token_stride", 512)
@@ -108,7 +142,7 @@ def attention_t(**k):
     a.n_heads, a.causal, a.sm_scale = 4, 1, 0.1
     for n, v in k.items():
         setattr(a, n, v)
-    return a
+    return bytes(a)
 
 
 BAD_CACHES = [(dict(bits=5), 4), (dict(head_dim=96), 2), (dict(n_kv_heads=0), 2), (dict(n_pages=0), 2), (dict(page_size=8), 2),
@@ -122,8 +156,8 @@ BAD_BATCHES = [(dict(n_seqs=-1), 2), (dict(tokens=-1), 2), (dict(max_pages=-1), 
 
 def test_cache_and_batch_refusals(L):
     app, att, ref = append_t(), attention_t(), C.byref
-    calls = [lambda c, b: L.hbl_kv_append(c, b, ref(app), N), lambda c, b: L.hbl_kv_read(c, b, P, P, N),
-             lambda c, b: L.hbl_attention(c, b, ref(att), P, 1 << 40, N)]
+    calls = [lambda c, b: L.hbl_kv_append(c, b, app, N), lambda c, b: L.hbl_kv_read(c, b, P, P, N),
+             lambda c, b: L.hbl_attention(c, b, att, P, 1 << 40, N)]
     for call in calls:
         assert call(None, ref(batch_t())) == 1 and call(ref(cache_t()), None) == 1
         for k, want in BAD_CACHES:
@@ -139,7 +173,7 @@ def test_cache_and_batch_refusals(L):
 
 def test_append_read_and_attention_refusals(L):
     ref = C.byref
-    ap = lambda **k: L.hbl_kv_append(ref(cache_t()), ref(batch_t()), ref(append_t(**k)), N)
+    ap = lambda **k: L.hbl_kv_append(ref(cache_t()), ref(batch_t()), append_t(**k), N)
     assert L.hbl_kv_append(ref(cache_t()), ref(batch_t()), None, N) == 1
     assert ap(eps=0.0) == 7 and ap(eps=math.nan) == 7
     assert ap(k=0) == 1 and ap(v=0) == 1
@@ -154,7 +188,7 @@ def test_append_read_and_attention_refusals(L):
     assert ap(**rot, q=1 << 20, q_out=(1 << 20) + 4) == 5
     assert ap(positions=(1 << 20) + 1) == 5
     assert L.hbl_kv_read(ref(cache_t()), ref(batch_t()), N, P, N) == 1 and L.hbl_kv_read(ref(cache_t()), ref(batch_t()), P, C.c_void_p(1032), N) == 5
-    at = lambda ws=P, n=1 << 40, **k: L.hbl_attention(ref(cache_t()), ref(batch_t()), ref(attention_t(**k)), ws, n, N)
+    at = lambda ws=P, n=1 << 40, **k: L.hbl_attention(ref(cache_t()), ref(batch_t()), attention_t(**k), ws, n, N)
     assert L.hbl_attention(ref(cache_t()), ref(batch_t()), None, P, 1 << 40, N) == 1
     assert at(n_heads=6) == 2 and at(n_heads=0) == 2 and at(sm_scale=math.inf) == 2 and at(sm_scale=math.nan) == 2
     assert at(q=0) == 1 and at(out=0) == 1 and at(q=(1 << 20) + 8) == 5 and at(out_token_stride=4) == 5 and at(lse=(1 << 20) + 2) == 5
@@ -163,9 +197,9 @@ def test_append_read_and_attention_refusals(L):
     long = batch_t(max_kv_len=65536, max_pages=4096)
     need = L.hbl_attention_workspace_bytes(ref(cache_t()), ref(long), 4)
     assert need > 0
-    assert L.hbl_attention(ref(cache_t()), ref(long), ref(attention_t()), N, 0, N) == 1
-    assert L.hbl_attention(ref(cache_t()), ref(long), ref(attention_t()), P, need - 1, N) == 6
-    assert L.hbl_attention(ref(cache_t()), ref(batch_t(max_q_len=0)), ref(attention_t()), P, 1 << 40, N) == 0
+    assert L.hbl_attention(ref(cache_t()), ref(long), attention_t(), N, 0, N) == 1
+    assert L.hbl_attention(ref(cache_t()), ref(long), attention_t(), P, need - 1, N) == 6
+    assert L.hbl_attention(ref(cache_t()), ref(batch_t(max_q_len=0)), attention_t(), P, 1 << 40, N) == 0
 
 
 def test_binding_refuses_what_is_not_on_the_gpu():
