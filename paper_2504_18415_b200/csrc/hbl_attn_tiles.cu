@@ -3,7 +3,8 @@
 //   S = Q ck^T (tcgen05.mma, fp32 in tensor memory);  s = sm_scale ks_j S;  p = 2^(s - m);  O += (p vs_j) cv
 //
 // A work item is 128 * NSUB query rows of one key head (row r: token r / group, head r % group, so that the heads that
-// share a key head share its tiles) against one piece of the keys.  One thread block per SM stays for all its items:
+// share a key head share its tiles) against one piece of the keys.  One thread block per SM, which goes on to the items of
+// blocks that have not started:
 //   warps 0-3, 4-7   softmax of sub-tile 0, 1: scores out of tensor memory, maximum, exponentials,
 //                    P back into tensor memory as bf16 in the place of the scores; at the end O out of tensor memory
 //   warps 8-11       producers: the tiles of keys and values into shared memory, 128-byte swizzle.  Codes become bf16
@@ -158,11 +159,22 @@ __device__ __forceinline__ int token_of(const TilesParams& p, int r) {
   return (int)((__umulhi((uint32_t)r, p.div_mul) + (uint32_t)r) >> p.div_shift);
 }
 
-// The n-th item of this thread block.  Items come in falling order of work (causal); every second round of the grid
-// is dealt backwards, so that nobody gets the larger one every time (measured on an 8192-token prompt, 1024 items: the
-// longest-working SM 18 % above the mean when dealt in one direction, head by head).
-__device__ __forceinline__ int item_at(int n) {
-  return n * (int)gridDim.x + (n & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+// The grid has one thread block to an item, but a block that runs takes over blocks that have not started yet
+// (clusterlaunchcontrol.try_cancel), item by item, so the items are dealt by who is free, in the grid's order, without a
+// counter in memory and without giving up shared or tensor memory in between.  One request per call; after one that
+// found nothing there may be no other.
+__device__ __forceinline__ void request_block(uint32_t answer, uint64_t* bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+               ::"r"(answer), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ bool taken_block(uint32_t answer, int& block) {
+  uint32_t ok, x;
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b128 r;\n ld.shared.b128 r, [%2];\n clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n"
+      " mov.u32 %1, 0;\n @p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok), "=r"(x) : "r"(answer) : "memory");
+  block = (int)x;
+  return ok != 0;
 }
 // One work item, as every role sees it.
 struct Item {
@@ -176,7 +188,6 @@ struct Item {
 template <int D>
 __device__ __forceinline__ bool decode_item(const TilesParams& p, int item, int lane, Item& o) {
   using G = TileGeo<D>;
-  if (item >= p.items) return false;
   o.split = item % p.p.splits;
   const int rest = item / p.p.splits;
   o.head = rest % p.c.n_kv_heads;
@@ -242,6 +253,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
   __shared__ __align__(8) uint64_t q_full, q_empty, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES], s_full[NSUB], p_full[NSUB][BK / 64],
       o_full[NSUB], item_full[2], item_empty[2];
   __shared__ Item item_slot[2];
+  __shared__ __align__(8) uint64_t steal_bar;
+  __shared__ __align__(16) uint4 steal_answer;
   __shared__ __align__(16) uint32_t bad_scale[STAGES][4];       // keys of the tile whose value scale is not finite
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag_s;
@@ -253,6 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
 
   if (threadIdx.x == 0) {
     mbar_init(&q_full, 64);
+    mbar_init(&steal_bar, 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(&item_full[s], 1);
       mbar_init(&item_empty[s], 4 * NSUB + 4 + 1 + 2);          // warps that work on items
@@ -854,8 +868,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         ++made;
       };
       Item w;
-      for (int n = 0; n * (int)gridDim.x < p.items && ok; ++n)
-        if (decode_item<D>(p, item_at(n), lane, w)) give(w);
+      int item = blockIdx.x;
+      for (uint32_t n = 0; ok; ++n) {
+        if (lane == 0) {                                        // the next one, while this one is looked up and handed out
+          mbar_expect_tx(&steal_bar, 16);
+          request_block(smem_u32(&steal_answer), &steal_bar);
+        }
+        if (decode_item<D>(p, item, lane, w)) give(w);
+        if (!ok) break;
+        if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(&steal_bar, n & 1, abort_flag, p.status)))) break;
+        const bool more = taken_block(smem_u32(&steal_answer), item);
+        fence_async();                                          // the answer has been read before the next one is written
+        __syncwarp();
+        if (!more) break;
+      }
       w.tiles = -1;
       if (ok) give(w);
     } else if (warp > 12) {
@@ -923,8 +949,7 @@ template <int BITS, int D>
 int launch_tiles_dim(TilesParams& p, cudaStream_t s) {
   auto kern = attn_tiles_kernel<BITS, D>;
   HBL_ALLOW_DYNAMIC_SMEM(kern, TileGeo<D>::SMEM);
-  const int grid = p.items < sm_count() ? p.items : sm_count();
-  HBL_CUDA_OK(launch_dependent(kern, dim3(grid), dim3(kThreads), TileGeo<D>::SMEM, s, p));
+  HBL_CUDA_OK(launch_dependent(kern, dim3(p.items), dim3(kThreads), TileGeo<D>::SMEM, s, p));
   note_launch();
   return HBL_OK;
 }
