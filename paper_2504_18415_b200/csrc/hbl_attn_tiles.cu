@@ -898,16 +898,23 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(&q_empty, (items & 1) ^ 1, abort_flag, p.status)))) break;
         ++items;
         const int c = tid % CH, first = tid / CH, step_tok = token_of(p, RPP), step_rem = RPP - step_tok * p.a.group;
-        int tok = token_of(p, w.r0 + first), rem = w.r0 + first - tok * p.a.group;
+        const int tok0 = token_of(p, w.r0 + first);
+        int rem = w.r0 + first - tok0 * p.a.group;
         const __nv_bfloat16* q = p.a.q + w.q0 * p.a.q_ts + (long)w.head * p.a.group * p.a.q_hs + 8 * c;
-        for (int rr = first; rr < N; rr += RPP) {
-          const bool live = w.r0 + rr < w.n_rows;
-          copy16(sq + (rr >> 7) * G::Q_BYTES + chunk_at(rr & 127, c, 128 * 128), live ? q + tok * p.a.q_ts + rem * p.a.q_hs : q, live);
-          tok += step_tok;
+        const __nv_bfloat16* from = q + tok0 * p.a.q_ts + rem * p.a.q_hs;
+        // from one row to the next that is this thread's: over whole tokens, and back by a token's heads where they end
+        const long ahead = step_tok * p.a.q_ts + step_rem * p.a.q_hs, back = p.a.q_ts - p.a.group * p.a.q_hs;
+        const int there = w.n_rows - w.r0;
+#pragma unroll 8
+        for (int i = 0; i < N / RPP; ++i) {
+          const int rr = first + RPP * i;
+          const bool live = rr < there;
+          copy16(sq + (rr >> 7) * G::Q_BYTES + chunk_at(rr & 127, c, 128 * 128), live ? from : q, live);
+          from += ahead;
           rem += step_rem;
           if (rem >= p.a.group) {
             rem -= p.a.group;
-            ++tok;
+            from += back;
           }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
