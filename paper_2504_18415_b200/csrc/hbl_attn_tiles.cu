@@ -89,6 +89,11 @@ __device__ __forceinline__ void tmem_st_row(uint32_t taddr, const uint32_t* r) {
                ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
                : "memory");
 }
+__device__ __forceinline__ void tmem_st_row16(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+               : "memory");
+}
 // Tensor memory in the layout of an mma.m16n8 result: 16 lanes (rows), a thread holds of every 8 columns the columns
 // 2t, 2t + 1 of row g (registers 0, 1) and of row g + 8 (2, 3), g = lane / 4, t = lane % 4.  Against one row to a thread
 // this leaves a thread a quarter of the columns, and so of the keys' scales, for four rows.
@@ -114,8 +119,8 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* r) {
 }
 // ... and 4 columns of 32 bits (8 bf16 values) at a time: row g column t (register 0), row g + 8 (1).
 __device__ __forceinline__ void tmem_st_p(uint32_t taddr, const uint32_t* r) {
-  asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -250,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
   constexpr int SOFT = CODES ? 184 : 192, PROD = CODES ? 88 : 64, REST = CODES ? 56 : 64;
   static_assert(2 * SOFT + PROD + REST <= 512, "setmaxnreg waits for registers that nobody gives back");
   extern __shared__ unsigned char smem_dyn[];
-  __shared__ __align__(8) uint64_t q_full, q_empty, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES], s_full[NSUB], p_full[NSUB][BK / 64],
+  __shared__ __align__(8) uint64_t q_full, q_empty, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES], s_full[NSUB], p_full[NSUB][2],
       o_full[NSUB], item_full[2], item_empty[2];
   __shared__ Item item_slot[2];
   __shared__ __align__(8) uint64_t steal_bar;
@@ -280,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
     }
     for (int i = 0; i < NSUB; ++i) {
       mbar_init(&s_full[i], 1);
-      for (int h = 0; h < BK / 64; ++h) mbar_init(&p_full[i][h], 4);
+      for (int h = 0; h < 2; ++h) mbar_init(&p_full[i][h], 4);
       mbar_init(&o_full[i], 1);
     }
     abort_flag_s = 0;
@@ -312,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
     // every column comes with two scales from shared memory.  Measured: bf16 prompt of 8192 tokens 590 us with one
     // row, 627 with four; 512 queries over 16384 tokens at 8 bits 292 with one, 241 with four.
     regs_up<SOFT>();
-    constexpr int R = CODES ? 4 : 1, NP = BK / 2 / R, NH = BK / 64, NPH = NP / NH;     // rows; pairs of columns of a row: all, of 64 keys
+    constexpr int R = CODES ? 4 : 1, NP = BK / 2 / R, NQ = BK / 32, NPQ = NP / NQ;     // rows; pairs of columns of a row: all, of 32 keys
     const int sub = wg, g = lane >> 2, t = R == 4 ? lane & 3 : 0, quad = warp & 3;
     const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
     const uint32_t s_addr = lane_base + G::S_COL + sub * BK, o_addr = lane_base + G::O_COL + sub * D;
@@ -351,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         float x[BK];
         if constexpr (R == 4) {
 #pragma unroll
-          for (int h = 0; h < NH; ++h) {
+          for (int h = 0; h < BK / 64; ++h) {
             tmem_ld64(s_addr + 64 * h, x + 32 * h);
             tmem_ld64(s_addr + LOWER + 64 * h, x + BK / 2 + 32 * h);
           }
@@ -444,20 +449,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
           }
         }
         float sum[R][4 / R > 1 ? 4 : 2] = {};
-        // 64 keys are handed over at a time, so that their product starts while the rest is computed; the hand-over waits
-        // for the stores, and so comes after the next 32 keys' exponentials have been started
-        auto hand_over = [&](int h) {
+        // All but the last 32 keys are handed over first, so that their product runs while the rest is computed and the last
+        // part's is short; the first hand-over, which waits for the stores, comes in the middle of the last part.
+        auto hand_over = [&](int part) {
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&p_full[sub][h]);
+          if (lane == 0) mbar_arrive(&p_full[sub][part]);
         };
 #pragma unroll
-        for (int h = 0; h < NH; ++h) {
-          uint32_t pk[32];
+        for (int u = 0; u < NQ; ++u) {
+          uint32_t pk[16];
 #pragma unroll
-          for (int c = 0; c < NPH; ++c) {
-            const int q = h * NPH + c;
+          for (int c = 0; c < NPQ; ++c) {
+            const int q = u * NPQ + c;
             const float2 v = CODES ? vs[4 * q] : make_float2(1.f, 1.f);
 #pragma unroll
             for (int i = 0; i < R; ++i) {
@@ -468,18 +473,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
               const int chain = R == 4 ? 0 : 2 * (c & 1);
               add2(sum[i][chain], sum[i][chain + 1], y0, y1);
               if (CODES) mul2(y0, y1, v.x, v.y);
-              pk[R == 4 ? (i >> 1) * 16 + 2 * c + (i & 1) : c] = pack2(y0, y1);
+              pk[R == 4 ? (i >> 1) * 8 + 2 * c + (i & 1) : c] = pack2(y0, y1);
             }
-            if (h > 0 && c == NPH / 2 - 1) hand_over(h - 1);
+            if (u == NQ - 1 && c == NPQ / 2 - 1) hand_over(0);
           }
           if constexpr (R == 4) {
-            tmem_st_p(s_addr + 32 * h, pk);
-            tmem_st_p(s_addr + LOWER + 32 * h, pk + 16);
+            tmem_st_p(s_addr + 16 * u, pk);
+            tmem_st_p(s_addr + LOWER + 16 * u, pk + 8);
           } else {
-            tmem_st_row(s_addr + 32 * h, pk);
+            tmem_st_row16(s_addr + 16 * u, pk);
           }
         }
-        hand_over(NH - 1);
+        hand_over(1);
 #pragma unroll
         for (int i = 0; i < R; ++i) l[i] += R == 4 ? sum[i][0] + sum[i][1] : (sum[i][0] + sum[i][1]) + (sum[i][R == 4 ? 0 : 2] + sum[i][R == 4 ? 0 : 3]);
         if (CODES) {
@@ -836,7 +841,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
           for (int i = 0; i < NSUB; ++i) {
 #pragma unroll
             for (int k = 0; k < BK / 16; ++k) {
-              if (k % 4 == 0 && !wait(&p_full[i][k / 4], it & 1)) break;
+              if ((k == 0 || k == BK / 16 - 2) && !wait(&p_full[i][k != 0], it & 1)) break;
               umma_ts(tm + G::O_COL + i * D, tm + G::S_COL + i * BK + 8 * k, vd + (uint64_t)((stage * G::KV_BYTES + k * 2048) >> 4),
                       G::IDESC_PV, (j | k) != 0, leader);
             }
