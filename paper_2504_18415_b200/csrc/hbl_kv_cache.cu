@@ -325,12 +325,18 @@ int launch_append_rows(AppendParams& p, cudaStream_t s) {
   note_launch();
   return HBL_OK;
 }
-// Four heads to a thread where a decoding step's worth of tokens still fills the GPU, one below.
+// One head to a thread for a decoding step, whose latency counts.  Where the call fills the GPU several: as many as leave
+// the fewest places of the token's blocks empty (96 heads of 128 elements, 16 to a row of the block: 4 to a thread fill
+// 96 of 128 places, 195 us for four 2048-token prompts; 3 fill all 96 in two blocks, 164; 6 in one, 151).  Among equals
+// the larger number, but at head_dim 256, where 6 run out of registers (341 us instead of 291).
 template <int BITS, int LPH, bool INTERLEAVED>
 int launch_append_layout(AppendParams& p, cudaStream_t s) {
-  const long threads = (long)p.b.tokens * (p.n_heads + 2 * p.c.n_kv_heads) * LPH;
-  if (threads >= (long)sm_count() * 2048 * 4) return launch_append_rows<BITS, LPH, INTERLEAVED, 4>(p, s);
-  return launch_append_rows<BITS, LPH, INTERLEAVED, 1>(p, s);
+  const int rows = p.n_heads + 2 * p.c.n_kv_heads, groups = kThreads / LPH;
+  if ((long)p.b.tokens * rows * LPH < (long)sm_count() * 2048 * 4) return launch_append_rows<BITS, LPH, INTERLEAVED, 1>(p, s);
+  auto places = [&](int n) { return (rows + groups * n - 1) / (groups * n) * n; };
+  if (LPH < 32 && places(6) <= places(4) && places(6) <= places(3)) return launch_append_rows<BITS, LPH, INTERLEAVED, LPH < 32 ? 6 : 4>(p, s);
+  if (places(4) <= places(3)) return launch_append_rows<BITS, LPH, INTERLEAVED, 4>(p, s);
+  return launch_append_rows<BITS, LPH, INTERLEAVED, 3>(p, s);
 }
 template <int BITS>
 int launch_append_bits(AppendParams& p, bool interleaved, cudaStream_t s) {
