@@ -226,3 +226,34 @@ def test_append_in_a_graph_follows_the_lengths():
             pg, sl = 4 * b + (n - 1) // 16, (n - 1) % 16
             assert torch.equal(decode(cache.k[pg, :, sl], 4, 128), u[b]) and torch.equal(cache.k_scale[pg, :, sl], s[b])
     assert hbl.hbl_check_status() == 0
+
+
+@pytest.mark.parametrize("bits", [3, 4, 8, 16])
+@pytest.mark.parametrize("H,KH,D", [(32, 32, 128), (32, 8, 128), (32, 32, 256), (16, 16, 64), (7, 1, 128)])
+def test_calls_that_fill_the_gpu(bits, H, KH, D):
+    """Many tokens: several heads to a thread, in every number that the launch chooses between."""
+    g = gen(bits + H + D)
+    page, T = 64, 2_500_000 // ((H + 2 * KH) * D // 8)
+    cache = new_cache(-(-T // page) + 1, page, KH, D, bits, 1 if bits < 8 else 0)
+    batch, tables = make_batch(g, cache, [T], [T], slots=[0] if bits < 8 else None)
+    k, v, q = heads(g, T, KH, D), heads(g, T, KH, D), heads(g, T, H, D)
+    table = hbl.hbl_rope_table(hbl.hbl_rope_frequencies(D), T)
+    for interleaved in (False, True):
+        q_out = hbl.hbl_kv_append(cache, batch, k, v, table=table, interleaved=interleaved, q=q)
+        ko, vo = hbl.hbl_kv_read(cache, batch)
+        assert hbl.hbl_check_status() == 0
+        pos = torch.arange(T, device="cuda", dtype=torch.int32)
+        assert torch.equal(q_out, hbl.hbl_rope(q, pos, table, interleaved=interleaved))
+        turned = hbl.hbl_rope(k.float(), pos, table, interleaved=interleaved)
+        pg, sl = torch.tensor(tables[0], device="cuda")[pos.long() // page], pos.long() % page
+        for x, buf, scale, out in ((turned, cache.k, cache.k_scale, ko), (v.float(), cache.v, cache.v_scale, vo)):
+            if bits == 16:
+                assert torch.equal(out, x.to(torch.bfloat16)) and torch.equal(buf[pg, :, sl], out)
+                continue
+            u, s = quant32(x, bits)
+            assert torch.equal(decode(buf[pg, :, sl], bits, D), u) and torch.equal(scale[pg, :, sl], s)
+            value = ((u - 2 ** (bits - 1)).float() * s[..., None]).to(torch.bfloat16)
+            if bits < 8:
+                u8, s8 = quant32(x[:1], 8)
+                value[0] = ((u8 - 128).float() * s8[..., None]).to(torch.bfloat16)[0]
+            assert torch.equal(out, value)
