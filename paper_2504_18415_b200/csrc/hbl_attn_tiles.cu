@@ -2,6 +2,9 @@
 //
 //   S = Q ck^T (tcgen05.mma, fp32 in tensor memory);  s = sm_scale ks_j S;  p = 2^(s - m);  O += (p vs_j) cv
 //
+// Q and ck are bf16 operands (codes are exact).  bf16 rows: p is rounded to bf16, as cv is.  Codes: p vs_j goes to fp16
+// against a running power of two above the value scales (eight times finer), cv is exact in fp16, too.
+//
 // A work item is 128 * NSUB query rows of one key head (row r: token r / group, head r % group, so that the heads that
 // share a key head share its tiles) against one piece of the keys.  One thread block per SM, which goes on to the items of
 // blocks that have not started:
@@ -46,7 +49,8 @@ struct TileGeo {
   // Instruction descriptor of kind::f16: D fp32 (1 at [4,6)), A and B bf16 (1 at [7,10), [10,13)), B MN-major (bit 16)
   // for the values, N >> 3 at [17,23), M >> 4 at [24,29).
   static constexpr uint32_t IDESC_QK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BK >> 3) << 17) | (8u << 24);
-  static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);
+  static constexpr uint32_t IDESC_PV_BF16 = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);
+  static constexpr uint32_t IDESC_PV_F16 = IDESC_PV_BF16 & ~((1u << 7) | (1u << 10));      // both fp16 (0)
 };
 
 // Shared-memory descriptors in the 128-byte swizzle (8 rows of 128 bytes make an atom of 1024): start >> 4 at [0,14),
@@ -261,6 +265,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
   __shared__ __align__(8) uint64_t steal_bar;
   __shared__ __align__(16) uint4 steal_answer;
   __shared__ __align__(16) uint32_t bad_scale[STAGES][4];       // keys of the tile whose value scale is not finite
+  __shared__ float2 unit_of_tile[STAGES];                       // what the value scales are held against: now, and before / now
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag_s;
   volatile int* abort_flag = &abort_flag_s;
@@ -345,6 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
       low = __reduce_min_sync(0xffffffffu, low);
       float neg[R], l[R];                                      // minus the maximum so far (0: none yet, see `some`), p's sum
       uint32_t some = 0;                                       // rows that have seen a key
+      float unit = 1.f;                                        // codes: O is in units of it
 #pragma unroll
       for (int i = 0; i < R; ++i) { neg[i] = 0.f; l[i] = 0.f; }
       for (int j = 0; j < tiles; ++j, ++it) {
@@ -404,6 +410,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
           top[i] = CODES ? c[0] : fmaf(c[0], scale, neg[i]);
           raise |= top[i] > (some >> i & 1 ? kLazy : -INFINITY);
         }
+        float regauge = 1.f;
+        if (CODES) {
+          const float2 y = unit_of_tile[stage];
+          unit = y.x;
+          regauge = y.y;
+          raise |= regauge != 1.f;
+        }
         if (__any_sync(0xffffffffu, raise)) {
           float f[R];
 #pragma unroll
@@ -433,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
                   tmem_ld16(o_addr + h * LOWER + 16 * c, o);
                   tmem_ld_wait();
 #pragma unroll
-                  for (int e = 0; e < 8; ++e) o[e] *= f[R == 4 ? 2 * h + (e >> 1 & 1) : 0];
+                  for (int e = 0; e < 8; ++e) o[e] *= f[R == 4 ? 2 * h + (e >> 1 & 1) : 0] * regauge;
                   tmem_st16(o_addr + h * LOWER + 16 * c, o);
                 }
               } else {
@@ -473,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
               const int chain = R == 4 ? 0 : 2 * (c & 1);
               add2(sum[i][chain], sum[i][chain + 1], y0, y1);
               if (CODES) mul2(y0, y1, v.x, v.y);
-              pk[R == 4 ? (i >> 1) * 8 + 2 * c + (i & 1) : c] = pack2(y0, y1);
+              pk[R == 4 ? (i >> 1) * 8 + 2 * c + (i & 1) : c] = CODES ? pack2_f16(y0, y1) : pack2(y0, y1);
             }
             if (u == NQ - 1 && c == NPQ / 2 - 1) hand_over(0);
           }
@@ -516,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
           l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
           l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
         }
-        inv[i] = l[i] == 0.f ? 0.f : __fdividef(1.f, l[i]);
+        inv[i] = l[i] == 0.f ? 0.f : __fdividef(unit, l[i]);
         if (some >> i & 16) inv[i] = __uint_as_float(0x7FC00000u);
         const int r = first + 8 * i;
         mine[i] = nullptr;
@@ -553,7 +566,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         ++done;
         tc_fence_after();
       }
-      const int e0 = BITS == 8 ? pair_lo<8>(t) : t, e1 = BITS == 8 ? pair_hi<8>(t) : t + 4;
+      const int e0 = BITS == 8 ? 2 * t : t, e1 = BITS == 8 ? 2 * t + 1 : t + 4;
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
         float o[32];
@@ -712,14 +725,23 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
             raw.r[i].load(src + row_of(t, rr) * (D * BITS / 8), piece, live(t, rr));
           }
         };
-        float ks = 0.f, vs = 0.f;                               // scales of key row tid of the tile
+        // Scales: ks of key row tid; value scales of all rows (32 i + lane), so that every warp finds the same `unit`
+        // for itself: a power of two no smaller than any value scale of the item so far.  p vs / unit * 2^7 is at most
+        // 2^15, what fp16 holds; it is rounded by 2^-12 of itself, or by 2^-32 unit where it is that small.
+        constexpr int VN = BK / 32;
+        float ks = 0.f, vs[VN];
         auto load_scales = [&](const Tile& t) {
-          if (tid >= BK) return;                                // (whole warps)
-          const long row = row_of(t, tid);
-          const bool l = live(t, tid);
-          ks = l ? __ldg(p.c.k_scale + row) : 0.f;
-          vs = l ? __ldg(p.c.v_scale + row) : 0.f;
+#pragma unroll
+          for (int i = 0; i < VN; ++i) {
+            const long row = row_of(t, 32 * i + lane);
+            vs[i] = live(t, 32 * i + lane) ? __ldg(p.c.v_scale + row) : 0.f;
+          }
+          if (tid < BK) {                                       // (whole warps)
+            const long row = row_of(t, tid);
+            ks = live(t, tid) ? __ldg(p.c.k_scale + row) : 0.f;
+          }
         };
+        float unit = 0x1p-100f;
         Raw raw, ahead;
         load(raw, tile, 0, 0);
         load_scales(tile);
@@ -739,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
               }
             }
           }
-#pragma unroll 1
+#pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
             const uint32_t dst = (kv == 0 ? sk : sv) + stage * G::KV_BYTES;
             uint64_t* empty = kv == 0 ? &k_empty[stage] : &v_empty[stage];
@@ -751,18 +773,37 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
               if (batch == 0) {
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(empty, ((it / STAGES) & 1) ^ 1, abort_flag, p.status)))) break;
                 if (kv == 0) {
-                  // scales of both with the keys: ks_j * sm_scale * log2(e), vs_j
-                  if (special && tid == 0) {
+                  // scales of both with the keys: ks_j * sm_scale * log2(e), vs_j / unit * 2^7
+                  if (special && lane == 0) {
                     const long brow = (long)bos_row * p.c.n_kv_heads + w.head;
-                    ks = bos_row >= 0 ? __ldg(p.c.bos_k_scale + brow) : 0.f;
-                    vs = bos_row >= 0 ? __ldg(p.c.bos_v_scale + brow) : 0.f;
+                    if (tid == 0) ks = bos_row >= 0 ? __ldg(p.c.bos_k_scale + brow) : 0.f;
+                    vs[0] = bos_row >= 0 ? __ldg(p.c.bos_v_scale + brow) : 0.f;
                   }
-                  const bool bad = (__float_as_uint(vs) & 0x7F800000u) == 0x7F800000u;
-                  const unsigned word = __ballot_sync(0xffffffffu, bad);
-                  if (lane == 0) bad_scale[stage][tid >> 5] = word;      // (BK 64: the upper two hold none)
+                  uint32_t most = 0, bad = 0;
+#pragma unroll
+                  for (int i = 0; i < VN; ++i) {
+                    const uint32_t x = __float_as_uint(fabsf(vs[i]));
+                    if (x >= 0x7F800000u) {
+                      bad |= 1u << i;
+                      vs[i] = 0.f;
+                    } else {
+                      most = max(most, min(x, 0x7E800000u));
+                    }
+                  }
+                  const float before = unit;
+                  unit = fmaxf(unit, __uint_as_float((__reduce_max_sync(0xffffffffu, most) + 0x7FFFFFu) & 0x7F800000u));
+                  const float to = 128.f / unit;
+                  const int mine = tid >> 5;                     // of the tile's 32-key groups
+                  float my_vs = 0.f;
+#pragma unroll
+                  for (int i = 0; i < VN; ++i)
+                    if (i == mine) my_vs = vs[i];
+                  const unsigned word = __ballot_sync(0xffffffffu, mine < VN && (bad >> mine & 1));
+                  if (lane == 0) bad_scale[stage][mine] = word;  // (BK 64: the upper two hold none)
+                  if (tid == 0) unit_of_tile[stage] = make_float2(unit * 0x1p-7f, before / unit);
                   if (tid < BK) {
                     scales[stage * 2 * BK + tid] = ks * scale;
-                    scales[stage * 2 * BK + BK + tid] = bad ? 0.f : vs;
+                    scales[stage * 2 * BK + BK + tid] = my_vs * to;
                   }
                   if (more) load_scales(after);
                 }
@@ -774,7 +815,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
 #pragma unroll
                 for (int u = 0; u < UN; ++u) {
                   uint32_t o[4];
-                  pairs<BITS>(raw.r[i], u, piece, o);
+                  if (kv == 0) pairs<BITS>(raw.r[i], u, piece, o);
+                  else pairs16<BITS>(raw.r[i], u, piece, o);
                   store16(dst + chunk_at(rr, piece * UN + u, G::HALF), o);
                 }
               }
@@ -788,9 +830,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
                 const uint2 u = __ldg(reinterpret_cast<const uint2*>((kv == 0 ? p.c.bos_k : p.c.bos_v) + brow * D) + tid);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                  const int lo = pair_lo<BITS>(k), hi = pair_hi<BITS>(k);
-                  o[k] = pack2((float)((int)(((lo < 4 ? u.x : u.y) >> (8 * (lo & 3))) & 255u) - 128),
-                               (float)((int)(((hi < 4 ? u.x : u.y) >> (8 * (hi & 3))) & 255u) - 128));
+                  auto value = [&](int e) { return (float)((int)(((e < 4 ? u.x : u.y) >> (8 * (e & 3))) & 255u) - 128); };
+                  o[k] = kv == 0 ? pack2(value(pair_lo<BITS>(k)), value(pair_hi<BITS>(k))) : pack2_f16(value(pair16_lo<BITS>(k)), value(pair16_hi<BITS>(k)));
                 }
               }
               store16(dst + chunk_at(0, tid, G::HALF), o);
@@ -843,7 +884,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
             for (int k = 0; k < BK / 16; ++k) {
               if ((k == 0 || k == BK / 16 - 2) && !wait(&p_full[i][k != 0], it & 1)) break;
               umma_ts(tm + G::O_COL + i * D, tm + G::S_COL + i * BK + 8 * k, vd + (uint64_t)((stage * G::KV_BYTES + k * 2048) >> 4),
-                      G::IDESC_PV, (j | k) != 0, leader);
+                      CODES ? G::IDESC_PV_F16 : G::IDESC_PV_BF16, (j | k) != 0, leader);
             }
             if (!ok) break;
             if (more) {
