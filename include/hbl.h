@@ -471,6 +471,7 @@ int hbl_kv_read(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, void* 
  * bits 16: a value that is NaN or infinite may reach every row of its sequence, rows it is masked for among them
  * (0 * inf); places beyond kv_len are never used, whatever they hold.
  * workspace: hbl_attention_workspace_bytes, 1024-byte aligned (NULL where that is 0); scratch, nothing in it is kept.
+ * Calls that may run at the same time need one each.  out may not overlap q or the cache.
  * n_heads a multiple of n_kv_heads. */
 typedef struct {
   const void* q;

@@ -44,10 +44,11 @@ constexpr int kStreamSlots = 64, kWorkspaceSlots = 256;
 constexpr int kMaxRecordedOutputs = 8;
 struct ByteRange { const char* lo; const char* hi; };
 struct StreamSlot {
-  cudaStream_t s; bool used, early;
+  cudaStream_t s; bool used, early, unflushed;
   int n_out; ByteRange out[kMaxRecordedOutputs];             // what the early-releasing call writes (its outputs)
 } g_streams[kStreamSlots] = {};
 bool g_stream_overflow = false;       // an early release on a stream that found no slot: every unknown stream counts as early
+bool g_unflushed_overflow = false;    // the same for streams whose last launch is to be followed by ordinary ones
 struct WorkspaceSlot { const void* ws; bool used; int last; } g_workspaces[kWorkspaceSlots] = {};
 }
 LaunchMode& launch_mode() {
@@ -70,6 +71,27 @@ void set_stream_released_early(cudaStream_t s, bool v) {
   if (!v && !g_stream_overflow) return;                       // nothing to remember
   if (free_slot >= 0) { g_streams[free_slot] = {}; g_streams[free_slot].s = s; g_streams[free_slot].used = true; g_streams[free_slot].early = v; }
   else if (v) g_stream_overflow = true;
+}
+bool stream_unflushed(cudaStream_t s) {
+  std::lock_guard<std::mutex> lock(g_overlap_mutex);
+  for (int i = 0; i < kStreamSlots; ++i)
+    if (g_streams[i].used && g_streams[i].s == s) return g_streams[i].unflushed;
+  return g_unflushed_overflow;
+}
+void set_stream_unflushed(cudaStream_t s, bool v) {
+  std::lock_guard<std::mutex> lock(g_overlap_mutex);
+  int free_slot = -1;
+  for (int i = 0; i < kStreamSlots; ++i) {
+    if (g_streams[i].used && g_streams[i].s == s) { g_streams[i].unflushed = v; return; }
+    if (!g_streams[i].used && free_slot < 0) free_slot = i;
+  }
+  if (!v) return;                                             // nothing to remember
+  if (free_slot < 0) { g_unflushed_overflow = true; return; }
+  g_streams[free_slot] = {};
+  g_streams[free_slot].s = s;
+  g_streams[free_slot].used = true;
+  g_streams[free_slot].early = g_stream_overflow;             // (as a stream without a slot counts)
+  g_streams[free_slot].unflushed = true;
 }
 namespace {
 // The outputs of the early-releasing call just launched on s (called right after set_stream_released_early(s, true)).

@@ -81,7 +81,7 @@ struct AttnCall {
   bool use_rows, use_tiles;
   int few_rows, few_tiles;             // the border as each kernel sees it
   AttnPlan rows, tiles;
-  size_t part_lse, workspace;          // partial results where the keys of a sequence are split
+  size_t rows_lse, tiles_o, tiles_lse, workspace;     // byte offsets of the parts (rows_o at 0), and the bytes of all
 };
 AttnCall plan_attention(const KvView& c, const BatchView& b, int n_heads) {
   AttnCall w{};
@@ -93,11 +93,20 @@ AttnCall plan_attention(const KvView& c, const BatchView& b, int n_heads) {
   w.rows.splits = w.tiles.splits = 1;
   if (w.use_rows) w.rows = plan_attention_rows(c, b, n_heads, w.few_rows);
   if (w.use_tiles) w.tiles = plan_attention_tiles(c, b, n_heads, w.few_tiles);
-  const int splits = w.rows.splits > w.tiles.splits ? w.rows.splits : w.tiles.splits;
-  if (splits <= 1) return w;
-  const size_t rows = (size_t)splits * b.tokens * n_heads;
-  w.part_lse = align_up(rows * c.head_dim * sizeof(float), 1024);
-  w.workspace = w.part_lse + align_up(rows * sizeof(float), 1024);
+  size_t off = 0;
+  auto take = [&](size_t& at, size_t floats) { at = off; off = align_up(off + floats * sizeof(float), 1024); };
+  if (w.rows.splits > 1) {
+    const size_t rows = (size_t)w.rows.splits * b.n_seqs * c.n_kv_heads * w.rows.cap;
+    size_t rows_o;
+    take(rows_o, rows * c.head_dim);
+    take(w.rows_lse, rows);
+  }
+  if (w.tiles.splits > 1) {
+    const size_t rows = (size_t)w.tiles.splits * b.tokens * n_heads;
+    take(w.tiles_o, rows * c.head_dim);
+    take(w.tiles_lse, rows);
+  }
+  w.workspace = off;
   return w;
 }
 
@@ -229,12 +238,13 @@ int hbl_attention(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, cons
   a.group = args->n_heads / c.n_kv_heads;
   a.causal = args->causal != 0;
   a.scale_log2 = args->sm_scale * 1.4426950408889634f;
-  float* part_o = static_cast<float*>(workspace);
-  float* part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.part_lse);
+  char* ws = static_cast<char*>(workspace);
+  const AttnParts parts = {reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + w.rows_lse), reinterpret_cast<float*>(ws + w.tiles_o),
+                           reinterpret_cast<float*>(ws + w.tiles_lse)};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (w.use_tiles && (rc = launch_attention_tiles(c, b, a, w.tiles, w.few_tiles, part_o, part_lse, s)) != HBL_OK) return rc;
-  if (w.use_rows && (rc = launch_attention_rows(c, b, a, w.rows, w.few_rows, part_o, part_lse, s)) != HBL_OK) return rc;
-  if (w.workspace > 0) return launch_attention_combine(c, b, a, w.rows, w.tiles, w.few_tiles, part_o, part_lse, s);
+  if (w.use_tiles && (rc = launch_attention_tiles(c, b, a, w.tiles, w.few_tiles, parts, s)) != HBL_OK) return rc;
+  if (w.use_rows && (rc = launch_attention_rows(c, b, a, w.rows, w.few_rows, parts, s)) != HBL_OK) return rc;
+  if (w.workspace > 0) return launch_attention_combine(c, b, a, w.rows, w.tiles, w.few_tiles, parts, s);
   return HBL_OK;
 }
 

@@ -28,8 +28,8 @@ struct RowsParams {
   BatchView b;
   AttnArgs a;
   AttnPlan p;
-  float* part_o;                 // [splits][tokens * n_heads][head_dim], normalised; splits > 1 only
-  float* part_lse;               // [splits][tokens * n_heads], log2 units
+  float* part_o;                 // [splits][n_seqs * n_kv_heads * cap][head_dim], normalised; splits > 1 only
+  float* part_lse;               // [splits][n_seqs * n_kv_heads * cap], log2 units
   int* status;
   int few;                       // sequences of more rows than this are another kernel's
 };
@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 4 : 2) attn_ro
     }
     __syncthreads();
   }
-  const long total_rows = (long)p.b.tokens * p.a.n_heads;
+  const long all_rows = (long)p.b.n_seqs * p.c.n_kv_heads * p.p.cap;
   for (int i = threadIdx.x; i < ROWS * (D / 4); i += kThreads) {
     const int rr = i / (D / 4), d = (i % (D / 4)) * 4, r = r0 + rr;
     if (r >= n_rows) break;
@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 4 : 2) attn_ro
     const float4 v = *reinterpret_cast<const float4*>(&so[rr][d]);
     const float lse2 = sum == 0.f ? -INFINITY : top + __log2f(sum);
     if (p.p.splits > 1) {
-      const long row = split * total_rows + (long)tok * p.a.n_heads + hq;
+      const long row = split * all_rows + ((long)b * p.c.n_kv_heads + head) * p.p.cap + r;
       *reinterpret_cast<float4*>(p.part_o + row * D + d) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
       if (d == 0) p.part_lse[row] = lse2;
     } else {
@@ -448,8 +448,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 4 : 2) attn_ro
 }
 
 // The pieces of a row together (whichever kernel computed them): out = sum_s 2^(lse_s - top) o_s / sum_s 2^(lse_s - top).
-// Where only the sequences of few rows are split, those rows are what the warps are dealt (sequence, key head, row: up to
-// `few` of them); looking every row of the call up cost 161 us on four 2048-token prompts, none of which was split.
+// The streaming kernel's rows are dealt to the warps by sequence, key head and row; where the tiles are split, too, all rows
+// of the call are.  (Looking every row up cost 161 us on four 2048-token prompts, none of which was split.)
 // `share` warps (1, 2, 4 or 8, by the number of pieces) take the pieces of a row in turn, four loads in flight each, and
 // add up through shared memory in a fixed order.
 struct CombineParams {
@@ -458,7 +458,7 @@ struct CombineParams {
   AttnArgs a;
   AttnPlan rows, tiles;          // of sequences of up to `few` rows, and of the others
   int few, share, short_only;
-  const float *part_o, *part_lse;
+  AttnParts w;
   int* status;
 };
 template <int D>
@@ -467,33 +467,48 @@ __global__ void __launch_bounds__(256) attn_combine_kernel(const __grid_constant
   __shared__ float s_acc[8][D], s_sum[8];
   grid_dependency_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = warp % p.share;
-  const long total_rows = (long)p.b.tokens * p.a.n_heads, unit = ((long)blockIdx.x * 8 + warp) / p.share;
-  long row = unit;
+  const long unit = ((long)blockIdx.x * 8 + warp) / p.share, short_rows = (long)p.b.n_seqs * p.c.n_kv_heads * p.rows.cap;
+  const long call_rows = (long)p.b.tokens * p.a.n_heads;
   int tok = 0, hq = 0, pieces = 0;                            // pieces 0: nothing to do
+  const float *part_o = nullptr, *part_lse = nullptr;
+  long row = 0, total_rows = 0;                               // in the parts
   auto pieces_of = [&](const AttnPlan& plan, const SeqLens& len) {
     return plan.splits > 1 ? max(1, min(plan.splits, (len.held + plan.chunk - 1) / plan.chunk)) : 0;      // (0: written whole)
   };
   SeqLens len;
-  if (p.short_only) {
-    const int per_seq = p.c.n_kv_heads * p.few, b = (int)(unit / per_seq), r = (int)(unit % p.few);
-    if (b < p.b.n_seqs && sequence_lengths(p.b, b, p.c.page_shift, p.status, len)) {
-      const long n_rows = (long)min(len.q_len, p.b.max_q_len) * p.a.group;
-      if (r < n_rows && n_rows <= p.few) {
-        tok = len.q0 + r / p.a.group;
-        hq = (int)(unit % per_seq) / p.few * p.a.group + r % p.a.group;
-        row = (long)tok * p.a.n_heads + hq;
-        pieces = pieces_of(p.rows, len);
-      }
+  int b = p.b.n_seqs;
+  if (p.short_only && unit < short_rows) {
+    b = (int)(unit / (p.c.n_kv_heads * p.rows.cap));
+    const int r = (int)(unit % p.rows.cap);
+    if (sequence_lengths(p.b, b, p.c.page_shift, p.status, len) && r < min(len.q_len, p.b.max_q_len) * p.a.group) {
+      tok = len.q0 + r / p.a.group;
+      hq = (int)(unit / p.rows.cap % p.c.n_kv_heads) * p.a.group + r % p.a.group;
+    } else {
+      b = p.b.n_seqs;
     }
-  } else if (row < total_rows) {
-    tok = (int)(row / p.a.n_heads);
-    hq = (int)(row % p.a.n_heads);
-    const int b = find_sequence(p.b.q_start, p.b.n_seqs, tok, lane);
-    if (b < p.b.n_seqs && sequence_lengths(p.b, b, p.c.page_shift, p.status, len) && tok >= len.q0 && tok - len.q0 < p.b.max_q_len)
-      pieces = pieces_of((long)min(len.q_len, p.b.max_q_len) * p.a.group > p.few ? p.tiles : p.rows, len);
+  } else if (!p.short_only && unit < call_rows) {
+    tok = (int)(unit / p.a.n_heads);
+    hq = (int)(unit % p.a.n_heads);
+    b = find_sequence(p.b.q_start, p.b.n_seqs, tok, lane);
+    if (b < p.b.n_seqs && !(sequence_lengths(p.b, b, p.c.page_shift, p.status, len) && tok >= len.q0 && tok - len.q0 < p.b.max_q_len)) b = p.b.n_seqs;
+  }
+  if (b < p.b.n_seqs) {
+    if ((long)min(len.q_len, p.b.max_q_len) * p.a.group > p.few) {
+      pieces = pieces_of(p.tiles, len);
+      part_o = p.w.tiles_o;
+      part_lse = p.w.tiles_lse;
+      row = (long)tok * p.a.n_heads + hq;
+      total_rows = call_rows;
+    } else {
+      pieces = pieces_of(p.rows, len);
+      part_o = p.w.rows_o;
+      part_lse = p.w.rows_lse;
+      row = ((long)b * p.c.n_kv_heads + hq / p.a.group) * p.rows.cap + (tok - len.q0) * p.a.group + hq % p.a.group;
+      total_rows = short_rows;
+    }
   }
   float top = -INFINITY;
-  for (int s = lane; s < pieces; s += 32) top = fmaxf(top, p.part_lse[s * total_rows + row]);
+  for (int s = lane; s < pieces; s += 32) top = fmaxf(top, part_lse[s * total_rows + row]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   float acc[E] = {}, sum = 0.f;
@@ -502,12 +517,12 @@ __global__ void __launch_bounds__(256) attn_combine_kernel(const __grid_constant
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int s = s0 + k * p.share;
-      const float x = s < pieces ? p.part_lse[s * total_rows + row] : -INFINITY;
+      const float x = s < pieces ? part_lse[s * total_rows + row] : -INFINITY;
       w[k] = x == -INFINITY ? 0.f : exp2_approx(x - top);     // (a NaN stays one)
 #pragma unroll
       for (int e = 0; e < E; ++e) v[k][e] = 0.f;
       if (s < pieces) {
-        const float* src = p.part_o + (s * total_rows + row) * D + lane * E;
+        const float* src = part_o + (s * total_rows + row) * D + lane * E;
 #pragma unroll
         for (int e = 0; e < E; e += 2) {
           const float2 y = *reinterpret_cast<const float2*>(src + e);
@@ -540,11 +555,11 @@ __global__ void __launch_bounds__(256) attn_combine_kernel(const __grid_constant
   uint32_t* dst = reinterpret_cast<uint32_t*>(p.a.out + tok * p.a.o_ts + hq * p.a.o_hs + lane * E);
 #pragma unroll
   for (int e = 0; e < E; e += 2) dst[e / 2] = pack2(acc[e] * inv, acc[e + 1] * inv);
-  if (lane == 0 && p.a.lse != nullptr) p.a.lse[row] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
+  if (lane == 0 && p.a.lse != nullptr) p.a.lse[(long)tok * p.a.n_heads + hq] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
 }
 
 long most_rows(const BatchView& b, int group, int few) {
-  const long rows = (long)b.max_q_len * group;
+  const long rows = (long)b.max_q_len * group;                // (few is the border, not the most: above it the other kernel works)
   return rows < few ? rows : few;
 }
 int rows_per_tile(const BatchView& b, int group, int few) { return most_rows(b, group, few) > 8 ? 16 : 8; }
@@ -554,9 +569,9 @@ int launch_rows_dim(RowsParams& p, cudaStream_t s) {
   const long blocks = (long)p.b.n_seqs * p.c.n_kv_heads * p.p.tiles * p.p.splits;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
   if (rows_per_tile(p.b, p.a.group, p.few) == 8)
-    HBL_CUDA_OK(launch_dependent(attn_rows_kernel<BITS, D, 1>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+    HBL_CUDA_OK(launch_waiting(attn_rows_kernel<BITS, D, 1>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
   else
-    HBL_CUDA_OK(launch_dependent(attn_rows_kernel<BITS, D, 2>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+    HBL_CUDA_OK(launch_waiting(attn_rows_kernel<BITS, D, 2>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
   note_launch();
   return HBL_OK;
 }
@@ -575,7 +590,8 @@ int launch_rows_bits(RowsParams& p, cudaStream_t s) {
 AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads, int few) {
   AttnPlan p{};
   const int group = n_heads / c.n_kv_heads, rows = rows_per_tile(b, group, few);
-  p.tiles = (int)((most_rows(b, group, few) + rows - 1) / rows);
+  p.cap = (int)most_rows(b, group, few);
+  p.tiles = (p.cap + rows - 1) / rows;
   const long base = (long)b.n_seqs * c.n_kv_heads * p.tiles;
   // pieces of at least 256 keys, as many as keep four thread blocks on every SM; none up to 512 keys, where the second
   // launch costs more than the shorter loops save (4 x 509 tokens: 14.8 us in two pieces, 12.7 in one; 4 x 1000: 16.8, 17.3)
@@ -590,11 +606,10 @@ AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads, i
   return p;
 }
 
-int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& plan, int few, float* part_o,
-                          float* part_lse, cudaStream_t s) {
+int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& plan, int few, const AttnParts& w,
+                          cudaStream_t s) {
   RowsParams p{};
-  p.few = few;
-  p.c = c; p.b = b; p.a = a; p.p = plan; p.part_o = part_o; p.part_lse = part_lse;
+  p.c = c; p.b = b; p.a = a; p.p = plan; p.few = few; p.part_o = w.rows_o; p.part_lse = w.rows_lse;
   p.status = device_status_word();
   if (p.status == nullptr) return HBL_ERR_CUDA;
   switch (c.bits) {
@@ -607,22 +622,22 @@ int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a
 }
 
 int launch_attention_combine(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& rows, const AttnPlan& tiles,
-                             int few, const float* part_o, const float* part_lse, cudaStream_t s) {
+                             int few, const AttnParts& w, cudaStream_t s) {
   CombineParams p{};
-  p.c = c; p.b = b; p.a = a; p.rows = rows; p.tiles = tiles; p.few = few; p.part_o = part_o; p.part_lse = part_lse;
+  p.c = c; p.b = b; p.a = a; p.rows = rows; p.tiles = tiles; p.few = few; p.w = w;
   p.status = device_status_word();
   if (p.status == nullptr) return HBL_ERR_CUDA;
   const int most = rows.splits > tiles.splits ? rows.splits : tiles.splits;
   p.share = most <= 4 ? 1 : most <= 8 ? 2 : most <= 16 ? 4 : 8;
-  const long all = (long)b.tokens * a.n_heads, few_rows = (long)b.n_seqs * c.n_kv_heads * few;
-  p.short_only = tiles.splits <= 1 && few_rows < all;
-  const long blocks = ((p.short_only ? few_rows : all) * p.share + 7) / 8;
+  p.short_only = tiles.splits <= 1;
+  const long units = p.short_only ? (long)b.n_seqs * c.n_kv_heads * rows.cap : (long)b.tokens * a.n_heads;
+  const long blocks = (units * p.share + 7) / 8;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
   const dim3 grid((unsigned)blocks), block(256);
   switch (c.head_dim) {
-    case 64: HBL_CUDA_OK(launch_dependent(attn_combine_kernel<64>, grid, block, 0, s, p)); break;
-    case 128: HBL_CUDA_OK(launch_dependent(attn_combine_kernel<128>, grid, block, 0, s, p)); break;
-    case 256: HBL_CUDA_OK(launch_dependent(attn_combine_kernel<256>, grid, block, 0, s, p)); break;
+    case 64: HBL_CUDA_OK(launch_waiting(attn_combine_kernel<64>, grid, block, 0, s, p)); break;
+    case 128: HBL_CUDA_OK(launch_waiting(attn_combine_kernel<128>, grid, block, 0, s, p)); break;
+    case 256: HBL_CUDA_OK(launch_waiting(attn_combine_kernel<256>, grid, block, 0, s, p)); break;
     default: return HBL_ERR_SHAPE;
   }
   note_launch();

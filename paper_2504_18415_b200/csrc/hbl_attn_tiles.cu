@@ -1002,7 +1002,7 @@ template <int BITS, int D>
 int launch_tiles_dim(TilesParams& p, cudaStream_t s) {
   auto kern = attn_tiles_kernel<BITS, D>;
   HBL_ALLOW_DYNAMIC_SMEM(kern, TileGeo<D>::SMEM);
-  HBL_CUDA_OK(launch_dependent(kern, dim3(p.items), dim3(kThreads), TileGeo<D>::SMEM, s, p));
+  HBL_CUDA_OK(launch_waiting(kern, dim3(p.items), dim3(kThreads), TileGeo<D>::SMEM, s, p));
   note_launch();
   return HBL_OK;
 }
@@ -1041,10 +1041,10 @@ AttnPlan plan_attention_tiles(const KvView& c, const BatchView& b, int n_heads, 
   return p;
 }
 
-int launch_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& plan, int few, float* part_o,
-                           float* part_lse, cudaStream_t s) {
+int launch_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& plan, int few, const AttnParts& w,
+                           cudaStream_t s) {
   TilesParams p{};
-  p.c = c; p.b = b; p.a = a; p.p = plan; p.part_o = part_o; p.part_lse = part_lse; p.few = few;
+  p.c = c; p.b = b; p.a = a; p.p = plan; p.few = few; p.part_o = w.tiles_o; p.part_lse = w.tiles_lse;
   p.status = device_status_word();
   if (p.status == nullptr) return HBL_ERR_CUDA;
   const long items = (long)plan.tiles * c.n_kv_heads * plan.splits;

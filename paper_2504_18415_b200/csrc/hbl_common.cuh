@@ -74,13 +74,19 @@ struct LaunchMode {
   bool releases_early = false;        // the next launch is such a contraction
 };
 LaunchMode& launch_mode();                                    // per host thread
+// The activation kernels read their inputs before they wait for the launch before them, which is sound behind a kernel
+// that is known to have been flushed, not behind one that has merely run out of thread blocks.  The kernels between q, k, v
+// and the input of W_o are launched by launch_waiting(): they wait first thing, so they may start early themselves, and the
+// library remembers, per stream, that whatever is launched after them without waiting first must be an ordinary launch.
+bool stream_unflushed(cudaStream_t s);                        // the library's last launch on s was one of those
+void set_stream_unflushed(cudaStream_t s, bool v);
 bool stream_released_early(cudaStream_t s);                   // the library's last launch on s releases early
 void set_stream_released_early(cudaStream_t s, bool v);
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_dependent(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
                                     Args... args) {
   const LaunchMode mode = launch_mode();
-  const bool programmatic = mode.overlap_ok || !stream_released_early(s);
+  const bool programmatic = (mode.overlap_ok || !stream_released_early(s)) && !stream_unflushed(s);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
@@ -93,6 +99,25 @@ inline cudaError_t launch_dependent(void (*kern)(KArgs...), dim3 grid, dim3 bloc
   cfg.numAttrs = 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
   set_stream_released_early(s, mode.releases_early);
+  set_stream_unflushed(s, false);
+  return e;
+}
+// For kernels that call grid_dependency_wait() before they touch memory.
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_waiting(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = stream_released_early(s) ? 0 : 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
+  set_stream_released_early(s, false);
+  set_stream_unflushed(s, true);
   return e;
 }
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -321,7 +321,7 @@ int launch_append_rows(AppendParams& p, cudaStream_t s) {
   p.blocks_per_token = (rows + per_block - 1) / per_block;
   const long blocks = (long)p.b.tokens * p.blocks_per_token;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
-  HBL_CUDA_OK(launch_dependent(kv_append_kernel<BITS, LPH, INTERLEAVED, ROWS>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+  HBL_CUDA_OK(launch_waiting(kv_append_kernel<BITS, LPH, INTERLEAVED, ROWS>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
   note_launch();
   return HBL_OK;
 }
@@ -354,7 +354,7 @@ int launch_read_rows(ReadParams& p, cudaStream_t s) {
   p.blocks_per_token = (2 * p.c.n_kv_heads + per_block - 1) / per_block;
   const long blocks = (long)p.b.tokens * p.blocks_per_token;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
-  HBL_CUDA_OK(launch_dependent(kv_read_kernel<BITS, LPH, ROWS>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+  HBL_CUDA_OK(launch_waiting(kv_read_kernel<BITS, LPH, ROWS>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
   note_launch();
   return HBL_OK;
 }

@@ -81,15 +81,18 @@ struct AttnArgs {
   float scale_log2;                    // sm_scale * log2(e): scores in units of log2
 };
 // How a call is split: the keys of a sequence go to `splits` thread blocks in pieces of `chunk`.
-struct AttnPlan { int splits, chunk, tiles; };
+// The pieces' results wait in the workspace: `cap` rows (queries of one key head) for every sequence and key head from the
+// streaming kernel, all rows of the call from the tiles.
+struct AttnPlan { int splits, chunk, tiles, cap; };
+struct AttnParts { float *rows_o, *rows_lse, *tiles_o, *tiles_lse; };      // [splits][rows][head_dim], [splits][rows]
 // Sequences of up to `few` query rows (tokens times heads that share a key head) go to one kernel, the others to the other.
 AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads, int few);
 AttnPlan plan_attention_tiles(const KvView& c, const BatchView& b, int n_heads, int few);
-int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, int few, float* part_o,
-                          float* part_lse, cudaStream_t s);
-int launch_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, int few, float* part_o,
-                           float* part_lse, cudaStream_t s);
+int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, int few, const AttnParts& w,
+                          cudaStream_t s);
+int launch_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, int few, const AttnParts& w,
+                           cudaStream_t s);
 int launch_attention_combine(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& rows, const AttnPlan& tiles,
-                             int few, const float* part_o, const float* part_lse, cudaStream_t s);
+                             int few, const AttnParts& w, cudaStream_t s);
 
 }  // namespace hbl

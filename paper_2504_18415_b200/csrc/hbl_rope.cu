@@ -170,7 +170,7 @@ int launch_one(RopeArgs& a, cudaStream_t s) {
   a.items = (long)a.tokens * a.groups * a.pieces;
   const long blocks = (a.items + kThreads - 1) / kThreads;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
-  HBL_CUDA_OK(launch_dependent(rope_kernel<T, INTERLEAVED, HEADS>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a));
+  HBL_CUDA_OK(launch_waiting(rope_kernel<T, INTERLEAVED, HEADS>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a));
   note_launch();
   return HBL_OK;
 }
@@ -192,7 +192,7 @@ int launch_rope_table(const double* freq, int n_freq, double amplitude, int firs
   if (n == 0) return HBL_OK;
   const long blocks = (n + kThreads - 1) / kThreads;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
-  HBL_CUDA_OK(launch_dependent(rope_table_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, f, n_freq, amplitude, first_pos, n,
+  HBL_CUDA_OK(launch_waiting(rope_table_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, f, n_freq, amplitude, first_pos, n,
                                reinterpret_cast<float2*>(table)));
   note_launch();
   return HBL_OK;
