@@ -466,10 +466,12 @@ int hbl_kv_read(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, void* 
  * number of queries) gets out = 0 and lse = -infinity.
  *   q, out    device bf16 [tokens, n_heads, head_dim], element strides as in hbl_rope
  *   lse       NULL, or device fp32 [tokens, n_heads]: log(sum_j p_j)
- * Products are of bf16 values: codes are exact in bf16 and their scales are applied in fp32, to the score (keys) and
- * to p (values), which is then rounded to bf16; scores, p's sum and the result are accumulated in fp32.
- * bits 16: a value that is NaN or infinite may reach every row of its sequence, rows it is masked for among them
- * (0 * inf); places beyond kv_len are never used, whatever they hold.
+ * Products are of 16-bit values on the tensor cores: bf16 (bits 16: p is rounded to it), codes exactly; their scales are
+ * applied in fp32, to the score (keys) and to p (values), and the product is rounded to fp16 against the largest scale.
+ * Scores, p's sum and the result are accumulated in fp32.
+ * Keys, values and scales that are NaN or infinite reach no row they are masked for; places beyond kv_len are never used,
+ * whatever they hold.  A row that sees such a key or value is NaN, at bits 16 perhaps in the value's elements alone; its lse
+ * may be NaN, too.
  * workspace: hbl_attention_workspace_bytes, 1024-byte aligned (NULL where that is 0); scratch, nothing in it is kept.
  * Calls that may run at the same time need one each.  out may not overlap q or the cache.
  * n_heads a multiple of n_kv_heads. */

@@ -145,6 +145,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 4 : 2) attn_ro
   // fp16: at most 2^15, rounded by 2^-12 of themselves, or by 2^-32 vr where they are that small.
   float neg[NT][2], qs[NT][2], l[NT][2], o[NT][MT][4];
   float vr = 0x1p-100f, inv_vr = 0x1p107f;
+  uint32_t poison = 0;                                         // bits 16: columns that saw a masked step's value that is not finite
   uint32_t some = 0;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -338,10 +339,32 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 4 : 2) attn_ro
           report_device_error(p.status, HBL_ERR_RANGE);
         } else {
           const bool masked = kb + 16 > low || (bos && kb == 0);
-          if (!CODES && kb + 16 > key1) {                      // 0 * what lies beyond the last key may not be 0
+          if (!CODES && masked) {
+            // 0 * a value that is not finite would reach the columns it is masked for: such values become zeros, and the
+            // columns that do see their key are marked; what lies beyond the last key becomes zeros, whatever it is
+            uint32_t bad = 0;                                  // keys of the step
 #pragma unroll
-            for (int h = 0; h < 4; ++h)
-              if (kb + 2 * t + (h & 1) + 8 * (h >> 1) >= key1) s.v[h].clear();
+            for (int h = 0; h < 4; ++h) {
+              const int r = 2 * t + (h & 1) + 8 * (h >> 1);
+              bool any = false;
+#pragma unroll
+              for (int i = 0; i < G::VLane::WORDS; ++i) {
+                const uint32_t x = s.v[h].w[i];
+                any |= (x & 0x7F800000u) == 0x7F800000u || (x & 0x7F80u) == 0x7F80u;
+              }
+              if (any || kb + r >= key1) s.v[h].clear();
+              if (any && kb + r < key1) bad |= 1u << r;
+            }
+            bad = __reduce_or_sync(0xffffffffu, bad);
+            if (bad != 0) {
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  const int n_seen = min(lim[nt][e], key1) - kb;
+                  if (n_seen > 0 && (bad & (n_seen >= 16 ? 0xFFFFu : (1u << n_seen) - 1))) poison |= 1u << (2 * nt + e);
+                }
+            }
           }
           float c[NT][4] = {};
 #pragma unroll
@@ -389,6 +412,10 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 4 : 2) attn_ro
       x += __shfl_xor_sync(0xffffffffu, x, 8);
       x += __shfl_xor_sync(0xffffffffu, x, 16);
       m[nt][e] = x == 0.f ? -INFINITY : -neg[nt][e];           // (a NaN has a place in the sum, too)
+      if (!CODES && (poison >> (2 * nt + e) & 1)) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) o[nt][i][e] = o[nt][i][e + 2] = __uint_as_float(0x7FC00000u);
+      }
       if (g == 0) {
         sm[warp][nt * 8 + 2 * t + e] = m[nt][e];
         sl[warp][nt * 8 + 2 * t + e] = x;

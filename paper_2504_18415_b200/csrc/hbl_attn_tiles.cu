@@ -193,6 +193,11 @@ struct Item {
   int key0, key1;                // keys of the piece that any row sees
   int tiles;                     // of BK keys; -1: no more items
 };
+// The first tile of a causal item in which some row masks a key.
+template <int D>
+__device__ __forceinline__ int first_masked(const TilesParams& p, const Item& w) {
+  return max(0, w.past + token_of(p, w.r0) + 1 - w.key0) / TileGeo<D>::BK;
+}
 // The whole warp takes part.  False: nothing to do.
 template <int D>
 __device__ __forceinline__ bool decode_item(const TilesParams& p, int item, int lane, Item& o) {
@@ -666,6 +671,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         // bf16 rows are copied asynchronously and announced one copy later, so that two are in flight; nothing that a
         // wait below needs depends on the one not announced yet
         uint64_t* copied = nullptr;
+        const int masked_from = p.a.causal ? first_masked<D>(p, w) : w.tiles;
         for (int j = 0; j < w.tiles; ++j, ++it) {
           const int stage = it % STAGES;
 #pragma unroll
@@ -681,6 +687,31 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
               copy16(dst + chunk_at(rr, tid % CH, G::HALF), col + row_of(tile, rr) * (2 * D), live(tile, rr));
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
+            if (kv == 1 && j >= masked_from) {
+              // A tile that some row masks: 0 * a value that is not finite would reach rows that mask its key.  Every thread
+              // looks through the pieces that it has copied; such a key's value becomes zeros and the key itself NaN, so
+              // that the rows that see it, and no others, become NaN.  (The same lanes hold a row's pieces of both.)
+              asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 2
+              for (int i = 0; i < BK / RPP; ++i) {
+                const uint32_t at = chunk_at(i * RPP + tid / CH, tid % CH, G::HALF);
+                uint32_t y[4], sum = 0;                         // 0 * y: zeros, or NaN where y is not finite
+                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(dst + at) : "memory");
+#pragma unroll
+                for (int k = 0; k < 4; ++k) asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(y[k]), "r"(0u));
+                const unsigned bad = __ballot_sync(0xffffffffu, (sum & 0x7FFF7FFFu) != 0);
+                if (bad >> (lane & ~(CH - 1)) & (CH == 32 ? ~0u : (1u << CH % 32) - 1)) {
+                  const uint32_t zero[4] = {0, 0, 0, 0}, nan[4] = {0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
+                  store16(dst + at, zero);
+                  store16(sk + stage * G::KV_BYTES + at, nan);
+                }
+              }
+              fence_async();
+              mbar_arrive(copied);                              // the keys
+              mbar_arrive(&v_full[stage]);
+              copied = nullptr;
+              continue;
+            }
             if (copied != nullptr) {
               asm volatile("cp.async.wait_group 1;" ::: "memory");
               fence_async();                                    // what the copies wrote is read next by the tensor cores
@@ -695,7 +726,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
           }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-        if (ok) {
+        if (ok && copied != nullptr) {
           fence_async();
           mbar_arrive(copied);
         }

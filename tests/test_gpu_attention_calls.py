@@ -153,3 +153,24 @@ def test_two_streams_at_once():
                 got.append(hbl.hbl_attention(cache, batch, x))                 # (each its own workspace)
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("q_len,group", [(2, 1), (6, 2), (200, 1), (130, 3)])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("back", [1, 2, 40])
+def test_a_value_that_is_not_finite_reaches_only_rows_that_see_it(D, q_len, group, what, back):
+    """bf16 rows: one element of a value among the call's own tokens; the rows before it are as without it."""
+    if back > q_len:
+        back = q_len
+    kv = q_len + 37
+    cache, batch, tables, q = setup(12, [q_len], [kv], 2 * group, 2, D, 16, 16)
+    clean = hbl.hbl_attention(cache, batch, q)
+    n = kv - back
+    cache.v[tables[0][n // 16], 1, n % 16, D // 2 + 3] = what
+    out = hbl.hbl_attention(cache, batch, q)
+    first = q_len - back                                                       # the first token that sees it
+    assert torch.equal(out[:first], clean[:first])
+    assert torch.equal(out[:, :group], clean[:, :group])                       # the other key head
+    assert not torch.isfinite(out[first:, group:, D // 2 + 3]).any()
+    assert hbl.hbl_check_status() == 0
