@@ -381,7 +381,8 @@ typedef enum {
  * in fp32 (each product and sum rounded once, not fused), one rounding to the output type.
  *   x, out       device, fp32 or bf16 (dtype), [tokens, n_heads, head_dim], element strides token_stride and
  *                head_stride (multiples of 8; elements of a head are contiguous), bases 16-byte aligned; out may be x
- *                itself with the same strides, and may not overlap x in any other way
+ *                itself with the same strides, and may not overlap x in any other way; x may be broadcast (strides of
+ *                0), an output of this call or the ones below may not
  *   positions    device int32 [tokens]; one outside [0, n_pos) is reported as HBL_ERR_RANGE and its token is not written
  *   table        from hbl_rope_table, n_pos rows of rot_dim / 2 pairs
  *   head_dim     a multiple of 8, 8..256; rot_dim a multiple of 16, 16..head_dim
@@ -427,7 +428,8 @@ typedef struct {
  *             beyond its first max_q_len are not computed by hbl_attention; a kv_len above max_kv_len costs time only.
  * Lengths are read on the device when the kernels run, so a captured call follows them when it is replayed.
  * A length above max_pages * page_size or 2^30 (the rest is left out), a negative one, or a page outside [0, n_pages) (its
- * tokens are neither written nor read) is reported as HBL_ERR_RANGE.  Several sequences may share pages that no call
+ * tokens are neither written nor read) is reported as HBL_ERR_RANGE. (hbl_attention's results for such a
+ * sequence are then not meaningful, the others' are.)  Several sequences may share pages that no call
  * writes; two tokens of one hbl_kv_append call may not have the same place. */
 typedef struct {
   const int32_t *q_start, *kv_len, *pages, *bos_slot;
@@ -470,8 +472,8 @@ int hbl_kv_read(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, void* 
  * applied in fp32, to the score (keys) and to p (values), and the product is rounded to fp16 against the largest scale.
  * Scores, p's sum and the result are accumulated in fp32.
  * Keys, values and scales that are NaN or infinite reach no row they are masked for; places beyond kv_len are never used,
- * whatever they hold.  A row that sees such a key or value is NaN, at bits 16 perhaps in the value's elements alone; its lse
- * may be NaN, too.
+ * whatever they hold.  A row that sees such a value or scale is NaN, at bits 16 perhaps in the value's elements alone; its
+ * lse may be NaN, too.  So is a row with a score that is NaN or +infinity; a key whose score is -infinity has no weight.
  * workspace: hbl_attention_workspace_bytes, 1024-byte aligned (NULL where that is 0); scratch, nothing in it is kept.
  * Calls that may run at the same time need one each.  out may not overlap q or the cache.
  * n_heads a multiple of n_kv_heads. */

@@ -17,6 +17,13 @@ int check_strided(const void* p, long long token_stride, long long head_stride) 
   if (token_stride < 0 || head_stride < 0) return HBL_ERR_SHAPE;
   return HBL_OK;
 }
+// One that is written: two of its heads may not lie on each other (a broadcast tensor's stride of 0).
+int check_written(const void* p, long long token_stride, long long head_stride, int tokens, int heads, int head_dim) {
+  const int rc = check_strided(p, token_stride, head_stride);
+  if (rc != HBL_OK) return rc;
+  if ((tokens > 1 && token_stride < head_dim) || (heads > 1 && head_stride < head_dim)) return HBL_ERR_SHAPE;
+  return tokens > 1 && heads > 1 && token_stride == head_stride ? HBL_ERR_SHAPE : HBL_OK;
+}
 int check_rotation(const float* table, int n_pos, int rot_dim, int head_dim, int layout) {
   if (layout != HBL_ROPE_HALF && layout != HBL_ROPE_INTERLEAVED) return HBL_ERR_FORMAT;
   if (rot_dim < 16 || rot_dim % 16 != 0 || rot_dim > head_dim || n_pos <= 0) return HBL_ERR_SHAPE;
@@ -157,7 +164,7 @@ int hbl_rope(const hbl_rope_t* a, void* stream) {
   if (a->tokens == 0) return HBL_OK;
   if (!a->x || !a->positions || !a->table || !a->out) return HBL_ERR_NULL;
   if ((rc = check_strided(a->x, a->x_token_stride, a->x_head_stride)) != HBL_OK) return rc;
-  if ((rc = check_strided(a->out, a->out_token_stride, a->out_head_stride)) != HBL_OK) return rc;
+  if ((rc = check_written(a->out, a->out_token_stride, a->out_head_stride, a->tokens, a->n_heads, a->head_dim)) != HBL_OK) return rc;
   if (a->x == a->out && (a->x_token_stride != a->out_token_stride || a->x_head_stride != a->out_head_stride)) return HBL_ERR_SHAPE;
   if (!aligned(a->positions, 4)) return HBL_ERR_ALIGN;
   return launch_rope(a->x, a->dtype, a->tokens, a->n_heads, a->head_dim, a->x_token_stride, a->x_head_stride, a->positions, a->table,
@@ -182,7 +189,7 @@ int hbl_kv_append(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, cons
   if ((rc = check_strided(a->v, a->v_token_stride, a->v_head_stride)) != HBL_OK) return rc;
   if (a->q) {
     if ((rc = check_strided(a->q, a->q_token_stride, a->q_head_stride)) != HBL_OK) return rc;
-    if ((rc = check_strided(a->q_out, a->q_out_token_stride, a->q_out_head_stride)) != HBL_OK) return rc;
+    if ((rc = check_written(a->q_out, a->q_out_token_stride, a->q_out_head_stride, b.tokens, a->n_heads, c.head_dim)) != HBL_OK) return rc;
     if (a->q == a->q_out && (a->q_token_stride != a->q_out_token_stride || a->q_head_stride != a->q_out_head_stride)) return HBL_ERR_SHAPE;
   }
   if (!aligned(a->positions, 4)) return HBL_ERR_ALIGN;
@@ -222,7 +229,7 @@ int hbl_attention(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, cons
   if (nothing(b) || b.max_q_len == 0) return HBL_OK;
   if (!args->q || !args->out) return HBL_ERR_NULL;
   if ((rc = check_strided(args->q, args->q_token_stride, args->q_head_stride)) != HBL_OK) return rc;
-  if ((rc = check_strided(args->out, args->out_token_stride, args->out_head_stride)) != HBL_OK) return rc;
+  if ((rc = check_written(args->out, args->out_token_stride, args->out_head_stride, b.tokens, args->n_heads, c.head_dim)) != HBL_OK) return rc;
   if (!aligned(args->lse, 4)) return HBL_ERR_ALIGN;
   const AttnCall w = plan_attention(c, b, args->n_heads);
   if (w.workspace > 0 && !workspace) return HBL_ERR_NULL;

@@ -1060,10 +1060,12 @@ AttnPlan plan_attention_tiles(const KvView& c, const BatchView& b, int n_heads, 
   if (by_seq < tiles) tiles = by_seq;
   p.tiles = (int)(tiles < 0x7fffffffL ? tiles : 0x7fffffffL);
   const long base = tiles * c.n_kv_heads;
-  // pieces of at least 1024 keys while there are fewer items than SMs
+  // pieces of at least 1024 keys while there are fewer items than SMs, and of at most 2^24 (131072 tiles, some 0.3 s): the
+  // kernel's bounded waits, of 2 s, last as long as an item
   const long want = base > 0 && base < sm_count() ? sm_count() / base : 1;
-  const long most = ((long)b.max_kv_len + 1023) / 1024;
+  const long most = ((long)b.max_kv_len + 1023) / 1024, least = ((long)b.max_kv_len + (1L << 24) - 1) >> 24;
   long n = want < most ? want : most;
+  if (n < least) n = least;
   if (n < 1) n = 1;
   p.chunk = (int)((((long)b.max_kv_len + n - 1) / n + 127) / 128 * 128);
   if (p.chunk < 128) p.chunk = 128;

@@ -212,3 +212,28 @@ def test_binding_refuses_what_is_not_on_the_gpu():
         hbl.KvBatch(z(2, dtype=torch.int32), z(1, dtype=torch.int32), z(1, 1, dtype=torch.int32), tokens=1, max_q_len=1, max_kv_len=1)
     with pytest.raises(ValueError):
         hbl.hbl_rope(z(1, 1, 16, dtype=torch.bfloat16), z(1, dtype=torch.int32), z(1, 8, 2))
+
+
+def test_outputs_whose_heads_lie_on_each_other_are_refused(L):
+    rope = lambda ts, hs, tokens=8, heads=4: L.hbl_rope(bytes(Rope(1024, 1 << 30, 1024, 1024, 0, 0, ts, hs, 1, tokens, heads, 128, 16, 128, 0, 0)), N)
+    assert rope(0, 128) == 2 and rope(512, 0) == 2 and rope(512, 120) == 2 and rope(120, 1024) == 2 and rope(128, 128) == 2
+    assert rope(0, 0, heads=1) == 2 and rope(0, 0, tokens=1) == 2
+    ref = C.byref
+    rot = dict(table=1 << 20, q=1 << 20, q_out=1 << 24)
+    ap = lambda **k: L.hbl_kv_append(ref(cache_t()), ref(batch_t()), append_t(**rot, **k), N)
+    assert ap(q_out_token_stride=0) == 2 and ap(q_out_head_stride=0) == 2 and ap(q_out_head_stride=120) == 2
+    assert ap(q_out_token_stride=512, q_out_head_stride=512) == 2
+    at = lambda **k: L.hbl_attention(ref(cache_t()), ref(batch_t()), attention_t(**k), P, 1 << 40, N)
+    assert at(out_token_stride=0) == 2 and at(out_head_stride=0) == 2 and at(out_head_stride=64) == 2
+    assert at(out_token_stride=512, out_head_stride=512) == 2
+
+
+def test_very_long_sequences_are_split(L):
+    # a piece stays far below what the kernel's bounded waits allow for
+    ref = C.byref
+    cache = cache_t(n_pages=262144, page_size=4096, n_kv_heads=1)
+    need = lambda n: L.hbl_attention_workspace_bytes(ref(cache), ref(batch_t(tokens=65536, max_q_len=65536, n_seqs=1, max_pages=262144, max_kv_len=n)), 4)
+    assert need(1 << 24) == 0
+    for pieces in (2, 64):
+        rows = pieces * 65536 * 4
+        assert need(pieces << 24) == rows * 128 * 4 + rows * 4
