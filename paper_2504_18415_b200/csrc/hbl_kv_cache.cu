@@ -87,25 +87,32 @@ __device__ __forceinline__ bool find_place(const KvView& c, const BatchView& s, 
 }
 
 // BITS 3, 4, 8 or 16; LPH = head_dim / 8 lanes to a head; a thread takes ROWS heads (queries, then keys, then
-// values) of one token.  A thread block works on one token.
-template <int BITS, int LPH, bool INTERLEAVED, int ROWS>
-__global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_constant__ AppendParams p) {
+// values) of one token.  A thread block works on one token.  EVEN: the numbers of heads are multiples of a warp's, so all
+// of a warp's heads are queries, or keys, or values, and what depends on that is decided once for the warp.
+// (Four 2048-token prompts of 96 heads: 8 bits 153 us without, 132 with it, bf16 81 and 72, 3 bits 151 and 148.)
+// Six heads to a thread at 3 and 4 bits: kept to 64 registers (4 bits 137 us; 171 with the 96 that it would take).
+template <int BITS, int LPH, bool INTERLEAVED, int ROWS, bool EVEN>
+__global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int GROUPS = kThreads / LPH;                      // heads side by side in the block
   constexpr int HPW = 32 / LPH;                               // ... and in a warp
   grid_dependency_wait();
   const int t = blockIdx.x / p.blocks_per_token, part = blockIdx.x % p.blocks_per_token;
-  const int lane = threadIdx.x & 31, j = threadIdx.x % LPH, group = threadIdx.x / LPH;
+  const int lane = threadIdx.x & 31, j = threadIdx.x % LPH, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
   const int kvh = p.c.n_kv_heads, first_v = p.n_heads + kvh, rows = first_v + kvh;
-  const __nv_bfloat16 *q = p.q + t * p.q_ts + 8 * j, *k = p.k + t * p.k_ts + 8 * j, *v = p.v + t * p.v_ts + 8 * j;
-  const int r0 = part * (ROWS * GROUPS) + group;              // the thread's rows: r0 + i * GROUPS
+  const __nv_bfloat16 *q = p.q + t * p.q_ts, *k = p.k + t * p.k_ts, *v = p.v + t * p.v_ts;
+  const int first = part * (ROWS * GROUPS) + warp * HPW;      // the warp's rows: first + i * GROUPS + 0 .. HPW - 1
+  const int own = lane / LPH;                                 // which of them is the thread's
+  // A row's number, as far as what it is goes by it; what is left of the thread's own is a multiple of the head's stride.
+  const int r0 = EVEN ? first : first + own, rest = EVEN ? own : 0;
   uint4 raw[ROWS];
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {
     const int r = r0 + i * GROUPS;
     raw[i] = make_uint4(0, 0, 0, 0);
     if (r < rows) {
-      const __nv_bfloat16* src = r < p.n_heads ? q + r * p.q_hs : r < first_v ? k + (r - p.n_heads) * p.k_hs : v + (r - first_v) * p.v_hs;
-      raw[i] = *reinterpret_cast<const uint4*>(src);
+      const long hs = r < p.n_heads ? p.q_hs : r < first_v ? p.k_hs : p.v_hs;
+      const __nv_bfloat16* src = r < p.n_heads ? q + r * hs : r < first_v ? k + (r - p.n_heads) * hs : v + (r - first_v) * hs;
+      raw[i] = *reinterpret_cast<const uint4*>(src + rest * hs + 8 * j);
     }
   }
   Place at;
@@ -145,7 +152,7 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_consta
     top[i] = 0;
     widen8(raw[i], x);
     const bool rotate = turned && r < first_v;
-    if (__any_sync(0xffffffffu, rotate)) {                     // (the whole warp: it shuffles)
+    if (EVEN ? p.table != nullptr && r < first_v : __any_sync(0xffffffffu, rotate)) {      // (the whole warp: it shuffles)
       if constexpr (!INTERLEAVED) {
         uint4 other;
         other.x = __shfl_sync(0xffffffffu, raw[i].x, partner);
@@ -168,26 +175,27 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_consta
       }
     }
     if (r < p.n_heads) {
-      *reinterpret_cast<uint4*>(p.q_out + t * p.qo_ts + r * p.qo_hs + 8 * j) = narrow8(x);
+      *reinterpret_cast<uint4*>(p.q_out + t * p.qo_ts + r * p.qo_hs + (rest * p.qo_hs + 8 * j)) = narrow8(x);
     } else if (BITS == 16 && r < rows) {
       const bool key = r < first_v;
-      const long row = row0 + ((long)(r - (key ? p.n_heads : first_v)) << p.c.page_shift);
+      const long row = row0 + ((long)(r - (key ? p.n_heads : first_v) + rest) << p.c.page_shift);
       *reinterpret_cast<uint4*>((key ? p.c.k : p.c.v) + (row * LPH + j) * 16) = narrow8(x);
     }
-    if (BITS < 16) {
+    if (BITS < 16 && !(EVEN && r < p.n_heads)) {
       // the head's largest magnitude, on the bit patterns: a NaN is larger than everything and is not lost
 #pragma unroll
       for (int e = 0; e < 8; ++e) top[i] = max(top[i], __float_as_uint(x[e]) & 0x7FFFFFFFu);
     }
   }
   if constexpr (BITS < 16) {
-    if (r0 + (ROWS - 1) * GROUPS - (lane / LPH) + HPW - 1 < p.n_heads) return;     // (uniform: the warp has queries only)
+    if (first + (ROWS - 1) * GROUPS + HPW - 1 < p.n_heads) return;     // (uniform: the warp has queries only)
     constexpr float C = (float)((1 << (BITS - 1)) - 1);
     // Both divisions of a head cost what they cost for a whole warp, so the warp's ROWS * HPW heads are put one to a lane
     // and divided together.
     uint32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
+      if (EVEN && first + i * GROUPS < p.n_heads) continue;
 #pragma unroll
       for (int o = LPH / 2; o > 0; o >>= 1) top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
       const uint32_t x = __shfl_sync(0xffffffffu, top[i], (lane % HPW) * LPH);
@@ -197,7 +205,7 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_consta
     const float gamma = finite ? __uint_as_float(mine) : 0.f;
     const float rq_mine = finite ? __fdiv_rn(C, __fadd_rn(gamma, p.eps)) : 0.f;
     if (lane < ROWS * HPW) {
-      const int r = r0 - lane / LPH + lane % HPW + (lane / HPW) * GROUPS;            // this lane's head
+      const int r = first + lane % HPW + (lane / HPW) * GROUPS;                      // this lane's head
       if (r >= p.n_heads && r < rows) {
         const bool key = r < first_v;
         const long row = row0 + ((long)(r - (key ? p.n_heads : first_v)) << p.c.page_shift);
@@ -207,7 +215,8 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_consta
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
       const int r = r0 + i * GROUPS;
-      const float rq = __shfl_sync(0xffffffffu, rq_mine, i * HPW + lane / LPH);
+      if (EVEN && (r < p.n_heads || r >= rows)) continue;
+      const float rq = __shfl_sync(0xffffffffu, rq_mine, i * HPW + own);
       float (&x)[8] = f[BITS == 16 ? 0 : i];
       if (top[i] >= 0x7F800000u) {                             // the head reads as NaN: its codes are those of zero
 #pragma unroll
@@ -215,7 +224,7 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_consta
       }
       const bool store = r >= p.n_heads && r < rows;
       const bool key = r < first_v;
-      const int head = r - (key ? p.n_heads : first_v);
+      const int head = r - (key ? p.n_heads : first_v) + rest;
       const long row = row0 + ((long)head << p.c.page_shift);
       const uint2 u = codes8<BITS>(x, rq);
       unsigned char* dst = (key ? p.c.k : p.c.v) + row * (LPH * BITS);
@@ -315,35 +324,44 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(const __grid_constant
   }
 }
 
-template <int BITS, int LPH, bool INTERLEAVED, int ROWS>
+template <int BITS, int LPH, bool INTERLEAVED, int ROWS, bool EVEN>
 int launch_append_rows(AppendParams& p, cudaStream_t s) {
   const int rows = p.n_heads + 2 * p.c.n_kv_heads, per_block = kThreads / LPH * ROWS;
   p.blocks_per_token = (rows + per_block - 1) / per_block;
   const long blocks = (long)p.b.tokens * p.blocks_per_token;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
-  HBL_CUDA_OK(launch_waiting(kv_append_kernel<BITS, LPH, INTERLEAVED, ROWS>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+  HBL_CUDA_OK(launch_waiting(kv_append_kernel<BITS, LPH, INTERLEAVED, ROWS, EVEN>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
   note_launch();
   return HBL_OK;
 }
 // One head to a thread for a decoding step, whose latency counts.  Where the call fills the GPU several: as many as leave
 // the fewest places of the token's blocks empty (96 heads of 128 elements, 16 to a row of the block: 4 to a thread fill
-// 96 of 128 places, 195 us for four 2048-token prompts; 3 fill all 96 in two blocks, 164; 6 in one, 151).  Among equals
-// the larger number, but at head_dim 256, where 6 run out of registers (341 us instead of 291).
-template <int BITS, int LPH, bool INTERLEAVED>
+// 96 of 128 places, 195 us for four 2048-token prompts at 3 bits; 3 fill all 96 in two blocks, 164; 6 in one, 151).
+// Among equals the larger number, but at head_dim 256, where 6 run out of registers (341 us instead of 291).  Uneven numbers
+// of heads (not EVEN) take 3, within 2 % of the best of the three.
+template <int BITS, int LPH, bool INTERLEAVED, bool EVEN>
 int launch_append_layout(AppendParams& p, cudaStream_t s) {
   const int rows = p.n_heads + 2 * p.c.n_kv_heads, groups = kThreads / LPH;
-  if ((long)p.b.tokens * rows * LPH < (long)sm_count() * 2048 * 4) return launch_append_rows<BITS, LPH, INTERLEAVED, 1>(p, s);
-  auto places = [&](int n) { return (rows + groups * n - 1) / (groups * n) * n; };
-  if (LPH < 32 && places(6) <= places(4) && places(6) <= places(3)) return launch_append_rows<BITS, LPH, INTERLEAVED, LPH < 32 ? 6 : 4>(p, s);
-  if (places(4) <= places(3)) return launch_append_rows<BITS, LPH, INTERLEAVED, 4>(p, s);
-  return launch_append_rows<BITS, LPH, INTERLEAVED, 3>(p, s);
+  if ((long)p.b.tokens * rows * LPH < (long)sm_count() * 2048 * 4) return launch_append_rows<BITS, LPH, INTERLEAVED, 1, EVEN>(p, s);
+  if constexpr (EVEN) {
+    auto places = [&](int n) { return (rows + groups * n - 1) / (groups * n) * n; };
+    if (LPH < 32 && places(6) <= places(4) && places(6) <= places(3)) return launch_append_rows<BITS, LPH, INTERLEAVED, LPH < 32 ? 6 : 4, EVEN>(p, s);
+    if (places(4) <= places(3)) return launch_append_rows<BITS, LPH, INTERLEAVED, 4, EVEN>(p, s);
+  }
+  return launch_append_rows<BITS, LPH, INTERLEAVED, 3, EVEN>(p, s);
+}
+template <int BITS, int LPH>
+int launch_append_heads(AppendParams& p, bool interleaved, cudaStream_t s) {
+  if ((p.n_heads | p.c.n_kv_heads) % (32 / LPH) == 0)
+    return interleaved ? launch_append_layout<BITS, LPH, true, true>(p, s) : launch_append_layout<BITS, LPH, false, true>(p, s);
+  return interleaved ? launch_append_layout<BITS, LPH, true, false>(p, s) : launch_append_layout<BITS, LPH, false, false>(p, s);
 }
 template <int BITS>
 int launch_append_bits(AppendParams& p, bool interleaved, cudaStream_t s) {
   switch (p.c.head_dim) {
-    case 64: return interleaved ? launch_append_layout<BITS, 8, true>(p, s) : launch_append_layout<BITS, 8, false>(p, s);
-    case 128: return interleaved ? launch_append_layout<BITS, 16, true>(p, s) : launch_append_layout<BITS, 16, false>(p, s);
-    case 256: return interleaved ? launch_append_layout<BITS, 32, true>(p, s) : launch_append_layout<BITS, 32, false>(p, s);
+    case 64: return launch_append_heads<BITS, 8>(p, interleaved, s);
+    case 128: return launch_append_heads<BITS, 16>(p, interleaved, s);
+    case 256: return launch_append_heads<BITS, 32>(p, interleaved, s);
     default: return HBL_ERR_SHAPE;
   }
 }
