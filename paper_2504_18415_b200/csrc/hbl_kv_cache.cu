@@ -56,7 +56,7 @@ struct AppendParams {
   const float4* table;
   const int32_t* positions;
   int* status;
-  int n_heads, n_pos, rot_dim, blocks_per_token;               // n_heads 0: no queries
+  int n_heads, n_pos, rot_dim, blocks_per_token, groups;       // n_heads 0: no queries; groups: heads side by side in a block
   float eps;
 };
 
@@ -93,21 +93,21 @@ __device__ __forceinline__ bool find_place(const KvView& c, const BatchView& s, 
 // Six heads to a thread at 3 and 4 bits: kept to 64 registers (4 bits 137 us; 171 with the 96 that it would take).
 template <int BITS, int LPH, bool INTERLEAVED, int ROWS, bool EVEN>
 __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_append_kernel(const __grid_constant__ AppendParams p) {
-  constexpr int GROUPS = kThreads / LPH;                      // heads side by side in the block
-  constexpr int HPW = 32 / LPH;                               // ... and in a warp
+  constexpr int HPW = 32 / LPH;                               // heads side by side in a warp
+  const int groups = p.groups;                                // ... and in the block
   grid_dependency_wait();
   const int t = blockIdx.x / p.blocks_per_token, part = blockIdx.x % p.blocks_per_token;
   const int lane = threadIdx.x & 31, j = threadIdx.x % LPH, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
   const int kvh = p.c.n_kv_heads, first_v = p.n_heads + kvh, rows = first_v + kvh;
   const __nv_bfloat16 *q = p.q + t * p.q_ts, *k = p.k + t * p.k_ts, *v = p.v + t * p.v_ts;
-  const int first = part * (ROWS * GROUPS) + warp * HPW;      // the warp's rows: first + i * GROUPS + 0 .. HPW - 1
+  const int first = part * (ROWS * groups) + warp * HPW;      // the warp's rows: first + i * groups + 0 .. HPW - 1
   const int own = lane / LPH;                                 // which of them is the thread's
   // A row's number, as far as what it is goes by it; what is left of the thread's own is a multiple of the head's stride.
   const int r0 = EVEN ? first : first + own, rest = EVEN ? own : 0;
   uint4 raw[ROWS];
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {
-    const int r = r0 + i * GROUPS;
+    const int r = r0 + i * groups;
     raw[i] = make_uint4(0, 0, 0, 0);
     if (r < rows) {
       const long hs = r < p.n_heads ? p.q_hs : r < first_v ? p.k_hs : p.v_hs;
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_ap
   uint32_t top[ROWS];
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {
-    const int r = r0 + i * GROUPS;
+    const int r = r0 + i * groups;
     float (&x)[8] = f[BITS == 16 ? 0 : i];
     top[i] = 0;
     widen8(raw[i], x);
@@ -188,14 +188,14 @@ __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_ap
     }
   }
   if constexpr (BITS < 16) {
-    if (first + (ROWS - 1) * GROUPS + HPW - 1 < p.n_heads) return;     // (uniform: the warp has queries only)
+    if (first + (ROWS - 1) * groups + HPW - 1 < p.n_heads) return;     // (uniform: the warp has queries only)
     constexpr float C = (float)((1 << (BITS - 1)) - 1);
     // Both divisions of a head cost what they cost for a whole warp, so the warp's ROWS * HPW heads are put one to a lane
     // and divided together.
     uint32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-      if (EVEN && first + i * GROUPS < p.n_heads) continue;
+      if (EVEN && first + i * groups < p.n_heads) continue;
 #pragma unroll
       for (int o = LPH / 2; o > 0; o >>= 1) top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
       const uint32_t x = __shfl_sync(0xffffffffu, top[i], (lane % HPW) * LPH);
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_ap
     const float gamma = finite ? __uint_as_float(mine) : 0.f;
     const float rq_mine = finite ? __fdiv_rn(C, __fadd_rn(gamma, p.eps)) : 0.f;
     if (lane < ROWS * HPW) {
-      const int r = first + lane % HPW + (lane / HPW) * GROUPS;                      // this lane's head
+      const int r = first + lane % HPW + (lane / HPW) * groups;                      // this lane's head
       if (r >= p.n_heads && r < rows) {
         const bool key = r < first_v;
         const long row = row0 + ((long)(r - (key ? p.n_heads : first_v)) << p.c.page_shift);
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_ap
     }
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-      const int r = r0 + i * GROUPS;
+      const int r = r0 + i * groups;
       if (EVEN && (r < p.n_heads || r >= rows)) continue;
       const float rq = __shfl_sync(0xffffffffu, rq_mine, i * HPW + own);
       float (&x)[8] = f[BITS == 16 ? 0 : i];
@@ -258,13 +258,12 @@ struct ReadParams {
   BatchView b;
   uint4 *k_out, *v_out;
   int* status;
-  int blocks_per_token;
+  int blocks_per_token, groups;
 };
 
 // A thread takes ROWS heads (keys, then values) of one token; a thread block works on one token.
 template <int BITS, int LPH, int ROWS>
 __global__ void __launch_bounds__(kThreads) kv_read_kernel(const __grid_constant__ ReadParams p) {
-  constexpr int GROUPS = kThreads / LPH;
   grid_dependency_wait();
   const int t = blockIdx.x / p.blocks_per_token, part = blockIdx.x % p.blocks_per_token;
   const int lane = threadIdx.x & 31, j = threadIdx.x % LPH, group = threadIdx.x / LPH, kvh = p.c.n_kv_heads;
@@ -276,7 +275,7 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(const __grid_constant
   float scale[ROWS];
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {
-    const int r = (part * ROWS + i) * GROUPS + group;
+    const int r = (part * ROWS + i) * p.groups + group;
     u[i] = make_uint2(0, 0);
     whole[i] = make_uint4(0, 0, 0, 0);
     scale[i] = 0.f;
@@ -303,7 +302,7 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(const __grid_constant
   }
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {
-    const int r = (part * ROWS + i) * GROUPS + group;
+    const int r = (part * ROWS + i) * p.groups + group;
     if (r >= 2 * kvh) continue;
     uint4 o = whole[i];
     if constexpr (BITS < 16) {
@@ -324,31 +323,36 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(const __grid_constant
   }
 }
 
+// Blocks to a token and heads side by side in a block, so that as few as can be of a token's places stay empty.  (Blocks of
+// 256 threads whatever the heads: sixteen 2048-token prompts of 16 and 2 heads 232 us instead of 106.)
+struct Deal { int blocks, groups; };
+Deal deal(int rows, int lph, int rows_per_thread) {
+  const int most = kThreads / lph, warp = 32 / lph;
+  Deal d;
+  d.blocks = (rows + rows_per_thread * most - 1) / (rows_per_thread * most);
+  const int need = (rows + rows_per_thread * d.blocks - 1) / (rows_per_thread * d.blocks);
+  d.groups = (need + warp - 1) / warp * warp;
+  return d;
+}
 template <int BITS, int LPH, bool INTERLEAVED, int ROWS, bool EVEN>
 int launch_append_rows(AppendParams& p, cudaStream_t s) {
-  const int rows = p.n_heads + 2 * p.c.n_kv_heads, per_block = kThreads / LPH * ROWS;
-  p.blocks_per_token = (rows + per_block - 1) / per_block;
-  const long blocks = (long)p.b.tokens * p.blocks_per_token;
+  const Deal d = deal(p.n_heads + 2 * p.c.n_kv_heads, LPH, ROWS);
+  p.blocks_per_token = d.blocks;
+  p.groups = d.groups;
+  const long blocks = (long)p.b.tokens * d.blocks;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
-  HBL_CUDA_OK(launch_waiting(kv_append_kernel<BITS, LPH, INTERLEAVED, ROWS, EVEN>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+  HBL_CUDA_OK(launch_waiting(kv_append_kernel<BITS, LPH, INTERLEAVED, ROWS, EVEN>, dim3((unsigned)blocks), dim3(d.groups * LPH), 0, s, p));
   note_launch();
   return HBL_OK;
 }
-// One head to a thread for a decoding step, whose latency counts.  Where the call fills the GPU several: as many as leave
-// the fewest places of the token's blocks empty (96 heads of 128 elements, 16 to a row of the block: 4 to a thread fill
-// 96 of 128 places, 195 us for four 2048-token prompts at 3 bits; 3 fill all 96 in two blocks, 164; 6 in one, 151).
-// Among equals the larger number, but at head_dim 256, where 6 run out of registers (341 us instead of 291).  Uneven numbers
-// of heads (not EVEN) take 3, within 2 % of the best of the three.
+// One head to a thread for a decoding step, whose latency counts.  Where the call fills the GPU six (four 2048-token prompts
+// of 96 heads at 3 bits: 148 us; four or three heads 163, two 180; 48 heads 64, 71, 70, 75), or four at head_dim 256, where six
+// run out of registers (341 us against 291).
 template <int BITS, int LPH, bool INTERLEAVED, bool EVEN>
 int launch_append_layout(AppendParams& p, cudaStream_t s) {
-  const int rows = p.n_heads + 2 * p.c.n_kv_heads, groups = kThreads / LPH;
-  if ((long)p.b.tokens * rows * LPH < (long)sm_count() * 2048 * 4) return launch_append_rows<BITS, LPH, INTERLEAVED, 1, EVEN>(p, s);
-  if constexpr (EVEN) {
-    auto places = [&](int n) { return (rows + groups * n - 1) / (groups * n) * n; };
-    if (LPH < 32 && places(6) <= places(4) && places(6) <= places(3)) return launch_append_rows<BITS, LPH, INTERLEAVED, LPH < 32 ? 6 : 4, EVEN>(p, s);
-    if (places(4) <= places(3)) return launch_append_rows<BITS, LPH, INTERLEAVED, 4, EVEN>(p, s);
-  }
-  return launch_append_rows<BITS, LPH, INTERLEAVED, 3, EVEN>(p, s);
+  if ((long)p.b.tokens * (p.n_heads + 2 * p.c.n_kv_heads) * LPH < (long)sm_count() * 2048 * 4)
+    return launch_append_rows<BITS, LPH, INTERLEAVED, 1, EVEN>(p, s);
+  return launch_append_rows<BITS, LPH, INTERLEAVED, LPH < 32 ? 6 : 4, EVEN>(p, s);
 }
 template <int BITS, int LPH>
 int launch_append_heads(AppendParams& p, bool interleaved, cudaStream_t s) {
@@ -368,11 +372,12 @@ int launch_append_bits(AppendParams& p, bool interleaved, cudaStream_t s) {
 
 template <int BITS, int LPH, int ROWS>
 int launch_read_rows(ReadParams& p, cudaStream_t s) {
-  const int per_block = kThreads / LPH * ROWS;
-  p.blocks_per_token = (2 * p.c.n_kv_heads + per_block - 1) / per_block;
-  const long blocks = (long)p.b.tokens * p.blocks_per_token;
+  const Deal d = deal(2 * p.c.n_kv_heads, LPH, ROWS);
+  p.blocks_per_token = d.blocks;
+  p.groups = d.groups;
+  const long blocks = (long)p.b.tokens * d.blocks;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
-  HBL_CUDA_OK(launch_waiting(kv_read_kernel<BITS, LPH, ROWS>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+  HBL_CUDA_OK(launch_waiting(kv_read_kernel<BITS, LPH, ROWS>, dim3((unsigned)blocks), dim3(d.groups * LPH), 0, s, p));
   note_launch();
   return HBL_OK;
 }
