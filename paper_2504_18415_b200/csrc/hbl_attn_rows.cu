@@ -51,8 +51,11 @@ struct Step {
   float ks[2], vs[2];
 };
 
+// Thread blocks on an SM: what the registers of a block's accumulators and steps in flight leave.
+constexpr int blocks_per_sm(int bits, int d, int nt) { return d > 128 ? 2 : nt == 1 ? 4 : bits < 16 ? 3 : 2; }
+
 template <int BITS, int D, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 4 : 2) attn_rows_kernel(const __grid_constant__ RowsParams p) {
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_rows_kernel(const __grid_constant__ RowsParams p) {
   using G = Geo<BITS, D>;
   constexpr int ROWS = 8 * NT;
   constexpr int MT = D / 16;                                  // 16-element tiles of the output
@@ -612,6 +615,39 @@ int launch_rows_bits(RowsParams& p, cudaStream_t s) {
   }
 }
 
+// How many pieces the keys of a sequence are dealt in.
+//   None up to 512 keys, where the second launch costs more than the shorter loops save (4 x 509 tokens: 14.8 us in two
+// pieces, 12.7 in one; 4 x 1000: 16.8, 17.3), and none of less than 256 keys.
+//   Few sequences: as many pieces as there is room for at once; with one more the last waits for a whole round (16 rows
+// over 16384 tokens at 8 bits: 65 us in 13 pieces, 85 in 14).
+//   As many as there is room for, or more: whole (32 x 4096 tokens of 32 key heads at 8 bits, 16 rows each: 208 us, in two
+// pieces 243; ragged with one row 113, 116).
+//   In between the host, which does not know the lengths, weighs two batches: every sequence as long as the bound says
+// (whole rounds of resident blocks; a round that is not full costs half of one and its part of the other half), and
+// lengths anywhere below it (the work, evenly spread, and half of a last piece), which is what it mostly is, so that it
+// counts twice.  A block costs as much as `fixed` keys before its first and after its last one (64 x 4096 tokens at 4 bits
+// in 1, 2, 4, 8 pieces: 275, 300, 350, 452 us).  64 ragged sequences of up to 16384 tokens, 8 key heads, 4 bits: 254 us in 1
+// piece, 198 in 2, 172 in 4, 174 in 8, 200 in 16.
+long pieces_of_keys(long base, int resident, long keys, long most, int bits) {
+  const long slots = (long)sm_count() * resident;
+  if (base <= 0 || most <= 1 || base >= slots) return 1;
+  if (8 * base <= slots) return slots / base < most ? slots / base : most;
+  const float fixed = bits == 16 ? 300.f : 600.f, load = (float)base / (float)slots;
+  long best = 1;
+  float least = 0.f;
+  for (long n = 1; n <= most && n <= 16; ++n) {
+    const long on_sm = (n * base + sm_count() - 1) / sm_count(), rest = on_sm % resident;
+    const float piece = (float)keys / (float)n + fixed;
+    const float even = ((float)(on_sm / resident) + (rest > 0 ? 0.5f + 0.5f * (float)rest / (float)resident : 0.f)) * piece;
+    const float uneven = load * 0.5f * ((float)keys + fixed * (float)(n + 1)) + 0.5f * piece;
+    if (n == 1 || even + 2.f * uneven < least) {
+      best = n;
+      least = even + 2.f * uneven;
+    }
+  }
+  return best;
+}
+
 }  // namespace
 
 AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads, int few) {
@@ -620,12 +656,8 @@ AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads, i
   p.cap = (int)most_rows(b, group, few);
   p.tiles = (p.cap + rows - 1) / rows;
   const long base = (long)b.n_seqs * c.n_kv_heads * p.tiles;
-  // pieces of at least 256 keys, as many as keep four thread blocks on every SM; none up to 512 keys, where the second
-  // launch costs more than the shorter loops save (4 x 509 tokens: 14.8 us in two pieces, 12.7 in one; 4 x 1000: 16.8, 17.3)
-  const long want = base > 0 ? ((long)sm_count() * 4 + base - 1) / base : 1;
   const long most = b.max_kv_len <= 512 ? 1 : ((long)b.max_kv_len + 255) / 256;
-  const long splits = want < most ? want : most;
-  const long n = splits < 1 ? 1 : splits;
+  const long n = pieces_of_keys(base, blocks_per_sm(c.bits, c.head_dim, rows / 8), b.max_kv_len, most, c.bits);
   p.chunk = (int)((((long)b.max_kv_len + n - 1) / n + 63) / 64 * 64);
   if (p.chunk < 64) p.chunk = 64;
   p.splits = (int)(((long)b.max_kv_len + p.chunk - 1) / p.chunk);
