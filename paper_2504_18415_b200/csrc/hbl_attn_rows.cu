@@ -6,7 +6,9 @@
 // the queries once a row is scaled by a power of two; p_j vs_j is rounded to fp16 against a running power of two above
 // the value scales.  These roundings are what the tensor core's operands cost; p's sum is taken before them, in fp32.
 //
-// Bound by the cache's bytes: every code is read once per 8 (16) query rows of its key head.  A thread block takes one
+// The cache is read once per 8 (16) query rows of its key head.  bf16 is bound by that (one sequence of 131072 tokens: 95 us,
+// 5.7 TB/s; 64 ragged ones of up to 4096 tokens 364), codes by logic operations and issue (64 x 4096 tokens of 32 key heads, one row:
+// 4 bits 275 us, 4.3 TB/s; ragged 175).  A thread block takes one
 // (sequence, key head, row tile, piece of the keys), its four warps take 16 keys in turn and meet only at the end, so there
 // is no barrier in the loop.  The keys are the M side of both products (S^T = K q^T, O^T = V^T P^T): 16 keys against 8
 // rows, no half-empty tile, and a lane's operand registers are exactly the bytes that it loads from the cache
@@ -32,7 +34,27 @@ struct RowsParams {
   float* part_lse;               // [splits][n_seqs * n_kv_heads * cap], log2 units
   int* status;
   int few;                       // sequences of more rows than this are another kernel's
+  int ordered;                   // long sequences first
 };
+
+// The t-th sequence of the batch in falling order of their lengths' quarter of the longest.  The whole warp asks for the
+// same t.  A batch of several rounds of blocks ends sooner when the long ones do not come last.
+__device__ __forceinline__ int sequence_by_length(const BatchView& s, int t, int lane) {
+  int most = 0;
+  for (int b0 = 0; b0 < s.n_seqs; b0 += 32)
+    if (b0 + lane < s.n_seqs) most = max(most, __ldg(s.kv_len + b0 + lane));
+  most = __reduce_max_sync(0xffffffffu, most);
+  const int step = most / 4 + 1;                               // lengths / step: 0 .. 3
+  for (int quarter = 3; quarter >= 0; --quarter)
+    for (int b0 = 0; b0 < s.n_seqs; b0 += 32) {
+      const bool mine = b0 + lane < s.n_seqs && max(__ldg(s.kv_len + min(b0 + lane, s.n_seqs - 1)), 0) / step == quarter;
+      const unsigned hits = __ballot_sync(0xffffffffu, mine);
+      const int n = __popc(hits);
+      if (t < n) return b0 + __ffs(__ballot_sync(0xffffffffu, mine && __popc(hits & ((1u << lane) - 1)) == t)) - 1;
+      t -= n;
+    }
+  return 0;                                                    // (not reached: every sequence is in one quarter)
+}
 
 template <int BITS, int D>
 struct Geo {
@@ -69,7 +91,9 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
   int id = blockIdx.x;
   const int split = id % p.p.splits; id /= p.p.splits;
   const int tile = id % p.p.tiles; id /= p.p.tiles;
-  const int head = id % p.c.n_kv_heads, b = id / p.c.n_kv_heads;
+  const int head = id % p.c.n_kv_heads;
+  int b = id / p.c.n_kv_heads;
+  if (p.ordered) b = sequence_by_length(p.b, b, lane);
   SeqLens len;
   if (!sequence_lengths(p.b, b, p.c.page_shift, p.status, len)) return;
   const int group = p.a.group;
@@ -669,6 +693,11 @@ int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a
                           cudaStream_t s) {
   RowsParams p{};
   p.c = c; p.b = b; p.a = a; p.p = plan; p.few = few; p.part_o = w.rows_o; p.part_lse = w.rows_lse;
+  // More blocks than fit at once, of whole sequences: the long ones first (64 ragged sequences of up to 4096 tokens at 4 bits
+  // 190 us in the batch's order, 175 in this; 128 of 8 key heads 113, 92; all of one length 275, 278).  Not for short ones, whose
+  // blocks would spend more on the look-up than it saves (up to 600 tokens: 59 us, 64), nor for batches whose look-up is long.
+  const long slots = (long)sm_count() * blocks_per_sm(c.bits, c.head_dim, rows_per_tile(b, a.group, few) / 8);
+  p.ordered = plan.splits == 1 && b.max_kv_len >= 1024 && b.n_seqs <= 128 && (long)b.n_seqs * c.n_kv_heads * plan.tiles > slots;
   p.status = device_status_word();
   if (p.status == nullptr) return HBL_ERR_CUDA;
   switch (c.bits) {

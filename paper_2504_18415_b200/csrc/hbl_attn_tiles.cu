@@ -14,7 +14,9 @@
 //                    (exactly) on the way; values beyond the sequence become zeros, whatever the cache holds there
 //   warp 12          issues the matrix instructions;  warps 13, 14: the queries into shared memory;  warp 15: looks up the items
 // The two sub-tiles alternate on the tensor core: while one's scores are being exponentiated the other's products run.
-// Bound by the tensor core and the exponential unit alike at head_dim 128 (256 x 128 scores: 2048 cycles each).
+// Bound by the tensor core and the exponential unit alike at head_dim 128 (256 x 128 scores: 2048 cycles each); a tile takes
+// some 3300 (8192-token prompt of 32 heads 490 us, 1120 TFLOP/s while the clock holds; 4096 of 16 heads 72 us, 950).  Over
+// codes some 5500, because the widening takes the producers as long (512 queries over 16384 tokens at 8 bits 220 us).
 //
 // The order of the elements inside each group of 8 of a head is free for Q K^T as long as Q and K agree, and for V it only
 // names the columns of O: codes are widened in the order that takes least work (hbl_attn_frag.cuh, `pairs`), the

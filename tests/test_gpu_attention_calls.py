@@ -174,3 +174,34 @@ def test_a_value_that_is_not_finite_reaches_only_rows_that_see_it(D, q_len, grou
     assert torch.equal(out[:, :group], clean[:, :group])                       # the other key head
     assert not torch.isfinite(out[first:, group:, D // 2 + 3]).any()
     assert hbl.hbl_check_status() == 0
+
+
+@pytest.mark.parametrize("bits", [3, 4, 8, 16])
+@pytest.mark.parametrize("n,q", [(40, 1), (65, 2), (128, 1), (70, 40)])
+def test_batches_of_several_rounds_whatever_the_order_of_their_lengths(bits, n, q):
+    """More blocks than fit on the GPU at once: long sequences are taken first, and each exactly once."""
+    rnd = torch.Generator().manual_seed(n)
+    kv_lens = torch.randint(1, 1500, (n,), generator=rnd).tolist()
+    kv_lens[3], kv_lens[n - 1], kv_lens[n // 2], kv_lens[7] = 0, 1500, 1500, 1
+    q_lens = [q if i % 9 == 2 else 0 if i % 11 == 5 else 1 for i in range(n)]
+    q_lens[3] = 0
+    kv_lens = [max(a, b) for a, b in zip(q_lens, kv_lens)]
+    cache, batch, tables, x = setup(n + bits, q_lens, kv_lens, 32, 16, 64, bits, 64, slots=bits < 8, extra=2)
+    check_attention(cache, batch, tables, q_lens, kv_lens, x, slots=list(range(n)) if bits < 8 else None)
+
+
+def test_a_length_that_makes_no_sense_harms_no_other_sequence():
+    n, kv_lens = 64, [(1100, 40, 700, 1300)[i % 4] for i in range(64)]
+    cache, batch, tables, q = setup(9, [1] * n, kv_lens, 16, 16, 64, 4, 64)
+    good = hbl.hbl_attention(cache, batch, q)
+    batch.kv_len[5], batch.kv_len[40] = -3, -2 ** 31
+    out = hbl.hbl_attention(cache, batch, q)
+    assert hbl.hbl_check_status() == 12
+    keep = [i for i in range(n) if i not in (5, 40)]
+    assert torch.equal(out[keep], good[keep])
+    batch.kv_len[5] = 2 ** 31 - 1                               # beyond its pages: what it has is used, and it is reported
+    batch.kv_len[40] = kv_lens[40]
+    out = hbl.hbl_attention(cache, batch, q)
+    assert hbl.hbl_check_status() == 12
+    keep = [i for i in range(n) if i != 5]
+    assert torch.equal(out[keep], good[keep])
