@@ -961,6 +961,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
       for (uint32_t n = 0; ok; ++n) {
         if (decode_item<D>(p, item, lane, w)) {
           give(w);
+          // (a long wait, which the softmax warp beside this one should not notice)
+          for (int i = 0; ok && i < 1000000 && !mbar_try(&near_end, (made - 1) & 1) && !*abort_flag; ++i) __nanosleep(500);
           if (!ok || !(ok = __all_sync(0xffffffffu, mbar_wait<true>(&near_end, (made - 1) & 1, abort_flag, p.status)))) break;
         }
         if (lane == 0) {
