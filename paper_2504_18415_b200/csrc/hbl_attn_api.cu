@@ -250,7 +250,7 @@ int hbl_attention(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, cons
                            reinterpret_cast<float*>(ws + w.tiles_lse)};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (w.use_tiles && (rc = launch_attention_tiles(c, b, a, w.tiles, w.few_tiles, parts, s)) != HBL_OK) return rc;
-  if (w.use_rows && (rc = launch_attention_rows(c, b, a, w.rows, w.few_rows, parts, s)) != HBL_OK) return rc;
+  if (w.use_rows && (rc = launch_attention_rows(c, b, a, w.rows, w.few_rows, parts, w.use_tiles, s)) != HBL_OK) return rc;
   if (w.workspace > 0) return launch_attention_combine(c, b, a, w.rows, w.tiles, w.few_tiles, parts, s);
   return HBL_OK;
 }

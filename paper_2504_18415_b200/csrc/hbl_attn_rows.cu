@@ -35,6 +35,7 @@ struct RowsParams {
   int* status;
   int few;                       // sequences of more rows than this are another kernel's
   int ordered;                   // long sequences first
+  int beside_tiles;              // launched behind the call's other kernel, of which it needs nothing
 };
 
 // The t-th sequence of the batch in falling order of their lengths' quarter of the longest.  The whole warp asks for the
@@ -86,7 +87,11 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
   __shared__ float sqs[ROWS];
   __shared__ float so[ROWS][D + 4];
   __shared__ float sm[kWarps][ROWS], sl[kWarps][ROWS];
-  grid_dependency_wait();
+  // Behind the tiles this kernel begins when all their blocks have, so what came before the call is complete already; it
+  // takes the SMs that they leave.  It may not be complete before they are, as what is launched next waits for this
+  // kernel alone: its last block waits for them.
+  const bool last = p.beside_tiles && blockIdx.x == gridDim.x - 1;
+  if (!p.beside_tiles) grid_dependency_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   int id = blockIdx.x;
   const int split = id % p.p.splits; id /= p.p.splits;
@@ -95,15 +100,17 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
   int b = id / p.c.n_kv_heads;
   if (p.ordered) b = sequence_by_length(p.b, b, lane);
   SeqLens len;
-  if (!sequence_lengths(p.b, b, p.c.page_shift, p.status, len)) return;
+  const bool sane = sequence_lengths(p.b, b, p.c.page_shift, p.status, len);
   const int group = p.a.group;
   const int n_rows = min(len.q_len, p.b.max_q_len) * group, r0 = tile * ROWS;
-  if (r0 >= n_rows || n_rows > p.few) return;
+  if (!sane || r0 >= n_rows || n_rows > p.few || (split > 0 && (long)split * p.p.chunk >= len.held)) {      // (no such piece: the combine step knows)
+    if (last) grid_dependency_wait();
+    return;
+  }
   const int last_tok = min(r0 + ROWS - 1, n_rows - 1) / group;
   // keys any row of the tile sees, and the piece of them that is this block's (the last piece takes what is left)
   const int seen = p.a.causal ? max(0, min(len.held, len.kv - len.q_len + last_tok + 1)) : len.held;
   const int key0 = split * p.p.chunk;
-  if (split > 0 && (long)split * p.p.chunk >= len.held) return;      // no such piece in this sequence: the combine step knows
   int key1 = split == p.p.splits - 1 ? seen : min(seen, key0 + p.p.chunk);
 
   // ---- queries as B fragments: row n = g of tile nt, its pairs in the order the keys' units have.  For codes they are
@@ -499,6 +506,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
       if (d == 0 && p.a.lse != nullptr) p.a.lse[(long)tok * p.a.n_heads + hq] = lse2 * 0.6931471805599453f;
     }
   }
+  if (last) grid_dependency_wait();
 }
 
 // The pieces of a row together (whichever kernel computed them): out = sum_s 2^(lse_s - top) o_s / sum_s 2^(lse_s - top).
@@ -690,9 +698,10 @@ AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads, i
 }
 
 int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& plan, int few, const AttnParts& w,
-                          cudaStream_t s) {
+                          bool beside_tiles, cudaStream_t s) {
   RowsParams p{};
   p.c = c; p.b = b; p.a = a; p.p = plan; p.few = few; p.part_o = w.rows_o; p.part_lse = w.rows_lse;
+  p.beside_tiles = beside_tiles;
   // More blocks than fit at once, of whole sequences: the long ones first (64 ragged sequences of up to 4096 tokens at 4 bits
   // 190 us in the batch's order, 175 in this; 128 of 8 key heads 113, 92; all of one length 275, 278).  Not for short ones, whose
   // blocks would spend more on the look-up than it saves (up to 600 tokens: 59 us, 64), nor for batches whose look-up is long.

@@ -165,6 +165,7 @@ struct TilesParams {
   float* part_o;
   float* part_lse;
   int* status;
+  int rows_follow;               // the call's next launch is the other kernel, which reads nothing of this one's
   int items, few;                // sequences of up to `few` rows are another kernel's (0: none)
   uint32_t div_mul;              // r / group = (umulhi(r, div_mul) + r) >> div_shift for 0 <= r < 2^31
   int div_shift;
@@ -316,6 +317,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   grid_dependency_wait();
+  if (p.rows_follow) grid_launch_dependents();                 // what came before is complete: the other kernel may begin
   // The n-th item of this block, from the warp that looks them up (all lanes of the calling warp; false: gave up).
   auto next_item = [&](uint32_t n, Item& w) {
     const bool ok = __all_sync(0xffffffffu, mbar_wait(&item_full[n & 1], (n >> 1) & 1, abort_flag, p.status));
@@ -1093,7 +1095,7 @@ AttnPlan plan_attention_tiles(const KvView& c, const BatchView& b, int n_heads, 
 int launch_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& plan, int few, const AttnParts& w,
                            cudaStream_t s) {
   TilesParams p{};
-  p.c = c; p.b = b; p.a = a; p.p = plan; p.few = few; p.part_o = w.tiles_o; p.part_lse = w.tiles_lse;
+  p.c = c; p.b = b; p.a = a; p.p = plan; p.few = few; p.part_o = w.tiles_o; p.part_lse = w.tiles_lse; p.rows_follow = few > 0;
   p.status = device_status_word();
   if (p.status == nullptr) return HBL_ERR_CUDA;
   const long items = (long)plan.tiles * c.n_kv_heads * plan.splits;

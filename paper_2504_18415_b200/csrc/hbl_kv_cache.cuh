@@ -89,7 +89,7 @@ struct AttnParts { float *rows_o, *rows_lse, *tiles_o, *tiles_lse; };      // [s
 AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads, int few);
 AttnPlan plan_attention_tiles(const KvView& c, const BatchView& b, int n_heads, int few);
 int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, int few, const AttnParts& w,
-                          cudaStream_t s);
+                          bool beside_tiles, cudaStream_t s);
 int launch_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, int few, const AttnParts& w,
                            cudaStream_t s);
 int launch_attention_combine(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& rows, const AttnPlan& tiles,

@@ -205,3 +205,39 @@ def test_a_length_that_makes_no_sense_harms_no_other_sequence():
     assert hbl.hbl_check_status() == 12
     keep = [i for i in range(n) if i != 5]
     assert torch.equal(out[keep], good[keep])
+
+
+@pytest.mark.parametrize("q_lens,kv_lens", [([500, 1, 0, 1], [500, 20, 3, 1]), ([600, 1, 1, 2], [9000, 40, 30, 20]), ([1, 2, 600], [60, 50, 600])])
+@pytest.mark.parametrize("bits", [4, 16])
+@pytest.mark.parametrize("graph", [False, True])
+def test_a_call_of_both_kernels_is_complete_for_what_comes_next(q_lens, kv_lens, bits, graph):
+    """The short sequences' kernel runs beside the long ones' and is done long before it; the next launch needs both."""
+    cache, batch, tables, q = setup(5, q_lens, kv_lens, 8, 8, 128, bits, 64)
+    n = sum(q_lens)
+    table = hbl.hbl_rope_table([0.0] * 64, 1)                   # angle 0: the next launch of the library copies
+    at = torch.zeros(n, dtype=torch.int32, device="cuda")
+    want, _ = check_attention(cache, batch, tables, q_lens, kv_lens, q)
+    size = hbl.hbl_attention_workspace_bytes(cache, batch, 8)
+    ws = hbl.new_workspace(size, q.device) if size else None
+    outs = [torch.empty_like(q) for _ in range(8)]
+    copies, others = [torch.empty_like(q) for _ in range(8)], [torch.empty_like(q) for _ in range(8)]
+
+    def run():
+        for o, c, x in zip(outs, copies, others):
+            o.zero_()
+            hbl.hbl_attention(cache, batch, q, out=o, workspace=ws)
+            hbl.hbl_rope(o, at, table, out=c)
+            x.copy_(o)
+
+    run()
+    if graph:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run()
+    for _ in range(5):
+        for x in copies + others:
+            x.fill_(3.0)
+        g.replay() if graph else run()
+        for x in copies + others:
+            assert torch.equal(x, want)
+    assert hbl.hbl_check_status() == 0
