@@ -102,7 +102,7 @@ inline cudaError_t launch_dependent(void (*kern)(KArgs...), dim3 grid, dim3 bloc
   set_stream_unflushed(s, false);
   return e;
 }
-// For kernels that call grid_dependency_wait() before they touch memory.
+// For kernels that call grid_dependency_wait() before they touch memory (or begin behind one that has, and is released by it).
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_waiting(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args... args) {
   cudaLaunchConfig_t cfg = {};
