@@ -528,6 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
               }
             }
           }
+          __syncwarp();                                         // every lane has read the stage's marks: lane 0 speaks for all
           if (lane == 0) mbar_arrive(&k_empty[stage]);
         }
       }
