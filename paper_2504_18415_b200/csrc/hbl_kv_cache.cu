@@ -9,8 +9,8 @@
 // dependent loads (sequence -> length -> page -> row).  A lane owns 8 consecutive elements of a head, so a head
 // is head_dim / 8 lanes and its maximum takes three to five shuffles; the partner of a rotated element lies in the same
 // lane (interleaved layout) or one shuffle away (half layout).  A thread takes ROWS heads of the same token: the table's
-// pairs are loaded once for all of them, and their loads are in flight together.  The loads of the data do not depend on
-// that chain and are issued before it.
+// pairs are loaded once for all of them, and their loads are in flight together.  The loads of the data depend on the
+// number of rows that there are, but not on that chain, and are issued before it.
 #include "hbl_kv_cache.cuh"
 
 namespace hbl {
@@ -99,6 +99,7 @@ __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_ap
   const int groups = p.groups;                                // ... and in the block
   grid_dependency_wait();
   const int t = blockIdx.x / p.blocks_per_token, part = blockIdx.x % p.blocks_per_token;
+  const bool there = t < __ldg(p.b.q_start + p.b.n_seqs);     // behind the last sequence the tensors need not have the row
   const int lane = threadIdx.x & 31, j = threadIdx.x % LPH, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
   const int kvh = p.c.n_kv_heads, first_v = p.n_heads + kvh, rows = first_v + kvh;
   const __nv_bfloat16 *q = p.q + t * p.q_ts, *k = p.k + t * p.k_ts, *v = p.v + t * p.v_ts;
@@ -111,14 +112,14 @@ __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_ap
   for (int i = 0; i < ROWS; ++i) {
     const int r = r0 + i * groups;
     raw[i] = make_uint4(0, 0, 0, 0);
-    if (r < rows) {
+    if (there && r < rows) {
       const long hs = r < p.n_heads ? p.q_hs : r < first_v ? p.k_hs : p.v_hs;
       const __nv_bfloat16* src = r < p.n_heads ? q + r * hs : r < first_v ? k + (r - p.n_heads) * hs : v + (r - first_v) * hs;
       raw[i] = *reinterpret_cast<const uint4*>(src + rest * hs + 8 * j);
     }
   }
   Place at;
-  if (!find_place<(BITS < 8)>(p.c, p.b, t, lane, p.status, at)) return;
+  if (!find_place<(BITS < 8)>(p.c, p.b, t, lane, p.status, at) || !there) return;
   const int turn = p.positions != nullptr ? __ldg(p.positions + t) : at.pos;
   if (p.table != nullptr && (turn < 0 || turn >= p.n_pos)) {
     report_device_error(p.status, HBL_ERR_RANGE);
