@@ -473,8 +473,10 @@ int hbl_kv_read(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, void* 
  * applied in fp32, to the score (keys) and to p (values), and the product is rounded to fp16 against the largest scale.
  * Scores, p's sum and the result are accumulated in fp32.
  * Keys, values and scales that are NaN or infinite reach no row they are masked for; places beyond kv_len are never used,
- * whatever they hold.  A row that sees such a value or scale is NaN, at bits 16 perhaps in the value's elements alone; its
- * lse may be NaN, too.  So is a row with a score that is NaN or +infinity; a key whose score is -infinity has no weight.
+ * whatever they hold.  A row that sees a value whose scale is not finite (bits 3, 4, 8) is NaN in all its elements; a row
+ * that sees a value that is not finite (bits 16) is NaN, or NaN or infinite in the value's elements alone.  The lse of such
+ * a row may be NaN, too.  Keys and their scales act by way of the score: a row with a score that is NaN or +infinity is
+ * NaN, and a key whose score is -infinity has no weight (though its value, where that is not finite, may count as seen).
  * workspace: hbl_attention_workspace_bytes, 1024-byte aligned (NULL where that is 0); scratch, nothing in it is kept.
  * Calls that may run at the same time need one each.  out may not overlap q or the cache.
  * n_heads a multiple of n_kv_heads. */

@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
         }
         top = fmaxf(top, c[nt][e]);
       }
-    const bool wide = CODES && fmaxf(fabsf(vs[0]), fabsf(vs[1])) > vr;       // (a scale that is not finite shows in the result)
+    const bool wide = CODES && fmaxf(fabsf(vs[0]), fabsf(vs[1])) > vr;       // (a scale that is not finite never counts, see vf)
     if (__any_sync(0xffffffffu, top > (some ? kLazy : -INFINITY) || wide)) {
       float fv = 1.f;
       if (CODES) {
@@ -265,7 +265,8 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
       }
       some = __all_sync(0xffffffffu, all);
     }
-    const float vf[2] = {vs[0] * inv_vr, vs[1] * inv_vr};
+    // (0 * a scale that is not finite is NaN: its weight is, so every element of a row that sees its key is, too)
+    const float vf[2] = {fmaf(vs[0], 0.f, vs[0] * inv_vr), fmaf(vs[1], 0.f, vs[1] * inv_vr)};
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float w[4];

@@ -49,3 +49,57 @@ def test_a_value_scale_that_is_not_finite_marks_the_rows_that_see_its_key_and_no
         assert torch.equal(bad.all(-1), seen) and torch.equal(bad.any(-1), seen)
         assert torch.isfinite(out).cpu()[~seen].all()
     assert hbl.hbl_check_status() == 0
+
+
+@pytest.mark.parametrize("bits", [3, 4, 8])
+@pytest.mark.parametrize("q_len,group", [(1, 1), (5, 2), (16, 1), (17, 1), (200, 1)])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("back", [1, 3, 60, 400])
+def test_a_value_scale_alone_that_is_not_finite(bits, q_len, group, what, back):
+    """The keys' scales are sound: a row that sees the value is NaN in all its elements, whichever kernel computes it."""
+    kv, page = q_len + 450, 16
+    cache, batch, tables, q = setup(2, [q_len], [kv], 2 * group, 2, 64, bits, page)
+    clean = hbl.hbl_attention(cache, batch, q)
+    n = kv - back
+    cache.v_scale[tables[0][n // page], 1, n % page] = what
+    out = hbl.hbl_attention(cache, batch, q)
+    first = max(0, q_len - back)                                              # the first token that sees it
+    assert torch.isnan(out[first:, group:]).all()
+    assert torch.equal(out[:first], clean[:first]) and torch.equal(out[:, :group], clean[:, :group])
+    assert hbl.hbl_check_status() == 0
+
+
+@pytest.mark.parametrize("bits", [3, 4])
+@pytest.mark.parametrize("q_len", [1, 40])
+def test_a_first_token_whose_value_scale_is_not_finite(bits, q_len):
+    kv = q_len + 90
+    g = gen(3)
+    cache = hbl.KvCache.empty(12, 16, 2, 64, bits, 2)
+    fill(g, cache)
+    batch, _ = make_batch(g, cache, [q_len], [kv], slots=[1])
+    q = heads(g, q_len, 2, 64)
+    clean = hbl.hbl_attention(cache, batch, q)
+    cache.bos_v_scale[1, 0] = float("inf")
+    out = hbl.hbl_attention(cache, batch, q)
+    assert torch.isnan(out[:, 0]).all() and torch.equal(out[:, 1], clean[:, 1])
+    assert hbl.hbl_check_status() == 0
+
+
+@pytest.mark.parametrize("q_len", [1, 6, 17, 300])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("back", [1, 5, 250])
+def test_a_bf16_value_that_is_not_finite(q_len, what, back):
+    """Its element is not finite in a row that sees it; the row's other elements are as without it, or the whole row is NaN."""
+    kv, D, e = q_len + 280, 128, 37
+    cache, batch, tables, q = setup(4, [q_len], [kv], 2, 2, D, 16, 32)
+    clean = hbl.hbl_attention(cache, batch, q)
+    n = kv - back
+    cache.v[tables[0][n // 32], 1, n % 32, e] = what
+    out = hbl.hbl_attention(cache, batch, q)
+    first = max(0, q_len - back)
+    assert torch.equal(out[:first], clean[:first]) and torch.equal(out[:, 0], clean[:, 0])
+    rows, was = out[first:, 1], clean[first:, 1]
+    assert not torch.isfinite(rows[:, e]).any()
+    other = torch.arange(D, device="cuda") != e
+    assert (torch.isnan(rows).all(-1) | (rows == was)[:, other].all(-1)).all()
+    assert hbl.hbl_check_status() == 0
