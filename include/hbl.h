@@ -429,9 +429,10 @@ typedef struct {
  * Lengths are read on the device when the kernels run, so a captured call follows them when it is replayed.
  * A length above max_pages * page_size or 2^30 (the rest is left out), a negative one, or a page outside [0, n_pages) (its
  * tokens are neither written nor read) is reported as HBL_ERR_RANGE. (hbl_attention's results for such a
- * sequence are then not meaningful, the others' are.)  Several sequences may share pages that no call
- * writes; two tokens of one hbl_kv_append call may not have the same place,
- * nor two first tokens the same row of bos_k / bos_v. */
+ * sequence are then not meaningful, the others' are.)  A q_start that decreases or passes `tokens` is reported by
+ * hbl_attention, by the other calls where a row's look-up comes upon it; nothing out of bounds is touched, but no results
+ * count.  Several sequences may share pages that no call writes; two tokens of one hbl_kv_append call may not have the same
+ * place, nor two first tokens the same row of bos_k / bos_v. */
 typedef struct {
   const int32_t *q_start, *kv_len, *pages, *bos_slot;
   int n_seqs, tokens, max_pages, max_q_len, max_kv_len;

@@ -217,8 +217,11 @@ __device__ __forceinline__ bool decode_item(const TilesParams& p, int item, int 
   for (int b0 = 0; b0 < p.b.n_seqs && b < 0; b0 += 32) {
     int n = 0;
     if (b0 + lane < p.b.n_seqs) {
-      const int q = min(__ldg(p.b.q_start + b0 + lane + 1) - __ldg(p.b.q_start + b0 + lane), p.b.max_q_len);
-      const long rows = (long)max(q, 0) * p.a.group;
+      const int q0 = __ldg(p.b.q_start + b0 + lane), q1 = __ldg(p.b.q_start + b0 + lane + 1);
+      // starts that make no sense have no tiles: those that there are (as many as the sound ones need) go to the others
+      const bool sane = q0 >= 0 && q1 >= q0 && q1 <= p.b.tokens;
+      if (!sane) report_device_error(p.status, HBL_ERR_RANGE);
+      const long rows = sane ? (long)min(q1 - q0, p.b.max_q_len) * p.a.group : 0;
       n = rows > p.few ? (int)((rows + G::ROWS - 1) / G::ROWS) : 0;
     }
     int sum = n;
