@@ -17,12 +17,30 @@ int check_strided(const void* p, long long token_stride, long long head_stride) 
   if (token_stride < 0 || head_stride < 0) return HBL_ERR_SHAPE;
   return HBL_OK;
 }
-// One that is written: two of its heads may not lie on each other (a broadcast tensor's stride of 0).
+// One that is written: two of its heads may not lie on each other, because different thread blocks write them.  Where neither
+// all heads of a token lie between one token and the next nor the other way round, head h of token t may lie on head h - i of
+// token t + j; so it does where i head strides and j token strides differ by less than a head.
+bool heads_overlap(long long token_stride, long long head_stride, long long tokens, long long heads, long long head_dim) {
+  using wide = __int128;                                        // strides are the caller's: products may pass 64 bits
+  if (tokens <= 1) return heads > 1 && head_stride < head_dim;
+  if (heads <= 1) return token_stride < head_dim;
+  if (token_stride < head_dim || head_stride < head_dim) return true;
+  if (token_stride >= (wide)(heads - 1) * head_stride + head_dim || head_stride >= (wide)(tokens - 1) * token_stride + head_dim) return false;
+  const bool by_head = heads <= tokens;                         // along the shorter axis, the nearest two of the other's
+  const long long n = by_head ? heads : tokens, m = by_head ? tokens : heads;
+  const long long step = by_head ? head_stride : token_stride, other = by_head ? token_stride : head_stride;
+  for (long long i = 1; i < n; ++i) {
+    const wide at = (wide)i * step, j = at / other;
+    if (j >= 1 && j < m && at - j * other < head_dim) return true;
+    if (j + 1 < m && (j + 1) * other - at < head_dim) return true;
+    if (j >= m) return false;                                   // beyond the last of them, and so is all that follows
+  }
+  return false;
+}
 int check_written(const void* p, long long token_stride, long long head_stride, int tokens, int heads, int head_dim) {
   const int rc = check_strided(p, token_stride, head_stride);
   if (rc != HBL_OK) return rc;
-  if ((tokens > 1 && token_stride < head_dim) || (heads > 1 && head_stride < head_dim)) return HBL_ERR_SHAPE;
-  return tokens > 1 && heads > 1 && token_stride == head_stride ? HBL_ERR_SHAPE : HBL_OK;
+  return heads_overlap(token_stride, head_stride, tokens, heads, head_dim) ? HBL_ERR_SHAPE : HBL_OK;
 }
 int check_rotation(const float* table, int n_pos, int rot_dim, int head_dim, int layout) {
   if (layout != HBL_ROPE_HALF && layout != HBL_ROPE_INTERLEAVED) return HBL_ERR_FORMAT;
