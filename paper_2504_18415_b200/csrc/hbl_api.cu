@@ -61,16 +61,31 @@ bool stream_released_early(cudaStream_t s) {
     if (g_streams[i].used && g_streams[i].s == s) return g_streams[i].early;
   return g_stream_overflow;
 }
+// A slot holds what is out of the ordinary about a stream: one with nothing to remember is given back, so that the streams a
+// program has had over its life do not fill the table.  (Once a stream has found no room, those without a slot count
+// as out of the ordinary; a slot that says that its stream is not is then kept.)
+namespace {
+void tidy(StreamSlot& slot) {
+  if (!slot.early && !slot.unflushed && !g_stream_overflow && !g_unflushed_overflow) slot.used = false;
+}
+}
 void set_stream_released_early(cudaStream_t s, bool v) {
   std::lock_guard<std::mutex> lock(g_overlap_mutex);
   int free_slot = -1;
   for (int i = 0; i < kStreamSlots; ++i) {
-    if (g_streams[i].used && g_streams[i].s == s) { g_streams[i].early = v; return; }
+    if (g_streams[i].used && g_streams[i].s == s) { g_streams[i].early = v; tidy(g_streams[i]); return; }
     if (!g_streams[i].used && free_slot < 0) free_slot = i;
   }
   if (!v && !g_stream_overflow) return;                       // nothing to remember
-  if (free_slot >= 0) { g_streams[free_slot] = {}; g_streams[free_slot].s = s; g_streams[free_slot].used = true; g_streams[free_slot].early = v; }
-  else if (v) g_stream_overflow = true;
+  if (free_slot >= 0) {
+    g_streams[free_slot] = {};
+    g_streams[free_slot].s = s;
+    g_streams[free_slot].used = true;
+    g_streams[free_slot].early = v;
+    g_streams[free_slot].unflushed = g_unflushed_overflow;    // (as a stream without a slot counts)
+  } else if (v) {
+    g_stream_overflow = true;
+  }
 }
 bool stream_unflushed(cudaStream_t s) {
   std::lock_guard<std::mutex> lock(g_overlap_mutex);
@@ -82,7 +97,7 @@ void set_stream_unflushed(cudaStream_t s, bool v) {
   std::lock_guard<std::mutex> lock(g_overlap_mutex);
   int free_slot = -1;
   for (int i = 0; i < kStreamSlots; ++i) {
-    if (g_streams[i].used && g_streams[i].s == s) { g_streams[i].unflushed = v; return; }
+    if (g_streams[i].used && g_streams[i].s == s) { g_streams[i].unflushed = v; tidy(g_streams[i]); return; }
     if (!g_streams[i].used && free_slot < 0) free_slot = i;
   }
   if (!v) return;                                             // nothing to remember
