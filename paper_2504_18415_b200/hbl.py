@@ -615,6 +615,8 @@ def hbl_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, sm_scale: flo
     if workspace is None:
         n = hbl_attention_workspace_bytes(cache, batch, H)
         workspace = new_workspace(n, dev) if n > 0 else None
+    if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
+        raise ValueError(f"workspace: expected a contiguous tensor on {dev}")
     ws, size = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
     _check(lib().hbl_attention(cache.ref, batch.ref, args, ws, size, _raw_stream(dev)), "hbl_attention")
     return out
