@@ -108,6 +108,48 @@ void set_stream_unflushed(cudaStream_t s, bool v) {
   g_streams[free_slot].early = g_stream_overflow;             // (as a stream without a slot counts)
   g_streams[free_slot].unflushed = true;
 }
+// ---- nodes of captures in progress (see remember_captured) ----
+namespace {
+// The latest ones, in a ring; nodes of captures that are over are never asked for, or at worst (an address used
+// again within one capture) cost an early start.  A capture that has had more than the ring holds counts every node as one.
+constexpr int kCapturedNodes = 4096;
+struct CapturedNode { unsigned long long capture; cudaGraphNode_t node; cudaStream_t s; CapturedAs kind; } g_captured[kCapturedNodes];
+unsigned long long g_captured_total = 0, g_captured_lost = 0;     // lost: the capture whose node was overwritten last (ids begin at 1)
+struct Capture { unsigned long long id; const cudaGraphNode_t* deps; size_t n; };      // id 0: none
+Capture capture_of(cudaStream_t s) {
+  Capture c = {0, nullptr, 0};
+  cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+  const cudaGraphEdgeData* edges = nullptr;
+  unsigned long long id = 0;
+  if (cudaStreamGetCaptureInfo_v3(s, &status, &id, nullptr, &c.deps, &edges, &c.n) != cudaSuccess) {
+    (void)cudaGetLastError();                                 // (the launch itself will say what is wrong with the stream)
+    return {0, nullptr, 0};
+  }
+  if (status == cudaStreamCaptureStatusActive) c.id = id;
+  return c;
+}
+}  // namespace
+void remember_captured(cudaStream_t s, CapturedAs kind) {
+  const Capture c = capture_of(s);
+  if (c.id == 0 || c.n != 1) return;                           // (behind a launch there is one: the launch)
+  std::lock_guard<std::mutex> lock(g_overlap_mutex);
+  CapturedNode& slot = g_captured[g_captured_total++ % kCapturedNodes];
+  if (slot.capture == c.id) g_captured_lost = c.id;
+  slot = {c.id, c.deps[0], s, kind};
+}
+bool captured_behind_one(cudaStream_t s) {
+  const Capture c = capture_of(s);
+  if (c.id == 0 || c.n == 0) return false;
+  std::lock_guard<std::mutex> lock(g_overlap_mutex);
+  if (g_captured_lost == c.id) return true;
+  const int held = g_captured_total < kCapturedNodes ? (int)g_captured_total : kCapturedNodes;
+  for (size_t d = 0; d < c.n; ++d)
+    for (int i = 0; i < held; ++i) {
+      const CapturedNode& x = g_captured[i];
+      if (x.capture == c.id && x.node == c.deps[d] && !(x.kind == CapturedAs::EarlyRelease && x.s == s)) return true;
+    }
+  return false;
+}
 namespace {
 // The outputs of the early-releasing call just launched on s (called right after set_stream_released_early(s, true)).
 void record_stream_outputs(cudaStream_t s, const ByteRange* out, int n) {

@@ -82,11 +82,18 @@ bool stream_unflushed(cudaStream_t s);                        // the library's l
 void set_stream_unflushed(cudaStream_t s, bool v);
 bool stream_released_early(cudaStream_t s);                   // the library's last launch on s releases early
 void set_stream_released_early(cudaStream_t s, bool v);
+// While a stream is captured, a launch with the programmatic attribute gets a programmatic edge from every kernel it depends
+// on, those that it waits for by an event on another stream included (outside a capture, events wait for whole kernels).
+// So the library also remembers which nodes of a capture are kernels of either kind.
+enum class CapturedAs { Waiting, EarlyRelease };
+void remember_captured(cudaStream_t s, CapturedAs kind);      // the launch just made on s; nothing if s is not captured
+// s is captured, and what its next launch depends on holds such a node (early releases of s itself aside: stream_released_early()).
+bool captured_behind_one(cudaStream_t s);
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_dependent(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
                                     Args... args) {
   const LaunchMode mode = launch_mode();
-  const bool programmatic = (mode.overlap_ok || !stream_released_early(s)) && !stream_unflushed(s);
+  const bool programmatic = (mode.overlap_ok || !stream_released_early(s)) && !stream_unflushed(s) && !captured_behind_one(s);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
@@ -100,6 +107,7 @@ inline cudaError_t launch_dependent(void (*kern)(KArgs...), dim3 grid, dim3 bloc
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
   set_stream_released_early(s, mode.releases_early);
   set_stream_unflushed(s, false);
+  if (mode.releases_early) remember_captured(s, CapturedAs::EarlyRelease);
   return e;
 }
 // For kernels that call grid_dependency_wait() before they touch memory (or begin behind one that has, and is released by it).
@@ -118,6 +126,7 @@ inline cudaError_t launch_waiting(void (*kern)(KArgs...), dim3 grid, dim3 block,
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
   set_stream_released_early(s, false);
   set_stream_unflushed(s, true);
+  remember_captured(s, CapturedAs::Waiting);
   return e;
 }
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
