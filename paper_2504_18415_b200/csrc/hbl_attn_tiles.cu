@@ -174,6 +174,10 @@ __device__ __forceinline__ int token_of(const TilesParams& p, int r) {
   return (int)((__umulhi((uint32_t)r, p.div_mul) + (uint32_t)r) >> p.div_shift);
 }
 
+// What scores are multiplied by.  A negative scale: the queries are negated.  Zero: a masked score, -infinity, has to stay one,
+// so the smallest number above it, which takes the largest product to 5e-7.
+__device__ __forceinline__ float score_scale(float scale_log2) { return fmaxf(fabsf(scale_log2), 0x1p-149f); }
+
 // The grid has one thread block to an item, but a block that runs takes over blocks that have not started yet
 // (clusterlaunchcontrol.try_cancel), item by item, so the items are dealt by who is about to be free, in the grid's order,
 // without a counter in memory and without giving up shared or tensor memory in between.  One request per call; after one
@@ -345,7 +349,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
     constexpr uint32_t LOWER = 16u << 16;                      // rows 16 .. 31 of the warp
     auto at = [](int i, int q) { return R == 4 ? (i >> 1) * (BK / 2) + 4 * q + 2 * (i & 1) : 2 * q; };   // pair q of row i among the registers
     constexpr int STEP = R == 4 ? 8 : 2;                       // its columns: STEP q + 2t, + 1
-    const float scale = fmaxf(fabsf(p.a.scale_log2), 1e-30f);  // (a negative one: the queries are negated; 0 * -inf is not -inf)
+    const float scale = score_scale(p.a.scale_log2);
     uint32_t it = 0, done = 0;                                 // tiles and items so far: barrier phases
     bool ok = true;
     for (uint32_t n = 0;; ++n) {
@@ -651,7 +655,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
     regs_down<PROD>();
     const int tid = threadIdx.x & 127;
     constexpr int CH = D / 8;                                   // 16-byte chunks of a row
-    const float scale = fmaxf(fabsf(p.a.scale_log2), 1e-30f);
+    const float scale = score_scale(p.a.scale_log2);
     uint32_t it = 0;
     bool ok = true;
     Item w;
