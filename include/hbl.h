@@ -480,7 +480,7 @@ int hbl_kv_read(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, void* 
  * NaN, and a key whose score is -infinity has no weight (though its value, where that is not finite, may count as seen).
  * workspace: hbl_attention_workspace_bytes, 1024-byte aligned (NULL where that is 0); scratch, nothing in it is kept.
  * Calls that may run at the same time need one each.  out may not overlap q or the cache.
- * n_heads a multiple of n_kv_heads. */
+ * n_heads a multiple of n_kv_heads, at most 2^20. */
 typedef struct {
   const void* q;
   void* out;

@@ -9,6 +9,7 @@ using namespace hbl;
 namespace {
 
 constexpr int kMaxRotDim = 256;
+constexpr int kMaxHeads = 1 << 20;      // rows of a call (token times head) and what the host computes of them stay in range
 
 // A [tokens, heads, dim] tensor with strides: every piece of 8 elements has to lie on a 16-byte boundary.
 int check_strided(const void* p, long long token_stride, long long head_stride) {
@@ -230,7 +231,7 @@ size_t hbl_attention_workspace_bytes(const hbl_kv_cache_t* cache, const hbl_kv_b
   KvView c{};
   BatchView b{};
   if (check_cache(cache, &c) != HBL_OK || check_batch(batch, &b) != HBL_OK || nothing(b)) return 0;
-  if (n_heads <= 0 || n_heads % c.n_kv_heads != 0) return 0;
+  if (n_heads <= 0 || n_heads > kMaxHeads || n_heads % c.n_kv_heads != 0) return 0;
   return plan_attention(c, b, n_heads).workspace;
 }
 
@@ -243,6 +244,7 @@ int hbl_attention(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, cons
   if ((rc = check_batch(batch, &b)) != HBL_OK) return rc;
   if (!args) return HBL_ERR_NULL;
   if (args->n_heads <= 0 || args->n_heads % c.n_kv_heads != 0) return HBL_ERR_SHAPE;
+  if (args->n_heads > kMaxHeads) return HBL_ERR_TOO_LARGE;
   if (!isfinite(args->sm_scale)) return HBL_ERR_SHAPE;
   if (nothing(b) || b.max_q_len == 0) return HBL_OK;
   if (!args->q || !args->out) return HBL_ERR_NULL;
