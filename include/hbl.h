@@ -425,7 +425,8 @@ typedef struct {
  *   pages     device int32 [n_seqs, max_pages]; entries beyond a sequence's length are not looked at
  *   bos_slot  device int32 [n_seqs]: the sequence's row of bos_k / bos_v; NULL: sequence b has row b
  *   max_q_len, max_kv_len   upper bounds of the lengths (host values: launch shapes go by them).  Tokens of a sequence
- *             beyond its first max_q_len are not computed by hbl_attention; a kv_len above max_kv_len costs time only.
+ *             beyond its first max_q_len are not computed by hbl_attention; a kv_len above max_kv_len costs time only
+ *             (tens of millions of tokens above it, a prompt's bounded waits run out: HBL_ERR_TIMEOUT).
  * Lengths are read on the device when the kernels run, so a captured call follows them when it is replayed.
  * A length above max_pages * page_size or 2^30 (the rest is left out), a negative one, or a page outside [0, n_pages) (its
  * tokens are neither written nor read) is reported as HBL_ERR_RANGE. (hbl_attention's results for such a

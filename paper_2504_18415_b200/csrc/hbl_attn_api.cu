@@ -101,7 +101,13 @@ int check_batch(const hbl_kv_batch_t* b, BatchView* v) {
 bool nothing(const BatchView& b) { return b.n_seqs == 0 || b.tokens == 0; }
 
 // How a call is made: sequences of up to `few` query rows on the streaming kernel, longer ones on the tensor-core
-// tiles; a single sequence, whose length the bound says, on one of them alone.
+// tiles; a single sequence, whose length the bound says, on one of them alone.  The streaming kernel reads
+// the keys once for 16 rows, so its time goes up in steps (8192 tokens, heads of 128, us at 8, 16, 32 rows: streaming / tiles):
+//                                3 bits                    4 bits                    8 bits                    16 bits
+//   1 sequence, 32 key heads     32 46  62 /  73  73  73   30 46  58 /  69  70  71   38 54  73 /  75  75  79   48 56  87 /  52  52  52
+//   32 sequences, 8 key heads   101 183 305 / 430 429 430  103 171 276 / 376 376 377  148 228 437 / 409 412 417  208 267 364 / 257 255 256
+// Up to 16 rows streaming wins over codes by far and loses at 16 bits by 8 % and 5 % from 9 rows on.  At 3 and 4 bits it still
+// wins at 32 rows (not at 48: 97 and 385 us, 93 and 344), at 8 bits the two meet there: the border there could be later.
 constexpr int kFewRows = 16;
 struct AttnCall {
   bool use_rows, use_tiles;

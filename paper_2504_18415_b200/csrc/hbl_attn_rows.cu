@@ -7,8 +7,8 @@
 // the value scales.  These roundings are what the tensor core's operands cost; p's sum is taken before them, in fp32.
 //
 // The cache is read once per 8 (16) query rows of its key head.  bf16 is bound by that (one sequence of 131072 tokens: 95 us,
-// 5.7 TB/s; 64 ragged ones of up to 4096 tokens 364), codes by logic operations and issue (64 x 4096 tokens of 32 key heads, one row:
-// 4 bits 275 us, 4.3 TB/s; ragged 175).  A thread block takes one
+// 5.7 TB/s; 64 ragged ones of up to 4096 tokens 364).  Codes (64 x 4096 tokens of 32 key heads, one row: 4 bits 275 us, 4.3 TB/s;
+// ragged 175) fill no unit: 60 % of the issue slots, 53 % of the logic pipe's cycles, 46 % of HBM's.  A thread block takes one
 // (sequence, key head, row tile, piece of the keys), its four warps take 16 keys in turn and meet only at the end, so there
 // is no barrier in the loop.  The keys are the M side of both products (S^T = K q^T, O^T = V^T P^T): 16 keys against 8
 // rows, no half-empty tile, and a lane's operand registers are exactly the bytes that it loads from the cache
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
 
   // Per column: minus the maximum so far (0: none yet), p's sum.  `some`: every column has a maximum.
   // vr: a power of two no smaller than any value scale so far.  The weights go to the tensor core as p vs / vr * 2^7 in
-  // fp16: at most 2^15, rounded by 2^-12 of themselves, or by 2^-32 vr where they are that small.
+  // fp16: at most 2^15, rounded by 2^-11 of themselves, or by 2^-32 vr where they are that small.
   float neg[NT][2], qs[NT][2], l[NT][2], o[NT][MT][4];
   float vr = 0x1p-100f, inv_vr = 0x1p107f;
   uint32_t poison = 0;                                         // bits 16: columns that saw a masked step's value that is not finite

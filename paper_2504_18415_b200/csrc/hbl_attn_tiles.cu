@@ -774,7 +774,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         };
         // Scales: ks of key row tid; value scales of all rows (32 i + lane), so that every warp finds the same `unit`
         // for itself: a power of two no smaller than any value scale of the item so far.  p vs / unit * 2^7 is at most
-        // 2^15, what fp16 holds; it is rounded by 2^-12 of itself, or by 2^-32 unit where it is that small.
+        // 2^15, what fp16 holds; it is rounded by 2^-11 of itself, or by 2^-32 unit where it is that small.
         constexpr int VN = BK / 32;
         float ks = 0.f, vs[VN];
         auto load_scales = [&](const Tile& t) {

@@ -4,9 +4,10 @@
 //   gamma = max_d |x[d]|,  u = round((2^(b-1) - 1) / (gamma + eps) * x) + 2^(b-1),  scale = gamma / (2^(b-1) - 1)
 //
 // Prompts: 2 bytes read and b / 8 written per element, queries 2 and 2.  bf16 rows are bound by HBM (four 2048-token
-// prompts of 96 heads with reading them back: 72 us, 5.6 TB/s), codes by the issue of instructions (71 % of the slots at 3
-// bits: widening, rotation, the maximum's shuffles, packing; 148 us, 2.9 TB/s).  A decoding step is bound by the chain of
-// dependent loads (sequence -> length -> page -> row).  A lane owns 8 consecutive elements of a head, so a head
+// prompts of 96 heads with reading them back: 72 us, 5.6 TB/s), codes by the issue of instructions (78 % of the slots at 3
+// bits: widening, rotation, the maximum's shuffles, packing, and choosing what each head is; 147 us, 2.9 TB/s).  Append and read
+// apart, 3, 4, 8, 16 bits: 113, 103, 104, 78 us and 47, 45, 41, 49.  A decoding step (64 tokens of 96 heads: 4.0 us and 2.2 us in
+// a replayed graph) is bound by the chain of dependent loads (sequence -> length -> page -> row).  A lane owns 8 consecutive elements of a head, so a head
 // is head_dim / 8 lanes and its maximum takes three to five shuffles; the partner of a rotated element lies in the same
 // lane (interleaved layout) or one shuffle away (half layout).  A thread takes ROWS heads of the same token: the table's
 // pairs are loaded once for all of them, and their loads are in flight together.  The loads of the data depend on the
