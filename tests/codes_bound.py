@@ -6,6 +6,8 @@ a weight p_j vs_j is rounded to fp16, whose half step is 2^-11 of the value (eps
     |out - ref| <= 2^-8 |ref| + (2^-11 + e) A + n 2^-30 max |v|,      A = sum_j p_j |v_j| / sum_j p_j,
 
 with the output's own rounding to bf16, e for what fp32 adds, and the fixed step of fp16 below 2^-14, each as derived there.
+That step is at most 2^-31 max vs in a weight; n 2^-30 max |v| counts codes of at most 2^(b-1).  A first token kept at 8 bits
+has codes of up to 2^7, so it adds 2^-24 max vs.
 """
 import math
 
@@ -17,8 +19,8 @@ FP16_HALF_STEP = torch.finfo(torch.float16).eps / 2
 BF16_HALF_STEP = torch.finfo(torch.bfloat16).eps / 2
 
 
-def bound(ref, A, e, n, v_max):
-    return BF16_HALF_STEP * ref.abs() + (FP16_HALF_STEP + e) * A + n * 2.0 ** -30 * v_max + 1e-30
+def bound(ref, A, e, n, v_max, first_scale=0.0):
+    return BF16_HALF_STEP * ref.abs() + (FP16_HALF_STEP + e) * A + n * 2.0 ** -30 * v_max + 2.0 ** -24 * first_scale + 1e-30
 
 
 def attention_codes64(cache, q, q_lens, kv_lens, tables, sm_scale, causal=True, slots=None):
@@ -41,6 +43,7 @@ def attention_codes64(cache, q, q_lens, kv_lens, tables, sm_scale, causal=True, 
             e = 2 * (D + 4) * 2.0 ** -23 * size + (nk / 16 + 64) * 2.0 ** -23 + 2.0 ** -20
             r = slice(at, at + nq)
             out[r, h] = p @ v
-            tol[r, h] = bound(out[r, h], p @ v.abs(), e[:, None], nk, v.abs().max())
+            vs = cache.v_scale[torch.as_tensor(tables[b], device=dev).long(), h // group].max()
+            tol[r, h] = bound(out[r, h], p @ v.abs(), e[:, None], nk, v.abs().max(), vs if slot8 is not None else 0.0)
         at += nq
     return out, tol
