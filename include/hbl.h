@@ -398,6 +398,50 @@ typedef struct {
 } hbl_rope_t;
 int hbl_rope(const hbl_rope_t* args /* host */, void* stream);
 
+/* Query and key heads divided by their root mean square, times a gain, and rotated, in one pass:
+ *   o = r R(gain * x),   r = 1 / sqrt(mean_d x[d]^2 + norm_eps),   R: the rotation of hbl_rope, the whole head in the mean.
+ * r is summed in fp64 and rounded once to fp32; gain * x, the rotation and the product with r are fp32 in that order, each product
+ * and sum rounded once; one rounding to the output type.
+ *   q, k         the two tensors; k.n_heads = 0: there is only q.  Both have the call's positions, types and head_dim
+ *     x, out       device, fp32 or bf16 (dtype), [tokens, n_heads, head_dim], strides as in hbl_rope; out may be x itself with
+ *                  the same strides, and may not overlap an input or the other output in any other way
+ *     gain         device [head_dim], fp32 or bf16 (gain_dtype), 16-byte aligned; NULL: ones
+ *   positions, table, n_pos, rot_dim, layout   as in hbl_rope; a token whose position is out of range is not written.  table NULL:
+ *                nothing is rotated (positions, n_pos, rot_dim and layout are then not looked at)
+ *   head_dim     a multiple of 8, 8..256;  norm_eps >= 0, finite (HBL_ERR_EPS otherwise); with 0 an all-zero head is NaN */
+typedef struct {
+  const void *x, *gain;
+  void* out;
+  long long x_token_stride, x_head_stride, out_token_stride, out_head_stride;
+} hbl_norm_rope_part_t;
+typedef struct {
+  hbl_norm_rope_part_t q, k;
+  const int32_t* positions;
+  const float* table;
+  int n_q_heads, n_k_heads, dtype, gain_dtype, tokens, head_dim, n_pos, rot_dim, layout;
+  float norm_eps;
+} hbl_norm_rope_t;
+int hbl_norm_rope(const hbl_norm_rope_t* args /* host */, void* stream);
+
+/* The backward pass of hbl_norm_rope, from the gradients with respect to its outputs:
+ *   t = R^T grad_out,  u = gain * t,   grad_x = r (u - x r^2 mean_d(x u)),   grad_gain[d] = sum over tokens and heads of t[d] x[d] r
+ * in fp32 throughout (of head magnitudes whose squares fp32 can add up), the sum over rows in an order that depends on the
+ * sizes alone: the same call gives the same bits.
+ *   part.x     the inputs of hbl_norm_rope;  part.out: grad_x, same type, written; it may be x or grad_out itself (same strides)
+ *   grad_out   device, type of x, element strides as in hbl_rope (0: broadcast)
+ *   grad_gain  device fp32 [head_dim], 4-byte aligned, overwritten; NULL: not wanted.  (gain NULL: that of a gain of ones)
+ * A token whose position is out of range is not written and adds nothing.  tokens = 0: the gains' gradients are zeros.
+ * workspace: hbl_norm_rope_grad_workspace_bytes, 1024-byte aligned (not looked at where both grad_gain are NULL); scratch.
+ * Calls that may run at the same time need one each. */
+typedef struct {
+  hbl_norm_rope_t forward;               /* q.out, k.out: the gradients with respect to q.x, k.x */
+  const void *q_grad, *k_grad;
+  float *q_grad_gain, *k_grad_gain;
+  long long q_grad_token_stride, q_grad_head_stride, k_grad_token_stride, k_grad_head_stride;
+} hbl_norm_rope_grad_t;
+size_t hbl_norm_rope_grad_workspace_bytes(int tokens, int n_q_heads, int n_k_heads, int head_dim);
+int hbl_norm_rope_grad(const hbl_norm_rope_grad_t* args /* host */, void* workspace, size_t workspace_bytes, void* stream);
+
 /* A paged cache of attention states (all pointers device, the caller's).  A page holds page_size tokens of every
  * key/value head; row (page, head, slot) has the number  (page * n_kv_heads + head) * page_size + slot.
  *   bits 3, 4, 8   k, v: head_dim * bits / 8 bytes per row, the codes of hbl_quantize_kv (u = q + 2^(bits-1), a
@@ -460,6 +504,19 @@ typedef struct {
 } hbl_kv_append_t;
 int hbl_kv_append(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_kv_append_t* args, void* stream);
 
+/* hbl_kv_append with the heads normalised first, in the same launch: keys and queries become r R(gain * x) as hbl_norm_rope
+ * has them (the fp32 values are quantized, not rounded in between), values are as they are.
+ *   q_gain, k_gain  device [head_dim], fp32 or bf16 (gain_dtype), 16-byte aligned; NULL: ones
+ *   norm_eps        >= 0, finite (HBL_ERR_EPS otherwise); with 0 an all-zero head is NaN
+ * Everything else as hbl_kv_append, but that queries may come without a table: they are then normalised only. */
+typedef struct {
+  const void *q_gain, *k_gain;
+  int gain_dtype;
+  float norm_eps;
+} hbl_head_norm_t;
+int hbl_kv_append_norm(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_kv_append_t* args, const hbl_head_norm_t* norm,
+                       void* stream);
+
 /* The batch's tokens out of the cache: k_out, v_out bf16 [tokens, n_kv_heads, head_dim] (contiguous, 16-byte aligned)
  * = scale * (u - 2^(bits-1)), one rounding (bits 16: the values as they are).  With q_start = the running sum of kv_len
  * whole sequences come out (to move them to another cache, or to keep a shared prefix). */
@@ -493,6 +550,16 @@ typedef struct {
 size_t hbl_attention_workspace_bytes(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, int n_heads);
 int hbl_attention(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_attention_t* args, void* workspace,
                   size_t workspace_bytes, void* stream);
+
+/* hbl_attention within a window: the token at position i of its sequence sees the tokens j <= i with j > i - window (itself
+ * and the window - 1 before it) or j < sinks (the sequence's first ones, which stay visible).  window >= 1, sinks >= 0, causal has to
+ * be 1 (HBL_ERR_SHAPE otherwise).  Everything else as hbl_attention, and:
+ * Entries of `pages` that hold no token that a row of the call sees are not looked at: such pages may be given to other
+ * sequences.  In a page that holds some, the tokens that no row sees may hold anything.  (hbl_kv_append writes the places of
+ * its own tokens only; hbl_kv_read reads what it is asked for.) */
+size_t hbl_attention_window_workspace_bytes(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, int n_heads, int window, int sinks);
+int hbl_attention_window(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_attention_t* args, int window, int sinks,
+                         void* workspace, size_t workspace_bytes, void* stream);
 
 /* Packed ternary -> int8 [N,K] row-major, values in {-1,0,1}. */
 int hbl_unpack_weights(const void* W_packed, int out_dim, int in_dim, int8_t* w_out, void* stream);

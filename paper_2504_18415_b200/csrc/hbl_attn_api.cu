@@ -98,7 +98,82 @@ int check_batch(const hbl_kv_batch_t* b, BatchView* v) {
   if (!aligned(b->q_start, 4) || !aligned(b->kv_len, 4) || !aligned(b->pages, 4) || !aligned(b->bos_slot, 4)) return HBL_ERR_ALIGN;
   return HBL_OK;
 }
+int check_gains(const void* q_gain, const void* k_gain, int gain_dtype, float norm_eps) {
+  if (gain_dtype != HBL_F32 && gain_dtype != HBL_BF16) return HBL_ERR_FORMAT;
+  if (!(norm_eps >= 0.0f) || !isfinite(norm_eps)) return HBL_ERR_EPS;
+  return aligned(q_gain, 16) && aligned(k_gain, 16) ? HBL_OK : HBL_ERR_ALIGN;
+}
+// hbl_norm_rope, and with `g` hbl_norm_rope_grad.
+int check_norm_rope(const hbl_norm_rope_t* a, const hbl_norm_rope_grad_t* g, NormRopeCall* c) {
+  if (!a) return HBL_ERR_NULL;
+  if (a->dtype != HBL_F32 && a->dtype != HBL_BF16) return HBL_ERR_FORMAT;
+  if (a->tokens < 0 || a->n_q_heads <= 0 || a->n_k_heads < 0) return HBL_ERR_SHAPE;
+  if (a->n_q_heads > kMaxHeads || a->n_k_heads > kMaxHeads) return HBL_ERR_TOO_LARGE;
+  if (a->head_dim < 8 || a->head_dim > kMaxRotDim || a->head_dim % 8 != 0) return HBL_ERR_SHAPE;
+  int rc = check_gains(a->q.gain, a->k.gain, a->gain_dtype, a->norm_eps);
+  if (rc != HBL_OK) return rc;
+  if (a->table) {
+    if ((rc = check_rotation(a->table, a->n_pos, a->rot_dim, a->head_dim, a->layout)) != HBL_OK) return rc;
+    if (a->tokens > 0 && !a->positions) return HBL_ERR_NULL;
+    if (!aligned(a->positions, 4)) return HBL_ERR_ALIGN;
+    c->positions = a->positions;
+    c->table = a->table;
+    c->n_pos = a->n_pos; c->rot_dim = a->rot_dim; c->interleaved = a->layout == HBL_ROPE_INTERLEAVED;
+  }
+  c->dtype = a->dtype; c->gain_dtype = a->gain_dtype; c->tokens = a->tokens; c->head_dim = a->head_dim; c->norm_eps = a->norm_eps;
+  const hbl_norm_rope_part_t* parts[2] = {&a->q, &a->k};
+  for (int i = 0; i < 2; ++i) {
+    const hbl_norm_rope_part_t& s = *parts[i];
+    NormRopePart& d = c->part[i];
+    d.n_heads = i == 0 ? a->n_q_heads : a->n_k_heads;
+    if (d.n_heads == 0) continue;
+    d.x = s.x; d.gain = s.gain; d.out = s.out;
+    d.x_ts = s.x_token_stride; d.x_hs = s.x_head_stride; d.o_ts = s.out_token_stride; d.o_hs = s.out_head_stride;
+    if (g) {
+      d.grad = i == 0 ? g->q_grad : g->k_grad;
+      d.grad_gain = i == 0 ? g->q_grad_gain : g->k_grad_gain;
+      d.g_ts = i == 0 ? g->q_grad_token_stride : g->k_grad_token_stride;
+      d.g_hs = i == 0 ? g->q_grad_head_stride : g->k_grad_head_stride;
+      if (!aligned(d.grad_gain, 4)) return HBL_ERR_ALIGN;
+    }
+    if (a->tokens == 0) continue;
+    if (!d.x || !d.out || (g && !d.grad)) return HBL_ERR_NULL;
+    if ((rc = check_strided(d.x, d.x_ts, d.x_hs)) != HBL_OK) return rc;
+    if (g && (rc = check_strided(d.grad, d.g_ts, d.g_hs)) != HBL_OK) return rc;
+    if ((rc = check_written(d.out, d.o_ts, d.o_hs, a->tokens, d.n_heads, a->head_dim)) != HBL_OK) return rc;
+    if (d.out == d.x && (d.o_ts != d.x_ts || d.o_hs != d.x_hs)) return HBL_ERR_SHAPE;
+    if (g && d.out == d.grad && (d.o_ts != d.g_ts || d.o_hs != d.g_hs)) return HBL_ERR_SHAPE;
+  }
+  // one output for both, or one gradient of the gains
+  if (a->n_k_heads > 0 && a->tokens > 0 && a->q.out == a->k.out) return HBL_ERR_SHAPE;
+  if (g && a->n_k_heads > 0 && g->q_grad_gain && g->q_grad_gain == g->k_grad_gain) return HBL_ERR_SHAPE;
+  return HBL_OK;
+}
 bool nothing(const BatchView& b) { return b.n_seqs == 0 || b.tokens == 0; }
+// hbl_kv_append, and with `norm` hbl_kv_append_norm.
+int append(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_kv_append_t* a, const hbl_head_norm_t* norm, cudaStream_t stream) {
+  KvView c{};
+  BatchView b{};
+  int rc = check_cache(cache, &c);
+  if (rc != HBL_OK) return rc;
+  if ((rc = check_batch(batch, &b)) != HBL_OK) return rc;
+  if (!a) return HBL_ERR_NULL;
+  if (c.bits != 16 && (!(a->eps > 0.0f) || !isfinite(a->eps))) return HBL_ERR_EPS;
+  if (a->table && (rc = check_rotation(a->table, a->n_pos, a->rot_dim, c.head_dim, a->layout)) != HBL_OK) return rc;
+  if (a->q && a->n_heads <= 0) return HBL_ERR_SHAPE;
+  if (nothing(b)) return HBL_OK;
+  if (!a->k || !a->v) return HBL_ERR_NULL;
+  if ((a->q != nullptr) != (a->q_out != nullptr) || (a->q && !a->table && !norm)) return HBL_ERR_NULL;
+  if ((rc = check_strided(a->k, a->k_token_stride, a->k_head_stride)) != HBL_OK) return rc;
+  if ((rc = check_strided(a->v, a->v_token_stride, a->v_head_stride)) != HBL_OK) return rc;
+  if (a->q) {
+    if ((rc = check_strided(a->q, a->q_token_stride, a->q_head_stride)) != HBL_OK) return rc;
+    if ((rc = check_written(a->q_out, a->q_out_token_stride, a->q_out_head_stride, b.tokens, a->n_heads, c.head_dim)) != HBL_OK) return rc;
+    if (a->q == a->q_out && (a->q_token_stride != a->q_out_token_stride || a->q_head_stride != a->q_out_head_stride)) return HBL_ERR_SHAPE;
+  }
+  if (!aligned(a->positions, 4)) return HBL_ERR_ALIGN;
+  return launch_kv_append(c, b, *a, norm, stream);
+}
 
 // How a call is made: sequences of up to `few` query rows on the streaming kernel, longer ones on the tensor-core
 // tiles; a single sequence, whose length the bound says, on one of them alone.  The streaming kernel reads
@@ -115,16 +190,16 @@ struct AttnCall {
   AttnPlan rows, tiles;
   size_t rows_lse, tiles_o, tiles_lse, workspace;     // byte offsets of the parts (rows_o at 0), and the bytes of all
 };
-AttnCall plan_attention(const KvView& c, const BatchView& b, int n_heads) {
+AttnCall plan_attention(const KvView& c, const BatchView& b, const AttnArgs& a) {
   AttnCall w{};
-  const int group = n_heads / c.n_kv_heads;
+  const int group = a.group, n_heads = a.n_heads;
   w.use_tiles = (long)b.max_q_len * group > kFewRows;
   w.use_rows = !w.use_tiles || b.n_seqs > 1;
   w.few_rows = kFewRows;
   w.few_tiles = w.use_rows ? kFewRows : 0;
   w.rows.splits = w.tiles.splits = 1;
-  if (w.use_rows) w.rows = plan_attention_rows(c, b, n_heads, w.few_rows);
-  if (w.use_tiles) w.tiles = plan_attention_tiles(c, b, n_heads, w.few_tiles);
+  if (w.use_rows) w.rows = plan_attention_rows(c, b, a, w.few_rows);
+  if (w.use_tiles) w.tiles = plan_attention_tiles(c, b, a, w.few_tiles);
   size_t off = 0;
   auto take = [&](size_t& at, size_t floats) { at = off; off = align_up(off + floats * sizeof(float), 1024); };
   if (w.rows.splits > 1) {
@@ -140,6 +215,59 @@ AttnCall plan_attention(const KvView& c, const BatchView& b, int n_heads) {
   }
   w.workspace = off;
   return w;
+}
+
+// A window of 0: everything is seen, and so it is where no sequence is longer than the window.
+AttnArgs masked_args(int n_heads, const KvView& c, int causal, int window, int sinks) {
+  AttnArgs a{};
+  a.n_heads = n_heads;
+  a.group = n_heads / c.n_kv_heads;
+  a.causal = causal != 0;
+  a.window = window < kMaxKvLen ? window : 0;
+  a.sinks = sinks < kMaxKvLen ? sinks : (int)kMaxKvLen;
+  return a;
+}
+size_t attention_bytes(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, int n_heads, int window, int sinks) {
+  KvView c{};
+  BatchView b{};
+  if (check_cache(cache, &c) != HBL_OK || check_batch(batch, &b) != HBL_OK || nothing(b)) return 0;
+  if (n_heads <= 0 || n_heads > kMaxHeads || n_heads % c.n_kv_heads != 0) return 0;
+  return plan_attention(c, b, masked_args(n_heads, c, 1, window, sinks)).workspace;
+}
+int attention(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_attention_t* args, int window, int sinks, void* workspace,
+              size_t workspace_bytes, cudaStream_t s) {
+  KvView c{};
+  BatchView b{};
+  int rc = check_cache(cache, &c);
+  if (rc != HBL_OK) return rc;
+  if ((rc = check_batch(batch, &b)) != HBL_OK) return rc;
+  if (!args) return HBL_ERR_NULL;
+  if (args->n_heads <= 0 || args->n_heads % c.n_kv_heads != 0) return HBL_ERR_SHAPE;
+  if (args->n_heads > kMaxHeads) return HBL_ERR_TOO_LARGE;
+  if (!isfinite(args->sm_scale)) return HBL_ERR_SHAPE;
+  if (nothing(b) || b.max_q_len == 0) return HBL_OK;
+  if (!args->q || !args->out) return HBL_ERR_NULL;
+  if ((rc = check_strided(args->q, args->q_token_stride, args->q_head_stride)) != HBL_OK) return rc;
+  if ((rc = check_written(args->out, args->out_token_stride, args->out_head_stride, b.tokens, args->n_heads, c.head_dim)) != HBL_OK) return rc;
+  if (!aligned(args->lse, 4)) return HBL_ERR_ALIGN;
+  AttnArgs a = masked_args(args->n_heads, c, args->causal, window, sinks);
+  const AttnCall w = plan_attention(c, b, a);
+  if (w.workspace > 0 && !workspace) return HBL_ERR_NULL;
+  if (!aligned(workspace, 1024)) return HBL_ERR_ALIGN;
+  if (workspace_bytes < w.workspace) return HBL_ERR_WORKSPACE;
+  a.q = static_cast<const __nv_bfloat16*>(args->q);
+  a.out = static_cast<__nv_bfloat16*>(args->out);
+  a.lse = args->lse;
+  a.q_ts = args->q_token_stride; a.q_hs = args->q_head_stride;
+  a.o_ts = args->out_token_stride; a.o_hs = args->out_head_stride;
+  a.scale_log2 = args->sm_scale * 1.4426950408889634f;
+  char* ws = static_cast<char*>(workspace);
+  const AttnParts parts = {reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + w.rows_lse), reinterpret_cast<float*>(ws + w.tiles_o),
+                           reinterpret_cast<float*>(ws + w.tiles_lse)};
+  if (w.use_tiles && (rc = launch_attention_tiles(c, b, a, w.tiles, w.few_tiles, parts, s)) != HBL_OK) return rc;
+  if (w.use_rows && (rc = launch_attention_rows(c, b, a, w.rows, w.few_rows, parts, w.use_tiles, s)) != HBL_OK) return rc;
+  if (w.workspace > 0) return launch_attention_combine(c, b, a, w.rows, w.tiles, w.few_tiles, parts, s);
+  return HBL_OK;
 }
 
 }  // namespace
@@ -197,28 +325,40 @@ int hbl_rope(const hbl_rope_t* a, void* stream) {
                      static_cast<cudaStream_t>(stream));
 }
 
-int hbl_kv_append(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_kv_append_t* a, void* stream) {
-  KvView c{};
-  BatchView b{};
-  int rc = check_cache(cache, &c);
+int hbl_norm_rope(const hbl_norm_rope_t* a, void* stream) {
+  NormRopeCall c{};
+  const int rc = check_norm_rope(a, nullptr, &c);
+  if (rc != HBL_OK || a->tokens == 0) return rc;
+  return launch_norm_rope(c, static_cast<cudaStream_t>(stream));
+}
+
+size_t hbl_norm_rope_grad_workspace_bytes(int tokens, int n_q_heads, int n_k_heads, int head_dim) {
+  if (tokens <= 0 || n_q_heads <= 0 || n_k_heads < 0 || head_dim < 8 || head_dim > kMaxRotDim || head_dim % 8 != 0) return 0;
+  return align_up((size_t)(norm_rope_grad_blocks() + 2) * head_dim * sizeof(float), 1024);
+}
+
+int hbl_norm_rope_grad(const hbl_norm_rope_grad_t* a, void* workspace, size_t workspace_bytes, void* stream) {
+  NormRopeCall c{};
+  const int rc = check_norm_rope(a ? &a->forward : nullptr, a, &c);
   if (rc != HBL_OK) return rc;
-  if ((rc = check_batch(batch, &b)) != HBL_OK) return rc;
-  if (!a) return HBL_ERR_NULL;
-  if (c.bits != 16 && (!(a->eps > 0.0f) || !isfinite(a->eps))) return HBL_ERR_EPS;
-  if (a->table && (rc = check_rotation(a->table, a->n_pos, a->rot_dim, c.head_dim, a->layout)) != HBL_OK) return rc;
-  if (a->q && a->n_heads <= 0) return HBL_ERR_SHAPE;
-  if (nothing(b)) return HBL_OK;
-  if (!a->k || !a->v) return HBL_ERR_NULL;
-  if ((a->q != nullptr) != (a->q_out != nullptr) || (a->q && !a->table)) return HBL_ERR_NULL;
-  if ((rc = check_strided(a->k, a->k_token_stride, a->k_head_stride)) != HBL_OK) return rc;
-  if ((rc = check_strided(a->v, a->v_token_stride, a->v_head_stride)) != HBL_OK) return rc;
-  if (a->q) {
-    if ((rc = check_strided(a->q, a->q_token_stride, a->q_head_stride)) != HBL_OK) return rc;
-    if ((rc = check_written(a->q_out, a->q_out_token_stride, a->q_out_head_stride, b.tokens, a->n_heads, c.head_dim)) != HBL_OK) return rc;
-    if (a->q == a->q_out && (a->q_token_stride != a->q_out_token_stride || a->q_head_stride != a->q_out_head_stride)) return HBL_ERR_SHAPE;
+  if (c.tokens > 0 && (c.part[0].grad_gain || c.part[1].grad_gain)) {
+    if (!workspace) return HBL_ERR_NULL;
+    if (!aligned(workspace, 1024)) return HBL_ERR_ALIGN;
+    if (workspace_bytes < hbl_norm_rope_grad_workspace_bytes(c.tokens, c.part[0].n_heads, c.part[1].n_heads, c.head_dim)) return HBL_ERR_WORKSPACE;
   }
-  if (!aligned(a->positions, 4)) return HBL_ERR_ALIGN;
-  return launch_kv_append(c, b, *a, static_cast<cudaStream_t>(stream));
+  return launch_norm_rope_grad(c, static_cast<float*>(workspace), static_cast<cudaStream_t>(stream));
+}
+
+int hbl_kv_append(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_kv_append_t* a, void* stream) {
+  return append(cache, batch, a, nullptr, static_cast<cudaStream_t>(stream));
+}
+
+int hbl_kv_append_norm(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_kv_append_t* a, const hbl_head_norm_t* norm,
+                       void* stream) {
+  if (!norm) return HBL_ERR_NULL;
+  const int rc = check_gains(norm->q_gain, norm->k_gain, norm->gain_dtype, norm->norm_eps);
+  if (rc != HBL_OK) return rc;
+  return append(cache, batch, a, norm, static_cast<cudaStream_t>(stream));
 }
 
 int hbl_kv_read(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, void* k_out, void* v_out, void* stream) {
@@ -234,51 +374,23 @@ int hbl_kv_read(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, void* 
 }
 
 size_t hbl_attention_workspace_bytes(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, int n_heads) {
-  KvView c{};
-  BatchView b{};
-  if (check_cache(cache, &c) != HBL_OK || check_batch(batch, &b) != HBL_OK || nothing(b)) return 0;
-  if (n_heads <= 0 || n_heads > kMaxHeads || n_heads % c.n_kv_heads != 0) return 0;
-  return plan_attention(c, b, n_heads).workspace;
+  return attention_bytes(cache, batch, n_heads, 0, 0);
 }
 
 int hbl_attention(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_attention_t* args, void* workspace,
                   size_t workspace_bytes, void* stream) {
-  KvView c{};
-  BatchView b{};
-  int rc = check_cache(cache, &c);
-  if (rc != HBL_OK) return rc;
-  if ((rc = check_batch(batch, &b)) != HBL_OK) return rc;
-  if (!args) return HBL_ERR_NULL;
-  if (args->n_heads <= 0 || args->n_heads % c.n_kv_heads != 0) return HBL_ERR_SHAPE;
-  if (args->n_heads > kMaxHeads) return HBL_ERR_TOO_LARGE;
-  if (!isfinite(args->sm_scale)) return HBL_ERR_SHAPE;
-  if (nothing(b) || b.max_q_len == 0) return HBL_OK;
-  if (!args->q || !args->out) return HBL_ERR_NULL;
-  if ((rc = check_strided(args->q, args->q_token_stride, args->q_head_stride)) != HBL_OK) return rc;
-  if ((rc = check_written(args->out, args->out_token_stride, args->out_head_stride, b.tokens, args->n_heads, c.head_dim)) != HBL_OK) return rc;
-  if (!aligned(args->lse, 4)) return HBL_ERR_ALIGN;
-  const AttnCall w = plan_attention(c, b, args->n_heads);
-  if (w.workspace > 0 && !workspace) return HBL_ERR_NULL;
-  if (!aligned(workspace, 1024)) return HBL_ERR_ALIGN;
-  if (workspace_bytes < w.workspace) return HBL_ERR_WORKSPACE;
-  AttnArgs a{};
-  a.q = static_cast<const __nv_bfloat16*>(args->q);
-  a.out = static_cast<__nv_bfloat16*>(args->out);
-  a.lse = args->lse;
-  a.q_ts = args->q_token_stride; a.q_hs = args->q_head_stride;
-  a.o_ts = args->out_token_stride; a.o_hs = args->out_head_stride;
-  a.n_heads = args->n_heads;
-  a.group = args->n_heads / c.n_kv_heads;
-  a.causal = args->causal != 0;
-  a.scale_log2 = args->sm_scale * 1.4426950408889634f;
-  char* ws = static_cast<char*>(workspace);
-  const AttnParts parts = {reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + w.rows_lse), reinterpret_cast<float*>(ws + w.tiles_o),
-                           reinterpret_cast<float*>(ws + w.tiles_lse)};
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (w.use_tiles && (rc = launch_attention_tiles(c, b, a, w.tiles, w.few_tiles, parts, s)) != HBL_OK) return rc;
-  if (w.use_rows && (rc = launch_attention_rows(c, b, a, w.rows, w.few_rows, parts, w.use_tiles, s)) != HBL_OK) return rc;
-  if (w.workspace > 0) return launch_attention_combine(c, b, a, w.rows, w.tiles, w.few_tiles, parts, s);
-  return HBL_OK;
+  return attention(cache, batch, args, 0, 0, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+size_t hbl_attention_window_workspace_bytes(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, int n_heads, int window, int sinks) {
+  if (window < 1 || sinks < 0) return 0;
+  return attention_bytes(cache, batch, n_heads, window, sinks);
+}
+
+int hbl_attention_window(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_attention_t* args, int window, int sinks,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  if (window < 1 || sinks < 0 || (args && !args->causal)) return HBL_ERR_SHAPE;
+  return attention(cache, batch, args, window, sinks, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -77,7 +77,7 @@ struct Step {
 // Thread blocks on an SM: what the registers of a block's accumulators and steps in flight leave.
 constexpr int blocks_per_sm(int bits, int d, int nt) { return d > 128 ? 2 : nt == 1 ? 4 : bits < 16 ? 3 : 2; }
 
-template <int BITS, int D, int NT>
+template <int BITS, int D, int NT, bool WINDOW>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_rows_kernel(const __grid_constant__ RowsParams p) {
   using G = Geo<BITS, D>;
   constexpr int ROWS = 8 * NT;
@@ -103,13 +103,18 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
   const bool sane = sequence_lengths(p.b, b, p.c.page_shift, p.status, len);
   const int group = p.a.group;
   const int n_rows = min(len.q_len, p.b.max_q_len) * group, r0 = tile * ROWS;
-  if (!sane || r0 >= n_rows || n_rows > p.few || (split > 0 && (long)split * p.p.chunk >= len.held)) {      // (no such piece: the combine step knows)
+  if (!sane || r0 >= n_rows || n_rows > p.few || (split > 0 && (long)split * p.p.chunk >= min(len.held, p.p.reach))) {      // (no such piece: the combine step knows)
     if (last) grid_dependency_wait();
     return;
   }
   const int last_tok = min(r0 + ROWS - 1, n_rows - 1) / group;
-  // keys any row of the tile sees, and the piece of them that is this block's (the last piece takes what is left)
-  const int seen = p.a.causal ? max(0, min(len.held, len.kv - len.q_len + last_tok + 1)) : len.held;
+  // keys any row of the tile sees (WINDOW: indexes of them, see KeyMap), and the piece of them that is this block's (the last
+  // piece takes what is left)
+  KeyMap map = {0, 0, 0};
+  if (WINDOW) map = map_keys(p.a, len.kv - len.q_len + r0 / group);
+  auto key_of = [&](int u) { return WINDOW && u >= map.sink_end ? u + map.gap : u; };
+  const int past = len.kv - len.q_len - (WINDOW ? map.gap : 0);
+  const int seen = p.a.causal ? max(0, min(len.held - (WINDOW ? map.gap : 0), past + last_tok + 1)) : len.held;
   const int key0 = split * p.p.chunk;
   int key1 = split == p.p.splits - 1 ? seen : min(seen, key0 + p.p.chunk);
 
@@ -168,11 +173,12 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int r = r0 + nt * 8 + 2 * t + e;
-      lim[nt][e] = r >= n_rows ? 0 : p.a.causal ? len.kv - len.q_len + r / group + 1 : seen;
+      lim[nt][e] = r >= n_rows ? 0 : p.a.causal ? past + r / group + 1 : seen;
       if (r < n_rows) low = min(low, lim[nt][e]);
     }
   low = min(low, key1);
-  low = __reduce_min_sync(0xffffffffu, low);                  // below it no key needs a mask
+  low = __reduce_min_sync(0xffffffffu, low);                  // below it no key needs a mask ...
+  const int expired = past + last_tok + 1 - p.a.window;       // ... WINDOW: but for those below this that are no sinks
 
   // Per column: minus the maximum so far (0: none yet), p's sum.  `some`: every column has a maximum.
   // vr: a power of two no smaller than any value scale so far.  The weights go to the tensor core as p vs / vr * 2^7 in
@@ -195,7 +201,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
       for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
   }
 
-  const bool bos = BITS < 8 && p.c.bos_k != nullptr;
+  const bool bos = BITS < 8 && p.c.bos_k != nullptr && (!WINDOW || p.a.sinks > 0 || (map.first | map.gap) == 0);
   int bos_row = -1;
   if (bos && key0 == 0 && key1 > 0) {
     const int slot = p.b.bos_slot != nullptr ? __ldg(p.b.bos_slot + b) : b;
@@ -205,7 +211,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
   const int* page_row = p.b.pages + (long)b * p.b.max_pages;
 
   // scores (c: keys g and g + 8, columns 2t and 2t + 1) to P^T fragments, with the running maximum.
-  // masked: keys beyond a column's limit, and key 0 where skip_first, do not count.
+  // masked: keys beyond a column's limit, or before its window, and key 0 where skip_first, do not count.
   auto softmax = [&](float (&c)[NT][4], int kb, const float (&ks)[2], const float (&vs)[2], bool masked, bool skip_first,
                      uint32_t (&pf)[NT][2]) {
     float top = -INFINITY;
@@ -218,6 +224,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
         if (masked) {
           const int key = kb + g + (e >> 1) * 8;
           if (key >= min(lim[nt][e & 1], key1) || (skip_first && key == 0)) c[nt][e] = -INFINITY;
+          if (WINDOW && key >= p.a.sinks && key < lim[nt][e & 1] - p.a.window) c[nt][e] = -INFINITY;
         }
         top = fmaxf(top, c[nt][e]);
       }
@@ -230,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
         for (int h = 0; h < 2; ++h) {
           const uint32_t x = __float_as_uint(fabsf(vs[h]));
           const int key = kb + g + 8 * h;
-          if (x < 0x7F000000u && key < key1) v = max(v, x);
+          if (x < 0x7F000000u && key < key1 && (!WINDOW || key >= map.first || key < p.a.sinks)) v = max(v, x);
         }
         v = (__reduce_max_sync(0xffffffffu, v) + 0x7FFFFFu) & 0x7F800000u;
         const float to = fmaxf(vr, __uint_as_float(v));
@@ -335,11 +342,11 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
   const float* vsp = CODES ? p.c.v_scale + g : nullptr;
   const uint32_t page_rows = (uint32_t)p.c.n_kv_heads << p.c.page_shift, head_rows = (uint32_t)head << p.c.page_shift;
   const int slot_mask = (1 << p.c.page_shift) - 1;
-  auto page_of = [&](int kb) { return kb < key1 ? __ldg(page_row + (kb >> p.c.page_shift)) : -1; };
+  auto page_of = [&](int kb) { return kb < key1 ? __ldg(page_row + (key_of(kb) >> p.c.page_shift)) : -1; };
   auto load = [&](Step<BITS, D>& s, int kb, int page) {
     const bool here = page >= 0 && page < p.c.n_pages;         // (-1 beyond the last key)
     if (here) {
-      const uint32_t row0 = (uint32_t)page * page_rows + head_rows + (uint32_t)(kb & slot_mask);
+      const uint32_t row0 = (uint32_t)page * page_rows + head_rows + (uint32_t)(key_of(kb) & slot_mask);
       const unsigned char* k = kp + (uint64_t)row0 * G::ROW_BYTES;
       const unsigned char* v = vp + (uint64_t)row0 * G::ROW_BYTES;
 #pragma unroll
@@ -373,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
         if (!here[d]) {
           report_device_error(p.status, HBL_ERR_RANGE);
         } else {
-          const bool masked = kb + 16 > low || (bos && kb == 0);
+          const bool masked = kb + 16 > low || (bos && kb == 0) || (WINDOW && kb < expired && kb + 16 > p.a.sinks);
           if (!CODES && masked) {
             // 0 * a value that is not finite would reach the columns it is masked for: such values become zeros, and the
             // columns that do see their key are marked; what lies beyond the last key becomes zeros, whatever it is
@@ -396,8 +403,10 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                  const int n_seen = min(lim[nt][e], key1) - kb;
-                  if (n_seen > 0 && (bad & (n_seen >= 16 ? 0xFFFFu : (1u << n_seen) - 1))) poison |= 1u << (2 * nt + e);
+                  auto below = [&](int u) { return u >= kb + 16 ? 0xFFFFu : u > kb ? (1u << (u - kb)) - 1 : 0u; };
+                  uint32_t visible = below(min(lim[nt][e], key1));
+                  if (WINDOW) visible &= ~below(lim[nt][e] - p.a.window) | below(p.a.sinks);
+                  if (bad & visible) poison |= 1u << (2 * nt + e);
                 }
             }
           }
@@ -536,7 +545,8 @@ __global__ void __launch_bounds__(256) attn_combine_kernel(const __grid_constant
   const float *part_o = nullptr, *part_lse = nullptr;
   long row = 0, total_rows = 0;                               // in the parts
   auto pieces_of = [&](const AttnPlan& plan, const SeqLens& len) {
-    return plan.splits > 1 ? max(1, min(plan.splits, (len.held + plan.chunk - 1) / plan.chunk)) : 0;      // (0: written whole)
+    const int held = min(len.held, plan.reach);
+    return plan.splits > 1 ? max(1, min(plan.splits, (held + plan.chunk - 1) / plan.chunk)) : 0;      // (0: written whole)
   };
   SeqLens len;
   int b = p.b.n_seqs;
@@ -627,25 +637,29 @@ long most_rows(const BatchView& b, int group, int few) {
 }
 int rows_per_tile(const BatchView& b, int group, int few) { return most_rows(b, group, few) > 8 ? 16 : 8; }
 
-template <int BITS, int D>
+template <int BITS, int D, bool WINDOW>
 int launch_rows_dim(RowsParams& p, cudaStream_t s) {
   const long blocks = (long)p.b.n_seqs * p.c.n_kv_heads * p.p.tiles * p.p.splits;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
   if (rows_per_tile(p.b, p.a.group, p.few) == 8)
-    HBL_CUDA_OK(launch_waiting(attn_rows_kernel<BITS, D, 1>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+    HBL_CUDA_OK(launch_waiting(attn_rows_kernel<BITS, D, 1, WINDOW>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
   else
-    HBL_CUDA_OK(launch_waiting(attn_rows_kernel<BITS, D, 2>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+    HBL_CUDA_OK(launch_waiting(attn_rows_kernel<BITS, D, 2, WINDOW>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
   note_launch();
   return HBL_OK;
 }
-template <int BITS>
-int launch_rows_bits(RowsParams& p, cudaStream_t s) {
+template <int BITS, bool WINDOW>
+int launch_rows_window(RowsParams& p, cudaStream_t s) {
   switch (p.c.head_dim) {
-    case 64: return launch_rows_dim<BITS, 64>(p, s);
-    case 128: return launch_rows_dim<BITS, 128>(p, s);
-    case 256: return launch_rows_dim<BITS, 256>(p, s);
+    case 64: return launch_rows_dim<BITS, 64, WINDOW>(p, s);
+    case 128: return launch_rows_dim<BITS, 128, WINDOW>(p, s);
+    case 256: return launch_rows_dim<BITS, 256, WINDOW>(p, s);
     default: return HBL_ERR_SHAPE;
   }
+}
+template <int BITS>
+int launch_rows_bits(RowsParams& p, cudaStream_t s) {
+  return p.a.window > 0 ? launch_rows_window<BITS, true>(p, s) : launch_rows_window<BITS, false>(p, s);
 }
 
 // How many pieces the keys of a sequence are dealt in.
@@ -683,17 +697,18 @@ long pieces_of_keys(long base, int resident, long keys, long most, int bits) {
 
 }  // namespace
 
-AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads, int few) {
+AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, int few) {
   AttnPlan p{};
-  const int group = n_heads / c.n_kv_heads, rows = rows_per_tile(b, group, few);
+  const int group = a.group, rows = rows_per_tile(b, group, few);
   p.cap = (int)most_rows(b, group, few);
   p.tiles = (p.cap + rows - 1) / rows;
-  const long base = (long)b.n_seqs * c.n_kv_heads * p.tiles;
-  const long most = b.max_kv_len <= 512 ? 1 : ((long)b.max_kv_len + 255) / 256;
-  const long n = pieces_of_keys(base, blocks_per_sm(c.bits, c.head_dim, rows / 8), b.max_kv_len, most, c.bits);
-  p.chunk = (int)((((long)b.max_kv_len + n - 1) / n + 63) / 64 * 64);
+  p.reach = reach_of(a, rows);
+  const long base = (long)b.n_seqs * c.n_kv_heads * p.tiles, keys = b.max_kv_len < p.reach ? b.max_kv_len : p.reach;
+  const long most = keys <= 512 ? 1 : (keys + 255) / 256;
+  const long n = pieces_of_keys(base, blocks_per_sm(c.bits, c.head_dim, rows / 8), keys, most, c.bits);
+  p.chunk = (int)(((keys + n - 1) / n + 63) / 64 * 64);
   if (p.chunk < 64) p.chunk = 64;
-  p.splits = (int)(((long)b.max_kv_len + p.chunk - 1) / p.chunk);
+  p.splits = (int)((keys + p.chunk - 1) / p.chunk);
   if (p.splits < 1) p.splits = 1;
   return p;
 }
@@ -707,7 +722,7 @@ int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a
   // 190 us in the batch's order, 175 in this; 128 of 8 key heads 113, 92; all of one length 275, 278).  Not for short ones, whose
   // blocks would spend more on the look-up than it saves (up to 600 tokens: 59 us, 64), nor for batches whose look-up is long.
   const long slots = (long)sm_count() * blocks_per_sm(c.bits, c.head_dim, rows_per_tile(b, a.group, few) / 8);
-  p.ordered = plan.splits == 1 && b.max_kv_len >= 1024 && b.n_seqs <= 128 && (long)b.n_seqs * c.n_kv_heads * plan.tiles > slots;
+  p.ordered = plan.splits == 1 && b.max_kv_len >= 1024 && plan.reach >= b.max_kv_len && b.n_seqs <= 128 && (long)b.n_seqs * c.n_kv_heads * plan.tiles > slots;
   p.status = device_status_word();
   if (p.status == nullptr) return HBL_ERR_CUDA;
   switch (c.bits) {

@@ -202,14 +202,16 @@ struct Item {
   int r0, n_rows;                // rows of the item, of the sequence
   int key0, key1;                // keys of the piece that any row sees
   int tiles;                     // of BK keys; -1: no more items
+  KeyMap map;                    // WINDOW: what `past` and the keys count, see there
+  int expired;                   // ... keys below it, but for the sinks, are masked by some row
 };
-// The first tile of a causal item in which some row masks a key.
+// The first tile of a causal item in which some row masks a key that is not its past.
 template <int D>
 __device__ __forceinline__ int first_masked(const TilesParams& p, const Item& w) {
   return max(0, w.past + token_of(p, w.r0) + 1 - w.key0) / TileGeo<D>::BK;
 }
 // The whole warp takes part.  False: nothing to do.
-template <int D>
+template <int D, bool WINDOW>
 __device__ __forceinline__ bool decode_item(const TilesParams& p, int item, int lane, Item& o) {
   using G = TileGeo<D>;
   o.split = item % p.p.splits;
@@ -250,9 +252,14 @@ __device__ __forceinline__ bool decode_item(const TilesParams& p, int item, int 
   o.past = len.kv - len.q_len;
   o.n_rows = min(len.q_len, p.b.max_q_len) * p.a.group;
   o.r0 = mine * G::ROWS;
-  if (o.split > 0 && (long)o.split * p.p.chunk >= len.held) return false;
+  if (o.split > 0 && (long)o.split * p.p.chunk >= min(len.held, p.p.reach)) return false;
   const int last_tok = token_of(p, min(o.r0 + G::ROWS - 1, o.n_rows - 1));
-  const int seen = p.a.causal ? max(0, min(len.held, o.past + last_tok + 1)) : len.held;
+  if (WINDOW) {
+    o.map = map_keys(p.a, o.past + token_of(p, o.r0));
+    o.past -= o.map.gap;
+    o.expired = o.past + last_tok + 1 - p.a.window;
+  }
+  const int seen = p.a.causal ? max(0, min(len.held - (WINDOW ? o.map.gap : 0), o.past + last_tok + 1)) : len.held;
   o.key0 = o.split * p.p.chunk;
   o.key1 = o.split == p.p.splits - 1 ? seen : min(seen, o.key0 + p.p.chunk);
   o.tiles = o.key1 > o.key0 ? (o.key1 - o.key0 + G::BK - 1) / G::BK : 0;
@@ -267,7 +274,7 @@ __device__ __forceinline__ void store16(uint32_t saddr, const uint32_t (&w)[4]) 
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(saddr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
 }
 
-template <int BITS, int D>
+template <int BITS, int D, bool WINDOW>
 __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_constant__ TilesParams p) {
   using G = TileGeo<D>;
   constexpr int NSUB = G::NSUB, BK = G::BK, STAGES = G::STAGES;
@@ -368,6 +375,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
       for (int i = 0; i < R; ++i)
         if (first + 8 * i < w.n_rows) low = min(low, limit(i));
       low = __reduce_min_sync(0xffffffffu, low);
+      auto from = [&](int i) { return w.past + token_of(p, first + 8 * i) + 1 - p.a.window; };     // WINDOW: where row i's begins
+      int expired = 0;                                         // below it some row of the warp masks what is no sink
+      if (WINDOW) {
+        int most = -0x40000000;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+          if (first + 8 * i < w.n_rows) most = max(most, from(i));
+        expired = __reduce_max_sync(0xffffffffu, most);
+      }
       float neg[R], l[R];                                      // minus the maximum so far (0: none yet, see `some`), p's sum
       uint32_t some = 0;                                       // rows that have seen a key
       float unit = 1.f;                                        // codes: O is in units of it
@@ -412,6 +428,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
             for (int q = 0; q < NP; ++q) {
               if (STEP * q >= seen) x[at(i, q)] = -INFINITY;
               if (STEP * q + 1 >= seen) x[at(i, q) + 1] = -INFINITY;
+            }
+          }
+        }
+        if (WINDOW && k0 < expired && k0 + BK > p.a.sinks) {
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            const int begin = from(i) - k0 - 2 * t, keep = p.a.sinks - k0 - 2 * t;
+#pragma unroll
+            for (int q = 0; q < NP; ++q) {
+              if (STEP * q < begin && STEP * q >= keep) x[at(i, q)] = -INFINITY;
+              if (STEP * q + 1 < begin && STEP * q + 1 >= keep) x[at(i, q) + 1] = -INFINITY;
             }
           }
         }
@@ -530,8 +557,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
             for (int i = 0; i < R; ++i) {
               const int seen = limit(i) - k0;
               for (int e = 0; e < BK / 32; ++e) {
-                const int n_seen = seen - 32 * e;
-                if (word[e] & (n_seen <= 0 ? 0u : n_seen >= 32 ? ~0u : (1u << n_seen) - 1)) some |= 16u << i;
+                auto below = [&](int n) { return n <= 32 * e ? 0u : n >= 32 * e + 32 ? ~0u : (1u << (n - 32 * e)) - 1; };
+                uint32_t visible = below(seen);
+                if (WINDOW) visible &= ~below(from(i) - k0) | below(p.a.sinks - k0);
+                if (word[e] & visible) some |= 16u << i;
               }
             }
           }
@@ -663,23 +692,28 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
       if (w.tiles == 0) continue;
       const int* page_row = p.b.pages + (long)w.b * p.b.max_pages;
       // pages of a tile's 16-key groups, one to a lane (a tile starts on a multiple of 64 keys; a group lies in one page)
+      auto key_of = [&](int u) { return WINDOW && u >= w.map.sink_end ? u + w.map.gap : u; };
       auto page_of = [&](int j) {
         const int key = w.key0 + j * BK + 16 * lane;
-        return lane < BK / 16 && key < w.key1 ? __ldg(page_row + (key >> p.c.page_shift)) : -1;
+        return lane < BK / 16 && key < w.key1 ? __ldg(page_row + (key_of(key) >> p.c.page_shift)) : -1;
       };
-      struct Tile { long group_row; unsigned good; int there; };
+      struct Tile { long group_row; unsigned good; int there, keep, begin; };
       auto open = [&](int j, int page) {
         const int k0 = w.key0 + j * BK;
         const bool in = page >= 0 && page < p.c.n_pages;
         if (lane < BK / 16 && k0 + 16 * lane < w.key1 && !in) report_device_error(p.status, HBL_ERR_RANGE);
         Tile t;
-        t.group_row = cache_row(p.c, in ? page : 0, w.head, (k0 + 16 * lane) & ((1 << p.c.page_shift) - 1));
+        t.group_row = cache_row(p.c, in ? page : 0, w.head, key_of(k0 + 16 * lane) & ((1 << p.c.page_shift) - 1));
         t.good = __ballot_sync(0xffffffffu, in);
         t.there = w.key1 - k0;                                  // keys of the tile that exist
+        if (WINDOW) {                                           // ... but for those that no row sees
+          t.keep = p.a.sinks - k0;
+          t.begin = w.map.first - k0;
+        }
         return t;
       };
       auto row_of = [&](const Tile& t, int rr) { return __shfl_sync(0xffffffffu, t.group_row, rr >> 4) + (rr & 15); };
-      auto live = [&](const Tile& t, int rr) { return rr < t.there && (t.good >> (rr >> 4) & 1); };
+      auto live = [&](const Tile& t, int rr) { return rr < t.there && (t.good >> (rr >> 4) & 1) && (!WINDOW || rr >= t.begin || rr < t.keep); };
       int next_page = page_of(0);
       Tile tile = open(0, next_page);
       next_page = page_of(1);
@@ -703,7 +737,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
               copy16(dst + chunk_at(rr, tid % CH, G::HALF), col + row_of(tile, rr) * (2 * D), live(tile, rr));
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
-            if (kv == 1 && j >= masked_from) {
+            if (kv == 1 && (j >= masked_from || (WINDOW && w.key0 + j * BK < w.expired && w.key0 + (j + 1) * BK > p.a.sinks))) {
               // A tile that some row masks: 0 * a value that is not finite would reach rows that mask its key.  Every thread
               // looks through the pieces that it has copied; such a key's value becomes zeros and the key itself NaN, so
               // that the rows that see it, and no others, become NaN.  (The same lanes hold a row's pieces of both.)
@@ -748,7 +782,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         }
       } else {
         int bos_row = -1;
-        if (BITS < 8 && p.c.bos_k != nullptr && w.key0 == 0) {
+        const bool bos = BITS < 8 && p.c.bos_k != nullptr && (!WINDOW || p.a.sinks > 0 || (w.map.first | w.map.gap) == 0);
+        if (bos && w.key0 == 0) {
           const int slot = p.b.bos_slot != nullptr ? __ldg(p.b.bos_slot + w.b) : w.b;
           if (slot >= 0 && slot < p.c.n_slots) bos_row = slot;
           else if (tid == 0) report_device_error(p.status, HBL_ERR_RANGE);
@@ -794,7 +829,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         load_scales(tile);
         for (int j = 0; j < w.tiles; ++j, ++it) {
           const int stage = it % STAGES;
-          const bool special = BITS < 8 && w.key0 + j == 0 && p.c.bos_k != nullptr, more = j + 1 < w.tiles;
+          const bool special = bos && w.key0 + j == 0, more = j + 1 < w.tiles;
           Tile after = tile;
           if (more) after = open(j + 1, next_page);
           next_page = page_of(j + 2);
@@ -969,7 +1004,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
       Item w;
       int item = blockIdx.x;
       for (uint32_t n = 0; ok; ++n) {
-        if (decode_item<D>(p, item, lane, w)) {
+        if (decode_item<D, WINDOW>(p, item, lane, w)) {
           give(w);
           // (a long wait, which the softmax warp beside this one should not notice)
           for (int i = 0; ok && i < 1000000 && !mbar_try(&near_end, (made - 1) & 1) && !*abort_flag; ++i) __nanosleep(500);
@@ -1055,29 +1090,35 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
   }
 }
 
-template <int BITS, int D>
+template <int BITS, int D, bool WINDOW>
 int launch_tiles_dim(TilesParams& p, cudaStream_t s) {
-  auto kern = attn_tiles_kernel<BITS, D>;
+  auto kern = attn_tiles_kernel<BITS, D, WINDOW>;
   HBL_ALLOW_DYNAMIC_SMEM(kern, TileGeo<D>::SMEM);
   HBL_CUDA_OK(launch_waiting(kern, dim3(p.items), dim3(kThreads), TileGeo<D>::SMEM, s, p));
   note_launch();
   return HBL_OK;
 }
-template <int BITS>
-int launch_tiles_bits(TilesParams& p, cudaStream_t s) {
+template <int BITS, bool WINDOW>
+int launch_tiles_window(TilesParams& p, cudaStream_t s) {
   switch (p.c.head_dim) {
-    case 64: return launch_tiles_dim<BITS, 64>(p, s);
-    case 128: return launch_tiles_dim<BITS, 128>(p, s);
-    case 256: return launch_tiles_dim<BITS, 256>(p, s);
+    case 64: return launch_tiles_dim<BITS, 64, WINDOW>(p, s);
+    case 128: return launch_tiles_dim<BITS, 128, WINDOW>(p, s);
+    case 256: return launch_tiles_dim<BITS, 256, WINDOW>(p, s);
     default: return HBL_ERR_SHAPE;
   }
+}
+template <int BITS>
+int launch_tiles_bits(TilesParams& p, cudaStream_t s) {
+  return p.a.window > 0 ? launch_tiles_window<BITS, true>(p, s) : launch_tiles_window<BITS, false>(p, s);
 }
 
 }  // namespace
 
-AttnPlan plan_attention_tiles(const KvView& c, const BatchView& b, int n_heads, int few) {
+AttnPlan plan_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& a, int few) {
   AttnPlan p{};
-  const int group = n_heads / c.n_kv_heads, rows = c.head_dim == 256 ? 128 : 256;
+  const int group = a.group, rows = c.head_dim == 256 ? 128 : 256;
+  p.reach = reach_of(a, rows);
+  const long keys = b.max_kv_len < p.reach ? b.max_kv_len : p.reach;
   // Whole tiles of all sequences together, and a partial one for each that has more than `few` rows.
   const long all = (long)b.tokens * group;
   const long partial = all / (few + 1) < b.n_seqs ? all / (few + 1) : b.n_seqs;
@@ -1089,13 +1130,13 @@ AttnPlan plan_attention_tiles(const KvView& c, const BatchView& b, int n_heads, 
   // pieces of at least 1024 keys while there are fewer items than SMs, and of at most 2^24 (131072 tiles, some 0.3 s): the
   // kernel's bounded waits, of 2 s, last as long as an item
   const long want = base > 0 && base < sm_count() ? sm_count() / base : 1;
-  const long most = ((long)b.max_kv_len + 1023) / 1024, least = ((long)b.max_kv_len + (1L << 24) - 1) >> 24;
+  const long most = (keys + 1023) / 1024, least = (keys + (1L << 24) - 1) >> 24;
   long n = want < most ? want : most;
   if (n < least) n = least;
   if (n < 1) n = 1;
-  p.chunk = (int)((((long)b.max_kv_len + n - 1) / n + 127) / 128 * 128);
+  p.chunk = (int)(((keys + n - 1) / n + 127) / 128 * 128);
   if (p.chunk < 128) p.chunk = 128;
-  p.splits = (int)(((long)b.max_kv_len + p.chunk - 1) / p.chunk);
+  p.splits = (int)((keys + p.chunk - 1) / p.chunk);
   if (p.splits < 1) p.splits = 1;
   return p;
 }

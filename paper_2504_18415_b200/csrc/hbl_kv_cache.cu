@@ -13,6 +13,7 @@
 // pairs are loaded once for all of them, and their loads are in flight together.  The loads of the data depend on the
 // number of rows that there are, but not on that chain, and are issued before it.
 #include "hbl_kv_cache.cuh"
+#include "hbl_piece.cuh"
 
 namespace hbl {
 namespace {
@@ -61,6 +62,9 @@ struct AppendParams {
   int* status;
   int n_heads, n_pos, rot_dim, blocks_per_token, groups;       // n_heads 0: no queries; groups: heads side by side in a block
   float eps;
+  const void *q_gain, *k_gain;                                 // hbl_kv_append_norm; NULL: ones
+  int gain_bf16;
+  float norm_eps;
 };
 
 // Where a token goes: the block's token t, looked up by every warp for itself.  False: nowhere (reported, or behind the
@@ -94,7 +98,9 @@ __device__ __forceinline__ bool find_place(const KvView& c, const BatchView& s, 
 // of a warp's heads are queries, or keys, or values, and what depends on that is decided once for the warp.
 // (Four 2048-token prompts of 96 heads: 8 bits 153 us without, 132 with it, bf16 81 and 72, 3 bits 151 and 148.)
 // Six heads to a thread at 3 and 4 bits: kept to 64 registers (4 bits 137 us; 171 with the 96 that it would take).
-template <int BITS, int LPH, bool INTERLEAVED, int ROWS, bool EVEN>
+// NORM: queries and keys are r R(gain x), r = 1 / sqrt(mean x^2 + eps).  R is linear, so r goes last; x's squares are summed in fp64
+// (a bf16 value's is exact) and r is rounded once, so that a key's codes are those of the fp32 formula, bit for bit.
+template <int BITS, int LPH, bool INTERLEAVED, int ROWS, bool EVEN, bool NORM>
 __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int HPW = 32 / LPH;                               // heads side by side in a warp
   const int groups = p.groups;                                // ... and in the block
@@ -155,6 +161,27 @@ __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_ap
     float (&x)[8] = f[BITS == 16 ? 0 : i];
     top[i] = 0;
     widen8(raw[i], x);
+    float inv = 1.f;                                           // (times one: a value)
+    const void* gain = nullptr;
+    if constexpr (NORM) {
+      if (EVEN ? r < first_v : __any_sync(0xffffffffu, r < first_v)) {
+        double sum = 0.0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = fma((double)x[e], (double)x[e], sum);
+#pragma unroll
+        for (int o = LPH / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (r < first_v) {
+          inv = inverse_root(sum / (8 * LPH) + (double)p.norm_eps);
+          gain = r < p.n_heads ? p.q_gain : p.k_gain;
+          if (gain != nullptr) {
+            float g[8];
+            load_gain(gain, p.gain_bf16, 8 * j, g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = __fmul_rn(x[e], g[e]);
+          }
+        }
+      }
+    }
     const bool rotate = turned && r < first_v;
     if (EVEN ? p.table != nullptr && r < first_v : __any_sync(0xffffffffu, rotate)) {      // (the whole warp: it shuffles)
       if constexpr (!INTERLEAVED) {
@@ -166,6 +193,12 @@ __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_ap
         if (rotate) {
           float g[8];
           widen8(other, g);
+          if (NORM && gain != nullptr) {
+            float h[8];
+            load_gain(gain, p.gain_bf16, 8 * (upper ? j - half8 : j + half8), h);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] = __fmul_rn(g[e], h[e]);
+          }
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = __fadd_rn(__fmul_rn(x[e], c[e]), __fmul_rn(g[e], s[e]));
         }
@@ -177,6 +210,10 @@ __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_ap
           x[2 * e + 1] = __fsub_rn(__fmul_rn(x2, c[e]), __fmul_rn(x1, s[e]));
         }
       }
+    }
+    if constexpr (NORM) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = __fmul_rn(x[e], inv);
     }
     if (r < p.n_heads) {
       *reinterpret_cast<uint4*>(p.q_out + t * p.qo_ts + r * p.qo_hs + (rest * p.qo_hs + 8 * j)) = narrow8(x);
@@ -338,40 +375,44 @@ Deal deal(int rows, int lph, int rows_per_thread) {
   d.groups = (need + warp - 1) / warp * warp;
   return d;
 }
-template <int BITS, int LPH, bool INTERLEAVED, int ROWS, bool EVEN>
+template <int BITS, int LPH, bool INTERLEAVED, int ROWS, bool EVEN, bool NORM>
 int launch_append_rows(AppendParams& p, cudaStream_t s) {
   const Deal d = deal(p.n_heads + 2 * p.c.n_kv_heads, LPH, ROWS);
   p.blocks_per_token = d.blocks;
   p.groups = d.groups;
   const long blocks = (long)p.b.tokens * d.blocks;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
-  HBL_CUDA_OK(launch_waiting(kv_append_kernel<BITS, LPH, INTERLEAVED, ROWS, EVEN>, dim3((unsigned)blocks), dim3(d.groups * LPH), 0, s, p));
+  HBL_CUDA_OK(launch_waiting(kv_append_kernel<BITS, LPH, INTERLEAVED, ROWS, EVEN, NORM>, dim3((unsigned)blocks), dim3(d.groups * LPH), 0, s, p));
   note_launch();
   return HBL_OK;
 }
 // One head to a thread for a decoding step, whose latency counts.  Where the call fills the GPU six (four 2048-token prompts
 // of 96 heads at 3 bits: 148 us; four or three heads 163, two 180; 48 heads 64, 71, 70, 75), or four at head_dim 256, where six
 // run out of registers (341 us against 291).
-template <int BITS, int LPH, bool INTERLEAVED, bool EVEN>
+template <int BITS, int LPH, bool INTERLEAVED, bool EVEN, bool NORM>
 int launch_append_layout(AppendParams& p, cudaStream_t s) {
   if ((long)p.b.tokens * (p.n_heads + 2 * p.c.n_kv_heads) * LPH < (long)sm_count() * 2048 * 4)
-    return launch_append_rows<BITS, LPH, INTERLEAVED, 1, EVEN>(p, s);
-  return launch_append_rows<BITS, LPH, INTERLEAVED, LPH < 32 ? 6 : 4, EVEN>(p, s);
+    return launch_append_rows<BITS, LPH, INTERLEAVED, 1, EVEN, NORM>(p, s);
+  return launch_append_rows<BITS, LPH, INTERLEAVED, LPH < 32 ? 6 : 4, EVEN, NORM>(p, s);
 }
-template <int BITS, int LPH>
+template <int BITS, int LPH, bool NORM>
 int launch_append_heads(AppendParams& p, bool interleaved, cudaStream_t s) {
   if ((p.n_heads | p.c.n_kv_heads) % (32 / LPH) == 0)
-    return interleaved ? launch_append_layout<BITS, LPH, true, true>(p, s) : launch_append_layout<BITS, LPH, false, true>(p, s);
-  return interleaved ? launch_append_layout<BITS, LPH, true, false>(p, s) : launch_append_layout<BITS, LPH, false, false>(p, s);
+    return interleaved ? launch_append_layout<BITS, LPH, true, true, NORM>(p, s) : launch_append_layout<BITS, LPH, false, true, NORM>(p, s);
+  return interleaved ? launch_append_layout<BITS, LPH, true, false, NORM>(p, s) : launch_append_layout<BITS, LPH, false, false, NORM>(p, s);
 }
-template <int BITS>
-int launch_append_bits(AppendParams& p, bool interleaved, cudaStream_t s) {
+template <int BITS, bool NORM>
+int launch_append_dim(AppendParams& p, bool interleaved, cudaStream_t s) {
   switch (p.c.head_dim) {
-    case 64: return launch_append_heads<BITS, 8>(p, interleaved, s);
-    case 128: return launch_append_heads<BITS, 16>(p, interleaved, s);
-    case 256: return launch_append_heads<BITS, 32>(p, interleaved, s);
+    case 64: return launch_append_heads<BITS, 8, NORM>(p, interleaved, s);
+    case 128: return launch_append_heads<BITS, 16, NORM>(p, interleaved, s);
+    case 256: return launch_append_heads<BITS, 32, NORM>(p, interleaved, s);
     default: return HBL_ERR_SHAPE;
   }
+}
+template <int BITS>
+int launch_append_bits(AppendParams& p, bool interleaved, bool norm, cudaStream_t s) {
+  return norm ? launch_append_dim<BITS, true>(p, interleaved, s) : launch_append_dim<BITS, false>(p, interleaved, s);
 }
 
 template <int BITS, int LPH, int ROWS>
@@ -403,7 +444,7 @@ int launch_read_bits(ReadParams& p, cudaStream_t s) {
 
 }  // namespace
 
-int launch_kv_append(const KvView& c, const BatchView& b, const hbl_kv_append_t& a, cudaStream_t s) {
+int launch_kv_append(const KvView& c, const BatchView& b, const hbl_kv_append_t& a, const hbl_head_norm_t* norm, cudaStream_t s) {
   AppendParams p{};
   p.c = c; p.b = b;
   p.k = static_cast<const __nv_bfloat16*>(a.k); p.v = static_cast<const __nv_bfloat16*>(a.v);
@@ -415,12 +456,15 @@ int launch_kv_append(const KvView& c, const BatchView& b, const hbl_kv_append_t&
   p.n_pos = a.n_pos; p.rot_dim = a.table != nullptr ? a.rot_dim : 0; p.eps = a.eps;
   p.status = device_status_word();
   if (p.status == nullptr) return HBL_ERR_CUDA;
+  if (norm != nullptr) {
+    p.q_gain = norm->q_gain; p.k_gain = norm->k_gain; p.gain_bf16 = norm->gain_dtype == HBL_BF16; p.norm_eps = norm->norm_eps;
+  }
   const bool inter = a.layout == HBL_ROPE_INTERLEAVED;
   switch (c.bits) {
-    case 3: return launch_append_bits<3>(p, inter, s);
-    case 4: return launch_append_bits<4>(p, inter, s);
-    case 8: return launch_append_bits<8>(p, inter, s);
-    case 16: return launch_append_bits<16>(p, inter, s);
+    case 3: return launch_append_bits<3>(p, inter, norm != nullptr, s);
+    case 4: return launch_append_bits<4>(p, inter, norm != nullptr, s);
+    case 8: return launch_append_bits<8>(p, inter, norm != nullptr, s);
+    case 16: return launch_append_bits<16>(p, inter, norm != nullptr, s);
     default: return HBL_ERR_BITS;
   }
 }

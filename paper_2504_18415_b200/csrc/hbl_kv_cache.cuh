@@ -69,7 +69,25 @@ int launch_rope_table(const double* freq, int n_freq, double amplitude, int firs
 int launch_rope(const void* x, int dtype, int tokens, int n_heads, int head_dim, long x_ts, long x_hs, const int32_t* positions,
                 const float* table, int n_pos, int rot_dim, int layout, int backward, void* out, long o_ts, long o_hs,
                 cudaStream_t s);
-int launch_kv_append(const KvView& c, const BatchView& b, const hbl_kv_append_t& a, cudaStream_t s);
+// Heads normalised and rotated (queries, keys), or the gradients of that.
+struct NormRopePart {
+  const void *x, *grad, *gain;         // grad: backward only;  gain NULL: ones
+  void* out;                           // o, or dx
+  float* grad_gain;                    // NULL: not wanted
+  long x_ts, x_hs, o_ts, o_hs, g_ts, g_hs;
+  int n_heads;
+};
+struct NormRopeCall {
+  NormRopePart part[2];
+  const int32_t* positions;
+  const float* table;                  // NULL: nothing is rotated
+  int dtype, gain_dtype, tokens, head_dim, n_pos, rot_dim, interleaved;
+  float norm_eps;
+};
+int norm_rope_grad_blocks();
+int launch_norm_rope(const NormRopeCall& c, cudaStream_t s);
+int launch_norm_rope_grad(const NormRopeCall& c, float* partial, cudaStream_t s);
+int launch_kv_append(const KvView& c, const BatchView& b, const hbl_kv_append_t& a, const hbl_head_norm_t* norm, cudaStream_t s);
 int launch_kv_read(const KvView& c, const BatchView& b, void* k_out, void* v_out, cudaStream_t s);
 
 struct AttnArgs {
@@ -79,15 +97,36 @@ struct AttnArgs {
   long q_ts, q_hs, o_ts, o_hs;
   int n_heads, group, causal;
   float scale_log2;                    // sm_scale * log2(e): scores in units of log2
+  int window, sinks;                   // hbl_attention_window (causal); window 0: everything is seen
 };
+// Which keys a tile of query rows goes over when there is a window: those before the first row's window are left out, apart
+// from the sinks, in whole groups of 16 (a group lies in one page).  Kernels count the keys that are left: index u is key u below
+// `sink_end` and key u + gap from there on.  A row at position pos sees the u < lim = pos + 1 - gap that are
+// >= lim - window or < sinks.  first: the first of the first row's window.
+struct KeyMap { int sink_end, gap, first; };
+__device__ __forceinline__ KeyMap map_keys(const AttnArgs& a, int first_pos) {
+  const int low = max(0, max(first_pos + 1, 0) - a.window);
+  KeyMap m;
+  m.sink_end = (min(a.sinks, low) + 15) & ~15;
+  m.gap = max(0, (low & ~15) - m.sink_end);
+  m.first = low - m.gap;
+  return m;
+}
+// Keys that a tile of `rows` query rows goes over at most.
+constexpr long kMaxWindow = 1L << 30;
+inline int reach_of(const AttnArgs& a, int rows) {
+  const long n = ((long)a.sinks + 15) / 16 * 16 + a.window + 16 + rows;
+  return a.window > 0 && n < kMaxWindow ? (int)n : (int)kMaxWindow;
+}
 // How a call is split: the keys of a sequence go to `splits` thread blocks in pieces of `chunk`.
 // The pieces' results wait in the workspace: `cap` rows (queries of one key head) for every sequence and key head from the
 // streaming kernel, all rows of the call from the tiles.
-struct AttnPlan { int splits, chunk, tiles, cap; };
+// A tile of rows goes over at most `reach` keys of its sequence.
+struct AttnPlan { int splits, chunk, tiles, cap, reach; };
 struct AttnParts { float *rows_o, *rows_lse, *tiles_o, *tiles_lse; };      // [splits][rows][head_dim], [splits][rows]
 // Sequences of up to `few` query rows (tokens times heads that share a key head) go to one kernel, the others to the other.
-AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, int n_heads, int few);
-AttnPlan plan_attention_tiles(const KvView& c, const BatchView& b, int n_heads, int few);
+AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, int few);
+AttnPlan plan_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& a, int few);
 int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, int few, const AttnParts& w,
                           bool beside_tiles, cudaStream_t s);
 int launch_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, int few, const AttnParts& w,

@@ -1,0 +1,374 @@
+// Query and key heads divided by their root mean square, times a gain, and rotated, in one pass; and the backward pass.
+//
+//   o = r R(g x),  r = 1 / sqrt(mean_d x^2 + eps);   R: c x1 - s x2, c x2 + s x1 on the pairs of the first rot_dim elements
+//   t = R^T do,  u = g t,  dx = r (u - x r^2 mean_d(x u)),  dg = sum over rows of t x r
+//
+// R is linear, so r goes last: one product for each element instead of one before the gain.  The statistic is
+// summed in fp64 and r rounded once, the products and sums of the rest are rounded one by one in fp32: o is the plain fp32
+// evaluation bit for bit (kv_append_kernel quantizes the same values).  The backward pass is fp32 throughout.
+//
+// A thread owns what rope_kernel's does: 8 elements of the interleaved layout, 8 + 8 partners of the half layout, 8 of the
+// part that is not rotated.  The L lanes of a head add up its statistic; HEADS heads of a token (all of q, or all of k)
+// share a thread's gains and the table's pairs, and their loads are in flight together.
+#include "hbl_kv_cache.cuh"
+#include "hbl_piece.cuh"
+
+namespace hbl {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct Part {                          // the queries, or the keys
+  const void *x, *gain;
+  void* out;                           // forward: o; backward: dx
+  const void* grad;                    // backward: do
+  float* partial;                      // backward: [blocks][head_dim], NULL: gain's gradient is not wanted
+  long x_ts, x_hs, o_ts, o_hs, g_ts, g_hs;
+  int n_heads, groups, blocks;
+  long units;                          // tokens * groups
+};
+struct NormArgs {
+  Part part[2];
+  const int32_t* positions;
+  const float4* table;                 // NULL: nothing is rotated
+  int* status;
+  int gain_bf16, n_pos, rot_dim, head_dim, pieces, rotated;
+  float eps;
+};
+
+// The pairs of a piece: cosines and sines.
+template <int PAIRS>
+__device__ __forceinline__ void load_pairs(const NormArgs& a, int pos, int piece, float (&c)[PAIRS], float (&s)[PAIRS]) {
+  const float4* row = a.table + ((long)pos * (a.rot_dim / 2) + piece * PAIRS) / 2;      // two pairs to a float4
+#pragma unroll
+  for (int i = 0; i < PAIRS / 2; ++i) {
+    const float4 v = __ldg(row + i);
+    c[2 * i] = v.x; s[2 * i] = v.y; c[2 * i + 1] = v.z; s[2 * i + 1] = v.w;
+  }
+}
+
+template <typename T, bool INTERLEAVED, int L, int HEADS>
+__global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_constant__ NormArgs a) {
+  constexpr int PAIRS = INTERLEAVED ? 4 : 8;
+  grid_dependency_wait();
+  const long all = a.part[0].units + a.part[1].units;
+  long unit = (long)blockIdx.x * (kThreads / L) + threadIdx.x / L;
+  const bool live = unit < all;
+  if (!live) unit = all - 1;                                   // (the warp shuffles as a whole)
+  const bool second = unit >= a.part[0].units;
+  const Part& w = a.part[second];
+  if (second) unit -= a.part[0].units;
+  const int t = (int)(unit / w.groups), h0 = (int)(unit % w.groups) * HEADS;
+  const int piece = threadIdx.x % L, n = min(HEADS, w.n_heads - h0);
+  const bool there = piece < a.pieces, turned = piece < a.rotated, two = !INTERLEAVED && turned;
+  const int half = a.rot_dim / 2, d = turned ? piece * 8 : a.rot_dim + (piece - a.rotated) * 8;
+  const T* x = static_cast<const T*>(w.x) + t * w.x_ts + h0 * w.x_hs + d;
+  Piece<T> p[HEADS], q[HEADS];
+#pragma unroll
+  for (int i = 0; i < HEADS; ++i)
+    if (i < n && there) {
+      p[i].load(x + i * w.x_hs);
+      if (two) q[i].load(x + i * w.x_hs + half);
+    }
+  float g[8], g2[8], c[PAIRS], s[PAIRS];
+  if (there) load_gain(w.gain, a.gain_bf16, d, g);
+  if (two) load_gain(w.gain, a.gain_bf16, d + half, g2);
+  int pos = 0;
+  bool good = live;
+  if (a.table != nullptr) {
+    pos = __ldg(a.positions + t);
+    if (pos < 0 || pos >= a.n_pos) {
+      report_device_error(a.status, HBL_ERR_RANGE);
+      good = false;
+    }
+    if (turned && good) load_pairs<PAIRS>(a, pos, piece, c, s);
+  }
+  T* out = static_cast<T*>(w.out) + t * w.o_ts + h0 * w.o_hs + d;
+#pragma unroll
+  for (int i = 0; i < HEADS; ++i) {
+    float f[8], e[8];
+    double sum = 0.0;
+    if (i < n && there) {
+      p[i].get(f);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum = fma((double)f[k], (double)f[k], sum);
+      if (two) {
+        q[i].get(e);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum = fma((double)e[k], (double)e[k], sum);
+      }
+    }
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float r = inverse_root(sum / a.head_dim + (double)a.eps);
+    if (i >= n || !there || !good) continue;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[k] = __fmul_rn(f[k], g[k]);
+    if (turned) {
+      if constexpr (INTERLEAVED) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float x1 = f[2 * k], x2 = f[2 * k + 1];
+          f[2 * k] = __fsub_rn(__fmul_rn(x1, c[k]), __fmul_rn(x2, s[k]));
+          f[2 * k + 1] = __fadd_rn(__fmul_rn(x2, c[k]), __fmul_rn(x1, s[k]));
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float x1 = f[k], x2 = __fmul_rn(e[k], g2[k]);
+          f[k] = __fsub_rn(__fmul_rn(x1, c[k]), __fmul_rn(x2, s[k]));
+          e[k] = __fmul_rn(__fadd_rn(__fmul_rn(x2, c[k]), __fmul_rn(x1, s[k])), r);
+        }
+        q[i].set(e);
+        q[i].store(out + i * w.o_hs + half);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[k] = __fmul_rn(f[k], r);
+    p[i].set(f);
+    p[i].store(out + i * w.o_hs);
+  }
+}
+
+// A thread keeps its piece of the head and goes over units (a token's HEADS heads), so that its share of dg stays in
+// registers; the block's shares are added in shared memory in the order of its threads, the blocks' by gain_grad_kernel.
+template <typename T, bool INTERLEAVED, int L, int HEADS>
+__global__ void __launch_bounds__(kThreads) norm_rope_grad_kernel(const __grid_constant__ NormArgs a) {
+  constexpr int PAIRS = INTERLEAVED ? 4 : 8, SLOTS = kThreads / L, N = INTERLEAVED ? 8 : 16;
+  __shared__ float share[SLOTS][L * N + 1];
+  grid_dependency_wait();
+  const bool second = (int)blockIdx.x >= a.part[0].blocks;
+  const Part& w = a.part[second];
+  const int block = blockIdx.x - (second ? a.part[0].blocks : 0);
+  const int piece = threadIdx.x % L, slot = threadIdx.x / L;
+  const bool there = piece < a.pieces, turned = piece < a.rotated, two = !INTERLEAVED && turned;
+  const int half = a.rot_dim / 2, d = turned ? piece * 8 : a.rot_dim + (piece - a.rotated) * 8;
+  float g[N], acc[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) g[k] = 0.f;
+  if (there) load_gain(w.gain, a.gain_bf16, d, *reinterpret_cast<float(*)[8]>(g));
+  if constexpr (!INTERLEAVED)
+    if (two) load_gain(w.gain, a.gain_bf16, d + half, *reinterpret_cast<float(*)[8]>(g + 8));
+#pragma unroll
+  for (int k = 0; k < N; ++k) acc[k] = 0.f;
+  const float inv_dim = 1.f / (float)a.head_dim;
+  for (long u0 = (long)block * SLOTS; u0 < w.units; u0 += (long)w.blocks * SLOTS) {
+    const bool live = u0 + slot < w.units;
+    const long unit = live ? u0 + slot : w.units - 1;
+    const int t = (int)(unit / w.groups), h0 = (int)(unit % w.groups) * HEADS;
+    const int n = live ? min(HEADS, w.n_heads - h0) : 0;
+    const T* x = static_cast<const T*>(w.x) + t * w.x_ts + h0 * w.x_hs + d;
+    const T* dy = static_cast<const T*>(w.grad) + t * w.g_ts + h0 * w.g_hs + d;
+    Piece<T> px[HEADS], qx[HEADS], py[HEADS], qy[HEADS];
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i)
+      if (i < n && there) {
+        px[i].load(x + i * w.x_hs);
+        py[i].load(dy + i * w.g_hs);
+        if (two) {
+          qx[i].load(x + i * w.x_hs + half);
+          qy[i].load(dy + i * w.g_hs + half);
+        }
+      }
+    float c[PAIRS], s[PAIRS];
+    bool good = true;
+    if (a.table != nullptr) {
+      const int pos = __ldg(a.positions + t);
+      if (pos < 0 || pos >= a.n_pos) {
+        report_device_error(a.status, HBL_ERR_RANGE);
+        good = false;
+      }
+      if (turned && good) load_pairs<PAIRS>(a, pos, piece, c, s);
+    }
+    T* out = static_cast<T*>(w.out) + t * w.o_ts + h0 * w.o_hs + d;
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) {
+      const bool mine = i < n && there && good;
+      float f[N], y[N], sum = 0.f, dot = 0.f;
+#pragma unroll
+      for (int k = 0; k < N; ++k) f[k] = y[k] = 0.f;
+      if (mine) {
+        px[i].get(*reinterpret_cast<float(*)[8]>(f));
+        py[i].get(*reinterpret_cast<float(*)[8]>(y));
+        if constexpr (!INTERLEAVED)
+          if (two) {
+            qx[i].get(*reinterpret_cast<float(*)[8]>(f + 8));
+            qy[i].get(*reinterpret_cast<float(*)[8]>(y + 8));
+          }
+        if (turned) {                                          // the transposed rotation
+#pragma unroll
+          for (int k = 0; k < PAIRS; ++k) {
+            float &y1 = y[INTERLEAVED ? 2 * k : k], &y2 = y[INTERLEAVED ? 2 * k + 1 : k + 8];
+            const float z1 = y1 * c[k] + y2 * s[k], z2 = y2 * c[k] - y1 * s[k];
+            y1 = z1;
+            y2 = z2;
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          sum = fmaf(f[k], f[k], sum);
+          dot = fmaf(f[k], y[k] * g[k], dot);
+        }
+      }
+#pragma unroll
+      for (int o = L / 2; o > 0; o >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        dot += __shfl_xor_sync(0xffffffffu, dot, o);
+      }
+      if (!mine) continue;
+      const float r = 1.f / sqrtf(fmaf(sum, inv_dim, a.eps)), m = r * r * (dot * inv_dim);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        acc[k] = fmaf(y[k], f[k] * r, acc[k]);
+        f[k] = r * (y[k] * g[k] - f[k] * m);
+      }
+      px[i].set(*reinterpret_cast<float(*)[8]>(f));
+      px[i].store(out + i * w.o_hs);
+      if constexpr (!INTERLEAVED)
+        if (two) {
+          qx[i].set(*reinterpret_cast<float(*)[8]>(f + 8));
+          qx[i].store(out + i * w.o_hs + half);
+        }
+    }
+  }
+  if (w.partial == nullptr) return;
+#pragma unroll
+  for (int k = 0; k < N; ++k) share[slot][piece * N + k] = acc[k];
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.head_dim; e += kThreads) {
+    // element e of the head: which thread's, and which of its
+    int at;
+    if (INTERLEAVED) at = e;
+    else if (e < a.rot_dim) at = (e % half) / 8 * N + (e >= half ? 8 : 0) + e % 8;
+    else at = (a.rotated + (e - a.rot_dim) / 8) * N + e % 8;
+    float sum = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < SLOTS; ++i) sum += share[i][at];
+    w.partial[(long)block * a.head_dim + e] = sum;
+  }
+}
+
+// dg = the blocks' shares added up, 32 elements to a block: 32 warps take a row of shares each in turn, then their sums
+// in the warps' order.
+struct GainArgs {
+  const float* partial[2];
+  float* out[2];
+  int blocks[2], head_dim;
+};
+__global__ void __launch_bounds__(1024) gain_grad_kernel(const __grid_constant__ GainArgs a) {
+  __shared__ float share[32][33];
+  grid_dependency_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane, which = blockIdx.y;
+  if (a.out[which] == nullptr) return;
+  float sum = 0.f;
+  if (e < a.head_dim)
+    for (int b = warp; b < a.blocks[which]; b += 32) sum += a.partial[which][(long)b * a.head_dim + e];
+  share[warp][lane] = sum;
+  __syncthreads();
+  if (warp != 0 || e >= a.head_dim) return;
+  sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) sum += share[i][lane];
+  a.out[which][e] = sum;
+}
+
+constexpr int kGradBlocksPerSm = 4;
+
+void set_pieces(NormArgs& n, const NormRopeCall& c) {
+  n.positions = c.positions;
+  n.table = reinterpret_cast<const float4*>(c.table);
+  n.gain_bf16 = c.gain_dtype == HBL_BF16;
+  n.n_pos = c.n_pos; n.rot_dim = c.table != nullptr ? c.rot_dim : 0; n.head_dim = c.head_dim; n.eps = c.norm_eps;
+  n.rotated = n.rot_dim / (c.interleaved ? 8 : 16);
+  n.pieces = n.rotated + (c.head_dim - n.rot_dim) / 8;
+  for (int i = 0; i < 2; ++i) {
+    const NormRopePart& s = c.part[i];
+    Part& d = n.part[i];
+    d.x = s.x; d.gain = s.gain; d.out = s.out; d.grad = s.grad;
+    d.x_ts = s.x_ts; d.x_hs = s.x_hs; d.o_ts = s.o_ts; d.o_hs = s.o_hs; d.g_ts = s.g_ts; d.g_hs = s.g_hs;
+    d.n_heads = s.n_heads;
+  }
+}
+void set_units(NormArgs& n, int tokens, int heads) {
+  for (Part& d : n.part) {
+    d.groups = (d.n_heads + heads - 1) / heads;
+    d.units = (long)tokens * d.groups;
+  }
+}
+
+template <typename T, bool INTERLEAVED, int L, int HEADS>
+int launch_forward(NormArgs& n, int tokens, cudaStream_t s) {
+  set_units(n, tokens, HEADS);
+  const long blocks = (n.part[0].units + n.part[1].units + kThreads / L - 1) / (kThreads / L);
+  if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
+  HBL_CUDA_OK(launch_waiting(norm_rope_kernel<T, INTERLEAVED, L, HEADS>, dim3((unsigned)blocks), dim3(kThreads), 0, s, n));
+  note_launch();
+  return HBL_OK;
+}
+template <typename T, bool INTERLEAVED, int L, int HEADS>
+int launch_backward(NormArgs& n, int tokens, cudaStream_t s) {
+  set_units(n, tokens, HEADS);
+  const long slots = kThreads / L, most = norm_rope_grad_blocks();
+  for (Part& d : n.part) {
+    const long share = most * d.units / (n.part[0].units + n.part[1].units), need = (d.units + slots - 1) / slots;
+    d.blocks = (int)(need < share ? need : share < 1 && need > 0 ? 1 : share);
+  }
+  if (n.part[1].partial != nullptr) n.part[1].partial += (long)n.part[0].blocks * n.head_dim;
+  HBL_CUDA_OK(launch_waiting(norm_rope_grad_kernel<T, INTERLEAVED, L, HEADS>, dim3(n.part[0].blocks + n.part[1].blocks), dim3(kThreads), 0, s, n));
+  note_launch();
+  return HBL_OK;
+}
+template <typename T, bool INTERLEAVED, int L>
+int launch_lanes(NormArgs& n, int tokens, bool backward, cudaStream_t s) {
+  const bool many = (long)tokens * (n.part[0].n_heads + n.part[1].n_heads) * L >= (long)sm_count() * 2048 * 4;
+  if (backward) return many ? launch_backward<T, INTERLEAVED, L, 2>(n, tokens, s) : launch_backward<T, INTERLEAVED, L, 1>(n, tokens, s);
+  return many ? launch_forward<T, INTERLEAVED, L, 4>(n, tokens, s) : launch_forward<T, INTERLEAVED, L, 1>(n, tokens, s);
+}
+template <typename T, bool INTERLEAVED>
+int launch_type(NormArgs& n, int tokens, bool backward, cudaStream_t s) {
+  if (n.pieces <= 8) return launch_lanes<T, INTERLEAVED, 8>(n, tokens, backward, s);
+  if (n.pieces <= 16) return launch_lanes<T, INTERLEAVED, 16>(n, tokens, backward, s);
+  return launch_lanes<T, INTERLEAVED, 32>(n, tokens, backward, s);
+}
+int launch_any(NormArgs& n, const NormRopeCall& c, bool backward, cudaStream_t s) {
+  n.status = device_status_word();
+  if (n.status == nullptr) return HBL_ERR_CUDA;
+  if (c.dtype == HBL_BF16)
+    return c.interleaved ? launch_type<__nv_bfloat16, true>(n, c.tokens, backward, s) : launch_type<__nv_bfloat16, false>(n, c.tokens, backward, s);
+  return c.interleaved ? launch_type<float, true>(n, c.tokens, backward, s) : launch_type<float, false>(n, c.tokens, backward, s);
+}
+
+}  // namespace
+
+// Thread blocks of the backward kernel at most (and one more, where a part would get none).
+int norm_rope_grad_blocks() { return sm_count() * kGradBlocksPerSm; }
+
+int launch_norm_rope(const NormRopeCall& c, cudaStream_t s) {
+  NormArgs n{};
+  set_pieces(n, c);
+  return launch_any(n, c, false, s);
+}
+
+int launch_norm_rope_grad(const NormRopeCall& c, float* partial, cudaStream_t s) {
+  NormArgs n{};
+  set_pieces(n, c);
+  GainArgs g{};
+  bool any = false;
+  for (int i = 0; i < 2; ++i) {
+    g.out[i] = c.part[i].grad_gain;
+    n.part[i].partial = g.out[i] != nullptr ? partial : nullptr;
+    any |= g.out[i] != nullptr;
+  }
+  const int rc = c.tokens > 0 ? launch_any(n, c, true, s) : HBL_OK;      // (no tokens: no shares, and zeros for their sum)
+  if (rc != HBL_OK || !any) return rc;
+  for (int i = 0; i < 2; ++i) {
+    g.partial[i] = n.part[i].partial;
+    g.blocks[i] = n.part[i].blocks;
+  }
+  g.head_dim = c.head_dim;
+  HBL_CUDA_OK(launch_waiting(gain_grad_kernel, dim3((c.head_dim + 31) / 32, 2), dim3(1024), 0, s, g));
+  note_launch();
+  return HBL_OK;
+}
+
+}  // namespace hbl

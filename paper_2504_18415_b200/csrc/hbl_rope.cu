@@ -10,6 +10,7 @@
 // interleaved layout, 8 + 8 of the half layout, 8 of the part that is only copied) for up to HEADS heads of a token, so the
 // 8 (4) pairs of the table it needs are loaded once for all of them and its HEADS loads are in flight together.
 #include "hbl_kv_cache.cuh"
+#include "hbl_piece.cuh"
 
 namespace hbl {
 namespace {
@@ -38,52 +39,6 @@ struct RopeArgs {
   long x_ts, x_hs, o_ts, o_hs;
   int tokens, n_heads, n_pos, rot_dim, pieces, rotated, groups, backward;
   long items;
-};
-
-// Eight consecutive elements, as loaded.
-template <typename T>
-struct Piece;
-template <>
-struct Piece<__nv_bfloat16> {
-  uint4 w;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = w; }
-  __device__ __forceinline__ void get(float (&f)[8]) const {
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = __uint_as_float(u[i] << 16);
-      f[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-    }
-  }
-  __device__ __forceinline__ void set(const float (&f)[8]) {
-    uint32_t u[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-      u[i] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-    w = make_uint4(u[0], u[1], u[2], u[3]);
-  }
-};
-template <>
-struct Piece<float> {
-  float4 a, b;
-  __device__ __forceinline__ void load(const float* p) {
-    a = *reinterpret_cast<const float4*>(p);
-    b = *reinterpret_cast<const float4*>(p + 4);
-  }
-  __device__ __forceinline__ void store(float* p) const {
-    *reinterpret_cast<float4*>(p) = a;
-    *reinterpret_cast<float4*>(p + 4) = b;
-  }
-  __device__ __forceinline__ void get(float (&f)[8]) const {
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-  }
-  __device__ __forceinline__ void set(const float (&f)[8]) {
-    a = make_float4(f[0], f[1], f[2], f[3]);
-    b = make_float4(f[4], f[5], f[6], f[7]);
-  }
 };
 
 template <typename T, bool INTERLEAVED, int HEADS>

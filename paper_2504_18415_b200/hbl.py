@@ -32,6 +32,8 @@ EXPORTS = [
     "hbl_selftest_wait_timeout", "hbl_quantize_act_int4_packed", "hbl_gemm_i32_int4_packed",
     "hbl_rope_frequencies", "hbl_rope_table", "hbl_rope", "hbl_kv_append", "hbl_kv_read",
     "hbl_attention_workspace_bytes", "hbl_attention",
+    "hbl_norm_rope", "hbl_norm_rope_grad", "hbl_norm_rope_grad_workspace_bytes", "hbl_kv_append_norm",
+    "hbl_attention_window", "hbl_attention_window_workspace_bytes",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -68,6 +70,9 @@ class hbl_kv_batch_t(C.Structure):
 _ROPE_T = struct.Struct("4P4q8i")          # x out positions table | strides of x, out | dtype tokens n_heads head_dim n_pos rot_dim layout backward
 _APPEND_T = struct.Struct("4P8q2P4if0P")     # k v q q_out | strides of k, v, q, q_out | table positions | n_heads n_pos rot_dim layout eps
 _ATTENTION_T = struct.Struct("3P4q2if0P")    # q out lse | strides of q, out | n_heads causal sm_scale
+_NORM_ROPE_T = struct.Struct("3P4q3P4q2P9if0P")   # x gain out, strides of x, out: of q, of k | positions table | n_q_heads n_k_heads dtype gain_dtype tokens head_dim n_pos rot_dim layout norm_eps
+_NORM_GRAD_T = struct.Struct("4P4q")         # behind _NORM_ROPE_T: q_grad k_grad q_grad_gain k_grad_gain | strides of q_grad, k_grad
+_HEAD_NORM_T = struct.Struct("2Pif0P")       # q_gain k_gain | gain_dtype norm_eps
 
 
 def lib() -> C.CDLL:
@@ -121,7 +126,16 @@ def lib() -> C.CDLL:
         L.hbl_attention_workspace_bytes.argtypes = [vp, vp, i]
         L.hbl_attention_workspace_bytes.restype = sz
         L.hbl_attention.argtypes = [vp, vp, args, vp, sz, vp]
-        for n in ("hbl_rope_frequencies", "hbl_rope_table", "hbl_rope", "hbl_kv_append", "hbl_kv_read", "hbl_attention"):
+        L.hbl_norm_rope.argtypes = [args, vp]
+        L.hbl_norm_rope_grad_workspace_bytes.argtypes = [i, i, i, i]
+        L.hbl_norm_rope_grad_workspace_bytes.restype = sz
+        L.hbl_norm_rope_grad.argtypes = [args, vp, sz, vp]
+        L.hbl_kv_append_norm.argtypes = [vp, vp, args, args, vp]
+        L.hbl_attention_window_workspace_bytes.argtypes = [vp, vp, i, i, i]
+        L.hbl_attention_window_workspace_bytes.restype = sz
+        L.hbl_attention_window.argtypes = [vp, vp, args, i, i, vp, sz, vp]
+        for n in ("hbl_rope_frequencies", "hbl_rope_table", "hbl_rope", "hbl_kv_append", "hbl_kv_read", "hbl_attention",
+                  "hbl_norm_rope", "hbl_norm_rope_grad", "hbl_kv_append_norm", "hbl_attention_window"):
             getattr(L, n).restype = C.c_int
         L.hbl_selftest_wait_timeout.restype = C.c_int
         L.hbl_selftest_wait_timeout.argtypes = [i, vp, vp]
@@ -552,11 +566,75 @@ def hbl_rope(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, inte
     return out
 
 
-def hbl_kv_append(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor | None = None,
-                  positions: torch.Tensor | None = None, interleaved: bool = False, q: torch.Tensor | None = None,
-                  q_out: torch.Tensor | None = None, eps: float = 1e-5) -> torch.Tensor | None:
-    """The batch's tokens into the cache: k rotated by `table` (None: as it is), k and v quantized.  q, where given, is
-    rotated by the same launch and returned (q_out may be q)."""
+def _norm_rope_args(q, q_gain, positions, table, k, k_gain, norm_eps, interleaved, q_out, k_out):
+    """(packed arguments, q_out, k_out) of the calls that normalise and rotate heads."""
+    dev, dtype = _on_gpu(q, "q"), q.dtype
+    T, H, D = q.shape
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=dtype, device=dev)
+    strides = _strided(q, dtype, q.shape, "q", dev) + _strided(q_out, dtype, q.shape, "q_out", dev)
+    kp = op = heads = 0
+    k_strides = (0, 0, 0, 0)
+    if k is not None:
+        heads = k.shape[1]
+        shape = (T, heads, D)
+        if k_out is None:
+            k_out = torch.empty(shape, dtype=dtype, device=dev)
+        k_strides = _strided(k, dtype, shape, "k", dev) + _strided(k_out, dtype, shape, "k_out", dev)
+        kp, op = k.data_ptr(), k_out.data_ptr()
+    elif k_gain is not None or k_out is not None:
+        raise ValueError("k_gain, k_out: there is no k")
+    qg, kg, kind = _gains(q_gain, k_gain, D, dev)
+    at, n_pos, rot = (0, 0, 0) if table is None else _rotation(table, dev)
+    where = 0 if table is None else _flat(positions, torch.int32, (T,), "positions", dev)
+    return _NORM_ROPE_T.pack(q.data_ptr(), qg, q_out.data_ptr(), *strides, kp, kg, op, *k_strides, where, at, H, heads, _dt(q), kind, T, D,
+                             n_pos, rot, interleaved, norm_eps), q_out, k_out
+
+
+def hbl_norm_rope(q: torch.Tensor, q_gain: torch.Tensor | None, positions: torch.Tensor | None, table: torch.Tensor | None,
+                  k: torch.Tensor | None = None, k_gain: torch.Tensor | None = None, norm_eps: float = 1e-6, interleaved: bool = False,
+                  q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None):
+    """Every head of q (and k) [tokens, heads, head_dim], bf16 or fp32, divided by its root mean square, times the gain ([head_dim],
+    fp32 or bf16; None: ones), rotated (table None: not).  Returns (q_out, k_out); they may be q and k."""
+    args, q_out, k_out = _norm_rope_args(q, q_gain, positions, table, k, k_gain, norm_eps, interleaved, q_out, k_out)
+    _check(lib().hbl_norm_rope(args, _raw_stream(q.device)), "hbl_norm_rope")
+    return q_out, k_out
+
+
+def hbl_norm_rope_grad_workspace_bytes(tokens: int, n_q_heads: int, n_k_heads: int, head_dim: int) -> int:
+    return int(lib().hbl_norm_rope_grad_workspace_bytes(tokens, n_q_heads, n_k_heads, head_dim))
+
+
+def hbl_norm_rope_grad(grad_q: torch.Tensor, q: torch.Tensor, q_gain: torch.Tensor | None, positions: torch.Tensor | None,
+                       table: torch.Tensor | None, grad_k: torch.Tensor | None = None, k: torch.Tensor | None = None,
+                       k_gain: torch.Tensor | None = None, norm_eps: float = 1e-6, interleaved: bool = False,
+                       dq: torch.Tensor | None = None, dk: torch.Tensor | None = None, gain_grads: bool = True,
+                       workspace: torch.Tensor | None = None):
+    """The backward pass of hbl_norm_rope: q, k its inputs, grad_q, grad_k the gradients with respect to its outputs (strides of 0
+    allowed).  Returns (dq, dq_gain, dk, dk_gain); dq and dk may be q or grad_q, k or grad_k.  The gains' gradients are fp32
+    [head_dim] (gain_grads False: None)."""
+    if (k is None) != (grad_k is None):
+        raise ValueError("k and grad_k come together")
+    args, dq, dk = _norm_rope_args(q, q_gain, positions, table, k, k_gain, norm_eps, interleaved, dq, dk)
+    dev, D = q.device, q.shape[2]
+    strides = _strided(grad_q, q.dtype, q.shape, "grad_q", dev)
+    strides += (0, 0) if k is None else _strided(grad_k, q.dtype, k.shape, "grad_k", dev)
+    q_sum = k_sum = None
+    ws = size = 0
+    if gain_grads:
+        q_sum = torch.empty(D, dtype=torch.float32, device=dev)
+        k_sum = None if k is None else torch.empty(D, dtype=torch.float32, device=dev)
+        if workspace is None:
+            workspace = new_workspace(hbl_norm_rope_grad_workspace_bytes(q.shape[0], q.shape[1], 0 if k is None else k.shape[1], D), dev)
+        ws, size = _scratch(workspace, dev)
+    args += _NORM_GRAD_T.pack(grad_q.data_ptr(), 0 if k is None else grad_k.data_ptr(), 0 if q_sum is None else q_sum.data_ptr(),
+                              0 if k_sum is None else k_sum.data_ptr(), *strides)
+    _check(lib().hbl_norm_rope_grad(args, ws, size, _raw_stream(dev)), "hbl_norm_rope_grad")
+    return dq, q_sum, dk, k_sum
+
+
+def _append_args(cache: KvCache, batch: KvBatch, k, v, table, positions, interleaved, q, q_out, eps):
+    """(packed arguments, q_out) of the calls that put tokens into a cache."""
     dev, bf16 = cache.device, torch.bfloat16
     if batch.device != dev:
         raise ValueError("cache and batch are on different devices")
@@ -574,9 +652,38 @@ def hbl_kv_append(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tens
         qp, op = q.data_ptr(), q_out.data_ptr()
     if table is not None:
         at, n_pos, rot = _rotation(table, dev)
-    args = _APPEND_T.pack(k.data_ptr(), v.data_ptr(), qp, op, kts, khs, vts, vhs, qts, qhs, ots, ohs, at,
-                          _flat(positions, torch.int32, (batch.tokens,), "positions", dev), heads, n_pos, rot, interleaved, eps)
-    _check(lib().hbl_kv_append(cache.ref, batch.ref, args, _raw_stream(dev)), "hbl_kv_append")
+    return _APPEND_T.pack(k.data_ptr(), v.data_ptr(), qp, op, kts, khs, vts, vhs, qts, qhs, ots, ohs, at,
+                          _flat(positions, torch.int32, (batch.tokens,), "positions", dev), heads, n_pos, rot, interleaved, eps), q_out
+
+
+def hbl_kv_append(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor | None = None,
+                  positions: torch.Tensor | None = None, interleaved: bool = False, q: torch.Tensor | None = None,
+                  q_out: torch.Tensor | None = None, eps: float = 1e-5) -> torch.Tensor | None:
+    """The batch's tokens into the cache: k rotated by `table` (None: as it is), k and v quantized.  q, where given, is
+    rotated by the same launch and returned (q_out may be q)."""
+    args, q_out = _append_args(cache, batch, k, v, table, positions, interleaved, q, q_out, eps)
+    _check(lib().hbl_kv_append(cache.ref, batch.ref, args, _raw_stream(cache.device)), "hbl_kv_append")
+    return q_out
+
+
+def _gains(q_gain: torch.Tensor | None, k_gain: torch.Tensor | None, D: int, device) -> tuple[int, int, int]:
+    """(address, address, type) of the gains of queries and keys, which have one type; None: 0."""
+    dtype = torch.float32 if q_gain is None and k_gain is None else (k_gain if q_gain is None else q_gain).dtype
+    kind = HBL_BF16 if dtype is torch.bfloat16 else HBL_F32
+    if kind == HBL_F32 and dtype is not torch.float32:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return _flat(q_gain, dtype, (D,), "q_gain", device), _flat(k_gain, dtype, (D,), "k_gain", device), kind
+
+
+def hbl_kv_append_norm(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, k_gain: torch.Tensor | None,
+                       table: torch.Tensor | None = None, positions: torch.Tensor | None = None, interleaved: bool = False,
+                       q: torch.Tensor | None = None, q_gain: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+                       norm_eps: float = 1e-6, eps: float = 1e-5) -> torch.Tensor | None:
+    """hbl_kv_append with every head of k and q divided by its root mean square and multiplied by the gain ([head_dim], fp32 or
+    bf16; None: ones) before it is rotated.  (Queries may come without a table: normalised only.)"""
+    args, q_out = _append_args(cache, batch, k, v, table, positions, interleaved, q, q_out, eps)
+    norm = _HEAD_NORM_T.pack(*_gains(q_gain, k_gain, cache.head_dim, cache.device), norm_eps)
+    _check(lib().hbl_kv_append_norm(cache.ref, batch.ref, args, norm, _raw_stream(cache.device)), "hbl_kv_append_norm")
     return q_out
 
 
@@ -594,11 +701,8 @@ def hbl_attention_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int) 
     return int(lib().hbl_attention_workspace_bytes(cache.ref, batch.ref, n_heads))
 
 
-def hbl_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, sm_scale: float | None = None, causal: bool = True,
-                  out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
-                  workspace: torch.Tensor | None = None) -> torch.Tensor:
-    """softmax(sm_scale q K^T) V over the cache, q bf16 [tokens, n_heads, head_dim] -> out of the same shape.  sm_scale:
-    1 / sqrt(head_dim) by default; causal: a token sees the tokens up to itself; lse: fp32 [tokens, n_heads], written."""
+def _attention_args(cache: KvCache, batch: KvBatch, q, sm_scale, causal, out, lse):
+    """(packed arguments, out) of the calls that attend to a cache."""
     dev, D, bf16 = cache.device, cache.head_dim, torch.bfloat16
     if batch.device != dev:
         raise ValueError("cache and batch are on different devices")
@@ -610,15 +714,47 @@ def hbl_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, sm_scale: flo
         out = torch.empty(shape, dtype=bf16, device=dev)
     qts, qhs = _strided(q, bf16, shape, "q", dev)
     ots, ohs = _strided(out, bf16, shape, "out", dev)
-    args = _ATTENTION_T.pack(q.data_ptr(), out.data_ptr(), _flat(lse, torch.float32, (batch.tokens, H), "lse", dev), qts, qhs, ots, ohs,
-                             H, causal, D ** -0.5 if sm_scale is None else sm_scale)
+    return _ATTENTION_T.pack(q.data_ptr(), out.data_ptr(), _flat(lse, torch.float32, (batch.tokens, H), "lse", dev), qts, qhs, ots, ohs,
+                             H, causal, D ** -0.5 if sm_scale is None else sm_scale), out
+
+
+def _scratch(workspace: torch.Tensor | None, device) -> tuple[int, int]:
+    """(address, bytes) of a workspace; None: (0, 0)."""
     if workspace is None:
-        n = hbl_attention_workspace_bytes(cache, batch, H)
-        workspace = new_workspace(n, dev) if n > 0 else None
-    if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
-        raise ValueError(f"workspace: expected a contiguous tensor on {dev}")
-    ws, size = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
-    _check(lib().hbl_attention(cache.ref, batch.ref, args, ws, size, _raw_stream(dev)), "hbl_attention")
+        return 0, 0
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on {device}")
+    return workspace.data_ptr(), workspace.numel()
+
+
+def hbl_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, sm_scale: float | None = None, causal: bool = True,
+                  out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                  workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """softmax(sm_scale q K^T) V over the cache, q bf16 [tokens, n_heads, head_dim] -> out of the same shape.  sm_scale:
+    1 / sqrt(head_dim) by default; causal: a token sees the tokens up to itself; lse: fp32 [tokens, n_heads], written."""
+    args, out = _attention_args(cache, batch, q, sm_scale, causal, out, lse)
+    if workspace is None:
+        n = hbl_attention_workspace_bytes(cache, batch, q.shape[1])
+        workspace = new_workspace(n, cache.device) if n > 0 else None
+    _check(lib().hbl_attention(cache.ref, batch.ref, args, *_scratch(workspace, cache.device), _raw_stream(cache.device)), "hbl_attention")
+    return out
+
+
+def hbl_attention_window_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int, window: int, sinks: int = 0) -> int:
+    return int(lib().hbl_attention_window_workspace_bytes(cache.ref, batch.ref, n_heads, window, sinks))
+
+
+def hbl_attention_window(cache: KvCache, batch: KvBatch, q: torch.Tensor, window: int, sinks: int = 0, sm_scale: float | None = None,
+                         out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                         workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """hbl_attention in which a token sees itself, the window - 1 tokens before it, and its sequence's first `sinks` tokens.
+    Pages that hold none of those are not looked at, and may be in use for something else."""
+    args, out = _attention_args(cache, batch, q, sm_scale, True, out, lse)
+    if workspace is None:
+        n = hbl_attention_window_workspace_bytes(cache, batch, q.shape[1], window, sinks)
+        workspace = new_workspace(n, cache.device) if n > 0 else None
+    _check(lib().hbl_attention_window(cache.ref, batch.ref, args, window, sinks, *_scratch(workspace, cache.device), _raw_stream(cache.device)),
+           "hbl_attention_window")
     return out
 
 
