@@ -16,7 +16,7 @@
 namespace hbl {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kForwardBlocksPerSm = 3;
 
 struct Part {                          // the queries, or the keys
   const void *x, *gain;
@@ -36,97 +36,176 @@ struct NormArgs {
   float eps;
 };
 
-// The pairs of a piece: cosines and sines.
+// The pairs of a piece: cosines and sines, two to an element.
 template <int PAIRS>
-__device__ __forceinline__ void load_pairs(const NormArgs& a, int pos, int piece, float (&c)[PAIRS], float (&s)[PAIRS]) {
+__device__ __forceinline__ void load_pairs(const NormArgs& a, int pos, int piece, float2 (&c)[PAIRS / 2], float2 (&s)[PAIRS / 2]) {
   const float4* row = a.table + ((long)pos * (a.rot_dim / 2) + piece * PAIRS) / 2;      // two pairs to a float4
 #pragma unroll
   for (int i = 0; i < PAIRS / 2; ++i) {
     const float4 v = __ldg(row + i);
-    c[2 * i] = v.x; s[2 * i] = v.y; c[2 * i + 1] = v.z; s[2 * i + 1] = v.w;
+    c[i] = make_float2(v.x, v.z);
+    s[i] = make_float2(v.y, v.w);
   }
 }
 
+// Where a thread is in its part's units (a token's HEADS heads each), and where it goes next.
+struct Walker {
+  long unit, units, step;
+  int t, group, groups, step_t, step_group;       // the token, and which of its groups of heads
+  __device__ __forceinline__ Walker(const Part& w, int block, int slots, int slot) {
+    groups = w.groups;
+    units = w.units;
+    step = (long)w.blocks * slots;
+    step_t = (int)(step / groups);
+    step_group = (int)(step % groups);
+    unit = (long)block * slots + slot;
+    t = (int)(unit / groups);
+    group = (int)(unit % groups);
+  }
+  __device__ __forceinline__ void next() {
+    unit += step;
+    t += step_t;
+    group += step_group;
+    if (group >= groups) {
+      group -= groups;
+      ++t;
+    }
+  }
+  __device__ __forceinline__ bool live() const { return unit < units; }
+};
+
+// Thread blocks stay and walk over the units of their part.  A thread copies its pieces of the next unit to shared memory, where
+// only it reads them, while it works on the current one's.
+template <typename T, bool INTERLEAVED, int HEADS>
+struct ForwardGeo {
+  static constexpr int BYTES = 8 * sizeof(T), PIECES = INTERLEAVED ? 1 : 2;      // of a thread and head
+  static constexpr int STAGE = HEADS * PIECES * BYTES * kThreads;
+};
 template <typename T, bool INTERLEAVED, int L, int HEADS>
-__global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_constant__ NormArgs a) {
-  constexpr int PAIRS = INTERLEAVED ? 4 : 8;
+__global__ void __launch_bounds__(kThreads, kForwardBlocksPerSm) norm_rope_kernel(const __grid_constant__ NormArgs a) {
+  using G = ForwardGeo<T, INTERLEAVED, HEADS>;
+  constexpr int PAIRS = INTERLEAVED ? 4 : 8, SLOTS = kThreads / L, Q = G::BYTES / 16;
+  extern __shared__ uint4 ring[];                              // [stage][head][piece][16 bytes of it][thread]
   grid_dependency_wait();
-  const long all = a.part[0].units + a.part[1].units;
-  long unit = (long)blockIdx.x * (kThreads / L) + threadIdx.x / L;
-  const bool live = unit < all;
-  if (!live) unit = all - 1;                                   // (the warp shuffles as a whole)
-  const bool second = unit >= a.part[0].units;
+  const bool second = (int)blockIdx.x >= a.part[0].blocks;
   const Part& w = a.part[second];
-  if (second) unit -= a.part[0].units;
-  const int t = (int)(unit / w.groups), h0 = (int)(unit % w.groups) * HEADS;
-  const int piece = threadIdx.x % L, n = min(HEADS, w.n_heads - h0);
+  const int block = blockIdx.x - (second ? a.part[0].blocks : 0), piece = threadIdx.x % L;
   const bool there = piece < a.pieces, turned = piece < a.rotated, two = !INTERLEAVED && turned;
   const int half = a.rot_dim / 2, d = turned ? piece * 8 : a.rot_dim + (piece - a.rotated) * 8;
-  const T* x = static_cast<const T*>(w.x) + t * w.x_ts + h0 * w.x_hs + d;
-  Piece<T> p[HEADS], q[HEADS];
+  Walker at(w, block, SLOTS, threadIdx.x / L);
+  uint4* const mine = ring + threadIdx.x;
+  auto slot = [&](int stage, int i, int half_of) { return mine + (stage * (G::STAGE / 16) + (i * G::PIECES + half_of) * Q * kThreads); };
+  auto copy = [&](int stage) {
+    if (there && at.live()) {
+      const int h0 = at.group * HEADS;
+      const T* x = static_cast<const T*>(w.x) + at.t * w.x_ts + h0 * w.x_hs + d;
 #pragma unroll
-  for (int i = 0; i < HEADS; ++i)
-    if (i < n && there) {
-      p[i].load(x + i * w.x_hs);
-      if (two) q[i].load(x + i * w.x_hs + half);
+      for (int i = 0; i < HEADS; ++i)
+        if (h0 + i < w.n_heads) {
+#pragma unroll
+          for (int b = 0; b < Q; ++b) {
+            copy_async16(slot(stage, i, 0) + b * kThreads, reinterpret_cast<const uint4*>(x + i * w.x_hs) + b);
+            if (two) copy_async16(slot(stage, i, 1) + b * kThreads, reinterpret_cast<const uint4*>(x + i * w.x_hs + half) + b);
+          }
+        }
     }
-  float g[8], g2[8], c[PAIRS], s[PAIRS];
-  if (there) load_gain(w.gain, a.gain_bf16, d, g);
-  if (two) load_gain(w.gain, a.gain_bf16, d + half, g2);
-  int pos = 0;
-  bool good = live;
-  if (a.table != nullptr) {
-    pos = __ldg(a.positions + t);
-    if (pos < 0 || pos >= a.n_pos) {
-      report_device_error(a.status, HBL_ERR_RANGE);
-      good = false;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  auto fetch = [&](int stage, int i, int half_of, float2 (&f)[4]) {
+    Piece<T> p;
+    p.load_from(slot(stage, i, half_of), kThreads);
+    p.get(*reinterpret_cast<float(*)[8]>(f));
+  };
+  auto position = [&]() { return a.table != nullptr && at.live() ? __ldg(a.positions + at.t) : 0; };
+  copy(0);
+  int pos = position();
+  float2 g[4], g2[4];
+  if (there) load_gain(w.gain, a.gain_bf16, d, *reinterpret_cast<float(*)[8]>(g));
+  if (two) load_gain(w.gain, a.gain_bf16, d + half, *reinterpret_cast<float(*)[8]>(g2));
+  const double inv_dim = 1.0 / a.head_dim;
+  int stage = 0;
+  for (long u0 = (long)block * SLOTS; u0 < w.units; u0 += (long)w.blocks * SLOTS, stage ^= 1) {
+    float2 c[PAIRS / 2], s[PAIRS / 2];
+    bool good = at.live();
+    if (a.table != nullptr) {
+      if (pos < 0 || pos >= a.n_pos) {
+        report_device_error(a.status, HBL_ERR_RANGE);
+        good = false;
+      }
+      if (turned && good) load_pairs<PAIRS>(a, pos, piece, c, s);
     }
-    if (turned && good) load_pairs<PAIRS>(a, pos, piece, c, s);
-  }
-  T* out = static_cast<T*>(w.out) + t * w.o_ts + h0 * w.o_hs + d;
+    const int h0 = at.group * HEADS, n = there ? min(HEADS, w.n_heads - h0) : 0;
+    T* out = static_cast<T*>(w.out) + at.t * w.o_ts + h0 * w.o_hs + d;
+    const bool filled = at.live();
+    at.next();
+    pos = position();
+    copy(stage ^ 1);
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    // the heads' statistics side by side: each is a chain of fp64 operations
+    double sum[HEADS];
 #pragma unroll
-  for (int i = 0; i < HEADS; ++i) {
-    float f[8], e[8];
-    double sum = 0.0;
-    if (i < n && there) {
-      p[i].get(f);
+    for (int i = 0; i < HEADS; ++i) {
+      float2 f[4];
+      sum[i] = 0.0;
+      if (i < n && filled) {
+        fetch(stage, i, 0, f);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) sum = fma((double)f[k], (double)f[k], sum);
-      if (two) {
-        q[i].get(e);
+        for (int k = 0; k < 4; ++k) sum[i] = fma((double)f[k].y, (double)f[k].y, fma((double)f[k].x, (double)f[k].x, sum[i]));
+        if (two) {
+          fetch(stage, i, 1, f);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum = fma((double)e[k], (double)e[k], sum);
+          for (int k = 0; k < 4; ++k) sum[i] = fma((double)f[k].y, (double)f[k].y, fma((double)f[k].x, (double)f[k].x, sum[i]));
+        }
       }
     }
 #pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    const float r = inverse_root(sum / a.head_dim + (double)a.eps);
-    if (i >= n || !there || !good) continue;
+    for (int o = L / 2; o > 0; o >>= 1) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) f[k] = __fmul_rn(f[k], g[k]);
-    if (turned) {
-      if constexpr (INTERLEAVED) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float x1 = f[2 * k], x2 = f[2 * k + 1];
-          f[2 * k] = __fsub_rn(__fmul_rn(x1, c[k]), __fmul_rn(x2, s[k]));
-          f[2 * k + 1] = __fadd_rn(__fmul_rn(x2, c[k]), __fmul_rn(x1, s[k]));
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float x1 = f[k], x2 = __fmul_rn(e[k], g2[k]);
-          f[k] = __fsub_rn(__fmul_rn(x1, c[k]), __fmul_rn(x2, s[k]));
-          e[k] = __fmul_rn(__fadd_rn(__fmul_rn(x2, c[k]), __fmul_rn(x1, s[k])), r);
-        }
-        q[i].set(e);
-        q[i].store(out + i * w.o_hs + half);
-      }
+      for (int i = 0; i < HEADS; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
     }
+    // and one root to a lane
+    double of_lane = sum[0];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) f[k] = __fmul_rn(f[k], r);
-    p[i].set(f);
-    p[i].store(out + i * w.o_hs);
+    for (int i = 1; i < HEADS; ++i)
+      if (piece % HEADS == i) of_lane = sum[i];
+    const float root = inverse_root(fma(of_lane, inv_dim, (double)a.eps));
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) {
+      const float r = __shfl_sync(0xffffffffu, root, i, L);
+      if (i >= n || !good) continue;
+      float2 f[4];
+      fetch(stage, i, 0, f);
+      Piece<T> o;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) f[k] = mul2(f[k], g[k]);
+      if (turned) {
+        if constexpr (INTERLEAVED) {
+          float* y = reinterpret_cast<float*>(f);
+          const float *cc = reinterpret_cast<const float*>(c), *ss = reinterpret_cast<const float*>(s);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float x1 = y[2 * k], x2 = y[2 * k + 1];
+            y[2 * k] = __fsub_rn(__fmul_rn(x1, cc[k]), __fmul_rn(x2, ss[k]));
+            y[2 * k + 1] = __fadd_rn(__fmul_rn(x2, cc[k]), __fmul_rn(x1, ss[k]));
+          }
+        } else {
+          float2 e[4];
+          fetch(stage, i, 1, e);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 x1 = f[k], x2 = mul2(e[k], g2[k]);
+            f[k] = sub2(mul2(x1, c[k]), mul2(x2, s[k]));
+            e[k] = mul2(add2(mul2(x2, c[k]), mul2(x1, s[k])), make_float2(r, r));
+          }
+          o.set(*reinterpret_cast<float(*)[8]>(e));
+          o.store(out + i * w.o_hs + half);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) f[k] = mul2(f[k], make_float2(r, r));
+      o.set(*reinterpret_cast<float(*)[8]>(f));
+      o.store(out + i * w.o_hs);
+    }
   }
 }
 
@@ -170,7 +249,8 @@ __global__ void __launch_bounds__(kThreads) norm_rope_grad_kernel(const __grid_c
           qy[i].load(dy + i * w.g_hs + half);
         }
       }
-    float c[PAIRS], s[PAIRS];
+    float2 c2[PAIRS / 2], s2[PAIRS / 2];
+    const float *c = reinterpret_cast<const float*>(c2), *s = reinterpret_cast<const float*>(s2);
     bool good = true;
     if (a.table != nullptr) {
       const int pos = __ldg(a.positions + t);
@@ -178,7 +258,7 @@ __global__ void __launch_bounds__(kThreads) norm_rope_grad_kernel(const __grid_c
         report_device_error(a.status, HBL_ERR_RANGE);
         good = false;
       }
-      if (turned && good) load_pairs<PAIRS>(a, pos, piece, c, s);
+      if (turned && good) load_pairs<PAIRS>(a, pos, piece, c2, s2);
     }
     T* out = static_cast<T*>(w.out) + t * w.o_ts + h0 * w.o_hs + d;
 #pragma unroll
@@ -296,23 +376,28 @@ void set_units(NormArgs& n, int tokens, int heads) {
   }
 }
 
+// Blocks for the two parts by their units, at most `most` (and one more, where a part would get none).
+void deal_blocks(NormArgs& n, int slots, long most) {
+  for (Part& d : n.part) {
+    const long share = most * d.units / (n.part[0].units + n.part[1].units), need = (d.units + slots - 1) / slots;
+    d.blocks = (int)(need < share ? need : share < 1 && need > 0 ? 1 : share);
+  }
+}
 template <typename T, bool INTERLEAVED, int L, int HEADS>
 int launch_forward(NormArgs& n, int tokens, cudaStream_t s) {
   set_units(n, tokens, HEADS);
-  const long blocks = (n.part[0].units + n.part[1].units + kThreads / L - 1) / (kThreads / L);
-  if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
-  HBL_CUDA_OK(launch_waiting(norm_rope_kernel<T, INTERLEAVED, L, HEADS>, dim3((unsigned)blocks), dim3(kThreads), 0, s, n));
+  deal_blocks(n, kThreads / L, (long)sm_count() * kForwardBlocksPerSm);
+  auto kern = norm_rope_kernel<T, INTERLEAVED, L, HEADS>;
+  constexpr int bytes = 2 * ForwardGeo<T, INTERLEAVED, HEADS>::STAGE;
+  HBL_ALLOW_DYNAMIC_SMEM(kern, bytes);
+  HBL_CUDA_OK(launch_waiting(kern, dim3(n.part[0].blocks + n.part[1].blocks), dim3(kThreads), bytes, s, n));
   note_launch();
   return HBL_OK;
 }
 template <typename T, bool INTERLEAVED, int L, int HEADS>
 int launch_backward(NormArgs& n, int tokens, cudaStream_t s) {
   set_units(n, tokens, HEADS);
-  const long slots = kThreads / L, most = norm_rope_grad_blocks();
-  for (Part& d : n.part) {
-    const long share = most * d.units / (n.part[0].units + n.part[1].units), need = (d.units + slots - 1) / slots;
-    d.blocks = (int)(need < share ? need : share < 1 && need > 0 ? 1 : share);
-  }
+  deal_blocks(n, kThreads / L, norm_rope_grad_blocks());
   if (n.part[1].partial != nullptr) n.part[1].partial += (long)n.part[0].blocks * n.head_dim;
   HBL_CUDA_OK(launch_waiting(norm_rope_grad_kernel<T, INTERLEAVED, L, HEADS>, dim3(n.part[0].blocks + n.part[1].blocks), dim3(kThreads), 0, s, n));
   note_launch();
@@ -322,7 +407,7 @@ template <typename T, bool INTERLEAVED, int L>
 int launch_lanes(NormArgs& n, int tokens, bool backward, cudaStream_t s) {
   const bool many = (long)tokens * (n.part[0].n_heads + n.part[1].n_heads) * L >= (long)sm_count() * 2048 * 4;
   if (backward) return many ? launch_backward<T, INTERLEAVED, L, 2>(n, tokens, s) : launch_backward<T, INTERLEAVED, L, 1>(n, tokens, s);
-  return many ? launch_forward<T, INTERLEAVED, L, 4>(n, tokens, s) : launch_forward<T, INTERLEAVED, L, 1>(n, tokens, s);
+  return many ? launch_forward<T, INTERLEAVED, L, sizeof(T) == 2 ? 4 : 2>(n, tokens, s) : launch_forward<T, INTERLEAVED, L, 1>(n, tokens, s);
 }
 template <typename T, bool INTERLEAVED>
 int launch_type(NormArgs& n, int tokens, bool backward, cudaStream_t s) {

@@ -12,6 +12,7 @@ template <>
 struct Piece<__nv_bfloat16> {
   uint4 w;
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void load_from(const uint4* p, int) { w = *p; }          // 16 bytes at a time, so far apart
   __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = w; }
   __device__ __forceinline__ void get(float (&f)[8]) const {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
@@ -34,6 +35,10 @@ struct Piece<__nv_bfloat16> {
 template <>
 struct Piece<float> {
   float4 a, b;
+  __device__ __forceinline__ void load_from(const uint4* p, int apart) {
+    a = *reinterpret_cast<const float4*>(p);
+    b = *reinterpret_cast<const float4*>(p + apart);
+  }
   __device__ __forceinline__ void load(const float* p) {
     a = *reinterpret_cast<const float4*>(p);
     b = *reinterpret_cast<const float4*>(p + 4);
@@ -50,6 +55,24 @@ struct Piece<float> {
     b = make_float4(f[4], f[5], f[6], f[7]);
   }
 };
+
+// Two fp32 operations to an instruction, each rounded as on its own; sums one by one, because a product and a sum that are both
+// packed come out contracted to one rounding.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  asm("{\n .reg .b64 u, v;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %3};\n mul.rn.f32x2 u, u, v;\n mov.b64 {%0, %1}, u;\n}"
+      : "+f"(a.x), "+f"(a.y) : "f"(b.x), "f"(b.y));
+  return a;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) { return make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y)); }
+__device__ __forceinline__ float2 sub2(float2 a, float2 b) { return make_float2(__fsub_rn(a.x, b.x), __fsub_rn(a.y, b.y)); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  asm("{\n .reg .b64 u, v, w;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %3};\n mov.b64 w, {%4, %5};\n fma.rn.f32x2 u, u, v, w;\n mov.b64 {%0, %1}, u;\n}"
+      : "+f"(a.x), "+f"(a.y) : "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return a;
+}
+__device__ __forceinline__ void copy_async16(uint4* dst, const uint4* src) {         // to shared memory
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
 
 // Gains of 8 consecutive elements; NULL: ones.
 __device__ __forceinline__ void load_gain(const void* gain, int bf16, int d, float (&g)[8]) {
