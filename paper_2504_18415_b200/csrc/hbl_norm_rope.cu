@@ -16,7 +16,7 @@
 namespace hbl {
 namespace {
 
-constexpr int kThreads = 256, kForwardBlocksPerSm = 3;
+constexpr int kThreads = 256, kForwardBlocksPerSm = 3, kBackwardBlocksPerSm = 2;
 
 struct Part {                          // the queries, or the keys
   const void *x, *gain;
@@ -209,121 +209,158 @@ __global__ void __launch_bounds__(kThreads, kForwardBlocksPerSm) norm_rope_kerne
   }
 }
 
-// A thread keeps its piece of the head and goes over units (a token's HEADS heads), so that its share of dg stays in
-// registers; the block's shares are added in shared memory in the order of its threads, the blocks' by gain_grad_kernel.
+// The same walk; a thread keeps its piece of the head, so that its share of dg stays in registers.  The block's shares are added
+// in shared memory in the order of its threads, the blocks' by gain_grad_kernel.
 template <typename T, bool INTERLEAVED, int L, int HEADS>
-__global__ void __launch_bounds__(kThreads) norm_rope_grad_kernel(const __grid_constant__ NormArgs a) {
-  constexpr int PAIRS = INTERLEAVED ? 4 : 8, SLOTS = kThreads / L, N = INTERLEAVED ? 8 : 16;
-  __shared__ float share[SLOTS][L * N + 1];
+struct BackwardGeo {
+  using F = ForwardGeo<T, INTERLEAVED, HEADS>;
+  static constexpr int N = 8 * F::PIECES, PITCH = L * N + 4, SLOTS = kThreads / L;
+  static constexpr int RING = 2 * 2 * F::STAGE, SHARES = SLOTS * PITCH * 4, SMEM = RING > SHARES ? RING : SHARES;
+};
+template <typename T, bool INTERLEAVED, int L, int HEADS>
+__global__ void __launch_bounds__(kThreads, kBackwardBlocksPerSm) norm_rope_grad_kernel(const __grid_constant__ NormArgs a) {
+  using G = ForwardGeo<T, INTERLEAVED, HEADS>;
+  using B = BackwardGeo<T, INTERLEAVED, L, HEADS>;
+  constexpr int PAIRS = INTERLEAVED ? 4 : 8, SLOTS = B::SLOTS, N = B::N, Q = G::BYTES / 16, P = G::PIECES;
+  extern __shared__ uint4 ring[];                              // [stage][x, do][head][piece][16 bytes of it][thread]
   grid_dependency_wait();
   const bool second = (int)blockIdx.x >= a.part[0].blocks;
   const Part& w = a.part[second];
-  const int block = blockIdx.x - (second ? a.part[0].blocks : 0);
-  const int piece = threadIdx.x % L, slot = threadIdx.x / L;
+  const int block = blockIdx.x - (second ? a.part[0].blocks : 0), piece = threadIdx.x % L;
   const bool there = piece < a.pieces, turned = piece < a.rotated, two = !INTERLEAVED && turned;
   const int half = a.rot_dim / 2, d = turned ? piece * 8 : a.rot_dim + (piece - a.rotated) * 8;
-  float g[N], acc[N];
+  Walker at(w, block, SLOTS, threadIdx.x / L);
+  uint4* const mine = ring + threadIdx.x;
+  auto slot = [&](int stage, int which, int i, int half_of) {
+    return mine + ((stage * 2 + which) * (G::STAGE / 16) + (i * P + half_of) * Q * kThreads);
+  };
+  auto copy = [&](int stage) {
+    if (there && at.live()) {
+      const int h0 = at.group * HEADS;
+      const T* x = static_cast<const T*>(w.x) + at.t * w.x_ts + h0 * w.x_hs + d;
+      const T* y = static_cast<const T*>(w.grad) + at.t * w.g_ts + h0 * w.g_hs + d;
 #pragma unroll
-  for (int k = 0; k < N; ++k) g[k] = 0.f;
+      for (int i = 0; i < HEADS; ++i)
+        if (h0 + i < w.n_heads) {
+#pragma unroll
+          for (int b = 0; b < Q; ++b) {
+            copy_async16(slot(stage, 0, i, 0) + b * kThreads, reinterpret_cast<const uint4*>(x + i * w.x_hs) + b);
+            copy_async16(slot(stage, 1, i, 0) + b * kThreads, reinterpret_cast<const uint4*>(y + i * w.g_hs) + b);
+            if (two) {
+              copy_async16(slot(stage, 0, i, 1) + b * kThreads, reinterpret_cast<const uint4*>(x + i * w.x_hs + half) + b);
+              copy_async16(slot(stage, 1, i, 1) + b * kThreads, reinterpret_cast<const uint4*>(y + i * w.g_hs + half) + b);
+            }
+          }
+        }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  auto fetch = [&](const uint4* from, float2* f) {
+    Piece<T> p;
+    p.load_from(from, kThreads);
+    p.get(*reinterpret_cast<float(*)[8]>(f));
+  };
+  auto position = [&]() { return a.table != nullptr && at.live() ? __ldg(a.positions + at.t) : 0; };
+  copy(0);
+  int pos = position();
+  float2 g[N / 2], acc[N / 2];
+#pragma unroll
+  for (int k = 0; k < N / 2; ++k) g[k] = acc[k] = make_float2(0.f, 0.f);
   if (there) load_gain(w.gain, a.gain_bf16, d, *reinterpret_cast<float(*)[8]>(g));
   if constexpr (!INTERLEAVED)
-    if (two) load_gain(w.gain, a.gain_bf16, d + half, *reinterpret_cast<float(*)[8]>(g + 8));
-#pragma unroll
-  for (int k = 0; k < N; ++k) acc[k] = 0.f;
+    if (two) load_gain(w.gain, a.gain_bf16, d + half, *reinterpret_cast<float(*)[8]>(g + 4));
   const float inv_dim = 1.f / (float)a.head_dim;
-  for (long u0 = (long)block * SLOTS; u0 < w.units; u0 += (long)w.blocks * SLOTS) {
-    const bool live = u0 + slot < w.units;
-    const long unit = live ? u0 + slot : w.units - 1;
-    const int t = (int)(unit / w.groups), h0 = (int)(unit % w.groups) * HEADS;
-    const int n = live ? min(HEADS, w.n_heads - h0) : 0;
-    const T* x = static_cast<const T*>(w.x) + t * w.x_ts + h0 * w.x_hs + d;
-    const T* dy = static_cast<const T*>(w.grad) + t * w.g_ts + h0 * w.g_hs + d;
-    Piece<T> px[HEADS], qx[HEADS], py[HEADS], qy[HEADS];
-#pragma unroll
-    for (int i = 0; i < HEADS; ++i)
-      if (i < n && there) {
-        px[i].load(x + i * w.x_hs);
-        py[i].load(dy + i * w.g_hs);
-        if (two) {
-          qx[i].load(x + i * w.x_hs + half);
-          qy[i].load(dy + i * w.g_hs + half);
-        }
-      }
-    float2 c2[PAIRS / 2], s2[PAIRS / 2];
-    const float *c = reinterpret_cast<const float*>(c2), *s = reinterpret_cast<const float*>(s2);
-    bool good = true;
+  int stage = 0;
+  for (long u0 = (long)block * SLOTS; u0 < w.units; u0 += (long)w.blocks * SLOTS, stage ^= 1) {
+    float2 c[PAIRS / 2], s[PAIRS / 2];
+    bool good = at.live();
     if (a.table != nullptr) {
-      const int pos = __ldg(a.positions + t);
       if (pos < 0 || pos >= a.n_pos) {
         report_device_error(a.status, HBL_ERR_RANGE);
         good = false;
       }
-      if (turned && good) load_pairs<PAIRS>(a, pos, piece, c2, s2);
+      if (turned && good) load_pairs<PAIRS>(a, pos, piece, c, s);
     }
-    T* out = static_cast<T*>(w.out) + t * w.o_ts + h0 * w.o_hs + d;
+    const int h0 = at.group * HEADS, n = there && good ? min(HEADS, w.n_heads - h0) : 0;
+    T* out = static_cast<T*>(w.out) + at.t * w.o_ts + h0 * w.o_hs + d;
+    at.next();
+    pos = position();
+    copy(stage ^ 1);
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
 #pragma unroll
     for (int i = 0; i < HEADS; ++i) {
-      const bool mine = i < n && there && good;
-      float f[N], y[N], sum = 0.f, dot = 0.f;
+      float2 f[N / 2], y[N / 2], sums = make_float2(0.f, 0.f), dots = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int k = 0; k < N; ++k) f[k] = y[k] = 0.f;
-      if (mine) {
-        px[i].get(*reinterpret_cast<float(*)[8]>(f));
-        py[i].get(*reinterpret_cast<float(*)[8]>(y));
+      for (int k = 0; k < N / 2; ++k) f[k] = y[k] = make_float2(0.f, 0.f);
+      if (i < n) {
+        fetch(slot(stage, 0, i, 0), f);
+        fetch(slot(stage, 1, i, 0), y);
         if constexpr (!INTERLEAVED)
           if (two) {
-            qx[i].get(*reinterpret_cast<float(*)[8]>(f + 8));
-            qy[i].get(*reinterpret_cast<float(*)[8]>(y + 8));
+            fetch(slot(stage, 0, i, 1), f + 4);
+            fetch(slot(stage, 1, i, 1), y + 4);
           }
         if (turned) {                                          // the transposed rotation
+          if constexpr (INTERLEAVED) {
+            const float *cc = reinterpret_cast<const float*>(c), *ss = reinterpret_cast<const float*>(s);
 #pragma unroll
-          for (int k = 0; k < PAIRS; ++k) {
-            float &y1 = y[INTERLEAVED ? 2 * k : k], &y2 = y[INTERLEAVED ? 2 * k + 1 : k + 8];
-            const float z1 = y1 * c[k] + y2 * s[k], z2 = y2 * c[k] - y1 * s[k];
-            y1 = z1;
-            y2 = z2;
+            for (int k = 0; k < 4; ++k) y[k] = make_float2(fmaf(y[k].y, ss[k], y[k].x * cc[k]), fmaf(-y[k].x, ss[k], y[k].y * cc[k]));
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float2 y1 = y[k], z = mul2(y[k + 4], c[k]);
+              y[k] = fma2(y[k + 4], s[k], mul2(y1, c[k]));
+              y[k + 4] = make_float2(fmaf(-y1.x, s[k].x, z.x), fmaf(-y1.y, s[k].y, z.y));
+            }
           }
         }
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-          sum = fmaf(f[k], f[k], sum);
-          dot = fmaf(f[k], y[k] * g[k], dot);
+        for (int k = 0; k < N / 2; ++k) {
+          sums = fma2(f[k], f[k], sums);
+          dots = fma2(f[k], mul2(y[k], g[k]), dots);
         }
       }
+      float sum = sums.x + sums.y, dot = dots.x + dots.y;
 #pragma unroll
       for (int o = L / 2; o > 0; o >>= 1) {
         sum += __shfl_xor_sync(0xffffffffu, sum, o);
         dot += __shfl_xor_sync(0xffffffffu, dot, o);
       }
-      if (!mine) continue;
-      const float r = 1.f / sqrtf(fmaf(sum, inv_dim, a.eps)), m = r * r * (dot * inv_dim);
+      if (i >= n) continue;
+      const float r = 1.f / sqrtf(fmaf(sum, inv_dim, a.eps)), m = -r * (r * r * (dot * inv_dim));
+      const float2 rr = make_float2(r, r), mm = make_float2(m, m);
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        acc[k] = fmaf(y[k], f[k] * r, acc[k]);
-        f[k] = r * (y[k] * g[k] - f[k] * m);
+      for (int k = 0; k < N / 2; ++k) {
+        acc[k] = fma2(y[k], mul2(f[k], rr), acc[k]);
+        f[k] = fma2(f[k], mm, mul2(mul2(y[k], g[k]), rr));
       }
-      px[i].set(*reinterpret_cast<float(*)[8]>(f));
-      px[i].store(out + i * w.o_hs);
+      Piece<T> o;
+      o.set(*reinterpret_cast<float(*)[8]>(f));
+      o.store(out + i * w.o_hs);
       if constexpr (!INTERLEAVED)
         if (two) {
-          qx[i].set(*reinterpret_cast<float(*)[8]>(f + 8));
-          qx[i].store(out + i * w.o_hs + half);
+          o.set(*reinterpret_cast<float(*)[8]>(f + 4));
+          o.store(out + i * w.o_hs + half);
         }
     }
   }
   if (w.partial == nullptr) return;
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();                                             // nobody reads or fills the ring any more
+  float* share = reinterpret_cast<float*>(ring);
 #pragma unroll
-  for (int k = 0; k < N; ++k) share[slot][piece * N + k] = acc[k];
+  for (int k = 0; k < N / 4; ++k)
+    *reinterpret_cast<float4*>(share + (threadIdx.x / L) * B::PITCH + piece * N + 4 * k) = make_float4(acc[2 * k].x, acc[2 * k].y, acc[2 * k + 1].x, acc[2 * k + 1].y);
   __syncthreads();
   for (int e = threadIdx.x; e < a.head_dim; e += kThreads) {
     // element e of the head: which thread's, and which of its
-    int at;
-    if (INTERLEAVED) at = e;
-    else if (e < a.rot_dim) at = (e % half) / 8 * N + (e >= half ? 8 : 0) + e % 8;
-    else at = (a.rotated + (e - a.rot_dim) / 8) * N + e % 8;
+    int from;
+    if (INTERLEAVED) from = e;
+    else if (e < a.rot_dim) from = (e % half) / 8 * N + (e >= half ? 8 : 0) + e % 8;
+    else from = (a.rotated + (e - a.rot_dim) / 8) * N + e % 8;
     float sum = 0.f;
 #pragma unroll 8
-    for (int i = 0; i < SLOTS; ++i) sum += share[i][at];
+    for (int i = 0; i < SLOTS; ++i) sum += share[i * B::PITCH + from];
     w.partial[(long)block * a.head_dim + e] = sum;
   }
 }
@@ -351,8 +388,6 @@ __global__ void __launch_bounds__(1024) gain_grad_kernel(const __grid_constant__
   for (int i = 0; i < 32; ++i) sum += share[i][lane];
   a.out[which][e] = sum;
 }
-
-constexpr int kGradBlocksPerSm = 4;
 
 void set_pieces(NormArgs& n, const NormRopeCall& c) {
   n.positions = c.positions;
@@ -399,14 +434,17 @@ int launch_backward(NormArgs& n, int tokens, cudaStream_t s) {
   set_units(n, tokens, HEADS);
   deal_blocks(n, kThreads / L, norm_rope_grad_blocks());
   if (n.part[1].partial != nullptr) n.part[1].partial += (long)n.part[0].blocks * n.head_dim;
-  HBL_CUDA_OK(launch_waiting(norm_rope_grad_kernel<T, INTERLEAVED, L, HEADS>, dim3(n.part[0].blocks + n.part[1].blocks), dim3(kThreads), 0, s, n));
+  auto kern = norm_rope_grad_kernel<T, INTERLEAVED, L, HEADS>;
+  constexpr int bytes = BackwardGeo<T, INTERLEAVED, L, HEADS>::SMEM;
+  HBL_ALLOW_DYNAMIC_SMEM(kern, bytes);
+  HBL_CUDA_OK(launch_waiting(kern, dim3(n.part[0].blocks + n.part[1].blocks), dim3(kThreads), bytes, s, n));
   note_launch();
   return HBL_OK;
 }
 template <typename T, bool INTERLEAVED, int L>
 int launch_lanes(NormArgs& n, int tokens, bool backward, cudaStream_t s) {
   const bool many = (long)tokens * (n.part[0].n_heads + n.part[1].n_heads) * L >= (long)sm_count() * 2048 * 4;
-  if (backward) return many ? launch_backward<T, INTERLEAVED, L, 2>(n, tokens, s) : launch_backward<T, INTERLEAVED, L, 1>(n, tokens, s);
+  if (backward) return many ? launch_backward<T, INTERLEAVED, L, sizeof(T) == 2 ? 2 : 1>(n, tokens, s) : launch_backward<T, INTERLEAVED, L, 1>(n, tokens, s);
   return many ? launch_forward<T, INTERLEAVED, L, sizeof(T) == 2 ? 4 : 2>(n, tokens, s) : launch_forward<T, INTERLEAVED, L, 1>(n, tokens, s);
 }
 template <typename T, bool INTERLEAVED>
@@ -426,7 +464,7 @@ int launch_any(NormArgs& n, const NormRopeCall& c, bool backward, cudaStream_t s
 }  // namespace
 
 // Thread blocks of the backward kernel at most (and one more, where a part would get none).
-int norm_rope_grad_blocks() { return sm_count() * kGradBlocksPerSm; }
+int norm_rope_grad_blocks() { return sm_count() * kBackwardBlocksPerSm; }
 
 int launch_norm_rope(const NormRopeCall& c, cudaStream_t s) {
   NormArgs n{};
