@@ -7,16 +7,16 @@
 // summed in fp64 and r rounded once, the products and sums of the rest are rounded one by one in fp32: o is the plain fp32
 // evaluation bit for bit (kv_append_kernel quantizes the same values).  The backward pass is fp32 throughout.
 //
-// A thread owns what rope_kernel's does: 8 elements of the interleaved layout, 8 + 8 partners of the half layout, 8 of the
-// part that is not rotated.  The L lanes of a head add up its statistic; HEADS heads of a token (all of q, or all of k)
-// share a thread's gains and the table's pairs, and their loads are in flight together.
+// A thread owns 16 elements of a head; the L lanes of a head add up its statistic.  Thread blocks stay and walk over the call's
+// heads, HEADS of a token at a time: the gains are loaded once, the table's pairs once for HEADS heads, and the next ones are
+// copied to shared memory while a thread works on the current ones.
 #include "hbl_kv_cache.cuh"
 #include "hbl_piece.cuh"
 
 namespace hbl {
 namespace {
 
-constexpr int kThreads = 256, kForwardBlocksPerSm = 3, kBackwardBlocksPerSm = 2;
+constexpr int kThreads = 256, kForwardBlocksPerSm = 2, kBackwardBlocksPerSm = 2;
 
 struct Part {                          // the queries, or the keys
   const void *x, *gain;
@@ -30,31 +30,97 @@ struct Part {                          // the queries, or the keys
 struct NormArgs {
   Part part[2];
   const int32_t* positions;
-  const float4* table;                 // NULL: nothing is rotated
+  const float2* table;                 // NULL: nothing is rotated
   int* status;
   int gain_bf16, n_pos, rot_dim, head_dim, pieces, rotated;
   float eps;
 };
 
-// The pairs of a piece: cosines and sines, two to an element.
-template <int PAIRS>
-__device__ __forceinline__ void load_pairs(const NormArgs& a, int pos, int piece, float2 (&c)[PAIRS / 2], float2 (&s)[PAIRS / 2]) {
-  const float4* row = a.table + ((long)pos * (a.rot_dim / 2) + piece * PAIRS) / 2;      // two pairs to a float4
+// A thread's 16 elements of a head, 16 bytes at a time: chunk k of lane j of the L' lanes that share a part is the part's chunk
+// k L' + j, so that neighbouring lanes read neighbouring bytes.  The partners of the half layout are then a thread's own (chunk k
+// and k + N / 2), like those of the interleaved one, which lie in a chunk.  FULL: head_dim is a multiple of 16, so that every
+// thread that has chunks at all has N.
+template <typename T, bool FULL>
+struct Chunks {
+  static constexpr int E = 16 / sizeof(T), N = 16 / E;          // elements of a chunk, chunks of a thread
+  bool there, turned;                  // any at all; in the rotated part
+  int d, step, n;                      // the first one's element, from one to the next, how many
+  int pair, pair_step;                 // the first one's pair in the table's row, from one to the next
+  __device__ __forceinline__ Chunks(const NormArgs& a, bool interleaved, int lane) {
+    turned = lane < a.rotated;
+    const int first = turned ? 0 : a.rot_dim, lanes = turned ? a.rotated : a.pieces - a.rotated, j = turned ? lane : lane - a.rotated;
+    there = lane < a.pieces;
+    d = first + j * E;
+    step = lanes * E;
+    n = turned ? N : there ? min(N, (a.head_dim - d + step - 1) / step) : 0;
+    if (FULL) n = N;
+    pair = interleaved ? d / 2 : d;
+    pair_step = interleaved ? step / 2 : step;
+  }
+};
+template <typename T>
+__device__ __forceinline__ void widen(const uint4& w, float2* f) {     // a chunk
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-  for (int i = 0; i < PAIRS / 2; ++i) {
-    const float4 v = __ldg(row + i);
+    for (int i = 0; i < 4; ++i) f[i] = make_float2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xFFFF0000u));
+  } else {
+    f[0] = make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
+    f[1] = make_float2(__uint_as_float(w.z), __uint_as_float(w.w));
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint4 narrow(const float2* f) {
+  if constexpr (sizeof(T) == 2) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(f[i].x, f[i].y);
+      u[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+  } else {
+    return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
+  }
+}
+// The gains of a thread's elements; NULL: ones.
+template <typename T, bool FULL>
+__device__ __forceinline__ void load_gains(const NormArgs& a, const void* gain, const Chunks<T, FULL>& own, float2 (&g)[8]) {
+  constexpr int E = Chunks<T, FULL>::E;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int k = 2 * i / E, d = own.d + k * own.step + 2 * i % E;
+    g[i] = make_float2(1.f, 1.f);
+    if (gain != nullptr && own.there && k < own.n) {
+      if (a.gain_bf16) {
+        const uint32_t u = __ldg(static_cast<const uint32_t*>(gain) + d / 2);
+        g[i] = make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+      } else {
+        g[i] = __ldg(reinterpret_cast<const float2*>(static_cast<const float*>(gain) + d));
+      }
+    }
+  }
+}
+// The 8 pairs of a thread's elements: cosines and sines, two to an element.
+template <bool INTERLEAVED, typename T, bool FULL>
+__device__ __forceinline__ void load_pairs(const NormArgs& a, int pos, const Chunks<T, FULL>& own, float2 (&c)[4], float2 (&s)[4]) {
+  constexpr int E = Chunks<T, FULL>::E / (INTERLEAVED ? 2 : 1);       // pairs of a chunk
+  const float2* row = a.table + (long)pos * (a.rot_dim / 2) + own.pair;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {                                // two pairs to a float4
+    const float4 v = __ldg(reinterpret_cast<const float4*>(row + (2 * i / E) * own.pair_step + 2 * i % E));
     c[i] = make_float2(v.x, v.z);
     s[i] = make_float2(v.y, v.w);
   }
 }
 
-// Where a thread is in its part's units (a token's HEADS heads each), and where it goes next.
+// Where a thread is in its part's units (a token's HEADS heads each).
 struct Walker {
   long unit, units, step;
   int t, group, groups, step_t, step_group;       // the token, and which of its groups of heads
-  __device__ __forceinline__ Walker(const Part& w, int block, int slots, int slot) {
+  __device__ __forceinline__ Walker(const Part& w, int block, int slots, int slot, bool there) {
     groups = w.groups;
-    units = w.units;
+    units = there ? w.units : 0;
     step = (long)w.blocks * slots;
     step_t = (int)(step / groups);
     step_group = (int)(step % groups);
@@ -73,70 +139,77 @@ struct Walker {
   }
   __device__ __forceinline__ bool live() const { return unit < units; }
 };
+// One unit of one tensor to shared memory, [head][chunk][thread], where only the thread itself reads it.
+template <int HEADS, typename T, bool FULL>
+__device__ __forceinline__ void copy_unit(uint4* to, const void* from, long ts, long hs, const Walker& at, int n_heads, const Chunks<T, FULL>& own) {
+  constexpr int N = Chunks<T, FULL>::N;
+  if (!at.live()) return;
+  const int h0 = at.group * HEADS;
+  const T* x = static_cast<const T*>(from) + at.t * ts + h0 * hs + own.d;
+#pragma unroll
+  for (int i = 0; i < HEADS; ++i)
+    if (h0 + i < n_heads) {
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (FULL || k < own.n) copy_async16(to + (i * N + k) * kThreads, reinterpret_cast<const uint4*>(x + i * hs + k * own.step));
+    }
+}
+template <typename T, int HEADS>
+constexpr int kUnitWords = HEADS * (int)sizeof(T) * kThreads;    // of 16 bytes, of all threads
+// A head's elements out of there; zeros where there are none.
+template <typename T, bool FULL>
+__device__ __forceinline__ void fetch(const uint4* from, const Chunks<T, FULL>& own, float2 (&f)[8]) {
+  constexpr int N = Chunks<T, FULL>::N, P = 8 / N;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    widen<T>(FULL || k < own.n ? from[k * kThreads] : make_uint4(0, 0, 0, 0), f + k * P);
+}
+template <typename T, bool FULL>
+__device__ __forceinline__ void store(T* out, const Chunks<T, FULL>& own, const float2 (&f)[8]) {
+  constexpr int N = Chunks<T, FULL>::N, P = 8 / N;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (FULL || k < own.n) *reinterpret_cast<uint4*>(out + k * own.step) = narrow<T>(f + k * P);
+}
+__device__ __forceinline__ float of(const float2 (&c)[4], int k) { return k & 1 ? c[k / 2].y : c[k / 2].x; }
+// A token's position; false (and reported): it has none.
+__device__ __forceinline__ bool sound(const NormArgs& a, int pos) {
+  if (pos >= 0 && pos < a.n_pos) return true;
+  report_device_error(a.status, HBL_ERR_RANGE);
+  return false;
+}
 
-// Thread blocks stay and walk over the units of their part.  A thread copies its pieces of the next unit to shared memory, where
-// only it reads them, while it works on the current one's.
-template <typename T, bool INTERLEAVED, int HEADS>
-struct ForwardGeo {
-  static constexpr int BYTES = 8 * sizeof(T), PIECES = INTERLEAVED ? 1 : 2;      // of a thread and head
-  static constexpr int STAGE = HEADS * PIECES * BYTES * kThreads;
-};
-template <typename T, bool INTERLEAVED, int L, int HEADS>
+template <typename T, bool INTERLEAVED, bool FULL, int L, int HEADS>
 __global__ void __launch_bounds__(kThreads, kForwardBlocksPerSm) norm_rope_kernel(const __grid_constant__ NormArgs a) {
-  using G = ForwardGeo<T, INTERLEAVED, HEADS>;
-  constexpr int PAIRS = INTERLEAVED ? 4 : 8, SLOTS = kThreads / L, Q = G::BYTES / 16;
-  extern __shared__ uint4 ring[];                              // [stage][head][piece][16 bytes of it][thread]
+  constexpr int SLOTS = kThreads / L, WORDS = kUnitWords<T, HEADS>, N = Chunks<T, FULL>::N;
+  extern __shared__ uint4 ring[];                              // two units
   grid_dependency_wait();
   const bool second = (int)blockIdx.x >= a.part[0].blocks;
   const Part& w = a.part[second];
-  const int block = blockIdx.x - (second ? a.part[0].blocks : 0), piece = threadIdx.x % L;
-  const bool there = piece < a.pieces, turned = piece < a.rotated, two = !INTERLEAVED && turned;
-  const int half = a.rot_dim / 2, d = turned ? piece * 8 : a.rot_dim + (piece - a.rotated) * 8;
-  Walker at(w, block, SLOTS, threadIdx.x / L);
-  uint4* const mine = ring + threadIdx.x;
-  auto slot = [&](int stage, int i, int half_of) { return mine + (stage * (G::STAGE / 16) + (i * G::PIECES + half_of) * Q * kThreads); };
+  const int block = blockIdx.x - (second ? a.part[0].blocks : 0), lane = threadIdx.x % L;
+  const Chunks<T, FULL> own(a, INTERLEAVED, lane);
+  Walker at(w, block, SLOTS, threadIdx.x / L, own.there);
   auto copy = [&](int stage) {
-    if (there && at.live()) {
-      const int h0 = at.group * HEADS;
-      const T* x = static_cast<const T*>(w.x) + at.t * w.x_ts + h0 * w.x_hs + d;
-#pragma unroll
-      for (int i = 0; i < HEADS; ++i)
-        if (h0 + i < w.n_heads) {
-#pragma unroll
-          for (int b = 0; b < Q; ++b) {
-            copy_async16(slot(stage, i, 0) + b * kThreads, reinterpret_cast<const uint4*>(x + i * w.x_hs) + b);
-            if (two) copy_async16(slot(stage, i, 1) + b * kThreads, reinterpret_cast<const uint4*>(x + i * w.x_hs + half) + b);
-          }
-        }
-    }
+    copy_unit<HEADS>(ring + threadIdx.x + stage * WORDS, w.x, w.x_ts, w.x_hs, at, w.n_heads, own);
     asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  auto fetch = [&](int stage, int i, int half_of, float2 (&f)[4]) {
-    Piece<T> p;
-    p.load_from(slot(stage, i, half_of), kThreads);
-    p.get(*reinterpret_cast<float(*)[8]>(f));
   };
   auto position = [&]() { return a.table != nullptr && at.live() ? __ldg(a.positions + at.t) : 0; };
   copy(0);
   int pos = position();
-  float2 g[4], g2[4];
-  if (there) load_gain(w.gain, a.gain_bf16, d, *reinterpret_cast<float(*)[8]>(g));
-  if (two) load_gain(w.gain, a.gain_bf16, d + half, *reinterpret_cast<float(*)[8]>(g2));
+  float2 g[8];
+  load_gains(a, w.gain, own, g);
   const double inv_dim = 1.0 / a.head_dim;
   int stage = 0;
   for (long u0 = (long)block * SLOTS; u0 < w.units; u0 += (long)w.blocks * SLOTS, stage ^= 1) {
-    float2 c[PAIRS / 2], s[PAIRS / 2];
+    float2 c[4], s[4];
     bool good = at.live();
     if (a.table != nullptr) {
-      if (pos < 0 || pos >= a.n_pos) {
-        report_device_error(a.status, HBL_ERR_RANGE);
-        good = false;
-      }
-      if (turned && good) load_pairs<PAIRS>(a, pos, piece, c, s);
+      good = sound(a, pos) && good;
+      if (own.turned && good) load_pairs<INTERLEAVED>(a, pos, own, c, s);
     }
-    const int h0 = at.group * HEADS, n = there ? min(HEADS, w.n_heads - h0) : 0;
-    T* out = static_cast<T*>(w.out) + at.t * w.o_ts + h0 * w.o_hs + d;
-    const bool filled = at.live();
+    const int h0 = at.group * HEADS, n = at.live() ? min(HEADS, w.n_heads - h0) : 0;
+    T* out = static_cast<T*>(w.out) + at.t * w.o_ts + h0 * w.o_hs + own.d;
+    const uint4* here = ring + threadIdx.x + stage * WORDS;
     at.next();
     pos = position();
     copy(stage ^ 1);
@@ -145,17 +218,12 @@ __global__ void __launch_bounds__(kThreads, kForwardBlocksPerSm) norm_rope_kerne
     double sum[HEADS];
 #pragma unroll
     for (int i = 0; i < HEADS; ++i) {
-      float2 f[4];
       sum[i] = 0.0;
-      if (i < n && filled) {
-        fetch(stage, i, 0, f);
+      if (i < n) {
+        float2 f[8];
+        fetch(here + i * N * kThreads, own, f);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sum[i] = fma((double)f[k].y, (double)f[k].y, fma((double)f[k].x, (double)f[k].x, sum[i]));
-        if (two) {
-          fetch(stage, i, 1, f);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) sum[i] = fma((double)f[k].y, (double)f[k].y, fma((double)f[k].x, (double)f[k].x, sum[i]));
-        }
+        for (int k = 0; k < 8; ++k) sum[i] = fma((double)f[k].y, (double)f[k].y, fma((double)f[k].x, (double)f[k].x, sum[i]));
       }
     }
 #pragma unroll
@@ -167,144 +235,94 @@ __global__ void __launch_bounds__(kThreads, kForwardBlocksPerSm) norm_rope_kerne
     double of_lane = sum[0];
 #pragma unroll
     for (int i = 1; i < HEADS; ++i)
-      if (piece % HEADS == i) of_lane = sum[i];
+      if (lane % HEADS == i) of_lane = sum[i];
     const float root = inverse_root(fma(of_lane, inv_dim, (double)a.eps));
 #pragma unroll
     for (int i = 0; i < HEADS; ++i) {
       const float r = __shfl_sync(0xffffffffu, root, i, L);
       if (i >= n || !good) continue;
-      float2 f[4];
-      fetch(stage, i, 0, f);
-      Piece<T> o;
+      float2 f[8];
+      fetch(here + i * N * kThreads, own, f);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) f[k] = mul2(f[k], g[k]);
-      if (turned) {
+      for (int k = 0; k < 8; ++k) f[k] = mul2(f[k], g[k]);
+      if (own.turned) {
         if constexpr (INTERLEAVED) {
-          float* y = reinterpret_cast<float*>(f);
-          const float *cc = reinterpret_cast<const float*>(c), *ss = reinterpret_cast<const float*>(s);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float x1 = y[2 * k], x2 = y[2 * k + 1];
-            y[2 * k] = __fsub_rn(__fmul_rn(x1, cc[k]), __fmul_rn(x2, ss[k]));
-            y[2 * k + 1] = __fadd_rn(__fmul_rn(x2, cc[k]), __fmul_rn(x1, ss[k]));
+          for (int k = 0; k < 8; ++k) {
+            const float2 x = mul2(f[k], make_float2(of(c, k), of(c, k))), y = mul2(f[k], make_float2(of(s, k), of(s, k)));
+            f[k] = make_float2(__fsub_rn(x.x, y.y), __fadd_rn(x.y, y.x));
           }
         } else {
-          float2 e[4];
-          fetch(stage, i, 1, e);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const float2 x1 = f[k], x2 = mul2(e[k], g2[k]);
+            const float2 x1 = f[k], x2 = f[k + 4];
             f[k] = sub2(mul2(x1, c[k]), mul2(x2, s[k]));
-            e[k] = mul2(add2(mul2(x2, c[k]), mul2(x1, s[k])), make_float2(r, r));
+            f[k + 4] = add2(mul2(x2, c[k]), mul2(x1, s[k]));
           }
-          o.set(*reinterpret_cast<float(*)[8]>(e));
-          o.store(out + i * w.o_hs + half);
         }
       }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) f[k] = mul2(f[k], make_float2(r, r));
-      o.set(*reinterpret_cast<float(*)[8]>(f));
-      o.store(out + i * w.o_hs);
+      for (int k = 0; k < 8; ++k) f[k] = mul2(f[k], make_float2(r, r));
+      store(out + i * w.o_hs, own, f);
     }
   }
 }
 
-// The same walk; a thread keeps its piece of the head, so that its share of dg stays in registers.  The block's shares are added
+// The same walk.  A thread keeps its elements of the head, so that its share of dg stays in registers; the block's shares are added
 // in shared memory in the order of its threads, the blocks' by gain_grad_kernel.
-template <typename T, bool INTERLEAVED, int L, int HEADS>
-struct BackwardGeo {
-  using F = ForwardGeo<T, INTERLEAVED, HEADS>;
-  static constexpr int N = 8 * F::PIECES, PITCH = L * N + 4, SLOTS = kThreads / L;
-  static constexpr int RING = 2 * 2 * F::STAGE, SHARES = SLOTS * PITCH * 4, SMEM = RING > SHARES ? RING : SHARES;
-};
-template <typename T, bool INTERLEAVED, int L, int HEADS>
+template <int L>
+struct Shares { static constexpr int PITCH = L * 16 + 4, BYTES = kThreads / L * PITCH * 4; };
+template <typename T, bool INTERLEAVED, bool FULL, int L, int HEADS>
 __global__ void __launch_bounds__(kThreads, kBackwardBlocksPerSm) norm_rope_grad_kernel(const __grid_constant__ NormArgs a) {
-  using G = ForwardGeo<T, INTERLEAVED, HEADS>;
-  using B = BackwardGeo<T, INTERLEAVED, L, HEADS>;
-  constexpr int PAIRS = INTERLEAVED ? 4 : 8, SLOTS = B::SLOTS, N = B::N, Q = G::BYTES / 16, P = G::PIECES;
-  extern __shared__ uint4 ring[];                              // [stage][x, do][head][piece][16 bytes of it][thread]
+  constexpr int SLOTS = kThreads / L, WORDS = kUnitWords<T, HEADS>, N = Chunks<T, FULL>::N, PITCH = Shares<L>::PITCH;
+  extern __shared__ uint4 ring[];                              // two units of x and do; at the end the shares
   grid_dependency_wait();
   const bool second = (int)blockIdx.x >= a.part[0].blocks;
   const Part& w = a.part[second];
-  const int block = blockIdx.x - (second ? a.part[0].blocks : 0), piece = threadIdx.x % L;
-  const bool there = piece < a.pieces, turned = piece < a.rotated, two = !INTERLEAVED && turned;
-  const int half = a.rot_dim / 2, d = turned ? piece * 8 : a.rot_dim + (piece - a.rotated) * 8;
-  Walker at(w, block, SLOTS, threadIdx.x / L);
-  uint4* const mine = ring + threadIdx.x;
-  auto slot = [&](int stage, int which, int i, int half_of) {
-    return mine + ((stage * 2 + which) * (G::STAGE / 16) + (i * P + half_of) * Q * kThreads);
-  };
+  const int block = blockIdx.x - (second ? a.part[0].blocks : 0), lane = threadIdx.x % L;
+  const Chunks<T, FULL> own(a, INTERLEAVED, lane);
+  Walker at(w, block, SLOTS, threadIdx.x / L, own.there);
   auto copy = [&](int stage) {
-    if (there && at.live()) {
-      const int h0 = at.group * HEADS;
-      const T* x = static_cast<const T*>(w.x) + at.t * w.x_ts + h0 * w.x_hs + d;
-      const T* y = static_cast<const T*>(w.grad) + at.t * w.g_ts + h0 * w.g_hs + d;
-#pragma unroll
-      for (int i = 0; i < HEADS; ++i)
-        if (h0 + i < w.n_heads) {
-#pragma unroll
-          for (int b = 0; b < Q; ++b) {
-            copy_async16(slot(stage, 0, i, 0) + b * kThreads, reinterpret_cast<const uint4*>(x + i * w.x_hs) + b);
-            copy_async16(slot(stage, 1, i, 0) + b * kThreads, reinterpret_cast<const uint4*>(y + i * w.g_hs) + b);
-            if (two) {
-              copy_async16(slot(stage, 0, i, 1) + b * kThreads, reinterpret_cast<const uint4*>(x + i * w.x_hs + half) + b);
-              copy_async16(slot(stage, 1, i, 1) + b * kThreads, reinterpret_cast<const uint4*>(y + i * w.g_hs + half) + b);
-            }
-          }
-        }
-    }
+    copy_unit<HEADS>(ring + threadIdx.x + 2 * stage * WORDS, w.x, w.x_ts, w.x_hs, at, w.n_heads, own);
+    copy_unit<HEADS>(ring + threadIdx.x + (2 * stage + 1) * WORDS, w.grad, w.g_ts, w.g_hs, at, w.n_heads, own);
     asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  auto fetch = [&](const uint4* from, float2* f) {
-    Piece<T> p;
-    p.load_from(from, kThreads);
-    p.get(*reinterpret_cast<float(*)[8]>(f));
   };
   auto position = [&]() { return a.table != nullptr && at.live() ? __ldg(a.positions + at.t) : 0; };
   copy(0);
   int pos = position();
-  float2 g[N / 2], acc[N / 2];
+  float2 g[8], acc[8];
+  load_gains(a, w.gain, own, g);
 #pragma unroll
-  for (int k = 0; k < N / 2; ++k) g[k] = acc[k] = make_float2(0.f, 0.f);
-  if (there) load_gain(w.gain, a.gain_bf16, d, *reinterpret_cast<float(*)[8]>(g));
-  if constexpr (!INTERLEAVED)
-    if (two) load_gain(w.gain, a.gain_bf16, d + half, *reinterpret_cast<float(*)[8]>(g + 4));
+  for (int k = 0; k < 8; ++k) acc[k] = make_float2(0.f, 0.f);
   const float inv_dim = 1.f / (float)a.head_dim;
   int stage = 0;
   for (long u0 = (long)block * SLOTS; u0 < w.units; u0 += (long)w.blocks * SLOTS, stage ^= 1) {
-    float2 c[PAIRS / 2], s[PAIRS / 2];
+    float2 c[4], s[4];
     bool good = at.live();
     if (a.table != nullptr) {
-      if (pos < 0 || pos >= a.n_pos) {
-        report_device_error(a.status, HBL_ERR_RANGE);
-        good = false;
-      }
-      if (turned && good) load_pairs<PAIRS>(a, pos, piece, c, s);
+      good = sound(a, pos) && good;
+      if (own.turned && good) load_pairs<INTERLEAVED>(a, pos, own, c, s);
     }
-    const int h0 = at.group * HEADS, n = there && good ? min(HEADS, w.n_heads - h0) : 0;
-    T* out = static_cast<T*>(w.out) + at.t * w.o_ts + h0 * w.o_hs + d;
+    const int h0 = at.group * HEADS, n = good ? min(HEADS, w.n_heads - h0) : 0;
+    T* out = static_cast<T*>(w.out) + at.t * w.o_ts + h0 * w.o_hs + own.d;
+    const uint4* here = ring + threadIdx.x + 2 * stage * WORDS;
     at.next();
     pos = position();
     copy(stage ^ 1);
     asm volatile("cp.async.wait_group 1;" ::: "memory");
 #pragma unroll
     for (int i = 0; i < HEADS; ++i) {
-      float2 f[N / 2], y[N / 2], sums = make_float2(0.f, 0.f), dots = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < N / 2; ++k) f[k] = y[k] = make_float2(0.f, 0.f);
+      float2 f[8], y[8], sums = make_float2(0.f, 0.f), dots = make_float2(0.f, 0.f);
       if (i < n) {
-        fetch(slot(stage, 0, i, 0), f);
-        fetch(slot(stage, 1, i, 0), y);
-        if constexpr (!INTERLEAVED)
-          if (two) {
-            fetch(slot(stage, 0, i, 1), f + 4);
-            fetch(slot(stage, 1, i, 1), y + 4);
-          }
-        if (turned) {                                          // the transposed rotation
+        fetch(here + i * N * kThreads, own, f);
+        fetch(here + WORDS + i * N * kThreads, own, y);
+        if (own.turned) {                                      // the transposed rotation
           if constexpr (INTERLEAVED) {
-            const float *cc = reinterpret_cast<const float*>(c), *ss = reinterpret_cast<const float*>(s);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) y[k] = make_float2(fmaf(y[k].y, ss[k], y[k].x * cc[k]), fmaf(-y[k].x, ss[k], y[k].y * cc[k]));
+            for (int k = 0; k < 8; ++k) {
+              const float2 z = mul2(y[k], make_float2(of(c, k), of(c, k)));
+              y[k] = make_float2(fmaf(y[k].y, of(s, k), z.x), fmaf(-y[k].x, of(s, k), z.y));
+            }
           } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -315,7 +333,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardBlocksPerSm) norm_rope_grad
           }
         }
 #pragma unroll
-        for (int k = 0; k < N / 2; ++k) {
+        for (int k = 0; k < 8; ++k) {
           sums = fma2(f[k], f[k], sums);
           dots = fma2(f[k], mul2(y[k], g[k]), dots);
         }
@@ -330,18 +348,11 @@ __global__ void __launch_bounds__(kThreads, kBackwardBlocksPerSm) norm_rope_grad
       const float r = 1.f / sqrtf(fmaf(sum, inv_dim, a.eps)), m = -r * (r * r * (dot * inv_dim));
       const float2 rr = make_float2(r, r), mm = make_float2(m, m);
 #pragma unroll
-      for (int k = 0; k < N / 2; ++k) {
+      for (int k = 0; k < 8; ++k) {
         acc[k] = fma2(y[k], mul2(f[k], rr), acc[k]);
         f[k] = fma2(f[k], mm, mul2(mul2(y[k], g[k]), rr));
       }
-      Piece<T> o;
-      o.set(*reinterpret_cast<float(*)[8]>(f));
-      o.store(out + i * w.o_hs);
-      if constexpr (!INTERLEAVED)
-        if (two) {
-          o.set(*reinterpret_cast<float(*)[8]>(f + 4));
-          o.store(out + i * w.o_hs + half);
-        }
+      store(out + i * w.o_hs, own, f);
     }
   }
   if (w.partial == nullptr) return;
@@ -349,18 +360,15 @@ __global__ void __launch_bounds__(kThreads, kBackwardBlocksPerSm) norm_rope_grad
   __syncthreads();                                             // nobody reads or fills the ring any more
   float* share = reinterpret_cast<float*>(ring);
 #pragma unroll
-  for (int k = 0; k < N / 4; ++k)
-    *reinterpret_cast<float4*>(share + (threadIdx.x / L) * B::PITCH + piece * N + 4 * k) = make_float4(acc[2 * k].x, acc[2 * k].y, acc[2 * k + 1].x, acc[2 * k + 1].y);
+  for (int i = 0; i < 8; ++i) {
+    const int k = 2 * i / Chunks<T, FULL>::E, d = own.d + k * own.step + 2 * i % Chunks<T, FULL>::E;
+    if (own.there && k < own.n) *reinterpret_cast<float2*>(share + (threadIdx.x / L) * PITCH + d) = acc[i];
+  }
   __syncthreads();
   for (int e = threadIdx.x; e < a.head_dim; e += kThreads) {
-    // element e of the head: which thread's, and which of its
-    int from;
-    if (INTERLEAVED) from = e;
-    else if (e < a.rot_dim) from = (e % half) / 8 * N + (e >= half ? 8 : 0) + e % 8;
-    else from = (a.rotated + (e - a.rot_dim) / 8) * N + e % 8;
     float sum = 0.f;
 #pragma unroll 8
-    for (int i = 0; i < SLOTS; ++i) sum += share[i * B::PITCH + from];
+    for (int i = 0; i < SLOTS; ++i) sum += share[i * PITCH + e];
     w.partial[(long)block * a.head_dim + e] = sum;
   }
 }
@@ -391,11 +399,11 @@ __global__ void __launch_bounds__(1024) gain_grad_kernel(const __grid_constant__
 
 void set_pieces(NormArgs& n, const NormRopeCall& c) {
   n.positions = c.positions;
-  n.table = reinterpret_cast<const float4*>(c.table);
+  n.table = reinterpret_cast<const float2*>(c.table);
   n.gain_bf16 = c.gain_dtype == HBL_BF16;
   n.n_pos = c.n_pos; n.rot_dim = c.table != nullptr ? c.rot_dim : 0; n.head_dim = c.head_dim; n.eps = c.norm_eps;
-  n.rotated = n.rot_dim / (c.interleaved ? 8 : 16);
-  n.pieces = n.rotated + (c.head_dim - n.rot_dim) / 8;
+  n.rotated = n.rot_dim / 16;
+  n.pieces = (c.head_dim + 15) / 16;
   for (int i = 0; i < 2; ++i) {
     const NormRopePart& s = c.part[i];
     Part& d = n.part[i];
@@ -418,40 +426,47 @@ void deal_blocks(NormArgs& n, int slots, long most) {
     d.blocks = (int)(need < share ? need : share < 1 && need > 0 ? 1 : share);
   }
 }
-template <typename T, bool INTERLEAVED, int L, int HEADS>
+template <typename T, bool INTERLEAVED, bool FULL, int L, int HEADS>
 int launch_forward(NormArgs& n, int tokens, cudaStream_t s) {
   set_units(n, tokens, HEADS);
   deal_blocks(n, kThreads / L, (long)sm_count() * kForwardBlocksPerSm);
-  auto kern = norm_rope_kernel<T, INTERLEAVED, L, HEADS>;
-  constexpr int bytes = 2 * ForwardGeo<T, INTERLEAVED, HEADS>::STAGE;
+  auto kern = norm_rope_kernel<T, INTERLEAVED, FULL, L, HEADS>;
+  constexpr int bytes = 2 * 16 * kUnitWords<T, HEADS>;
   HBL_ALLOW_DYNAMIC_SMEM(kern, bytes);
   HBL_CUDA_OK(launch_waiting(kern, dim3(n.part[0].blocks + n.part[1].blocks), dim3(kThreads), bytes, s, n));
   note_launch();
   return HBL_OK;
 }
-template <typename T, bool INTERLEAVED, int L, int HEADS>
+template <typename T, bool INTERLEAVED, bool FULL, int L, int HEADS>
 int launch_backward(NormArgs& n, int tokens, cudaStream_t s) {
   set_units(n, tokens, HEADS);
   deal_blocks(n, kThreads / L, norm_rope_grad_blocks());
   if (n.part[1].partial != nullptr) n.part[1].partial += (long)n.part[0].blocks * n.head_dim;
-  auto kern = norm_rope_grad_kernel<T, INTERLEAVED, L, HEADS>;
-  constexpr int bytes = BackwardGeo<T, INTERLEAVED, L, HEADS>::SMEM;
+  auto kern = norm_rope_grad_kernel<T, INTERLEAVED, FULL, L, HEADS>;
+  constexpr int units = 4 * 16 * kUnitWords<T, HEADS>, bytes = units > Shares<L>::BYTES ? units : Shares<L>::BYTES;
   HBL_ALLOW_DYNAMIC_SMEM(kern, bytes);
   HBL_CUDA_OK(launch_waiting(kern, dim3(n.part[0].blocks + n.part[1].blocks), dim3(kThreads), bytes, s, n));
   note_launch();
   return HBL_OK;
 }
+// Several heads to a unit once that still leaves every SM a full set of threads; one while the call is small and its latency is
+// what counts (and for a head_dim that is no multiple of 16).
 template <typename T, bool INTERLEAVED, int L>
 int launch_lanes(NormArgs& n, int tokens, bool backward, cudaStream_t s) {
-  const bool many = (long)tokens * (n.part[0].n_heads + n.part[1].n_heads) * L >= (long)sm_count() * 2048 * 4;
-  if (backward) return many ? launch_backward<T, INTERLEAVED, L, sizeof(T) == 2 ? 2 : 1>(n, tokens, s) : launch_backward<T, INTERLEAVED, L, 1>(n, tokens, s);
-  return many ? launch_forward<T, INTERLEAVED, L, sizeof(T) == 2 ? 4 : 2>(n, tokens, s) : launch_forward<T, INTERLEAVED, L, 1>(n, tokens, s);
+  const bool full = n.head_dim % 16 == 0, many = full && (long)tokens * (n.part[0].n_heads + n.part[1].n_heads) * L >= (long)sm_count() * 2048 * 4;
+  constexpr int F = sizeof(T) == 2 ? 4 : 2;
+  if (backward) {
+    if (many) return launch_backward<T, INTERLEAVED, true, L, F / 2>(n, tokens, s);
+    return full ? launch_backward<T, INTERLEAVED, true, L, 1>(n, tokens, s) : launch_backward<T, INTERLEAVED, false, L, 1>(n, tokens, s);
+  }
+  if (many) return launch_forward<T, INTERLEAVED, true, L, F>(n, tokens, s);
+  return full ? launch_forward<T, INTERLEAVED, true, L, 1>(n, tokens, s) : launch_forward<T, INTERLEAVED, false, L, 1>(n, tokens, s);
 }
 template <typename T, bool INTERLEAVED>
 int launch_type(NormArgs& n, int tokens, bool backward, cudaStream_t s) {
+  if (n.pieces <= 4) return launch_lanes<T, INTERLEAVED, 4>(n, tokens, backward, s);
   if (n.pieces <= 8) return launch_lanes<T, INTERLEAVED, 8>(n, tokens, backward, s);
-  if (n.pieces <= 16) return launch_lanes<T, INTERLEAVED, 16>(n, tokens, backward, s);
-  return launch_lanes<T, INTERLEAVED, 32>(n, tokens, backward, s);
+  return launch_lanes<T, INTERLEAVED, 16>(n, tokens, backward, s);
 }
 int launch_any(NormArgs& n, const NormRopeCall& c, bool backward, cudaStream_t s) {
   n.status = device_status_word();

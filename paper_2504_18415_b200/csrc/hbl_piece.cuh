@@ -12,7 +12,6 @@ template <>
 struct Piece<__nv_bfloat16> {
   uint4 w;
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void load_from(const uint4* p, int) { w = *p; }          // 16 bytes at a time, so far apart
   __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = w; }
   __device__ __forceinline__ void get(float (&f)[8]) const {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
@@ -35,10 +34,6 @@ struct Piece<__nv_bfloat16> {
 template <>
 struct Piece<float> {
   float4 a, b;
-  __device__ __forceinline__ void load_from(const uint4* p, int apart) {
-    a = *reinterpret_cast<const float4*>(p);
-    b = *reinterpret_cast<const float4*>(p + apart);
-  }
   __device__ __forceinline__ void load(const float* p) {
     a = *reinterpret_cast<const float4*>(p);
     b = *reinterpret_cast<const float4*>(p + 4);
