@@ -51,6 +51,44 @@ __device__ __forceinline__ uint2 codes8(const float (&f)[8], float rq) {
   return make_uint2(low_bytes(u[0], u[1], u[2], u[3]), low_bytes(u[4], u[5], u[6], u[7]));
 }
 
+// ROWS sums over the LPH lanes of a head, each of which ends up with one of them (row_lane(i) with that of row i): half of the
+// rows' shares go to the other half of the lanes, and so on, so that each lane's share is added once.
+template <int ROWS, int LPH>
+__device__ __forceinline__ constexpr int row_lane(int i) {
+  return ROWS == 1 ? 0 : ROWS <= 4 ? (i >> 1 & 1) * (LPH / 2) + (i & 1) * (LPH / 4) : (i >> 2 & 1) * (LPH / 2) + (i >> 1 & 1) * (LPH / 4) + (i & 1) * (LPH / 8);
+}
+template <int ROWS, int LPH>
+__device__ __forceinline__ double sum_rows(const double (&s)[ROWS], int lane) {
+  constexpr int P = ROWS == 1 ? 1 : ROWS <= 4 ? 4 : 8;
+  static_assert(ROWS <= 8 && P <= LPH, "a lane to a row");
+  double v[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) v[i] = i < ROWS ? s[i < ROWS ? i : 0] : 0.0;
+  int o = LPH / 2;
+#pragma unroll
+  for (int n = P / 2; n > 0; n >>= 1, o >>= 1) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const double mine = up ? v[i + n] : v[i], give = up ? v[i] : v[i + n];
+      v[i] = mine + __shfl_xor_sync(0xffffffffu, give, o);
+    }
+  }
+  for (; o > 0; o >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+  return v[0];
+}
+// 8 elements times their gains, from element d on.
+__device__ __forceinline__ void scale8(float (&x)[8], const void* gain, int bf16, int d) {
+  float g[8];
+  load_gain(gain, bf16, d, g);
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const float2 y = mul2(make_float2(x[e], x[e + 1]), make_float2(g[e], g[e + 1]));
+    x[e] = y.x;
+    x[e + 1] = y.y;
+  }
+}
+
 struct AppendParams {
   KvView c;
   BatchView b;
@@ -101,7 +139,7 @@ __device__ __forceinline__ bool find_place(const KvView& c, const BatchView& s, 
 // NORM: queries and keys are r R(gain x), r = 1 / sqrt(mean x^2 + eps).  R is linear, so r goes last; x's squares are summed in fp64
 // (a bf16 value's is exact) and r is rounded once, so that a key's codes are those of the fp32 formula, bit for bit.
 template <int BITS, int LPH, bool INTERLEAVED, int ROWS, bool EVEN, bool NORM>
-__global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_append_kernel(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(kThreads, ROWS >= 4 && (NORM || (ROWS == 6 && BITS < 8)) ? 4 : 0) kv_append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int HPW = 32 / LPH;                               // heads side by side in a warp
   const int groups = p.groups;                                // ... and in the block
   grid_dependency_wait();
@@ -152,6 +190,20 @@ __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_ap
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) { c[i] = 1.f; s[i] = 0.f; }
   }
+  float root = 1.f;                                            // NORM: of the lane's row, see row_lane
+  if constexpr (NORM) {
+    double sum[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      sum[i] = 0.0;
+      if (EVEN && r0 + i * groups >= first_v) continue;
+      float x[8];
+      widen8(raw[i], x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[i] = fma((double)x[e], (double)x[e], sum[i]);
+    }
+    root = inverse_root(fma(sum_rows<ROWS, LPH>(sum, lane), 1.0 / (8 * LPH), (double)p.norm_eps));
+  }
   const long row0 = cache_row(p.c, at.page, 0, at.slot);      // head h: row0 + (h << page_shift)
   float f[BITS == 16 ? 1 : ROWS][8];
   uint32_t top[ROWS];
@@ -161,46 +213,42 @@ __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_ap
     float (&x)[8] = f[BITS == 16 ? 0 : i];
     top[i] = 0;
     widen8(raw[i], x);
-    float inv = 1.f;                                           // (times one: a value)
-    const void* gain = nullptr;
+    const float inv = NORM ? __shfl_sync(0xffffffffu, root, (lane & ~(LPH - 1)) + row_lane<ROWS, LPH>(i)) : 1.f;
     if constexpr (NORM) {
-      if (EVEN ? r < first_v : __any_sync(0xffffffffu, r < first_v)) {
-        double sum = 0.0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fma((double)x[e], (double)x[e], sum);
-#pragma unroll
-        for (int o = LPH / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (r < first_v) {
-          inv = inverse_root(sum / (8 * LPH) + (double)p.norm_eps);
-          gain = r < p.n_heads ? p.q_gain : p.k_gain;
-          if (gain != nullptr) {
-            float g[8];
-            load_gain(gain, p.gain_bf16, 8 * j, g);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = __fmul_rn(x[e], g[e]);
-          }
-        }
-      }
+      const void* gain = r < p.n_heads ? p.q_gain : r < first_v ? p.k_gain : nullptr;
+      if (gain != nullptr) scale8(x, gain, p.gain_bf16, 8 * j);
     }
     const bool rotate = turned && r < first_v;
     if (EVEN ? p.table != nullptr && r < first_v : __any_sync(0xffffffffu, rotate)) {      // (the whole warp: it shuffles)
       if constexpr (!INTERLEAVED) {
-        uint4 other;
-        other.x = __shfl_sync(0xffffffffu, raw[i].x, partner);
-        other.y = __shfl_sync(0xffffffffu, raw[i].y, partner);
-        other.z = __shfl_sync(0xffffffffu, raw[i].z, partner);
-        other.w = __shfl_sync(0xffffffffu, raw[i].w, partner);
-        if (rotate) {
-          float g[8];
+        float g[8];
+        if constexpr (NORM) {                                  // (with its gain: eight shuffles, against four, the gain and its product)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) g[e] = __shfl_sync(0xffffffffu, x[e], partner);
+        } else {
+          uint4 other;
+          other.x = __shfl_sync(0xffffffffu, raw[i].x, partner);
+          other.y = __shfl_sync(0xffffffffu, raw[i].y, partner);
+          other.z = __shfl_sync(0xffffffffu, raw[i].z, partner);
+          other.w = __shfl_sync(0xffffffffu, raw[i].w, partner);
           widen8(other, g);
-          if (NORM && gain != nullptr) {
-            float h[8];
-            load_gain(gain, p.gain_bf16, 8 * (upper ? j - half8 : j + half8), h);
+        }
+        if (rotate) {
+          // (packed products: 3-bit prompts 185 -> 181 us with the norm, but 148 -> 152 without)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) g[e] = __fmul_rn(g[e], h[e]);
+          for (int e = 0; e < 8; e += 2) {
+            float2 own = make_float2(x[e], x[e + 1]), its = make_float2(g[e], g[e + 1]);
+            const float2 cs = make_float2(c[e], c[e + 1]), sn = make_float2(s[e], s[e + 1]);
+            if constexpr (NORM) {
+              own = mul2(own, cs);
+              its = mul2(its, sn);
+            } else {
+              own = make_float2(__fmul_rn(own.x, cs.x), __fmul_rn(own.y, cs.y));
+              its = make_float2(__fmul_rn(its.x, sn.x), __fmul_rn(its.y, sn.y));
+            }
+            x[e] = __fadd_rn(own.x, its.x);
+            x[e + 1] = __fadd_rn(own.y, its.y);
           }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = __fadd_rn(__fmul_rn(x[e], c[e]), __fmul_rn(g[e], s[e]));
         }
       } else if (rotate) {
 #pragma unroll
@@ -211,9 +259,13 @@ __global__ void __launch_bounds__(kThreads, ROWS == 6 && BITS < 8 ? 4 : 0) kv_ap
         }
       }
     }
-    if constexpr (NORM) {
+    if (NORM && r < first_v) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = __fmul_rn(x[e], inv);
+      for (int e = 0; e < 8; e += 2) {
+        const float2 y = mul2(make_float2(x[e], x[e + 1]), make_float2(inv, inv));
+        x[e] = y.x;
+        x[e + 1] = y.y;
+      }
     }
     if (r < p.n_heads) {
       *reinterpret_cast<uint4*>(p.q_out + t * p.qo_ts + r * p.qo_hs + (rest * p.qo_hs + 8 * j)) = narrow8(x);

@@ -449,12 +449,13 @@ int launch_backward(NormArgs& n, int tokens, cudaStream_t s) {
   note_launch();
   return HBL_OK;
 }
-// Several heads to a unit once that still leaves every SM a full set of threads; one while the call is small and its latency is
-// what counts (and for a head_dim that is no multiple of 16).
+// Several heads to a unit once there are as many units as places for them (1024 tokens of 32 and 8 heads: 8.8 us; one to a unit
+// 9.5), one while the call is small (and for a head_dim that is no multiple of 16).
 template <typename T, bool INTERLEAVED, int L>
 int launch_lanes(NormArgs& n, int tokens, bool backward, cudaStream_t s) {
-  const bool full = n.head_dim % 16 == 0, many = full && (long)tokens * (n.part[0].n_heads + n.part[1].n_heads) * L >= (long)sm_count() * 2048 * 4;
   constexpr int F = sizeof(T) == 2 ? 4 : 2;
+  const long places = (long)sm_count() * kForwardBlocksPerSm * (kThreads / L), heads = (long)tokens * (n.part[0].n_heads + n.part[1].n_heads);
+  const bool full = n.head_dim % 16 == 0, many = full && heads >= places * F;
   if (backward) {
     if (many) return launch_backward<T, INTERLEAVED, true, L, F / 2>(n, tokens, s);
     return full ? launch_backward<T, INTERLEAVED, true, L, 1>(n, tokens, s) : launch_backward<T, INTERLEAVED, false, L, 1>(n, tokens, s);
