@@ -85,8 +85,9 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
   constexpr bool CODES = BITS < 16;
   __shared__ uint4 sq[NT][G::KU][32];
   __shared__ float sqs[ROWS];
-  __shared__ float so[ROWS][D + 4];
-  __shared__ float sm[kWarps][ROWS], sl[kWarps][ROWS];
+  constexpr bool APART = NT * D <= 256;                        // there is room for every warp's results
+  __shared__ __align__(16) float so[APART ? kWarps : 1][ROWS][D + 4];
+  __shared__ float sm[kWarps][ROWS], sl[kWarps][ROWS], sv[kWarps];
   // Behind the tiles this kernel begins when all their blocks have, so what came before the call is complete already; it
   // takes the SMs that they leave.  It may not be complete before they are, as what is launched next waits for this
   // kernel alone: its last block waits for them.
@@ -118,11 +119,46 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
   const int key0 = split * p.p.chunk;
   int key1 = split == p.p.splits - 1 ? seen : min(seen, key0 + p.p.chunk);
 
+  // ---- the keys, 16 at a time: the first loads, which take longest, before the queries.  All 16 rows of a step are read, those
+  // beyond the last key too: a page is there as a whole, and what they hold is masked.  Row numbers fit 32 bits (checked on the
+  // host): one multiply-add an address. ----
+  const int* page_row = p.b.pages + (long)b * p.b.max_pages;
+  Step<BITS, D> st[G::AHEAD];
+  const unsigned char* kp = p.c.k + (g * G::ROW_BYTES);
+  const unsigned char* vp = p.c.v + (2 * t * G::ROW_BYTES);
+  const float* ksp = CODES ? p.c.k_scale + g : nullptr;
+  const float* vsp = CODES ? p.c.v_scale + g : nullptr;
+  const uint32_t page_rows = (uint32_t)p.c.n_kv_heads << p.c.page_shift, head_rows = (uint32_t)head << p.c.page_shift;
+  const int slot_mask = (1 << p.c.page_shift) - 1;
+  auto page_of = [&](int kb) { return kb < key1 ? __ldg(page_row + (key_of(kb) >> p.c.page_shift)) : -1; };
+  auto load = [&](Step<BITS, D>& s, int kb, int page) {
+    const bool here = page >= 0 && page < p.c.n_pages;         // (-1 beyond the last key)
+    if (here) {
+      const uint32_t row0 = (uint32_t)page * page_rows + head_rows + (uint32_t)(key_of(kb) & slot_mask);
+      const unsigned char* k = kp + (uint64_t)row0 * G::ROW_BYTES;
+      const unsigned char* v = vp + (uint64_t)row0 * G::ROW_BYTES;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        s.k[h].load(k + 8 * h * G::ROW_BYTES, t);
+        if (CODES) {
+          s.ks[h] = __ldg(ksp + (uint64_t)row0 + 8 * h);
+          s.vs[h] = __ldg(vsp + (uint64_t)row0 + 8 * h);
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 4; ++h) s.v[h].load(v + ((h & 1) + 8 * (h >> 1)) * G::ROW_BYTES, g);
+    }
+    return here;
+  };
+  constexpr int STRIDE = 16 * kWarps;
+  int kb = key0 + 16 * warp;
+  int ahead_kb = kb, ahead_page = page_of(kb);
   // ---- queries as B fragments: row n = g of tile nt, its pairs in the order the keys' units have.  For codes they are
   // fp16, scaled by the power of two that brings the row's largest magnitude near 2^15: a bf16 value keeps all its bits
   // down to 2^-29 of that.  A warp takes whole rows. ----
-  for (int rr = warp; rr < ROWS; rr += kWarps) {
-    const int r = r0 + rr, nt = rr >> 3;
+#pragma unroll
+  for (int i = 0; i < ROWS / kWarps; ++i) {
+    const int rr = warp + i * kWarps, r = r0 + rr, nt = rr >> 3;
     constexpr int CH = D / 8, PER = CH > 32 ? CH / 32 : 1;     // 16-byte pieces of a row: one to a lane
     static_assert(PER == 1, "a row is at most 32 pieces");
     uint4 w = make_uint4(0, 0, 0, 0);
@@ -208,7 +244,6 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
     if (slot >= 0 && slot < p.c.n_slots) bos_row = slot;
     else report_device_error(p.status, HBL_ERR_RANGE);        // its first token is then left out
   }
-  const int* page_row = p.b.pages + (long)b * p.b.max_pages;
 
   // scores (c: keys g and g + 8, columns 2t and 2t + 1) to P^T fragments, with the running maximum.
   // masked: keys beyond a column's limit, or before its window, and key 0 where skip_first, do not count.
@@ -333,38 +368,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
     }
   }
 
-  // ---- the keys, 16 at a time.  All 16 rows of a step are read, those beyond the last key too: a page is there as a
-  // whole, and what they hold is masked.  Row numbers fit 32 bits (checked on the host): one multiply-add an address. ----
-  Step<BITS, D> st[G::AHEAD];
-  const unsigned char* kp = p.c.k + (g * G::ROW_BYTES);
-  const unsigned char* vp = p.c.v + (2 * t * G::ROW_BYTES);
-  const float* ksp = CODES ? p.c.k_scale + g : nullptr;
-  const float* vsp = CODES ? p.c.v_scale + g : nullptr;
-  const uint32_t page_rows = (uint32_t)p.c.n_kv_heads << p.c.page_shift, head_rows = (uint32_t)head << p.c.page_shift;
-  const int slot_mask = (1 << p.c.page_shift) - 1;
-  auto page_of = [&](int kb) { return kb < key1 ? __ldg(page_row + (key_of(kb) >> p.c.page_shift)) : -1; };
-  auto load = [&](Step<BITS, D>& s, int kb, int page) {
-    const bool here = page >= 0 && page < p.c.n_pages;         // (-1 beyond the last key)
-    if (here) {
-      const uint32_t row0 = (uint32_t)page * page_rows + head_rows + (uint32_t)(key_of(kb) & slot_mask);
-      const unsigned char* k = kp + (uint64_t)row0 * G::ROW_BYTES;
-      const unsigned char* v = vp + (uint64_t)row0 * G::ROW_BYTES;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        s.k[h].load(k + 8 * h * G::ROW_BYTES, t);
-        if (CODES) {
-          s.ks[h] = __ldg(ksp + (uint64_t)row0 + 8 * h);
-          s.vs[h] = __ldg(vsp + (uint64_t)row0 + 8 * h);
-        }
-      }
-#pragma unroll
-      for (int h = 0; h < 4; ++h) s.v[h].load(v + ((h & 1) + 8 * (h >> 1)) * G::ROW_BYTES, g);
-    }
-    return here;
-  };
-  constexpr int STRIDE = 16 * kWarps;
-  int kb = key0 + 16 * warp;
-  int ahead_kb = kb, ahead_page = page_of(kb);
+  // ---- the keys ----
   bool here[G::AHEAD];
 #pragma unroll
   for (int d = 0; d < G::AHEAD; ++d) {
@@ -446,7 +450,6 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
   }
 
   // ---- the four warps' results together ----
-  float m[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -455,56 +458,81 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
       x += __shfl_xor_sync(0xffffffffu, x, 4);
       x += __shfl_xor_sync(0xffffffffu, x, 8);
       x += __shfl_xor_sync(0xffffffffu, x, 16);
-      m[nt][e] = x == 0.f ? -INFINITY : -neg[nt][e];           // (a NaN has a place in the sum, too)
       if (!CODES && (poison >> (2 * nt + e) & 1)) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) o[nt][i][e] = o[nt][i][e + 2] = __uint_as_float(0x7FC00000u);
       }
       if (g == 0) {
-        sm[warp][nt * 8 + 2 * t + e] = m[nt][e];
+        sm[warp][nt * 8 + 2 * t + e] = x == 0.f ? -INFINITY : -neg[nt][e];     // (a NaN has a place in the sum, too)
         sl[warp][nt * 8 + 2 * t + e] = x;
       }
     }
-  __syncthreads();
-  float f[NT][2];
+  if (lane == 0) sv[warp] = CODES ? vr * 0x1p-7f : 1.f;
+  // a warp's maximum, and what its results are in units of, against those of all: (0 where there was no key)
+  auto top_of = [&](int r) {
+    float top = sm[0][r];
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
+    for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sm[w][r]);
+    return top;
+  };
+  auto share = [&](int w, int r, float top) { return exp2_approx(sm[w][r] - (top == -INFINITY ? 0.f : top)); };
+  auto put = [&](float (&to)[ROWS][D + 4], bool first, const float (&f)[NT][2]) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int r = nt * 8 + 2 * t + e;
-      float top = sm[0][r];
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sm[w][r]);
-      f[nt][e] = exp2_approx(m[nt][e] - (top == -INFINITY ? 0.f : top)) * (CODES ? vr * 0x1p-7f : 1.f);     // (0 where there was no key)
-    }
-  for (int w = 0; w < kWarps; ++w) {
-    if (warp == w) {
+      for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+        for (int e = 0; e < 4; ++e) {
+          const int d = 8 * G::VLane::unit_of(i / 4, g) + 2 * (i & 3) + (e >> 1);
+          float& x = to[nt * 8 + 2 * t + (e & 1)][d];
+          const float y = o[nt][i][e] * f[nt][e & 1];
+          x = first ? y : x + y;
+        }
+  };
+  if constexpr (APART) {                                       // side by side, joined by who writes them out
+    float one[NT][2];
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int d = 8 * G::VLane::unit_of(i / 4, g) + 2 * (i & 3) + (e >> 1);
-            float& x = so[nt * 8 + 2 * t + (e & 1)][d];
-            const float y = o[nt][i][e] * f[nt][e & 1];
-            x = w == 0 ? y : x + y;
-          }
-    }
+    for (int nt = 0; nt < NT; ++nt) one[nt][0] = one[nt][1] = 1.f;
+    put(so[warp], true, one);
     __syncthreads();
+  } else {                                                     // one after the other
+    __syncthreads();
+    float f[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = nt * 8 + 2 * t + e;
+        f[nt][e] = share(warp, r, top_of(r)) * sv[warp];
+      }
+    for (int w = 0; w < kWarps; ++w) {
+      if (warp == w) put(so[0], w == 0, f);
+      __syncthreads();
+    }
   }
   const long all_rows = (long)p.b.n_seqs * p.c.n_kv_heads * p.p.cap;
   for (int i = threadIdx.x; i < ROWS * (D / 4); i += kThreads) {
     const int rr = i / (D / 4), d = (i % (D / 4)) * 4, r = r0 + rr;
     if (r >= n_rows) break;
-    float top = sm[0][rr], sum = 0.f;
+    const float top = top_of(rr);
+    float4 v = *reinterpret_cast<const float4*>(&so[0][rr][d]);
+    float sum = 0.f;
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sm[w][rr]);
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) sum += sl[w][rr] * exp2_approx(sm[w][rr] - (top == -INFINITY ? 0.f : top));
+    for (int w = 0; w < kWarps; ++w) {
+      const float f = share(w, rr, top);
+      sum += sl[w][rr] * f;
+      if constexpr (APART) {
+        const float4 x = *reinterpret_cast<const float4*>(&so[w][rr][d]);
+        const float by = f * sv[w];
+        if (w == 0) {
+          v = make_float4(x.x * by, x.y * by, x.z * by, x.w * by);
+        } else {
+          v.x += x.x * by; v.y += x.y * by; v.z += x.z * by; v.w += x.w * by;
+        }
+      }
+    }
     const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
     const int tok = len.q0 + r / group, hq = head * group + r % group;
-    const float4 v = *reinterpret_cast<const float4*>(&so[rr][d]);
     const float lse2 = sum == 0.f ? -INFINITY : top + __log2f(sum);
     if (p.p.splits > 1) {
       const long row = split * all_rows + ((long)b * p.c.n_kv_heads + head) * p.p.cap + r;
