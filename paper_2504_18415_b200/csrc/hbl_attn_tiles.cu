@@ -205,10 +205,21 @@ struct Item {
   KeyMap map;                    // WINDOW: what `past` and the keys count, see there
   int expired;                   // ... keys below it, but for the sinks, are masked by some row
 };
-// The first tile of a causal item in which some row masks a key that is not its past.
-template <int D>
-__device__ __forceinline__ int first_masked(const TilesParams& p, const Item& w) {
-  return max(0, w.past + token_of(p, w.r0) + 1 - w.key0) / TileGeo<D>::BK;
+// The tiles of an item in which some row masks a key (not counting keys beyond the last): those from `from` on, WINDOW: and those
+// from `sunk` to `old`.
+struct MaskedTiles {
+  int from, sunk, old;
+  __device__ __forceinline__ bool has(int j, bool window) const { return j >= from || (window && j >= sunk && j < old); }
+};
+template <int D, bool WINDOW>
+__device__ __forceinline__ MaskedTiles masked_tiles(const TilesParams& p, const Item& w) {
+  constexpr int BK = TileGeo<D>::BK;
+  MaskedTiles m = {p.a.causal ? max(0, w.past + token_of(p, w.r0) + 1 - w.key0) / BK : w.tiles, 0, 0};
+  if (WINDOW) {
+    m.sunk = max(0, p.a.sinks - w.key0) / BK;                  // the tile in which the sinks end
+    m.old = (max(0, w.expired - w.key0) + BK - 1) / BK;
+  }
+  return m;
 }
 // The whole warp takes part.  False: nothing to do.
 template <int D, bool WINDOW>
@@ -289,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
   __shared__ Item item_slot[2];
   __shared__ __align__(8) uint64_t steal_bar, near_end;
   __shared__ __align__(16) uint4 steal_answer;
-  __shared__ __align__(16) uint32_t bad_scale[STAGES][4];       // keys of the tile whose value scale is not finite
+  __shared__ __align__(16) uint32_t bad_value[STAGES][4];       // keys of the tile whose value, or its scale, is not finite
   __shared__ float2 unit_of_tile[STAGES];                       // what the value scales are held against: now, and before / now
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag_s;
@@ -376,6 +387,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         if (first + 8 * i < w.n_rows) low = min(low, limit(i));
       low = __reduce_min_sync(0xffffffffu, low);
       auto from = [&](int i) { return w.past + token_of(p, first + 8 * i) + 1 - p.a.window; };     // WINDOW: where row i's begins
+      // Of the tile's keys 32 e .. 32 e + 31 those that a row sees: below `end`, and not before `begin` or below `keep`.
+      auto visible = [](int e, int end, int begin, int keep) {
+        auto below = [&](int n) { return n <= 32 * e ? 0u : n >= 32 * e + 32 ? ~0u : (1u << (n - 32 * e)) - 1; };
+        return WINDOW ? below(end) & (~below(begin) | below(keep)) : below(end);
+      };
       int expired = 0;                                         // below it some row of the warp masks what is no sink
       if (WINDOW) {
         int most = -0x40000000;
@@ -384,6 +400,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
           if (first + 8 * i < w.n_rows) most = max(most, from(i));
         expired = __reduce_max_sync(0xffffffffu, most);
       }
+      MaskedTiles marked = {0, 0, 0};
+      if (!CODES) marked = masked_tiles<D, WINDOW>(p, w);
       float neg[R], l[R];                                      // minus the maximum so far (0: none yet, see `some`), p's sum
       uint32_t some = 0;                                       // rows that have seen a key
       float unit = 1.f;                                        // codes: O is in units of it
@@ -434,11 +452,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         if (WINDOW && k0 < expired && k0 + BK > p.a.sinks) {
 #pragma unroll
           for (int i = 0; i < R; ++i) {
-            const int begin = from(i) - k0 - 2 * t, keep = p.a.sinks - k0 - 2 * t;
+            const int begin = from(i) - k0 - 2 * t;
+            if (k0 >= p.a.sinks) {
 #pragma unroll
-            for (int q = 0; q < NP; ++q) {
-              if (STEP * q < begin && STEP * q >= keep) x[at(i, q)] = -INFINITY;
-              if (STEP * q + 1 < begin && STEP * q + 1 >= keep) x[at(i, q) + 1] = -INFINITY;
+              for (int q = 0; q < NP; ++q) {
+                if (STEP * q < begin) x[at(i, q)] = -INFINITY;
+                if (STEP * q + 1 < begin) x[at(i, q) + 1] = -INFINITY;
+              }
+            } else {
+              const int keep = p.a.sinks - k0 - 2 * t;
+#pragma unroll
+              for (int q = 0; q < NP; ++q) {
+                if (STEP * q < begin && STEP * q >= keep) x[at(i, q)] = -INFINITY;
+                if (STEP * q + 1 < begin && STEP * q + 1 >= keep) x[at(i, q) + 1] = -INFINITY;
+              }
             }
           }
         }
@@ -544,24 +571,33 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
             tmem_st_row16(s_addr + 16 * u, pk);
           }
         }
-        hand_over(1);
-#pragma unroll
-        for (int i = 0; i < R; ++i) l[i] += R == 4 ? sum[i][0] + sum[i][1] : (sum[i][0] + sum[i][1]) + (sum[i][R == 4 ? 0 : 2] + sum[i][R == 4 ? 0 : 3]);
-        if (CODES) {
-          // a value scale that is not finite came as zero (0 * it would reach rows it is masked for): rows that see
-          // its key are marked, and their results become NaN
-          const uint4 b = *reinterpret_cast<const uint4*>(bad_scale[stage]);
+        // What is not finite came as zero (0 * it would reach rows it is masked for): rows that see its key are marked, and their
+        // results become NaN.
+        if (!CODES && marked.has(j, WINDOW)) {              // (the product below needs the values as well)
+          if (!(ok = __all_sync(0xffffffffu, mbar_wait(&v_full[stage], (it / STAGES) & 1, abort_flag, p.status)))) break;
+          const uint4 b = *reinterpret_cast<const uint4*>(bad_value[stage]);
           if (b.x | b.y | b.z | b.w) {
             const uint32_t word[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
             for (int i = 0; i < R; ++i) {
               const int seen = limit(i) - k0;
-              for (int e = 0; e < BK / 32; ++e) {
-                auto below = [&](int n) { return n <= 32 * e ? 0u : n >= 32 * e + 32 ? ~0u : (1u << (n - 32 * e)) - 1; };
-                uint32_t visible = below(seen);
-                if (WINDOW) visible &= ~below(from(i) - k0) | below(p.a.sinks - k0);
-                if (word[e] & visible) some |= 16u << i;
-              }
+              for (int e = 0; e < BK / 32; ++e)
+                if (word[e] & visible(e, seen, WINDOW ? from(i) - k0 : 0, p.a.sinks - k0)) some |= 16u << i;
+            }
+          }
+        }
+        hand_over(1);
+#pragma unroll
+        for (int i = 0; i < R; ++i) l[i] += R == 4 ? sum[i][0] + sum[i][1] : (sum[i][0] + sum[i][1]) + (sum[i][R == 4 ? 0 : 2] + sum[i][R == 4 ? 0 : 3]);
+        if (CODES) {
+          const uint4 b = *reinterpret_cast<const uint4*>(bad_value[stage]);
+          if (b.x | b.y | b.z | b.w) {
+            const uint32_t word[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+              const int seen = limit(i) - k0;
+              for (int e = 0; e < BK / 32; ++e)
+                if (word[e] & visible(e, seen, WINDOW ? from(i) - k0 : 0, p.a.sinks - k0)) some |= 16u << i;
             }
           }
           __syncwarp();                                         // every lane has read the stage's marks: lane 0 speaks for all
@@ -697,7 +733,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         const int key = w.key0 + j * BK + 16 * lane;
         return lane < BK / 16 && key < w.key1 ? __ldg(page_row + (key_of(key) >> p.c.page_shift)) : -1;
       };
-      struct Tile { long group_row; unsigned good; int there, keep, begin; };
+      struct Tile { long group_row; unsigned good; int there; };
       auto open = [&](int j, int page) {
         const int k0 = w.key0 + j * BK;
         const bool in = page >= 0 && page < p.c.n_pages;
@@ -706,14 +742,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         t.group_row = cache_row(p.c, in ? page : 0, w.head, key_of(k0 + 16 * lane) & ((1 << p.c.page_shift) - 1));
         t.good = __ballot_sync(0xffffffffu, in);
         t.there = w.key1 - k0;                                  // keys of the tile that exist
-        if (WINDOW) {                                           // ... but for those that no row sees
-          t.keep = p.a.sinks - k0;
-          t.begin = w.map.first - k0;
-        }
         return t;
       };
       auto row_of = [&](const Tile& t, int rr) { return __shfl_sync(0xffffffffu, t.group_row, rr >> 4) + (rr & 15); };
-      auto live = [&](const Tile& t, int rr) { return rr < t.there && (t.good >> (rr >> 4) & 1) && (!WINDOW || rr >= t.begin || rr < t.keep); };
+      auto live = [&](const Tile& t, int rr) { return rr < t.there && (t.good >> (rr >> 4) & 1); };
       int next_page = page_of(0);
       Tile tile = open(0, next_page);
       next_page = page_of(1);
@@ -721,7 +753,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         // bf16 rows are copied asynchronously and announced one copy later, so that two are in flight; nothing that a
         // wait below needs depends on the one not announced yet
         uint64_t* copied = nullptr;
-        const int masked_from = p.a.causal ? first_masked<D>(p, w) : w.tiles;
+        const MaskedTiles marked = masked_tiles<D, WINDOW>(p, w);
         for (int j = 0; j < w.tiles; ++j, ++it) {
           const int stage = it % STAGES;
 #pragma unroll
@@ -737,35 +769,39 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
               copy16(dst + chunk_at(rr, tid % CH, G::HALF), col + row_of(tile, rr) * (2 * D), live(tile, rr));
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
-            if (kv == 1 && (j >= masked_from || (WINDOW && w.key0 + j * BK < w.expired && w.key0 + (j + 1) * BK > p.a.sinks))) {
+            if (copied != nullptr) {
+              asm volatile("cp.async.wait_group 1;" ::: "memory");
+              fence_async();                                    // what the copies wrote is read next by the tensor cores
+              mbar_arrive(copied);
+              copied = nullptr;
+            }
+            if (kv == 1 && marked.has(j, WINDOW)) {
               // A tile that some row masks: 0 * a value that is not finite would reach rows that mask its key.  Every thread
-              // looks through the pieces that it has copied; such a key's value becomes zeros and the key itself NaN, so
-              // that the rows that see it, and no others, become NaN.  (The same lanes hold a row's pieces of both.)
+              // looks through the pieces that it has copied; such a value becomes zeros and its key is marked, so that the rows
+              // that see it, and no others, become NaN.  (The lanes that hold a row lie side by side.)
+              if (tid < 4) bad_value[stage][tid] = 0;           // (whoever read the stage's last marks has seen its products begin)
               asm volatile("cp.async.wait_all;" ::: "memory");
-#pragma unroll 2
+              asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll 4
               for (int i = 0; i < BK / RPP; ++i) {
                 const uint32_t at = chunk_at(i * RPP + tid / CH, tid % CH, G::HALF);
                 uint32_t y[4], sum = 0;                         // 0 * y: zeros, or NaN where y is not finite
                 asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(dst + at) : "memory");
 #pragma unroll
                 for (int k = 0; k < 4; ++k) asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(y[k]), "r"(0u));
-                const unsigned bad = __ballot_sync(0xffffffffu, (sum & 0x7FFF7FFFu) != 0);
-                if (bad >> (lane & ~(CH - 1)) & (CH == 32 ? ~0u : (1u << CH % 32) - 1)) {
-                  const uint32_t zero[4] = {0, 0, 0, 0}, nan[4] = {0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
-                  store16(dst + at, zero);
-                  store16(sk + stage * G::KV_BYTES + at, nan);
+                if (__any_sync(0xffffffffu, (sum & 0x7FFF7FFFu) != 0)) {
+                  const unsigned bad = __ballot_sync(0xffffffffu, (sum & 0x7FFF7FFFu) != 0);
+                  if (bad >> (lane & ~(CH - 1)) & (CH == 32 ? ~0u : (1u << CH % 32) - 1)) {
+                    const uint32_t zero[4] = {0, 0, 0, 0};
+                    store16(dst + at, zero);
+                    const int rr = i * RPP + tid / CH;
+                    if (tid % CH == 0) atomicOr(&bad_value[stage][rr >> 5], 1u << (rr & 31));
+                  }
                 }
               }
               fence_async();
-              mbar_arrive(copied);                              // the keys
               mbar_arrive(&v_full[stage]);
-              copied = nullptr;
               continue;
-            }
-            if (copied != nullptr) {
-              asm volatile("cp.async.wait_group 1;" ::: "memory");
-              fence_async();                                    // what the copies wrote is read next by the tensor cores
-              mbar_arrive(copied);
             }
             copied = kv == 0 ? &k_full[stage] : &v_full[stage];
           }
@@ -812,11 +848,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         // 2^15, what fp16 holds; it is rounded by 2^-11 of itself, or by 2^-32 unit where it is that small.
         constexpr int VN = BK / 32;
         float ks = 0.f, vs[VN];
-        auto load_scales = [&](const Tile& t) {
+        auto load_scales = [&](const Tile& t) {                  // (a value that no row sees does not count)
+          const int keep = p.a.sinks - (w.key1 - t.there), begin = w.map.first - (w.key1 - t.there);
 #pragma unroll
           for (int i = 0; i < VN; ++i) {
-            const long row = row_of(t, 32 * i + lane);
-            vs[i] = live(t, 32 * i + lane) ? __ldg(p.c.v_scale + row) : 0.f;
+            const int rr = 32 * i + lane;
+            const long row = row_of(t, rr);
+            vs[i] = live(t, rr) && (!WINDOW || rr >= begin || rr < keep) ? __ldg(p.c.v_scale + row) : 0.f;
           }
           if (tid < BK) {                                       // (whole warps)
             const long row = row_of(t, tid);
@@ -881,7 +919,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
                   for (int i = 0; i < VN; ++i)
                     if (i == mine) my_vs = vs[i];
                   const unsigned word = __ballot_sync(0xffffffffu, mine < VN && (bad >> mine & 1));
-                  if (lane == 0) bad_scale[stage][mine] = word;  // (BK 64: the upper two hold none)
+                  if (lane == 0) bad_value[stage][mine] = word;  // (BK 64: the upper two hold none)
                   if (tid == 0) unit_of_tile[stage] = make_float2(unit * 0x1p-7f, before / unit);
                   if (tid < BK) {
                     scales[stage * 2 * BK + tid] = ks * scale;
