@@ -22,7 +22,6 @@ namespace {
 using namespace frag;
 
 constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
 constexpr float kLazy = 8.f;
 
 struct RowsParams {
@@ -77,17 +76,17 @@ struct Step {
 // Thread blocks on an SM: what the registers of a block's accumulators and steps in flight leave.
 constexpr int blocks_per_sm(int bits, int d, int nt) { return d > 128 ? 2 : nt == 1 ? 4 : bits < 16 ? 3 : 2; }
 
-template <int BITS, int D, int NT, bool WINDOW>
-__global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_rows_kernel(const __grid_constant__ RowsParams p) {
+template <int BITS, int D, int NT, bool WINDOW, int W>
+__global__ void __launch_bounds__(32 * W, blocks_per_sm(BITS, D, NT) * kWarps / W) attn_rows_kernel(const __grid_constant__ RowsParams p) {
   using G = Geo<BITS, D>;
   constexpr int ROWS = 8 * NT;
   constexpr int MT = D / 16;                                  // 16-element tiles of the output
   constexpr bool CODES = BITS < 16;
   __shared__ uint4 sq[NT][G::KU][32];
   __shared__ float sqs[ROWS];
-  constexpr bool APART = NT * D <= 256;                        // there is room for every warp's results
-  __shared__ __align__(16) float so[APART ? kWarps : 1][ROWS][D + 4];
-  __shared__ float sm[kWarps][ROWS], sl[kWarps][ROWS], sv[kWarps];
+  constexpr bool APART = NT * D * W <= 256 * 4;                        // there is room for every warp's results
+  __shared__ __align__(16) float so[APART ? W : 1][ROWS][D + 4];
+  __shared__ float sm[W][ROWS], sl[W][ROWS], sv[W];
   // Behind the tiles this kernel begins when all their blocks have, so what came before the call is complete already; it
   // takes the SMs that they leave.  It may not be complete before they are, as what is launched next waits for this
   // kernel alone: its last block waits for them.
@@ -150,15 +149,15 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
     }
     return here;
   };
-  constexpr int STRIDE = 16 * kWarps;
+  constexpr int STRIDE = 16 * W;
   int kb = key0 + 16 * warp;
   int ahead_kb = kb, ahead_page = page_of(kb);
   // ---- queries as B fragments: row n = g of tile nt, its pairs in the order the keys' units have.  For codes they are
   // fp16, scaled by the power of two that brings the row's largest magnitude near 2^15: a bf16 value keeps all its bits
   // down to 2^-29 of that.  A warp takes whole rows. ----
 #pragma unroll
-  for (int i = 0; i < ROWS / kWarps; ++i) {
-    const int rr = warp + i * kWarps, r = r0 + rr, nt = rr >> 3;
+  for (int i = 0; i < ROWS / W; ++i) {
+    const int rr = warp + i * W, r = r0 + rr, nt = rr >> 3;
     constexpr int CH = D / 8, PER = CH > 32 ? CH / 32 : 1;     // 16-byte pieces of a row: one to a lane
     static_assert(PER == 1, "a row is at most 32 pieces");
     uint4 w = make_uint4(0, 0, 0, 0);
@@ -472,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
   auto top_of = [&](int r) {
     float top = sm[0][r];
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sm[w][r]);
+    for (int w = 1; w < W; ++w) top = fmaxf(top, sm[w][r]);
     return top;
   };
   auto share = [&](int w, int r, float top) { return exp2_approx(sm[w][r] - (top == -INFINITY ? 0.f : top)); };
@@ -505,20 +504,20 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(BITS, D, NT)) attn_row
         const int r = nt * 8 + 2 * t + e;
         f[nt][e] = share(warp, r, top_of(r)) * sv[warp];
       }
-    for (int w = 0; w < kWarps; ++w) {
+    for (int w = 0; w < W; ++w) {
       if (warp == w) put(so[0], w == 0, f);
       __syncthreads();
     }
   }
   const long all_rows = (long)p.b.n_seqs * p.c.n_kv_heads * p.p.cap;
-  for (int i = threadIdx.x; i < ROWS * (D / 4); i += kThreads) {
+  for (int i = threadIdx.x; i < ROWS * (D / 4); i += 32 * W) {
     const int rr = i / (D / 4), d = (i % (D / 4)) * 4, r = r0 + rr;
     if (r >= n_rows) break;
     const float top = top_of(rr);
     float4 v = *reinterpret_cast<const float4*>(&so[0][rr][d]);
     float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float f = share(w, rr, top);
       sum += sl[w][rr] * f;
       if constexpr (APART) {
@@ -669,10 +668,21 @@ template <int BITS, int D, bool WINDOW>
 int launch_rows_dim(RowsParams& p, cudaStream_t s) {
   const long blocks = (long)p.b.n_seqs * p.c.n_kv_heads * p.p.tiles * p.p.splits;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
-  if (rows_per_tile(p.b, p.a.group, p.few) == 8)
-    HBL_CUDA_OK(launch_waiting(attn_rows_kernel<BITS, D, 1, WINDOW>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+  const bool narrow = rows_per_tile(p.b, p.a.group, p.few) == 8;
+  // Within a window: eight warps where every block has an SM to itself (4 x 509 tokens at 8 bits, window of 128: 7.4 us, 8.5; of
+  // 500: 9.8, 12.6; 64 x 4096 tokens, of 1024: 107, 94), as far as there is room for their results.
+  if constexpr (WINDOW && D <= 128) {
+    if (blocks <= sm_count() && (narrow || D <= 64)) {
+      if (narrow) HBL_CUDA_OK(launch_waiting(attn_rows_kernel<BITS, D, 1, WINDOW, 8>, dim3((unsigned)blocks), dim3(256), 0, s, p));
+      else HBL_CUDA_OK(launch_waiting(attn_rows_kernel<BITS, D, D <= 64 ? 2 : 1, WINDOW, 8>, dim3((unsigned)blocks), dim3(256), 0, s, p));
+      note_launch();
+      return HBL_OK;
+    }
+  }
+  if (narrow)
+    HBL_CUDA_OK(launch_waiting(attn_rows_kernel<BITS, D, 1, WINDOW, kWarps>, dim3((unsigned)blocks), dim3(32 * kWarps), 0, s, p));
   else
-    HBL_CUDA_OK(launch_waiting(attn_rows_kernel<BITS, D, 2, WINDOW>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p));
+    HBL_CUDA_OK(launch_waiting(attn_rows_kernel<BITS, D, 2, WINDOW, kWarps>, dim3((unsigned)blocks), dim3(32 * kWarps), 0, s, p));
   note_launch();
   return HBL_OK;
 }
