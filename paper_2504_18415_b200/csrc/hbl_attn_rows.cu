@@ -152,6 +152,30 @@ __global__ void __launch_bounds__(32 * W, blocks_per_sm(BITS, D, NT) * kWarps / 
   constexpr int STRIDE = 16 * W;
   int kb = key0 + 16 * warp;
   int ahead_kb = kb, ahead_page = page_of(kb);
+  // The first token at 8 bits: by the warp whose turn key 0 is, or, within a window, by the one that has least to do; its rows
+  // are asked for here.
+  const bool bos = BITS < 8 && p.c.bos_k != nullptr && (!WINDOW || p.a.sinks > 0 || (map.first | map.gap) == 0);
+  constexpr int BOS_WARP = WINDOW ? W - 1 : 0;
+  int bos_row = -1;
+  if (bos && key0 == 0 && key1 > 0) {
+    const int slot = p.b.bos_slot != nullptr ? __ldg(p.b.bos_slot + b) : b;
+    if (slot >= 0 && slot < p.c.n_slots) bos_row = slot;
+    else report_device_error(p.status, HBL_ERR_RANGE);        // its first token is then left out
+  }
+  uint2 bos_k[BITS < 8 ? G::KU : 1], bos_v[BITS < 8 ? G::VU : 1];
+  float bos_ks = 0.f, bos_vs = 0.f;
+  if constexpr (BITS < 8) {
+    if (bos_row >= 0 && warp == BOS_WARP) {
+      const long brow = (long)bos_row * p.c.n_kv_heads + head;
+#pragma unroll
+      for (int i = 0; i < G::KU; ++i) bos_k[i] = __ldg(reinterpret_cast<const uint2*>(p.c.bos_k + brow * D) + G::KLane::unit_of(i, t));
+#pragma unroll
+      for (int i = 0; i < G::VU; ++i) bos_v[i] = __ldg(reinterpret_cast<const uint2*>(p.c.bos_v + brow * D) + G::VLane::unit_of(i, g));
+      bos_ks = __ldg(p.c.bos_k_scale + brow);
+      bos_vs = __ldg(p.c.bos_v_scale + brow);
+    }
+  }
+
   // ---- queries as B fragments: row n = g of tile nt, its pairs in the order the keys' units have.  For codes they are
   // fp16, scaled by the power of two that brings the row's largest magnitude near 2^15: a bf16 value keeps all its bits
   // down to 2^-29 of that.  A warp takes whole rows. ----
@@ -236,14 +260,6 @@ __global__ void __launch_bounds__(32 * W, blocks_per_sm(BITS, D, NT) * kWarps / 
       for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
   }
 
-  const bool bos = BITS < 8 && p.c.bos_k != nullptr && (!WINDOW || p.a.sinks > 0 || (map.first | map.gap) == 0);
-  int bos_row = -1;
-  if (bos && key0 == 0 && key1 > 0) {
-    const int slot = p.b.bos_slot != nullptr ? __ldg(p.b.bos_slot + b) : b;
-    if (slot >= 0 && slot < p.c.n_slots) bos_row = slot;
-    else report_device_error(p.status, HBL_ERR_RANGE);        // its first token is then left out
-  }
-
   // scores (c: keys g and g + 8, columns 2t and 2t + 1) to P^T fragments, with the running maximum.
   // masked: keys beyond a column's limit, or before its window, and key 0 where skip_first, do not count.
   auto softmax = [&](float (&c)[NT][4], int kb, const float (&ks)[2], const float (&vs)[2], bool masked, bool skip_first,
@@ -323,17 +339,16 @@ __global__ void __launch_bounds__(32 * W, blocks_per_sm(BITS, D, NT) * kWarps / 
     }
   };
 
-  // ---- the first token at 8 bits: one key, by the warp whose turn key 0 is ----
+  // ---- the first token at 8 bits: one key ----
   if constexpr (BITS < 8) {
-    if (bos_row >= 0 && warp == 0) {
+    if (bos_row >= 0 && warp == BOS_WARP) {
       auto value = [](const uint2& u, int e) { return (float)((int)(((e < 4 ? u.x : u.y) >> (8 * (e & 3))) & 255u) - 128); };
-      const long brow = (long)bos_row * p.c.n_kv_heads + head;
       float c[NT][4] = {};
 #pragma unroll
       for (int i = 0; i < G::KU; ++i) {
         uint32_t a[4] = {0, 0, 0, 0};
         if (g == 0) {
-          const uint2 u = __ldg(reinterpret_cast<const uint2*>(p.c.bos_k + brow * D) + G::KLane::unit_of(i, t));
+          const uint2 u = bos_k[i];
 #pragma unroll
           for (int j = 0; j < 4; ++j) a[j] = pack2_f16(value(u, pair16_lo<BITS>(j)), value(u, pair16_hi<BITS>(j)));
         }
@@ -345,7 +360,7 @@ __global__ void __launch_bounds__(32 * W, blocks_per_sm(BITS, D, NT) * kWarps / 
         }
       }
       // key 0 alone: the other rows of the step are put out of it
-      const float ks[2] = {__ldg(p.c.bos_k_scale + brow), 0.f}, vs[2] = {g == 0 ? __ldg(p.c.bos_v_scale + brow) : 0.f, 0.f};
+      const float ks[2] = {bos_ks, 0.f}, vs[2] = {g == 0 ? bos_vs : 0.f, 0.f};
       const int whole = key1;
       key1 = 1;
       uint32_t pf[NT][2];
@@ -355,7 +370,7 @@ __global__ void __launch_bounds__(32 * W, blocks_per_sm(BITS, D, NT) * kWarps / 
       for (int i = 0; i < G::VU; ++i) {
         uint32_t a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         if (t == 0) {
-          const uint2 u = __ldg(reinterpret_cast<const uint2*>(p.c.bos_v + brow * D) + G::VLane::unit_of(i, g));
+          const uint2 u = bos_v[i];
 #pragma unroll
           for (int e = 0; e < 8; ++e) a[e] = pack2_f16(value(u, e), 0.f);
         }
