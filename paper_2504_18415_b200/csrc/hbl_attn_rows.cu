@@ -37,17 +37,17 @@ struct RowsParams {
   int beside_tiles;              // launched behind the call's other kernel, of which it needs nothing
 };
 
-// The t-th sequence of the batch in falling order of their lengths' quarter of the longest.  The whole warp asks for the
+// The t-th sequence of the batch in falling order of their lengths' (or the window's) quarter of the longest.  The whole warp asks for the
 // same t.  A batch of several rounds of blocks ends sooner when the long ones do not come last.
-__device__ __forceinline__ int sequence_by_length(const BatchView& s, int t, int lane) {
+__device__ __forceinline__ int sequence_by_length(const BatchView& s, int reach, int t, int lane) {
   int most = 0;
   for (int b0 = 0; b0 < s.n_seqs; b0 += 32)
-    if (b0 + lane < s.n_seqs) most = max(most, __ldg(s.kv_len + b0 + lane));
+    if (b0 + lane < s.n_seqs) most = max(most, min(reach, __ldg(s.kv_len + b0 + lane)));
   most = __reduce_max_sync(0xffffffffu, most);
   const int step = most / 4 + 1;                               // lengths / step: 0 .. 3
   for (int quarter = 3; quarter >= 0; --quarter)
     for (int b0 = 0; b0 < s.n_seqs; b0 += 32) {
-      const bool mine = b0 + lane < s.n_seqs && max(__ldg(s.kv_len + min(b0 + lane, s.n_seqs - 1)), 0) / step == quarter;
+      const bool mine = b0 + lane < s.n_seqs && max(min(reach, __ldg(s.kv_len + min(b0 + lane, s.n_seqs - 1))), 0) / step == quarter;
       const unsigned hits = __ballot_sync(0xffffffffu, mine);
       const int n = __popc(hits);
       if (t < n) return b0 + __ffs(__ballot_sync(0xffffffffu, mine && __popc(hits & ((1u << lane) - 1)) == t)) - 1;
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(32 * W, blocks_per_sm(BITS, D, NT) * kWarps / 
   const int tile = id % p.p.tiles; id /= p.p.tiles;
   const int head = id % p.c.n_kv_heads;
   int b = id / p.c.n_kv_heads;
-  if (p.ordered) b = sequence_by_length(p.b, b, lane);
+  if (p.ordered) b = sequence_by_length(p.b, p.p.reach, b, lane);
   SeqLens len;
   const bool sane = sequence_lengths(p.b, b, p.c.page_shift, p.status, len);
   const int group = p.a.group;
@@ -775,7 +775,7 @@ int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a
   // 190 us in the batch's order, 175 in this; 128 of 8 key heads 113, 92; all of one length 275, 278).  Not for short ones, whose
   // blocks would spend more on the look-up than it saves (up to 600 tokens: 59 us, 64), nor for batches whose look-up is long.
   const long slots = (long)sm_count() * blocks_per_sm(c.bits, c.head_dim, rows_per_tile(b, a.group, few) / 8);
-  p.ordered = plan.splits == 1 && b.max_kv_len >= 1024 && plan.reach >= b.max_kv_len && b.n_seqs <= 128 && (long)b.n_seqs * c.n_kv_heads * plan.tiles > slots;
+  p.ordered = plan.splits == 1 && (b.max_kv_len < plan.reach ? b.max_kv_len : plan.reach) >= 1024 && b.n_seqs <= 128 && (long)b.n_seqs * c.n_kv_heads * plan.tiles > slots;
   p.status = device_status_word();
   if (p.status == nullptr) return HBL_ERR_CUDA;
   switch (c.bits) {
