@@ -58,18 +58,14 @@ def batch_of(g, cache, q_lens, kv_lens, extra=0):
     return batch, pos, pages[seq, pos // page].long(), pos % page
 
 
-@pytest.mark.parametrize("bits", [3, 4, 8, 16])
-@pytest.mark.parametrize("interleaved", [False, True])
-@pytest.mark.parametrize("q_lens,kv_lens", [([1], [1]), ([1, 1, 1], [700, 17, 1]), ([100, 3, 41], [100, 60, 500]), ([700, 900], [700, 900])])
-@pytest.mark.parametrize("H,KH,D,rot,gain", [(4, 4, 128, 128, BF16), (7, 1, 128, 64, torch.float32), (8, 2, 64, 32, None), (3, 3, 256, 256, BF16), (4, 2, 128, 0, BF16)])
-def test_the_cache_holds_the_formula(bits, interleaved, q_lens, kv_lens, H, KH, D, rot, gain):
+def check_cache(bits, interleaved, q_lens, kv_lens, H, KH, D, rot, gain):
     g = gen(sum(kv_lens) + D + bits)
     cache = hbl.KvCache.empty(sum(-(-n // 32) for n in kv_lens) + 2, 32, KH, D, bits, len(kv_lens) if bits < 8 else 0)
     batch, pos, page, slot = batch_of(g, cache, q_lens, kv_lens)
     T = len(pos)
     q, k, v = heads(g, T, H, D), heads(g, T, KH, D), heads(g, T, KH, D)
     gq, gk = (None if gain is None else gain_of(g, D, gain) for _ in range(2))
-    table = hbl.hbl_rope_table(hbl.hbl_rope_frequencies(rot), 1024) if rot else None
+    table = hbl.hbl_rope_table(hbl.hbl_rope_frequencies(rot), max(kv_lens) + 1) if rot else None
     q_out = hbl.hbl_kv_append_norm(cache, batch, k, v, gk, table=table, interleaved=interleaved, q=q, q_gain=gq, norm_eps=EPS)
     assert hbl.hbl_check_status() == 0
     rows = table[pos] if rot else None
@@ -87,6 +83,22 @@ def test_the_cache_holds_the_formula(bits, interleaved, q_lens, kv_lens, H, KH, 
             starts = (pos == 0).nonzero().flatten()
             seq = [b for b, (a, n) in enumerate(zip(q_lens, kv_lens)) if a == n]
             assert torch.equal(first[seq].long(), u[starts]) and torch.equal(first_scale[seq], sc[starts])
+
+
+@pytest.mark.parametrize("bits", [3, 4, 8, 16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("q_lens,kv_lens", [([1], [1]), ([1, 1, 1], [700, 17, 1]), ([100, 3, 41], [100, 60, 500]), ([700, 900], [700, 900])])
+@pytest.mark.parametrize("H,KH,D,rot,gain", [(4, 4, 128, 128, BF16), (7, 1, 128, 64, torch.float32), (8, 2, 64, 32, None), (3, 3, 256, 256, BF16), (4, 2, 128, 0, BF16)])
+def test_the_cache_holds_the_formula(bits, interleaved, q_lens, kv_lens, H, KH, D, rot, gain):
+    check_cache(bits, interleaved, q_lens, kv_lens, H, KH, D, rot, gain)
+
+
+@pytest.mark.parametrize("bits", [3, 4, 8, 16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("T,H,KH,D,rot,gain", [(9001, 4, 4, 128, 128, BF16), (9001, 7, 1, 128, 64, torch.float32), (13000, 8, 2, 64, 64, BF16), (14000, 7, 3, 64, 32, None),
+                                               (5000, 5, 2, 256, 128, BF16), (4001, 32, 8, 128, 128, BF16)])
+def test_prompts_of_several_heads_to_a_thread(bits, interleaved, T, H, KH, D, rot, gain):
+    check_cache(bits, interleaved, [T - 5, 5], [T - 5, 64], H, KH, D, rot, gain)
 
 
 @pytest.mark.parametrize("bits", [4, 16])

@@ -131,6 +131,26 @@ def test_a_large_call(interleaved):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("T,H,KH,D,rot", [(1501, 32, 7, 128, 64), (2100, 40, 9, 64, 64), (1001, 23, 1, 256, 128), (3001, 15, 9, 96, 48), (6000, 9, 9, 80, 80)])
+def test_calls_of_several_heads_to_a_thread(dtype, interleaved, T, H, KH, D, rot):
+    """More heads than places for them, numbers that are no multiples of what a thread takes, every width of lanes."""
+    g = gen(T)
+    table = table_of(rot, 3000)
+    pos = torch.randint(0, 3000, (T,), device="cuda", generator=g, dtype=torch.int32)
+    fused = heads(g, T, H + KH, D).to(dtype)
+    q, k = fused[:, :H], fused[:, H:]
+    dy = torch.randn(T, H + KH, D, device="cuda", generator=g).to(dtype)
+    gq, gk = gain_of(g, D, BF16), gain_of(g, D, BF16)
+    y = hbl.hbl_norm_rope(q, gq, pos, table, k=k, k_gain=gk, interleaved=interleaved)
+    d = hbl.hbl_norm_rope_grad(dy[:, :H], q, gq, pos, table, grad_k=dy[:, H:], k=k, k_gain=gk, interleaved=interleaved)
+    assert hbl.hbl_check_status() == 0
+    for x, w, gain, out, dx in ((q, dy[:, :H], gq, y[0], d[:2]), (k, dy[:, H:], gk, y[1], d[2:])):
+        check_forward(out, x, gain, table, pos, 1e-6, interleaved)
+        check_backward(dx, w, x, gain, table, pos, 1e-6, interleaved)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("interleaved", [False, True])
 def test_forward_is_the_fp32_evaluation_bit_for_bit(dtype, interleaved):
     g = gen(3)
     table = table_of(128, 1000)
