@@ -1,9 +1,11 @@
-"""64-bit reference of the attention within a window, with the tolerances that states_ref.py derives (the sums are no longer
-than those of the whole sequence, so its bounds hold)."""
+"""64-bit reference of the attention within a window, with the tolerances that states_ref.py (bf16) and codes_bound.py (codes)
+derive: the sums are no longer than those of the whole sequence, so their bounds hold.  What the weights are held against, max vs and
+max |v|, is that of the keys that some row of the sequence sees."""
 import math
 
 import torch
 
+from codes_bound import bound
 from paper_2504_18415_b200 import hbl
 from states_ref import F8, sequence_values
 
@@ -43,9 +45,12 @@ def window64(cache, q, q_lens, kv_lens, tables, window, sinks, sm_scale=None, sl
             e_s = (D + 4) * 2.0 ** -23 * size
             steps = (nk / 16 + 64) * 2.0 ** -23
             e = 2 * e_s + steps + 2.0 ** -20
-            t = 2.0 ** -8 * o.abs() + (2.0 ** -8 + e)[..., None] * (p @ v.abs()) * 1.01 + 1e-30
-            if cache.bits < 16:
-                t = t + nk * 2.0 ** -30 * v.abs().max()
+            if cache.bits == 16:
+                t = 2.0 ** -8 * o.abs() + (2.0 ** -8 + e)[..., None] * (p @ v.abs()) * 1.01 + 1e-30
+            else:
+                at_key = torch.arange(nk, device=dev)
+                scales = torch.where(mask.any(0), cache.v_scale[pages[at_key // cache.page_size].long(), h, at_key % cache.page_size], 0.0)
+                t = bound(o, p @ v.abs(), e[..., None], nk, v.abs().max(), 0.0 if slot8 is None else scales.max()) * 1.01
             hh = slice(h * group, (h + 1) * group)
             out[r, hh], tol[r, hh], lse[r, hh] = o.transpose(0, 1), t.transpose(0, 1), z.T
             tol_lse[r, hh] = (e_s + steps + 2.0 ** -20 * (1 + z.abs())).T
