@@ -445,10 +445,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
           const int end = limit(0) - k0, begin = from(0) - k0, keep = p.a.sinks - k0;
 #pragma unroll
           for (int e = 0; e < NQ; ++e) {
-            const uint32_t m = visible(e, end, begin, keep);
+            const int g0 = k0 + 32 * e;                         // few of a tile's groups lie on a border
+            if (g0 + 32 > low || (g0 < expired && g0 + 32 > p.a.sinks)) {
+              const uint32_t m = visible(e, end, begin, keep);
 #pragma unroll
-            for (int c = 0; c < 32; ++c)
-              if (!(m >> c & 1)) x[(32 * e + c) % BK] = -INFINITY;
+              for (int c = 0; c < 32; ++c)
+                if (!(m >> c & 1)) x[(32 * e + c) % BK] = -INFINITY;
+            }
           }
         }
         if (!BITWISE && masked) {
