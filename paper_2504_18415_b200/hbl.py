@@ -568,27 +568,32 @@ def hbl_rope(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, inte
 
 def _norm_rope_args(q, q_gain, positions, table, k, k_gain, norm_eps, interleaved, q_out, k_out):
     """(packed arguments, q_out, k_out) of the calls that normalise and rotate heads."""
-    dev, dtype = _on_gpu(q, "q"), q.dtype
-    T, H, D = q.shape
+    dev, dtype, shape = _on_gpu(q, "q"), q.dtype, q.shape
+    T, H, D = shape
+    qts, qhs, es = q.stride()
+    if es != 1:
+        raise ValueError("q: the elements of a head have to be contiguous")
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=dtype, device=dev)
-    strides = _strided(q, dtype, q.shape, "q", dev) + _strided(q_out, dtype, q.shape, "q_out", dev)
-    kp = op = heads = 0
-    k_strides = (0, 0, 0, 0)
+        q_out = torch.empty(shape, dtype=dtype, device=dev)
+    qots, qohs = _strided(q_out, dtype, shape, "q_out", dev)
+    kp = op = heads = kts = khs = kots = kohs = 0
     if k is not None:
-        heads = k.shape[1]
-        shape = (T, heads, D)
+        shape = k.shape
+        heads = shape[1]
+        kts, khs = _strided(k, dtype, (T, heads, D), "k", dev)
         if k_out is None:
             k_out = torch.empty(shape, dtype=dtype, device=dev)
-        k_strides = _strided(k, dtype, shape, "k", dev) + _strided(k_out, dtype, shape, "k_out", dev)
+        kots, kohs = _strided(k_out, dtype, shape, "k_out", dev)
         kp, op = k.data_ptr(), k_out.data_ptr()
     elif k_gain is not None or k_out is not None:
         raise ValueError("k_gain, k_out: there is no k")
     qg, kg, kind = _gains(q_gain, k_gain, D, dev)
-    at, n_pos, rot = (0, 0, 0) if table is None else _rotation(table, dev)
-    where = 0 if table is None else _flat(positions, torch.int32, (T,), "positions", dev)
-    return _NORM_ROPE_T.pack(q.data_ptr(), qg, q_out.data_ptr(), *strides, kp, kg, op, *k_strides, where, at, H, heads, _dt(q), kind, T, D,
-                             n_pos, rot, interleaved, norm_eps), q_out, k_out
+    at = n_pos = rot = where = 0
+    if table is not None:
+        at, n_pos, rot = _rotation(table, dev)
+        where = _flat(positions, torch.int32, (T,), "positions", dev)
+    return _NORM_ROPE_T.pack(q.data_ptr(), qg, q_out.data_ptr(), qts, qhs, qots, qohs, kp, kg, op, kts, khs, kots, kohs, where, at, H, heads,
+                             _dt(q), kind, T, D, n_pos, rot, interleaved, norm_eps), q_out, k_out
 
 
 def hbl_norm_rope(q: torch.Tensor, q_gain: torch.Tensor | None, positions: torch.Tensor | None, table: torch.Tensor | None,
