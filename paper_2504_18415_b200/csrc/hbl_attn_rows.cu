@@ -6,14 +6,19 @@
 // the queries once a row is scaled by a power of two; p_j vs_j is rounded to fp16 against a running power of two above
 // the value scales.  These roundings are what the tensor core's operands cost; p's sum is taken before them, in fp32.
 //
-// The cache is read once per 8 (16) query rows of its key head.  bf16 is bound by that (one sequence of 131072 tokens: 95 us,
-// 5.7 TB/s; 64 ragged ones of up to 4096 tokens 364).  Codes (64 x 4096 tokens of 32 key heads, one row: 4 bits 275 us, 4.3 TB/s;
-// ragged 175) fill no unit: 60 % of the issue slots, 53 % of the logic pipe's cycles, 46 % of HBM's.  A thread block takes one
+// The cache is read once per 8 (16) query rows of its key head.  bf16 is bound by that (one sequence of 131072 tokens: 91 us,
+// 5.9 TB/s; 64 ragged ones of up to 4096 tokens 357).  Codes (64 x 4096 tokens of 32 key heads, one row: 4 bits 263 us, 4.3 TB/s;
+// ragged 159) fill no unit: 60 % of the issue slots, 53 % of the logic pipe's cycles, 46 % of HBM's.  A thread block takes one
 // (sequence, key head, row tile, piece of the keys), its four warps take 16 keys in turn and meet only at the end, so there
 // is no barrier in the loop.  The keys are the M side of both products (S^T = K q^T, O^T = V^T P^T): 16 keys against 8
 // rows, no half-empty tile, and a lane's operand registers are exactly the bytes that it loads from the cache
 // (hbl_attn_frag.cuh), so nothing passes through shared memory but the queries.  The running maximum is only
 // raised when a score exceeds it by more than 2^8 (p stays below 256): most steps rescale nothing and exchange nothing.
+//
+// Within a window (WINDOW) a block counts the keys that its rows see (KeyMap) and finds their pages from that; the rest is the same.
+// 64 ragged sequences of up to 4096 tokens, window 1024, 4 bits: 87 us; what a block costs beside its keys is a third of that (27 us at
+// a window of 64), so its chain is kept short: pages and the first token's rows are asked for before the queries, the
+// warps' results lie side by side and are joined once (one warp after the other: 105 us).
 #include "hbl_attn_frag.cuh"
 
 namespace hbl {
@@ -684,8 +689,8 @@ int launch_rows_dim(RowsParams& p, cudaStream_t s) {
   const long blocks = (long)p.b.n_seqs * p.c.n_kv_heads * p.p.tiles * p.p.splits;
   if (blocks > 0x7fffffffL) return HBL_ERR_TOO_LARGE;
   const bool narrow = rows_per_tile(p.b, p.a.group, p.few) == 8;
-  // Within a window: eight warps where every block has an SM to itself (4 x 509 tokens at 8 bits, window of 128: 7.4 us, 8.5; of
-  // 500: 9.8, 12.6; 64 x 4096 tokens, of 1024: 107, 94), as far as there is room for their results.
+  // Within a window: eight warps where every block has an SM to itself (4 x 509 tokens at 8 bits, window of 128: 7.1 us, with four
+  // 8.5; of 500: 9.5, 12.6; 64 x 4096 tokens, of 1024: 107, 94), as far as there is room for their results.
   if constexpr (WINDOW && D <= 128) {
     if (blocks <= sm_count() && (narrow || D <= 64)) {
       if (narrow) HBL_CUDA_OK(launch_waiting(attn_rows_kernel<BITS, D, 1, WINDOW, 8>, dim3((unsigned)blocks), dim3(256), 0, s, p));
@@ -715,7 +720,8 @@ int launch_rows_bits(RowsParams& p, cudaStream_t s) {
   return p.a.window > 0 ? launch_rows_window<BITS, true>(p, s) : launch_rows_window<BITS, false>(p, s);
 }
 
-// How many pieces the keys of a sequence are dealt in.
+// How many pieces the keys of a sequence are dealt in.  (The figures are of results joined warp by warp; joined at once a block costs
+// some 2 us less.  The rule is kept.)
 //   None up to 512 keys, where the second launch costs more than the shorter loops save (4 x 509 tokens: 14.8 us in two
 // pieces, 12.7 in one; 4 x 1000: 16.8, 17.3), and none of less than 256 keys.
 //   Few sequences: as many pieces as there is room for at once; with one more the last waits for a whole round (16 rows
@@ -772,8 +778,9 @@ int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a
   p.c = c; p.b = b; p.a = a; p.p = plan; p.few = few; p.part_o = w.rows_o; p.part_lse = w.rows_lse;
   p.beside_tiles = beside_tiles;
   // More blocks than fit at once, of whole sequences: the long ones first (64 ragged sequences of up to 4096 tokens at 4 bits
-  // 190 us in the batch's order, 175 in this; 128 of 8 key heads 113, 92; all of one length 275, 278).  Not for short ones, whose
-  // blocks would spend more on the look-up than it saves (up to 600 tokens: 59 us, 64), nor for batches whose look-up is long.
+  // 190 us in the batch's order, 175 in this; 128 of 8 key heads 113, 92; all of one length 275, 278; window of 1024, ragged 88, 87, of
+  // 2048 137, 130).  Not for short ones, whose blocks would spend more on the look-up than it saves (up to 600 tokens: 59 us, 64;
+  // window of 256: 42, 44), nor for batches whose look-up is long.
   const long slots = (long)sm_count() * blocks_per_sm(c.bits, c.head_dim, rows_per_tile(b, a.group, few) / 8);
   p.ordered = plan.splits == 1 && (b.max_kv_len < plan.reach ? b.max_kv_len : plan.reach) >= 1024 && b.n_seqs <= 128 && (long)b.n_seqs * c.n_kv_heads * plan.tiles > slots;
   p.status = device_status_word();
