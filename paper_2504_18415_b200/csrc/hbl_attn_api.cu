@@ -185,6 +185,24 @@ int append(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_k
 // Up to 16 rows streaming wins over codes by far and loses at 16 bits by 8 % and 5 % from 9 rows on.  At 3 and 4 bits it still
 // wins at 32 rows (not at 48: 97 and 385 us, 93 and 344), at 8 bits the two meet there: the border there could be later.
 constexpr int kFewRows = 16;
+// Within a window the keys are few, and a tile's way through its roles (12 us for the first, 2 to 3 for each other) is long against
+// 16 rows' way over them, as long as there are not too many of those for the GPU: by the keys that an SM goes over, once
+// for every 16 rows (us, streaming / tiles; 2 or 32 sequences, 8 key heads of 128):
+//   keys to an SM            500          900          1700         3500         7000
+//   4 bits               24 /  38     22 /  38     27 /  48     58 /  83     89 /  84
+//   8 bits               29 /  38     27 /  39     35 /  50     81 /  85    122 /  86
+//   16 bits              23 /  25     22 /  27     33 /  34     64 /  52    119 /  53
+int few_rows(const KvView& c, const BatchView& b, const AttnArgs& a) {
+  if (a.window == 0) return kFewRows;
+  const long seen = (long)a.sinks + a.window + b.max_q_len, keys = seen < b.max_kv_len ? seen : b.max_kv_len;
+  const long most = c.bits < 8 ? 4500 : c.bits == 8 ? 3000 : 1500;
+  const long rows = (long)b.max_q_len * a.group;
+  for (int few = 128; few > kFewRows; few /= 2) {
+    const long tiles = ((rows < few ? rows : few) + 15) / 16;
+    if ((double)b.n_seqs * c.n_kv_heads * tiles * keys <= (double)most * sm_count()) return few;
+  }
+  return kFewRows;
+}
 struct AttnCall {
   bool use_rows, use_tiles;
   int few_rows, few_tiles;             // the border as each kernel sees it
@@ -193,11 +211,11 @@ struct AttnCall {
 };
 AttnCall plan_attention(const KvView& c, const BatchView& b, const AttnArgs& a) {
   AttnCall w{};
-  const int group = a.group, n_heads = a.n_heads;
-  w.use_tiles = (long)b.max_q_len * group > kFewRows;
+  const int group = a.group, n_heads = a.n_heads, few = few_rows(c, b, a);
+  w.use_tiles = (long)b.max_q_len * group > few;
   w.use_rows = !w.use_tiles || b.n_seqs > 1;
-  w.few_rows = kFewRows;
-  w.few_tiles = w.use_rows ? kFewRows : 0;
+  w.few_rows = few;
+  w.few_tiles = w.use_rows ? few : 0;
   w.rows.splits = w.tiles.splits = 1;
   if (w.use_rows) w.rows = plan_attention_rows(c, b, a, w.few_rows);
   if (w.use_tiles) w.tiles = plan_attention_tiles(c, b, a, w.few_tiles);

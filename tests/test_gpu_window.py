@@ -208,6 +208,17 @@ def test_many_sequences():
     check_window(cache, batch, tables, q_lens, kv_lens, q, 90, 4)
 
 
+@pytest.mark.parametrize("bits", [3, 4, 8, 16])
+@pytest.mark.parametrize("H,KH,D", [(4, 2, 64), (2, 2, 128), (2, 1, 256)])
+def test_chunks_of_a_large_batch(bits, H, KH, D):
+    """So many of them, and such a window, that even short chunks are no longer dealt with 16 rows at a time."""
+    q_lens = [17 + (7 * i) % 100 for i in range(60)]
+    kv_lens = [q + 600 + (97 * i) % 2500 for i, q in enumerate(q_lens)]
+    cache, batch, tables, q, slots = setup(19, q_lens, kv_lens, H, KH, D, bits, 32, bos=bits < 8)
+    check_window(cache, batch, tables, q_lens, kv_lens, q, 2100, 20, slots=slots)
+    check_window(cache, batch, tables, q_lens, kv_lens, q, 130, 3, slots=slots)
+
+
 def test_strided_queries_and_outputs():
     q_lens, kv_lens = [1, 30], [90, 31]
     cache, batch, tables, q, _ = setup(71, q_lens, kv_lens, 4, 2, 128, 4, 32, extra=0)
