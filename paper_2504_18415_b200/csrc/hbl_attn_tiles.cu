@@ -460,7 +460,24 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
             }
           }
         }
-        if (!BITWISE && masked) {
+        if (WINDOW && R == 4 && (masked || old)) {
+          // the thread's columns 8 q + 2 t, + 1 of a row as bits 2 q, 2 q + 1
+          auto first_of = [&](int n) {
+            const int c = min(max(n - 2 * t, 0), BK), k = 2 * (c >> 3) + min(c & 7, 2);
+            return k == 0 ? 0u : ~0u >> (32 - k);
+          };
+          const uint32_t keep = first_of(p.a.sinks - k0);
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            const uint32_t m = first_of(limit(i) - k0) & (~first_of(from(i) - k0) | keep);
+#pragma unroll
+            for (int q = 0; q < NP; ++q) {
+              if (!(m >> (2 * q % 32) & 1)) x[at(i, q)] = -INFINITY;
+              if (!(m >> ((2 * q + 1) % 32) & 1)) x[at(i, q) + 1] = -INFINITY;
+            }
+          }
+        }
+        if (!WINDOW && masked) {
 #pragma unroll
           for (int i = 0; i < R; ++i) {
             const int seen = limit(i) - k0 - 2 * t;
@@ -468,26 +485,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
             for (int q = 0; q < NP; ++q) {
               if (STEP * q >= seen) x[at(i, q)] = -INFINITY;
               if (STEP * q + 1 >= seen) x[at(i, q) + 1] = -INFINITY;
-            }
-          }
-        }
-        if (!BITWISE && old) {
-#pragma unroll
-          for (int i = 0; i < R; ++i) {
-            const int begin = from(i) - k0 - 2 * t;
-            if (k0 >= p.a.sinks) {
-#pragma unroll
-              for (int q = 0; q < NP; ++q) {
-                if (STEP * q < begin) x[at(i, q)] = -INFINITY;
-                if (STEP * q + 1 < begin) x[at(i, q) + 1] = -INFINITY;
-              }
-            } else {
-              const int keep = p.a.sinks - k0 - 2 * t;
-#pragma unroll
-              for (int q = 0; q < NP; ++q) {
-                if (STEP * q < begin && STEP * q >= keep) x[at(i, q)] = -INFINITY;
-                if (STEP * q + 1 < begin && STEP * q + 1 >= keep) x[at(i, q) + 1] = -INFINITY;
-              }
             }
           }
         }
@@ -536,15 +533,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
 #pragma unroll 1
             for (int c = 0; c < D / (R == 4 ? 16 : 32); ++c) {      // (few registers: the scores are held meanwhile)
               if constexpr (R == 4) {
+                float o[16];
+                tmem_ld16(o_addr + 16 * c, o);
+                tmem_ld16(o_addr + LOWER + 16 * c, o + 8);
+                tmem_ld_wait();
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  float o[8];
-                  tmem_ld16(o_addr + h * LOWER + 16 * c, o);
-                  tmem_ld_wait();
-#pragma unroll
-                  for (int e = 0; e < 8; ++e) o[e] *= f[R == 4 ? 2 * h + (e >> 1 & 1) : 0] * regauge;
-                  tmem_st16(o_addr + h * LOWER + 16 * c, o);
-                }
+                for (int e = 0; e < 16; ++e) o[e] *= f[R == 4 ? 2 * (e >> 3) + (e >> 1 & 1) : 0] * regauge;
+                tmem_st16(o_addr + 16 * c, o);
+                tmem_st16(o_addr + LOWER + 16 * c, o + 8);
               } else {
                 float o[32];
                 tmem_ld_row(o_addr + 32 * c, o);
