@@ -27,7 +27,8 @@
 //
 // Within a window (WINDOW) an item counts the keys that its rows see (KeyMap): the tiles hold the sinks' groups of 16 and then the
 // window's, and each row masks what lies before its own window.  8192-token prompt of 32 heads, window 1024, 4 sinks: 203 us, 11 tiles
-// to an item of 256 rows where 8.03 are seen; masks and the looks at values are 35 us of it.  2048 queries over 16384 at 8 bits, window 2048: 157.
+// to an item of 256 rows where 8.03 are seen; masks and the looks at values are 25 to 35 us of it.  2048 queries over 16384 at 8 bits, window
+// 2048: 154.
 // bf16 values of a tile that some row masks are looked through after their keys have been announced (before: 243 us for that
 // prompt); what is not finite becomes zeros and is marked.
 #include "hbl_attn_frag.cuh"
@@ -444,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
             for (int i = 0; i < R; ++i) fma2(x[at(i, q)], x[at(i, q) + 1], s.x, s.y, neg[i]);
           }
         }
-        // (bits against comparisons for the window's masks: bf16, heads of 64 138 us, 176; codes with their four rows 410, 360)
+        // (a window's masks by bits: bf16 prompt, window of 256 132 us, with comparisons 139; codes 154, 156)
         constexpr bool BITWISE = WINDOW && R == 1;
         const bool old = WINDOW && k0 < expired && k0 + BK > p.a.sinks;
         if (BITWISE && (masked || old)) {

@@ -326,3 +326,40 @@ def test_captured_and_on_another_stream():
         graph.replay()
     assert all(torch.equal(a, b) for a, b in zip(got, both()))
     assert hbl.hbl_check_status() == 0
+
+
+@pytest.mark.parametrize("T,H,KH", [(1, 1, 0), (9, 8, 2), (128, 8, 3), (129, 8, 3), (4, 300, 1)])
+def test_small_gradients_captured_side_by_side(T, H, KH):
+    """Calls that add up the gains' gradients within one launch, around the border to those that take two; two graphs on two streams."""
+    g = gen(12)
+    D = 128
+    table = table_of(D, 512)
+    sets = []
+    for _ in range(2):
+        pos = torch.randint(0, 512, (T,), device="cuda", generator=g, dtype=torch.int32)
+        x, w = heads(g, T, H + KH, D), torch.randn(T, H + KH, D, device="cuda", generator=g).to(BF16)
+        gains = [gain_of(g, D, BF16) for _ in range(2)]
+        ws = hbl.new_workspace(hbl.hbl_norm_rope_grad_workspace_bytes(T, H, KH, D))
+        kw = dict(k=x[:, H:], k_gain=gains[1], grad_k=w[:, H:]) if KH else {}
+
+        def call(x=x, w=w, gains=gains, pos=pos, kw=kw, ws=ws):
+            return hbl.hbl_norm_rope_grad(w[:, :H], x[:, :H], gains[0], pos, table, workspace=ws, **kw)
+
+        want = call()
+        check_backward(want[:2], w[:, :H], x[:, :H], gains[0], table, pos, 1e-6, False)
+        if KH:
+            check_backward(want[2:], w[:, H:], x[:, H:], gains[1], table, pos, 1e-6, False)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = call()
+        sets.append((graph, got, want, torch.cuda.Stream(), call))             # (the call holds what the graph reads)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for graph, _, _, stream, _ in sets:
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for _, got, want, _, _ in sets:
+        assert all(a is None and b is None or torch.equal(a, b) for a, b in zip(got, want))
+    assert hbl.hbl_check_status() == 0
