@@ -307,7 +307,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
   __shared__ Item item_slot[2];
   __shared__ __align__(8) uint64_t steal_bar, near_end;
   __shared__ __align__(16) uint4 steal_answer;
-  __shared__ __align__(16) uint32_t bad_value[STAGES][4];       // keys of the tile whose value, or its scale, is not finite
+  // Keys of the tile whose value, or its scale, is not finite: key 32 e + c is bit c of word e.  The bf16 producers' warps all write to
+  // them; so a stage has two sets in turn, and the next tile's is made 0 before this one's values are announced: whoever may fill
+  // the stage again comes after that, and nobody has to wait for another warp.
+  __shared__ __align__(16) uint32_t bad_value[STAGES][CODES ? 1 : 2][4];
   __shared__ float2 unit_of_tile[STAGES];                       // what the value scales are held against: now, and before / now
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag_s;
@@ -337,6 +340,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
       for (int h = 0; h < 2; ++h) mbar_init(&p_full[i][h], 4);
       mbar_init(&o_full[i], 1);
     }
+    if (!CODES)
+      for (int s = 0; s < STAGES; ++s)
+        for (int e = 0; e < 4; ++e) bad_value[s][0][e] = 0;
     abort_flag_s = 0;
     mbar_fence_init();
   }
@@ -594,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         // results become NaN.
         if (!CODES && marked.has(j, WINDOW)) {              // (the product below needs the values as well)
           if (!(ok = __all_sync(0xffffffffu, mbar_wait(&v_full[stage], (it / STAGES) & 1, abort_flag, p.status)))) break;
-          const uint4 b = *reinterpret_cast<const uint4*>(bad_value[stage]);
+          const uint4 b = *reinterpret_cast<const uint4*>(bad_value[stage][CODES ? 0 : (it / STAGES) & 1]);
           if (b.x | b.y | b.z | b.w) {
             const uint32_t word[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
@@ -609,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
 #pragma unroll
         for (int i = 0; i < R; ++i) l[i] += R == 4 ? sum[i][0] + sum[i][1] : (sum[i][0] + sum[i][1]) + (sum[i][R == 4 ? 0 : 2] + sum[i][R == 4 ? 0 : 3]);
         if (CODES) {
-          const uint4 b = *reinterpret_cast<const uint4*>(bad_value[stage]);
+          const uint4 b = *reinterpret_cast<const uint4*>(bad_value[stage][0]);
           if (b.x | b.y | b.z | b.w) {
             const uint32_t word[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
@@ -794,13 +800,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
               mbar_arrive(copied);
               copied = nullptr;
             }
+            if (kv == 1 && tid < 4) bad_value[stage][(it / STAGES & 1) ^ 1][tid] = 0;    // (its readers have seen the last products begin)
             if (kv == 1 && marked.has(j, WINDOW)) {
               // A tile that some row masks: 0 * a value that is not finite would reach rows that mask its key.  Every thread
               // looks through the pieces that it has copied; such a value becomes zeros and its key is marked, so that the rows
               // that see it, and no others, become NaN.  (The lanes that hold a row lie side by side.)
-              if (tid < 4) bad_value[stage][tid] = 0;           // (whoever read the stage's last marks has seen its products begin)
               asm volatile("cp.async.wait_all;" ::: "memory");
-              asm volatile("bar.sync 1, 128;" ::: "memory");
               uint32_t any = 0;
               auto look = [&](int i) {                          // 0 * y summed up: zeros, or NaN where y is not finite
                 uint32_t y[4], sum = 0;
@@ -819,7 +824,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
                     const uint32_t zero[4] = {0, 0, 0, 0};
                     const int rr = i * RPP + tid / CH;
                     store16(dst + chunk_at(rr, tid % CH, G::HALF), zero);
-                    if (tid % CH == 0) atomicOr(&bad_value[stage][rr >> 5], 1u << (rr & 31));
+                    if (tid % CH == 0) atomicOr(&bad_value[stage][it / STAGES & 1][rr >> 5], 1u << (rr & 31));
                   }
                 }
               fence_async();
@@ -942,7 +947,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
                   for (int i = 0; i < VN; ++i)
                     if (i == mine) my_vs = vs[i];
                   const unsigned word = __ballot_sync(0xffffffffu, mine < VN && (bad >> mine & 1));
-                  if (lane == 0) bad_value[stage][mine] = word;  // (BK 64: the upper two hold none)
+                  if (lane == 0) bad_value[stage][0][mine] = word;  // (BK 64: the upper two hold none)
                   if (tid == 0) unit_of_tile[stage] = make_float2(unit * 0x1p-7f, before / unit);
                   if (tid < BK) {
                     scales[stage * 2 * BK + tid] = ks * scale;

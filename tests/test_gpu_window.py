@@ -161,6 +161,29 @@ def test_what_is_not_finite_reaches_the_rows_that_see_it_and_no_others(bits, q_l
     assert torch.equal(out[~sees], clean[~sees])
 
 
+@pytest.mark.parametrize("window", [0, 40])
+@pytest.mark.parametrize("bits,D", [(16, 64), (16, 128), (16, 256), (8, 128), (4, 256)])
+def test_each_key_of_a_tile_with_a_value_that_is_not_finite(bits, D, window):
+    """Sequence b's key b has one: the rows that see it become NaN or infinite there, and no others."""
+    n, page, sinks = 150, 32, 3
+    cache, batch, tables, q, _ = setup(63, [n] * n, [n] * n, 1, 1, D, bits, page, extra=0)
+
+    def run():
+        return hbl.hbl_attention_window(cache, batch, q, window, sinks) if window else hbl.hbl_attention(cache, batch, q)
+    clean = run()
+    for b in range(n):
+        at = tables[b][b // page], 0, b % page
+        if bits == 16:
+            cache.v[(*at, b * 7 % D)] = [float("nan"), float("inf"), -float("inf")][b % 3]
+        else:
+            cache.v_scale[at] = [float("nan"), float("inf")][b % 2]
+    out = run()
+    seen = visible(n, n, window, sinks) if window else torch.ones(n, n, device="cuda").tril().bool()
+    sees = seen.T.reshape(n * n)                                             # row r of sequence b: does it see key b
+    assert (~torch.isfinite(out[sees])).any(-1).all()
+    assert torch.equal(out[~sees], clean[~sees])
+
+
 @pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("q_len", [1, 60])
 def test_a_large_scale_outside_the_window_does_not_coarsen_the_weights(bits, q_len):
