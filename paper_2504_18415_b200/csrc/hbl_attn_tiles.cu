@@ -26,7 +26,7 @@
 // threads themselves (the scores' barrier says that the products before it are complete, so O is at rest).
 //
 // Within a window (WINDOW) an item counts the keys that its rows see (KeyMap): the tiles hold the sinks' groups of 16 and then the
-// window's, and each row masks what lies before its own window.  8192-token prompt of 32 heads, window 1024, 4 sinks: 203 us, 11 tiles
+// window's, and each row masks what lies before its own window.  8192-token prompt of 32 heads, window 1024, 4 sinks: 205 us, 11 tiles
 // to an item of 256 rows where 8.03 are seen; masks and the looks at values are 25 to 35 us of it.  2048 queries over 16384 at 8 bits, window
 // 2048: 154.
 // bf16 values of a tile that some row masks are looked through after their keys have been announced (before: 243 us for that
