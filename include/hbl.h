@@ -425,8 +425,8 @@ int hbl_norm_rope(const hbl_norm_rope_t* args /* host */, void* stream);
 
 /* The backward pass of hbl_norm_rope, from the gradients with respect to its outputs:
  *   t = R^T grad_out,  u = gain * t,   grad_x = r (u - x r^2 mean_d(x u)),   grad_gain[d] = sum over tokens and heads of t[d] x[d] r
- * in fp32 throughout (of head magnitudes whose squares fp32 can add up), the sum over rows in an order that depends on the
- * sizes alone: the same call gives the same bits.
+ * in fp32 (the squares of large and small heads in fp64: whatever the forward pass takes has its gradients), the sum over rows
+ * in an order that depends on the sizes alone: the same call gives the same bits.
  *   part.x     the inputs of hbl_norm_rope;  part.out: grad_x, same type, written; it may be x or grad_out itself (same strides)
  *   grad_out   device, type of x, element strides as in hbl_rope (0: broadcast)
  *   grad_gain  device fp32 [head_dim], 4-byte aligned, overwritten; NULL: not wanted.  (gain NULL: that of a gain of ones)

@@ -5,7 +5,9 @@
 //
 // R is linear, so r goes last: one product for each element instead of one before the gain.  The statistic is
 // summed in fp64 and r rounded once, the products and sums of the rest are rounded one by one in fp32: o is the plain fp32
-// evaluation bit for bit (kv_append_kernel quantizes the same values).  The backward pass is fp32 throughout.
+// evaluation bit for bit (kv_append_kernel quantizes the same values).  The backward pass is fp32, but for heads whose mean square and eps
+// lie outside 2^-60 .. 2^60: their squares, or r^2, could leave its range, so the statistic is summed in fp64 there, and x r goes
+// into the other sum, whose terms are then of u's size.
 //
 // A thread owns 16 elements of a head; the L lanes of a head add up its statistic.  Thread blocks stay and walk over the call's
 // heads, HEADS of a token at a time: the gains are loaded once, the table's pairs once for HEADS heads, and the next ones are
@@ -361,13 +363,40 @@ __global__ void __launch_bounds__(kThreads, kBackwardBlocksPerSm) norm_rope_grad
         sum += __shfl_xor_sync(0xffffffffu, sum, o);
         dot += __shfl_xor_sync(0xffffffffu, dot, o);
       }
+      const float square = fmaf(sum, inv_dim, a.eps);
+      const bool within = square > 0x1p-60f && square < 0x1p60f;
+      float r = 1.f / sqrtf(square);
+      dot *= r;                                                // sum of x r u
+      if (__any_sync(0xffffffffu, i < n && !within)) {         // heads whose squares, or r^2, are not for fp32
+        double wide = 0.0;
+        if (i < n) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) wide = fma((double)f[k].y, (double)f[k].y, fma((double)f[k].x, (double)f[k].x, wide));
+        }
+#pragma unroll
+        for (int o = L / 2; o > 0; o >>= 1) wide += __shfl_xor_sync(0xffffffffu, wide, o);
+        const float root = inverse_root(fma(wide, 1.0 / a.head_dim, (double)a.eps));
+        float2 own_dots = make_float2(0.f, 0.f);
+        if (i < n) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) own_dots = fma2(mul2(f[k], make_float2(root, root)), mul2(y[k], g[k]), own_dots);
+        }
+        float own_dot = own_dots.x + own_dots.y;
+#pragma unroll
+        for (int o = L / 2; o > 0; o >>= 1) own_dot += __shfl_xor_sync(0xffffffffu, own_dot, o);
+        if (!within) {
+          r = root;
+          dot = own_dot;
+        }
+      }
       if (i >= n) continue;
-      const float r = 1.f / sqrtf(fmaf(sum, inv_dim, a.eps)), m = -r * (r * r * (dot * inv_dim));
+      const float m = -r * (dot * inv_dim);
       const float2 rr = make_float2(r, r), mm = make_float2(m, m);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        acc[k] = fma2(y[k], mul2(f[k], rr), acc[k]);
-        f[k] = fma2(f[k], mm, mul2(mul2(y[k], g[k]), rr));
+        const float2 z = mul2(f[k], rr);
+        acc[k] = fma2(y[k], z, acc[k]);
+        f[k] = fma2(z, mm, mul2(mul2(y[k], g[k]), rr));
       }
       store(out + i * w.o_hs, own, f);
     }
