@@ -274,9 +274,8 @@ __global__ void __launch_bounds__(kThreads, kForwardBlocksPerSm) norm_rope_kerne
   }
 }
 
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+// Not the aligned form: the loops before it part a warp's lanes at widths that are no multiple of 32.
+__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ float of_block(const float* mine, int rank) {       // the same place in another block of the cluster
   uint32_t at;
   float x;
