@@ -179,29 +179,44 @@ int append(const hbl_kv_cache_t* cache, const hbl_kv_batch_t* batch, const hbl_k
 // tiles; a single sequence, whose length the bound says, on one of them alone.  The streaming kernel reads
 // the keys once for 16 rows, so its time goes up in steps (8192 tokens, heads of 128, us at 8, 16, 32 rows: streaming / tiles):
 //                                3 bits                    4 bits                    8 bits                    16 bits
-//   1 sequence, 32 key heads     32 46  62 /  73  73  73   30 46  58 /  69  70  71   38 54  73 /  75  75  79   48 56  87 /  52  52  52
-//   32 sequences, 8 key heads   101 183 305 / 430 429 430  103 171 276 / 376 376 377  148 228 437 / 409 412 417  208 267 364 / 257 255 256
-// (taken when the streaming kernel joined its results warp by warp: it is up to a quarter faster now, the tiles are as they were).
-// Up to 16 rows streaming wins over codes by far and loses at 16 bits by 8 % and 5 % from 9 rows on.  At 3 and 4 bits it still
-// wins at 32 rows (not at 48: 97 and 385 us, 93 and 344), at 8 bits the two meet there: the border there could be later.
+//   1 sequence, 32 key heads     22  29  45 /  66  66  67   21  28  42 /  64  65  66   28  36  55 /  67  67  68   33  37  60 /  45  46  46
+//   32 sequences, 8 key heads    90 141 281 / 451 451 452   82 130 259 / 391 393 397  134 186 426 / 400 402 405  184 222 338 / 255 255 258
+// Up to 16 rows streaming wins everywhere; at 3 and 4 bits, and of one sequence at 8, it still wins at 32 rows: the border there could be later.
 constexpr int kFewRows = 16;
-// Within a window the keys are few, and a tile's way through its roles (12 us for the first, 2 to 3 for each other) is long against
-// 16 rows' way over them, as long as there are not too many of those for the GPU: by the keys that an SM goes over, once
-// for every 16 rows (us, streaming / tiles; 2 or 32 sequences, 8 key heads of 128):
-//   keys to an SM            500          900          1700         3500         7000
-//   4 bits               24 /  38     22 /  38     27 /  48     58 /  83     89 /  84
-//   8 bits               29 /  38     27 /  39     35 /  50     81 /  85    122 /  86
-//   16 bits              23 /  25     22 /  27     33 /  34     64 /  52    119 /  53
+// Within a window the keys are few, and a tile's way through its roles is long against 16 rows' way over them.  Where no sequence has more
+// than 128 rows, the call goes to the kernel that should be done first, by what the two cost (us, fitted to 88 calls of each kind, 1 to
+// 32 sequences of 5 to 32 tokens, 32 and 8 heads, windows of 128 to 4000, each on both kernels, which the sums give within 3 to 9 % rms):
+//   streaming: start + rounds (round + key * keys of a block) + 2.5 if the keys are split; a round that is not full counts as half of one
+//              and its part of the other half
+//   tiles:     start + rounds (round + tile * tiles of an item * (1 to 1.5, as the GPU fills)) + 3.5 if they are split
+// None of those calls takes over 21 % more than on the other kernel, and of 400 others (1 to 64 sequences, 1 to 32 key heads, groups of 1 to 16,
+// ragged or not) three do, 56 % at most.  Both sides, streaming / tiles: 16 sequences of 32 tokens, heads of 128, 4 bits, window of
+// 128 37 / 24 us, of 32 sequences of 8 24 / 37; one of 8, of 512 14 / 27; one of 8, heads of 256, 16 bits, window of 128 26 / 13.
+struct Costs { float start, round, key, tiles_start, tiles_round, tile; };
+constexpr Costs kCosts[3][3] = {       // heads of 64, 128, 256; 3 and 4, 8, 16 bits
+    {{0.8f, 8.1f, .014f, 7.3f, 4.1f, 2.2f}, {0.4f, 7.7f, .017f, 7.7f, 3.7f, 2.2f}, {1.0f, 5.0f, .016f, 5.8f, 3.3f, 1.5f}},
+    {{2.5f, 9.4f, .020f, 9.9f, 6.2f, 2.5f}, {2.5f, 10.2f, .029f, 9.8f, 5.7f, 2.7f}, {2.0f, 6.9f, .021f, 7.1f, 3.8f, 1.7f}},
+    {{4.6f, 20.3f, .024f, 10.2f, 3.0f, 2.2f}, {3.8f, 19.0f, .034f, 7.4f, 1.7f, 3.3f}, {0.9f, 20.0f, .080f, 7.5f, 3.8f, 1.3f}}};
+constexpr int kFewRowsInWindow = 128;
 int few_rows(const KvView& c, const BatchView& b, const AttnArgs& a) {
-  if (a.window == 0) return kFewRows;
-  const long seen = (long)a.sinks + a.window + b.max_q_len, keys = seen < b.max_kv_len ? seen : b.max_kv_len;
-  const long most = c.bits < 8 ? 4500 : c.bits == 8 ? 3000 : 1500;
   const long rows = (long)b.max_q_len * a.group;
-  for (int few = 128; few > kFewRows; few /= 2) {
-    const long tiles = ((rows < few ? rows : few) + 15) / 16;
-    if ((double)b.n_seqs * c.n_kv_heads * tiles * keys <= (double)most * sm_count()) return few;
-  }
-  return kFewRows;
+  if (a.window == 0 || rows <= kFewRows || rows > kFewRowsInWindow) return kFewRows;
+  const Costs& cost = kCosts[c.head_dim / 128][c.bits < 8 ? 0 : c.bits / 16 + 1];
+  const long reach = (long)a.sinks + a.window + b.max_q_len + 15, sms = sm_count();
+  const float keys = (float)(reach < b.max_kv_len ? reach : b.max_kv_len);
+  const AttnPlan s = plan_attention_rows(c, b, a, kFewRowsInWindow), t = plan_attention_tiles(c, b, a, kFewRows);
+  const long resident = attention_rows_resident(c, b, a, kFewRowsInWindow);
+  // the batch's row tiles: whole ones of all its rows, and what sequences of the most rows (of any number: half a tile) have beside those
+  const float part = fmaxf(0.5f, (float)s.tiles - (float)rows / 16.f), row_tiles = (float)b.tokens * (float)a.group / 16.f + (float)b.n_seqs * part;
+  const float blocks = fminf((float)b.n_seqs * (float)s.tiles, row_tiles) * (float)c.n_kv_heads * (float)s.splits;
+  const long on_sm = (long)ceilf(blocks / (float)sms), rest = on_sm % resident;
+  const float rounds = (float)(on_sm / resident) + (rest > 0 ? 0.5f + 0.5f * (float)rest / (float)resident : 0.f);
+  const float streaming = cost.start + rounds * (cost.round + cost.key * fminf(keys, (float)s.chunk)) + (s.splits > 1 ? 2.5f : 0.f);
+  const long items = (long)t.tiles * c.n_kv_heads * t.splits;
+  const float full = fminf(1.f, (float)items / (float)sms), of_item = ceilf(fminf(keys, (float)t.chunk) / (c.head_dim == 256 ? 64.f : 128.f));
+  const float tiles = cost.tiles_start + (float)((items + sms - 1) / sms) * (cost.tiles_round + cost.tile * of_item * (1.f + 0.5f * full)) +
+                      (t.splits > 1 ? 3.5f : 0.f);
+  return streaming <= tiles ? kFewRowsInWindow : kFewRows;
 }
 struct AttnCall {
   bool use_rows, use_tiles;

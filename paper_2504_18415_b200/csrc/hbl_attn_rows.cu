@@ -756,6 +756,10 @@ long pieces_of_keys(long base, int resident, long keys, long most, int bits) {
 
 }  // namespace
 
+int attention_rows_resident(const KvView& c, const BatchView& b, const AttnArgs& a, int few) {
+  return blocks_per_sm(c.bits, c.head_dim, rows_per_tile(b, a.group, few) / 8);
+}
+
 AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, int few) {
   AttnPlan p{};
   const int group = a.group, rows = rows_per_tile(b, group, few);
@@ -781,7 +785,7 @@ int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a
   // 190 us in the batch's order, 175 in this; 128 of 8 key heads 113, 92; all of one length 275, 278; window of 1024, ragged 88, 87, of
   // 2048 137, 130).  Not for short ones, whose blocks would spend more on the look-up than it saves (up to 600 tokens: 59 us, 64;
   // window of 256: 42, 44), nor for batches whose look-up is long.
-  const long slots = (long)sm_count() * blocks_per_sm(c.bits, c.head_dim, rows_per_tile(b, a.group, few) / 8);
+  const long slots = (long)sm_count() * attention_rows_resident(c, b, a, few);
   p.ordered = plan.splits == 1 && (b.max_kv_len < plan.reach ? b.max_kv_len : plan.reach) >= 1024 && b.n_seqs <= 128 && (long)b.n_seqs * c.n_kv_heads * plan.tiles > slots;
   p.status = device_status_word();
   if (p.status == nullptr) return HBL_ERR_CUDA;

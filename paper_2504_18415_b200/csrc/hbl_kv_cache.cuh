@@ -127,6 +127,7 @@ struct AttnParts { float *rows_o, *rows_lse, *tiles_o, *tiles_lse; };      // [s
 // Sequences of up to `few` query rows (tokens times heads that share a key head) go to one kernel, the others to the other.
 AttnPlan plan_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, int few);
 AttnPlan plan_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& a, int few);
+int attention_rows_resident(const KvView& c, const BatchView& b, const AttnArgs& a, int few);     // its thread blocks to an SM
 int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, int few, const AttnParts& w,
                           bool beside_tiles, cudaStream_t s);
 int launch_attention_tiles(const KvView& c, const BatchView& b, const AttnArgs& a, const AttnPlan& p, int few, const AttnParts& w,
