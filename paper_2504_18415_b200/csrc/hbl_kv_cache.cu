@@ -102,10 +102,15 @@ struct AppendParams {
   int* status;
   int n_heads, n_pos, rot_dim, blocks_per_token, groups;       // n_heads 0: no queries; groups: heads side by side in a block
   float eps;
+};
+// (Apart: with these in AppendParams every append takes 0.3 us longer to launch.)
+struct AppendNormParams : AppendParams {
   const void *q_gain, *k_gain;                                 // hbl_kv_append_norm; NULL: ones
   int gain_bf16;
   float norm_eps;
 };
+template <bool NORM> struct ParamsOf { using type = AppendParams; };
+template <> struct ParamsOf<true> { using type = AppendNormParams; };
 
 // Where a token goes: the block's token t, looked up by every warp for itself.  False: nowhere (reported, or behind the
 // last sequence).
@@ -141,7 +146,7 @@ __device__ __forceinline__ bool find_place(const KvView& c, const BatchView& s, 
 // NORM: queries and keys are r R(gain x), r = 1 / sqrt(mean x^2 + eps).  R is linear, so r goes last; x's squares are summed in fp64
 // (a bf16 value's is exact) and r is rounded once, so that a key's codes are those of the fp32 formula, bit for bit.
 template <int BITS, int LPH, bool INTERLEAVED, int ROWS, bool EVEN, bool NORM>
-__global__ void __launch_bounds__(kThreads, ROWS >= 4 && (NORM || (ROWS == 6 && BITS < 8)) ? 4 : 0) kv_append_kernel(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(kThreads, ROWS >= 4 && (NORM || (ROWS == 6 && BITS < 8)) ? 4 : 0) kv_append_kernel(const __grid_constant__ typename ParamsOf<NORM>::type p) {
   constexpr int HPW = 32 / LPH;                               // heads side by side in a warp
   const int groups = p.groups;                                // ... and in the block
   grid_dependency_wait();
@@ -430,7 +435,7 @@ Deal deal(int rows, int lph, int rows_per_thread) {
   return d;
 }
 template <int BITS, int LPH, bool INTERLEAVED, int ROWS, bool EVEN, bool NORM>
-int launch_append_rows(AppendParams& p, cudaStream_t s) {
+int launch_append_rows(typename ParamsOf<NORM>::type& p, cudaStream_t s) {
   const Deal d = deal(p.n_heads + 2 * p.c.n_kv_heads, LPH, ROWS);
   p.blocks_per_token = d.blocks;
   p.groups = d.groups;
@@ -444,19 +449,19 @@ int launch_append_rows(AppendParams& p, cudaStream_t s) {
 // of 96 heads at 3 bits: 148 us; four or three heads 163, two 180; 48 heads 64, 71, 70, 75), or four at head_dim 256, where six
 // run out of registers (341 us against 291).
 template <int BITS, int LPH, bool INTERLEAVED, bool EVEN, bool NORM>
-int launch_append_layout(AppendParams& p, cudaStream_t s) {
+int launch_append_layout(typename ParamsOf<NORM>::type& p, cudaStream_t s) {
   if ((long)p.b.tokens * (p.n_heads + 2 * p.c.n_kv_heads) * LPH < (long)sm_count() * 2048 * 4)
     return launch_append_rows<BITS, LPH, INTERLEAVED, 1, EVEN, NORM>(p, s);
   return launch_append_rows<BITS, LPH, INTERLEAVED, LPH < 32 ? 6 : 4, EVEN, NORM>(p, s);
 }
 template <int BITS, int LPH, bool NORM>
-int launch_append_heads(AppendParams& p, bool interleaved, cudaStream_t s) {
+int launch_append_heads(typename ParamsOf<NORM>::type& p, bool interleaved, cudaStream_t s) {
   if ((p.n_heads | p.c.n_kv_heads) % (32 / LPH) == 0)
     return interleaved ? launch_append_layout<BITS, LPH, true, true, NORM>(p, s) : launch_append_layout<BITS, LPH, false, true, NORM>(p, s);
   return interleaved ? launch_append_layout<BITS, LPH, true, false, NORM>(p, s) : launch_append_layout<BITS, LPH, false, false, NORM>(p, s);
 }
 template <int BITS, bool NORM>
-int launch_append_dim(AppendParams& p, bool interleaved, cudaStream_t s) {
+int launch_append_dim(typename ParamsOf<NORM>::type& p, bool interleaved, cudaStream_t s) {
   switch (p.c.head_dim) {
     case 64: return launch_append_heads<BITS, 8, NORM>(p, interleaved, s);
     case 128: return launch_append_heads<BITS, 16, NORM>(p, interleaved, s);
@@ -465,8 +470,8 @@ int launch_append_dim(AppendParams& p, bool interleaved, cudaStream_t s) {
   }
 }
 template <int BITS>
-int launch_append_bits(AppendParams& p, bool interleaved, bool norm, cudaStream_t s) {
-  return norm ? launch_append_dim<BITS, true>(p, interleaved, s) : launch_append_dim<BITS, false>(p, interleaved, s);
+int launch_append_bits(AppendNormParams& p, bool interleaved, bool norm, cudaStream_t s) {
+  return norm ? launch_append_dim<BITS, true>(p, interleaved, s) : launch_append_dim<BITS, false>(static_cast<AppendParams&>(p), interleaved, s);
 }
 
 template <int BITS, int LPH, int ROWS>
@@ -499,7 +504,7 @@ int launch_read_bits(ReadParams& p, cudaStream_t s) {
 }  // namespace
 
 int launch_kv_append(const KvView& c, const BatchView& b, const hbl_kv_append_t& a, const hbl_head_norm_t* norm, cudaStream_t s) {
-  AppendParams p{};
+  AppendNormParams p{};
   p.c = c; p.b = b;
   p.k = static_cast<const __nv_bfloat16*>(a.k); p.v = static_cast<const __nv_bfloat16*>(a.v);
   p.q = static_cast<const __nv_bfloat16*>(a.q); p.q_out = static_cast<__nv_bfloat16*>(a.q_out);
