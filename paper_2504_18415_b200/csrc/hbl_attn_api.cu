@@ -186,17 +186,18 @@ constexpr int kFewRows = 16;
 // Within a window the keys are few, and a tile's way through its roles is long against 16 rows' way over them.  Where no sequence has more
 // than 128 rows, the call goes to the kernel that should be done first, by what the two cost (us, fitted to 88 calls of each kind, 1 to
 // 32 sequences of 5 to 32 tokens, 32 and 8 heads, windows of 128 to 4000, each on both kernels, which the sums give within 3 to 9 % rms):
-//   streaming: start + rounds (round + key * keys of a block) + 2.5 if the keys are split; a round that is not full counts as half of one
-//              and its part of the other half
-//   tiles:     start + rounds (round + tile * tiles of an item * (1 to 1.5, as the GPU fills)) + 3.5 if they are split
-// None of those calls takes over 21 % more than on the other kernel, and of 400 others (1 to 64 sequences, 1 to 32 key heads, groups of 1 to 16,
-// ragged or not) three do, 56 % at most.  Both sides, streaming / tiles: 16 sequences of 32 tokens, heads of 128, 4 bits, window of
-// 128 37 / 24 us, of 32 sequences of 8 24 / 37; one of 8, of 512 14 / 27; one of 8, heads of 256, 16 bits, window of 128 26 / 13.
+//   streaming: start + rounds (round + key * keys of a block) + 2.5 if the keys are split; of a round that is not full half counts, and
+//              its part of the other half
+//   tiles:     start + rounds (round + tile * tiles of an item) + 3.5 if they are split; of a round that is not full three quarters, and
+//              its part of the last
+// None of those calls takes over 18 % more than on the other kernel, and of 400 others (1 to 64 sequences, 1 to 32 key heads, groups of 1 to
+// 16, ragged or not) three do, 57 % at most.  Streaming / tiles: 16 sequences of 32 tokens, heads of 128, 4 bits, window of
+// 128 37 / 24 us, 32 of 8 24 / 37; one of 8, of 512 14 / 27; one of 8, heads of 256, 16 bits, window of 128 26 / 13.
 struct Costs { float start, round, key, tiles_start, tiles_round, tile; };
 constexpr Costs kCosts[3][3] = {       // heads of 64, 128, 256; 3 and 4, 8, 16 bits
-    {{0.8f, 8.1f, .014f, 7.3f, 4.1f, 2.2f}, {0.4f, 7.7f, .017f, 7.7f, 3.7f, 2.2f}, {1.0f, 5.0f, .016f, 5.8f, 3.3f, 1.5f}},
-    {{2.5f, 9.4f, .020f, 9.9f, 6.2f, 2.5f}, {2.5f, 10.2f, .029f, 9.8f, 5.7f, 2.7f}, {2.0f, 6.9f, .021f, 7.1f, 3.8f, 1.7f}},
-    {{4.6f, 20.3f, .024f, 10.2f, 3.0f, 2.2f}, {3.8f, 19.0f, .034f, 7.4f, 1.7f, 3.3f}, {0.9f, 20.0f, .080f, 7.5f, 3.8f, 1.3f}}};
+    {{0.9f, 8.0f, .014f, 8.4f, 4.5f, 3.0f}, {0.7f, 7.5f, .017f, 8.9f, 4.0f, 3.0f}, {0.9f, 5.2f, .016f, 7.1f, 2.8f, 2.1f}},
+    {{2.8f, 9.3f, .020f, 10.9f, 6.7f, 3.5f}, {2.4f, 10.3f, .029f, 10.7f, 6.4f, 3.8f}, {2.2f, 6.7f, .021f, 8.0f, 4.0f, 2.4f}},
+    {{4.7f, 20.3f, .024f, 8.8f, 4.9f, 3.2f}, {3.9f, 19.0f, .034f, 4.3f, 5.5f, 4.8f}, {0.7f, 20.1f, .081f, 7.0f, 5.3f, 1.9f}}};
 constexpr int kFewRowsInWindow = 128;
 int few_rows(const KvView& c, const BatchView& b, const AttnArgs& a) {
   const long rows = (long)b.max_q_len * a.group;
@@ -205,17 +206,20 @@ int few_rows(const KvView& c, const BatchView& b, const AttnArgs& a) {
   const long reach = (long)a.sinks + a.window + b.max_q_len + 15, sms = sm_count();
   const float keys = (float)(reach < b.max_kv_len ? reach : b.max_kv_len);
   const AttnPlan s = plan_attention_rows(c, b, a, kFewRowsInWindow), t = plan_attention_tiles(c, b, a, kFewRows);
-  const long resident = attention_rows_resident(c, b, a, kFewRowsInWindow);
+  // of `units` side by side, a round that is not full costing `least` of one at least
+  auto rounds = [](long units, long places, float least) {
+    const long rest = units % places;
+    return (float)(units / places) + (rest > 0 ? least + (1.f - least) * (float)rest / (float)places : 0.f);
+  };
   // the batch's row tiles: whole ones of all its rows, and what sequences of the most rows (of any number: half a tile) have beside those
   const float part = fmaxf(0.5f, (float)s.tiles - (float)rows / 16.f), row_tiles = (float)b.tokens * (float)a.group / 16.f + (float)b.n_seqs * part;
   const float blocks = fminf((float)b.n_seqs * (float)s.tiles, row_tiles) * (float)c.n_kv_heads * (float)s.splits;
-  const long on_sm = (long)ceilf(blocks / (float)sms), rest = on_sm % resident;
-  const float rounds = (float)(on_sm / resident) + (rest > 0 ? 0.5f + 0.5f * (float)rest / (float)resident : 0.f);
-  const float streaming = cost.start + rounds * (cost.round + cost.key * fminf(keys, (float)s.chunk)) + (s.splits > 1 ? 2.5f : 0.f);
-  const long items = (long)t.tiles * c.n_kv_heads * t.splits;
-  const float full = fminf(1.f, (float)items / (float)sms), of_item = ceilf(fminf(keys, (float)t.chunk) / (c.head_dim == 256 ? 64.f : 128.f));
-  const float tiles = cost.tiles_start + (float)((items + sms - 1) / sms) * (cost.tiles_round + cost.tile * of_item * (1.f + 0.5f * full)) +
-                      (t.splits > 1 ? 3.5f : 0.f);
+  const float streaming = cost.start + (s.splits > 1 ? 2.5f : 0.f) +
+                          rounds((long)ceilf(blocks / (float)sms), attention_rows_resident(c, b, a, kFewRowsInWindow), 0.5f) *
+                              (cost.round + cost.key * fminf(keys, (float)s.chunk));
+  const float of_item = ceilf(fminf(keys, (float)t.chunk) / (c.head_dim == 256 ? 64.f : 128.f));
+  const float tiles = cost.tiles_start + (t.splits > 1 ? 3.5f : 0.f) +
+                      rounds((long)t.tiles * c.n_kv_heads * t.splits, sms, 0.75f) * (cost.tiles_round + cost.tile * of_item);
   return streaming <= tiles ? kFewRowsInWindow : kFewRows;
 }
 struct AttnCall {
