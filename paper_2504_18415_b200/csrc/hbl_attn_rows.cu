@@ -89,8 +89,11 @@ __global__ void __launch_bounds__(32 * W, blocks_per_sm(BITS, D, NT) * kWarps / 
   constexpr bool CODES = BITS < 16;
   __shared__ uint4 sq[NT][G::KU][32];
   __shared__ float sqs[ROWS];
-  constexpr bool APART = NT * D * W <= 256 * 4;                        // there is room for every warp's results
-  __shared__ __align__(16) float so[APART ? W : 1][ROWS][D + 4];
+  // Places for warps' results: one to a warp where there is room.  Two for 8-bit rows of 128, of which four blocks have 128 KB in flight:
+  // shared memory comes out of the cache that their lanes' pieces of a row meet in (32 x 4096 tokens of 32 key heads: 239 us, with two or
+  // one 229; 64 ragged 251, 245, 251; 8 x 2000 40.9, 39.8, 42.6; 4 x 509 11.7, 11.9, 13.4).
+  constexpr int SLOTS = NT * D * W > 256 * 4 ? 1 : BITS == 8 && D == 128 && NT == 1 && W == 4 ? 2 : W;
+  __shared__ __align__(16) float so[SLOTS][ROWS][D + 4];
   __shared__ float sm[W][ROWS], sl[W][ROWS], sv[W];
   // Behind the tiles this kernel begins when all their blocks have, so what came before the call is complete already; it
   // takes the SMs that they leave.  It may not be complete before they are, as what is launched next waits for this
@@ -468,7 +471,7 @@ __global__ void __launch_bounds__(32 * W, blocks_per_sm(BITS, D, NT) * kWarps / 
     }
   }
 
-  // ---- the four warps' results together ----
+  // ---- the warps' results together ----
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -508,13 +511,13 @@ __global__ void __launch_bounds__(32 * W, blocks_per_sm(BITS, D, NT) * kWarps / 
           x = first ? y : x + y;
         }
   };
-  if constexpr (APART) {                                       // side by side, joined by who writes them out
+  if constexpr (SLOTS == W) {                                  // side by side, joined by who writes them out
     float one[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) one[nt][0] = one[nt][1] = 1.f;
     put(so[warp], true, one);
     __syncthreads();
-  } else {                                                     // one after the other
+  } else {                                                     // as many as there are places, and the next on top of them
     __syncthreads();
     float f[NT][2];
 #pragma unroll
@@ -524,8 +527,8 @@ __global__ void __launch_bounds__(32 * W, blocks_per_sm(BITS, D, NT) * kWarps / 
         const int r = nt * 8 + 2 * t + e;
         f[nt][e] = share(warp, r, top_of(r)) * sv[warp];
       }
-    for (int w = 0; w < W; ++w) {
-      if (warp == w) put(so[0], w == 0, f);
+    for (int w = 0; w < W; w += SLOTS) {
+      if (warp / SLOTS * SLOTS == w) put(so[warp % SLOTS], w == 0, f);
       __syncthreads();
     }
   }
@@ -540,7 +543,7 @@ __global__ void __launch_bounds__(32 * W, blocks_per_sm(BITS, D, NT) * kWarps / 
     for (int w = 0; w < W; ++w) {
       const float f = share(w, rr, top);
       sum += sl[w][rr] * f;
-      if constexpr (APART) {
+      if constexpr (SLOTS == W) {
         const float4 x = *reinterpret_cast<const float4*>(&so[w][rr][d]);
         const float by = f * sv[w];
         if (w == 0) {
@@ -550,6 +553,12 @@ __global__ void __launch_bounds__(32 * W, blocks_per_sm(BITS, D, NT) * kWarps / 
         }
       }
     }
+    if constexpr (SLOTS < W)
+#pragma unroll
+      for (int w = 1; w < SLOTS; ++w) {
+        const float4 x = *reinterpret_cast<const float4*>(&so[w][rr][d]);
+        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+      }
     const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
     const int tok = len.q0 + r / group, hq = head * group + r % group;
     const float lse2 = sum == 0.f ? -INFINITY : top + __log2f(sum);
