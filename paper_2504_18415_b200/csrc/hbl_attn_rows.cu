@@ -729,20 +729,19 @@ int launch_rows_bits(RowsParams& p, cudaStream_t s) {
   return p.a.window > 0 ? launch_rows_window<BITS, true>(p, s) : launch_rows_window<BITS, false>(p, s);
 }
 
-// How many pieces the keys of a sequence are dealt in.  (The figures are of results joined warp by warp; joined at once a block costs
-// some 2 us less.  The rule is kept.)
-//   None up to 512 keys, where the second launch costs more than the shorter loops save (4 x 509 tokens: 14.8 us in two
-// pieces, 12.7 in one; 4 x 1000: 16.8, 17.3), and none of less than 256 keys.
+// How many pieces the keys of a sequence are dealt in.
+//   None up to 512 keys, where the second launch costs more than the shorter loops save (4 x 509 tokens: 11.2 us in two
+// pieces, 9.6 in one; 4 x 1000: 14.1, 14.0), and none of less than 256 keys.
 //   Few sequences: as many pieces as there is room for at once; with one more the last waits for a whole round (16 rows
-// over 16384 tokens at 8 bits: 65 us in 13 pieces, 85 in 14).
-//   As many as there is room for, or more: whole (32 x 4096 tokens of 32 key heads at 8 bits, 16 rows each: 208 us, in two
-// pieces 243; ragged with one row 113, 116).
+// over 16384 tokens at 8 bits: 57 us in 13 pieces, 70 in 14).
+//   As many as there is room for, or more: whole (32 x 4096 tokens of 32 key heads at 8 bits, ragged with one row: 106 us, in two
+// pieces 115; not always: 16 rows each 382, 361).
 //   In between the host, which does not know the lengths, weighs two batches: every sequence as long as the bound says
 // (whole rounds of resident blocks; a round that is not full costs half of one and its part of the other half), and
 // lengths anywhere below it (the work, evenly spread, and half of a last piece), which is what it mostly is, so that it
 // counts twice.  A block costs as much as `fixed` keys before its first and after its last one (64 x 4096 tokens at 4 bits
-// in 1, 2, 4, 8 pieces: 275, 300, 350, 452 us).  64 ragged sequences of up to 16384 tokens, 8 key heads, 4 bits: 254 us in 1
-// piece, 198 in 2, 172 in 4, 174 in 8, 200 in 16.
+// in 1, 2, 4, 8 pieces: 264, 274, 302, 358 us).  64 ragged sequences of up to 16384 tokens, 8 key heads, 4 bits: 252 us in 1
+// piece, 189 in 2, 162 in 4, 159 in 8, 174 in 16.
 long pieces_of_keys(long base, int resident, long keys, long most, int bits) {
   const long slots = (long)sm_count() * resident;
   if (base <= 0 || most <= 1 || base >= slots) return 1;
@@ -791,9 +790,9 @@ int launch_attention_rows(const KvView& c, const BatchView& b, const AttnArgs& a
   p.c = c; p.b = b; p.a = a; p.p = plan; p.few = few; p.part_o = w.rows_o; p.part_lse = w.rows_lse;
   p.beside_tiles = beside_tiles;
   // More blocks than fit at once, of whole sequences: the long ones first (64 ragged sequences of up to 4096 tokens at 4 bits
-  // 190 us in the batch's order, 175 in this; 128 of 8 key heads 113, 92; all of one length 275, 278; window of 1024, ragged 88, 87, of
-  // 2048 137, 130).  Not for short ones, whose blocks would spend more on the look-up than it saves (up to 600 tokens: 59 us, 64;
-  // window of 256: 42, 44), nor for batches whose look-up is long.
+  // 178 us in the batch's order, 159 in this; 128 of 8 key heads 99, 82; all of one length 260, 263; window of 1024, ragged 88, 87, of
+  // 2048 138, 131).  Not for short ones, whose blocks would spend more on the look-up than it saves (up to 600 tokens: 41 us, 44;
+  // window of 256: 41, 44), nor for batches whose look-up is long.
   const long slots = (long)sm_count() * attention_rows_resident(c, b, a, few);
   p.ordered = plan.splits == 1 && (b.max_kv_len < plan.reach ? b.max_kv_len : plan.reach) >= 1024 && b.n_seqs <= 128 && (long)b.n_seqs * c.n_kv_heads * plan.tiles > slots;
   p.status = device_status_word();

@@ -13,9 +13,9 @@
 // heads, HEADS of a token at a time: the gains are loaded once, the table's pairs once for HEADS heads, and the next ones are
 // copied to shared memory while a thread works on the current ones.
 //
-// Bound by HBM and by what hides its latency: 16384 tokens of 32 and 8 heads of 128 in bf16 62.7 us forward (0.84 of what the bytes
-// need), 92.7 us backward (0.84); 8192 in fp32 61.8 and 78.9 (0.84, 0.98).  Registers leave two blocks to an SM (three, spilling: 70 us
-// forward, 164 backward); issue slots 60 %.  The loads straight into registers: 73 and 127.  The statistic in fp32 would save 5 us.
+// Bound by HBM and by what hides its latency: 16384 tokens of 32 and 8 heads of 128 in bf16 62.8 us forward (0.84 of what the bytes
+// need), 94.2 us backward (0.83); 8192 in fp32 61.2 and 81.4 (0.85, 0.95).  Registers leave two blocks to an SM (three, spilling: 70 us
+// forward, 164 backward); issue slots 60 %.  The loads straight into registers: 73 and 127.  The statistic in fp32 would save 6 us.
 #include "hbl_kv_cache.cuh"
 #include "hbl_piece.cuh"
 
