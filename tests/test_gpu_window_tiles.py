@@ -207,3 +207,29 @@ def test_a_captured_chunk_follows_the_cache():
             ref, _, tol, _ = window64(cache, x, q_lens, lens, tables, 1300, 4)
             assert ((o.to(F8) - ref).abs() <= tol).all()
     assert hbl.hbl_check_status() == 0
+
+
+def test_calls_at_the_same_time():
+    """Two streams, a workspace each: split chunks beside a batch of chunks and steps, over one cache, again and again."""
+    cache, batch, tables, q, _ = setup(98, [300], [6000], 4, 2, 128, 4, 64, extra=0)
+    lens = [200, 1, 40], [2900, 3100, 50]
+    g = gen(97)
+    starts = torch.tensor([0, 200, 201, 241], dtype=torch.int32, device="cuda")
+    other = hbl.KvBatch(starts, torch.tensor(lens[1], dtype=torch.int32, device="cuda"), batch.pages[:, :64].expand(3, -1).contiguous(), tokens=241,
+                        max_q_len=200, max_kv_len=3100)                       # (three sequences with the first one's tokens)
+    q2 = heads(g, 241, 4, 128)
+    calls = [(batch, q, 4096, 17, [300], [6000], tables), (other, q2, 1500, 5, *lens, [tables[0][:64]] * 3)]
+    spaces = [hbl.new_workspace(max(1, hbl.hbl_attention_window_workspace_bytes(cache, b, 4, w, s))) for b, _, w, s, *_ in calls]
+    assert spaces[0].numel() > 1
+    want = [check_window(cache, b, t, ql, kl, x, w, s)[0] for b, x, w, s, ql, kl, t in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(30):
+        for i, (b, x, w, s, *_) in enumerate(calls):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(hbl.hbl_attention_window(cache, b, x, w, s, workspace=spaces[i]))
+    torch.cuda.synchronize()
+    for a, outs in zip(want, got):
+        assert all(torch.equal(a, o) for o in outs)
+    assert hbl.hbl_check_status() == 0
