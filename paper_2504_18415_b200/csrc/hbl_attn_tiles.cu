@@ -30,7 +30,7 @@
 // to an item of 256 rows where 8.03 are seen; masks and the looks at values are 25 to 35 us of it.  2048 queries over 16384 at 8 bits, window
 // 2048: 154.
 // bf16 values of a tile that some row masks are looked through after their keys have been announced (before: 243 us for that
-// prompt); what is not finite becomes zeros and is marked.
+// prompt); what is not finite becomes zeros and is marked.  (Rows of 64: see NAN_KEYS.)
 #include "hbl_attn_frag.cuh"
 #include "hbl_pipeline.cuh"
 
@@ -307,6 +307,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
   __shared__ Item item_slot[2];
   __shared__ __align__(8) uint64_t steal_bar, near_end;
   __shared__ __align__(16) uint4 steal_answer;
+  // Rows of 64 announce a masked tile's keys after their values have been looked through, and a key whose value is not finite becomes NaN:
+  // at this width the softmax warps' look at the marks costs more than the wait (8 ragged prompts of up to 600 tokens, 32 heads: 35.8 us, with
+  // marks 37.0; window of 256 over 2048 tokens 23.9, 24.7; heads of 128 without a window 35.4, 34.4).
+  constexpr bool NAN_KEYS = BITS == 16 && D == 64;
   // Keys of the tile whose value, or its scale, is not finite: key 32 e + c is bit c of word e.  The bf16 producers' warps all write to
   // them; so a stage has two sets in turn, and the next tile's is made 0 before this one's values are announced: whoever may fill
   // the stage again comes after that, and nobody has to wait for another warp.
@@ -598,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
         }
         // What is not finite came as zero (0 * it would reach rows it is masked for): rows that see its key are marked, and their
         // results become NaN.
-        if (!CODES && marked.has(j, WINDOW)) {              // (the product below needs the values as well)
+        if (!CODES && !NAN_KEYS && marked.has(j, WINDOW)) { // (the product below needs the values as well)
           if (!(ok = __all_sync(0xffffffffu, mbar_wait(&v_full[stage], (it / STAGES) & 1, abort_flag, p.status)))) break;
           const uint4 b = *reinterpret_cast<const uint4*>(bad_value[stage][CODES ? 0 : (it / STAGES) & 1]);
           if (b.x | b.y | b.z | b.w) {
@@ -794,17 +798,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
               copy16(dst + chunk_at(rr, tid % CH, G::HALF), col + row_of(tile, rr) * (2 * D), live(tile, rr));
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
-            if (copied != nullptr) {
+            const bool masked = kv == 1 && marked.has(j, WINDOW);
+            if (copied != nullptr && !(NAN_KEYS && masked)) {
               asm volatile("cp.async.wait_group 1;" ::: "memory");
               fence_async();                                    // what the copies wrote is read next by the tensor cores
               mbar_arrive(copied);
               copied = nullptr;
             }
-            if (kv == 1 && tid < 4) bad_value[stage][(it / STAGES & 1) ^ 1][tid] = 0;    // (its readers have seen the last products begin)
-            if (kv == 1 && marked.has(j, WINDOW)) {
+            if (!NAN_KEYS && kv == 1 && tid < 4) bad_value[stage][(it / STAGES & 1) ^ 1][tid] = 0;    // (its readers have seen the last products begin)
+            if (masked) {
               // A tile that some row masks: 0 * a value that is not finite would reach rows that mask its key.  Every thread
-              // looks through the pieces that it has copied; such a value becomes zeros and its key is marked, so that the rows
-              // that see it, and no others, become NaN.  (The lanes that hold a row lie side by side.)
+              // looks through the pieces that it has copied; such a value becomes zeros and its key is marked, or becomes NaN itself
+              // (NAN_KEYS), so that the rows that see it, and no others, become NaN.  (The lanes that hold a row lie side by side.)
               asm volatile("cp.async.wait_all;" ::: "memory");
               uint32_t any = 0;
               auto look = [&](int i) {                          // 0 * y summed up: zeros, or NaN where y is not finite
@@ -824,10 +829,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tiles_kernel(const __grid_co
                     const uint32_t zero[4] = {0, 0, 0, 0};
                     const int rr = i * RPP + tid / CH;
                     store16(dst + chunk_at(rr, tid % CH, G::HALF), zero);
-                    if (tid % CH == 0) atomicOr(&bad_value[stage][it / STAGES & 1][rr >> 5], 1u << (rr & 31));
+                    if (NAN_KEYS) {                             // (the same lanes have copied the key's pieces)
+                      const uint32_t nan[4] = {0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
+                      store16(sk + stage * G::KV_BYTES + chunk_at(rr, tid % CH, G::HALF), nan);
+                    } else if (tid % CH == 0) atomicOr(&bad_value[stage][it / STAGES & 1][rr >> 5], 1u << (rr & 31));
                   }
                 }
               fence_async();
+              if (NAN_KEYS) {
+                mbar_arrive(copied);                            // the keys
+                copied = nullptr;
+              }
               mbar_arrive(&v_full[stage]);
               continue;
             }
